@@ -435,6 +435,126 @@ int iodf_level_images_per_cta(const iodf_model* m, int level);
 /* Number of kernel launches one iodf_forward / iodf_inverse call enqueues. */
 int iodf_launches_per_call(const iodf_model* m, int inverse);
 
+/*
+ * Single integer layers beside the flow and the coder, for networks that run between the library's own
+ * steps: a refinement of the prior parameters between iodf_forward (or iodf_inverse_level) and
+ * iodf_rans_encode (or iodf_rans_decode_block) leaves the flow invertible as long as both sides compute the
+ * same integers, which these do. The element types of their operands:
+ */
+#define IODF_I8 1u
+#define IODF_U8 2u
+#define IODF_I16 3u
+#define IODF_I32 4u
+
+/*
+ * Projection with low-rank adapters of many requests at once. The shared part is a 1x1 layer (Eq. 5,
+ * Eq. "quant_conv", Sec. 4.1) over rows (pixels of images, or tokens); an adapter a of rank R adds
+ * R further input channels that are themselves an 8-bit projection of the same row:
+ *   h[j] = clip(rq(sum_k down_a[j][k] x[k]; M_a[j], s_a[j]), -128, 127)                       j < R
+ *   y[n] = out(rq(sum_k W[n][k] x[k] + sum_j up_a[n][j] h[j] + bias[n]; M0[n], s[n]))
+ * with one int32 accumulator and one rounding; out() is the layer's ReLU, then its clip. Which rows use which
+ * adapter is data of the call: request q owns the rows seg_start[q] <= row < seg_start[q+1] and
+ * adapter slot seg_adapter[q], or none (-1; a slot that holds no adapter adds nothing either).
+ *
+ * iodf_proj_create: layer.k must be 1, weights int8 [c_out][c_in] and requant bias, M0, s of c_out each at the
+ * layer's offsets into the HOST arrays (copied). x_type is IODF_I8 or IODF_U8; y_type is IODF_I32, or
+ * IODF_I8 / IODF_U8 when the layer's clip lies in that range. max_adapters <= 65536 slots (0: none) of rank
+ * <= max_rank <= 128. Errors: EINVAL (also: M0, s, offsets, clip), EUNSUPPORTED (k, more than 32768
+ * channels), EOVERFLOW (worst-case accumulator), EVERSION, ENOMEM, ECUDA.
+ *
+ * iodf_proj_set_adapter: replaces slot `slot` (HOST arrays, copied: down int8 [rank][c_in], down_requant
+ * M[rank] then s[rank], up int8 [c_out][rank]); rank 0 empties it. Ordered on `cuda_stream`, which it
+ * synchronises (EINVAL while that is being captured); calls on other streams that use the slot must have
+ * ended. EOVERFLOW if the adapter could carry the accumulator out of the int32 range.
+ *
+ * iodf_proj_forward: x DEV [rows] x c_in elements, row stride ldx >= c_in bytes, a multiple of 16, x
+ * 16-byte aligned; y DEV [rows] x c_out elements of y_type, row stride ldy >= c_out elements, aligned to its
+ * element. seg_start DEV int32 [n_seg + 1], seg_adapter DEV int32 [n_seg]; with n_seg = 0 (both may be NULL) every row is
+ * computed without an adapter. Rows in no request are not written. 0 <= rows <= max_rows. Allocates nothing,
+ * may be captured; the handle's workspace serves one call at a time (also for replayed graphs). Requests whose
+ * bounds decrease or leave 0..rows, and slots outside -1..max_adapters-1, are counted on the device and
+ * reported by iodf_proj_check (IODF_EDATA). Such a slot counts as -1; with bad bounds any row may be left
+ * unwritten or computed without its adapter, and nothing outside the buffers is touched.
+ */
+typedef struct {
+  uint32_t abi_version;                /* IODF_ABI_VERSION                                           */
+  iodf_layer_desc layer;
+  uint32_t x_type, y_type;
+  uint32_t max_rows;
+  uint32_t max_adapters, max_rank;
+} iodf_proj_desc;
+
+typedef struct iodf_proj iodf_proj;
+
+int iodf_proj_create(const iodf_proj_desc* desc, const int8_t* weights, size_t weights_count, const int32_t* requant,
+                     size_t requant_count, int device, iodf_proj** out);
+void iodf_proj_destroy(iodf_proj* p);
+int iodf_proj_set_adapter(iodf_proj* p, uint32_t slot, uint32_t rank, const int8_t* down, const int32_t* down_requant,
+                          const int8_t* up, void* cuda_stream);
+int iodf_proj_forward(iodf_proj* p, const void* x, size_t ldx, int rows, const int32_t* seg_start,
+                      const int32_t* seg_adapter, int n_seg, void* y, size_t ldy, void* cuda_stream);
+/* Synchronise the stream; IODF_EDATA if a call since the last check met bad requests (their number in
+ * *bad_requests, HOST, may be NULL), IODF_ETIMEOUT if a bounded wait gave up. Clears both. */
+int iodf_proj_check(iodf_proj* p, void* cuda_stream, uint32_t* bad_requests);
+
+/*
+ * Norms before and after a block with its gate and residual scale (the binary gates of Sec. 4.4 and the
+ * rezero scale of Sec. 5 around a block of Eq. 3), in one pass over the rows:
+ *   a = N(b) or b;  delta[c] = rq(a[c] * gate[c]; mult[c], shift);  r'[c] = clip(r[c] + delta[c], res_lo, res_hi)
+ *   n[c] = clip(rq(N(r')[c]; n_mult[c], n_shift) + n_bias[c], n_lo, n_hi)
+ * r is the residual stream, b the block's output, n the next block's 8-bit input. Values of b and r are
+ * taken in 24 bits, clip(v, -2^23, 2^23 - 1). Multipliers are any int32 but -2^31 (gain, residual scale and
+ * the units of both sides), shifts 1..31. The gate is uint8 per row and channel, or one per channel.
+ * The norm N over a row's C values, in integers (a 2-norm; the factor sqrt(C) of a root mean square
+ * belongs to the multipliers):
+ *   v' = v (IODF_NORM_RMS) or v - floor((2 sum v + C) / (2 C)) (IODF_NORM_CENTRED)
+ *   D = sum v'^2 + eps, t even with 2^60 <= D 2^t < 2^62, sigma = floor(sqrt(D 2^t)), rho = floor((2^61 - 1) / sigma)
+ *   N(v) = floor((v' rho + 2^(38 - t/2)) / 2^(39 - t/2))          about 2^22 v' / sqrt(D)
+ *
+ * iodf_norm_desc: res_type IODF_I16 or IODF_I32, [res_lo, res_hi] inside that type and 24 bits; block_type 0
+ * (no block: only n is computed), IODF_I8 or IODF_I32; post_norm / pre_norm 0 (b is added as it is; no n) or a norm;
+ * n_type IODF_I8 or IODF_U8 with [n_lo, n_hi] inside; eps in [1, 2^60]; channels <= 8192. mult, n_mult
+ * and n_bias (|.| < 2^30) are HOST arrays of `channels`, copied; unused ones may be NULL.
+ *
+ * iodf_norm_forward: element (row, c) of a residual stream lies at image_stride * (row / pixels) +
+ * channel_stride * c + pixel_stride * (row % pixels) elements; either channel_stride is 1 (rows: pixels = rows),
+ * or pixel_stride is 1 (planes, the layout of z and prior; channels <= 256 then). b, gate and n are DEV rows with
+ * strides ldb, ldg, ldn in elements; ldg = 0: one gate per channel; gate NULL: none. r_out may be r with the same
+ * view (in place), else the two must not overlap; it is NULL exactly if there is no block, n exactly if there is
+ * no pre_norm. Pointers are aligned to their elements. Any rows >= 0. Enqueues one kernel, allocates nothing, keeps
+ * no workspace: calls on one handle may overlap.
+ */
+#define IODF_NORM_RMS 1u
+#define IODF_NORM_CENTRED 2u
+
+typedef struct {
+  uint32_t abi_version;                /* IODF_ABI_VERSION                                           */
+  uint32_t channels;
+  uint32_t res_type, block_type;
+  uint32_t post_norm, pre_norm;
+  uint32_t n_type;
+  int32_t shift, n_shift;
+  int32_t res_lo, res_hi;
+  int32_t n_lo, n_hi;
+  uint64_t eps;
+  const int32_t* mult;                 /* HOST                                                       */
+  const int32_t* n_mult;               /* HOST                                                       */
+  const int32_t* n_bias;               /* HOST                                                       */
+} iodf_norm_desc;
+
+typedef struct {
+  uint64_t pixels;
+  uint64_t image_stride, channel_stride, pixel_stride;
+} iodf_view;
+
+typedef struct iodf_norm iodf_norm;
+
+int iodf_norm_create(const iodf_norm_desc* desc, int device, iodf_norm** out);
+void iodf_norm_destroy(iodf_norm* nm);
+int iodf_norm_forward(iodf_norm* nm, int rows, const void* r, const iodf_view* r_view, const void* b, size_t ldb,
+                      const uint8_t* gate, size_t ldg, void* r_out, const iodf_view* out_view, void* n, size_t ldn,
+                      void* cuda_stream);
+
 const char* iodf_strerror(int status);
 int iodf_last_cuda_error(const iodf_model* m); /* the cudaError_t behind the last IODF_ECUDA          */
 

@@ -21,6 +21,8 @@ DECLARED_SYMBOLS = ["iodf_create", "iodf_destroy", "iodf_get_layout", "iodf_forw
                     "iodf_static_scratch_bytes_per_image", "iodf_check", "iodf_launches_per_call",
                     "iodf_selftest_timeout", "iodf_int8_mma_peak", "iodf_level_kernel_name",
                     "iodf_level_images_per_cta",
+                    "iodf_proj_create", "iodf_proj_destroy", "iodf_proj_set_adapter", "iodf_proj_forward",
+                    "iodf_proj_check", "iodf_norm_create", "iodf_norm_destroy", "iodf_norm_forward",
                     "iodf_strerror", "iodf_last_cuda_error"]
 
 
@@ -73,6 +75,24 @@ class CodecLayout(C.Structure):
                 ("block_elems", C.c_uint64 * (IODF_MAX_LEVELS + 1)),
                 ("block_first_stream", C.c_uint32 * (IODF_MAX_LEVELS + 1)),
                 ("block_streams", C.c_uint32 * (IODF_MAX_LEVELS + 1))]
+
+
+class ProjDesc(C.Structure):
+    _fields_ = [("abi_version", C.c_uint32), ("layer", LayerDesc), ("x_type", C.c_uint32), ("y_type", C.c_uint32),
+                ("max_rows", C.c_uint32), ("max_adapters", C.c_uint32), ("max_rank", C.c_uint32)]
+
+
+class NormDesc(C.Structure):
+    _fields_ = [("abi_version", C.c_uint32), ("channels", C.c_uint32), ("res_type", C.c_uint32),
+                ("block_type", C.c_uint32), ("post_norm", C.c_uint32), ("pre_norm", C.c_uint32),
+                ("n_type", C.c_uint32), ("shift", C.c_int32), ("n_shift", C.c_int32), ("res_lo", C.c_int32),
+                ("res_hi", C.c_int32), ("n_lo", C.c_int32), ("n_hi", C.c_int32), ("eps", C.c_uint64),
+                ("mult", C.c_void_p), ("n_mult", C.c_void_p), ("n_bias", C.c_void_p)]
+
+
+class View(C.Structure):
+    _fields_ = [("pixels", C.c_uint64), ("image_stride", C.c_uint64), ("channel_stride", C.c_uint64),
+                ("pixel_stride", C.c_uint64)]
 
 
 class IodfError(RuntimeError):
@@ -157,6 +177,23 @@ def load_library(path=None):
     L.iodf_level_images_per_cta.argtypes = [vp, C.c_int]
     L.iodf_launches_per_call.restype = C.c_int
     L.iodf_launches_per_call.argtypes = [vp, C.c_int]
+    L.iodf_proj_create.restype = C.c_int
+    L.iodf_proj_create.argtypes = [C.POINTER(ProjDesc), vp, C.c_size_t, vp, C.c_size_t, C.c_int, C.POINTER(vp)]
+    L.iodf_proj_destroy.restype = None
+    L.iodf_proj_destroy.argtypes = [vp]
+    L.iodf_proj_set_adapter.restype = C.c_int
+    L.iodf_proj_set_adapter.argtypes = [vp, C.c_uint32, C.c_uint32, vp, vp, vp, vp]
+    L.iodf_proj_forward.restype = C.c_int
+    L.iodf_proj_forward.argtypes = [vp, vp, C.c_size_t, C.c_int, vp, vp, C.c_int, vp, C.c_size_t, vp]
+    L.iodf_proj_check.restype = C.c_int
+    L.iodf_proj_check.argtypes = [vp, vp, C.POINTER(C.c_uint32)]
+    L.iodf_norm_create.restype = C.c_int
+    L.iodf_norm_create.argtypes = [C.POINTER(NormDesc), C.c_int, C.POINTER(vp)]
+    L.iodf_norm_destroy.restype = None
+    L.iodf_norm_destroy.argtypes = [vp]
+    L.iodf_norm_forward.restype = C.c_int
+    L.iodf_norm_forward.argtypes = [vp, C.c_int, vp, C.POINTER(View), vp, C.c_size_t, vp, C.c_size_t, vp,
+                                    C.POINTER(View), vp, C.c_size_t, vp]
     L.iodf_strerror.restype = C.c_char_p
     L.iodf_strerror.argtypes = [C.c_int]
     L.iodf_last_cuda_error.restype = C.c_int
@@ -544,3 +581,216 @@ def iodf_level_images_per_cta(model, level):
     if n < 0:
         raise IodfError(n, "iodf_level_images_per_cta")
     return n
+
+
+# ---- single integer layers ---------------------------------------------------------------------------------
+IODF_I8, IODF_U8, IODF_I16, IODF_I32 = 1, 2, 3, 4
+IODF_NORM_RMS, IODF_NORM_CENTRED = 1, 2
+
+
+def _type_code(dtype, allowed):
+    import torch
+    codes = {torch.int8: IODF_I8, torch.uint8: IODF_U8, torch.int16: IODF_I16, torch.int32: IODF_I32}
+    if dtype not in codes or codes[dtype] not in allowed:
+        raise ValueError("element type %s is not one of the operator's" % (dtype,))
+    return codes[dtype]
+
+
+def _on(t, handle, dtype, what):
+    if not t.is_cuda or t.device.index != handle.device or t.dtype != dtype:
+        raise ValueError("%s must be a %s tensor on cuda:%d" % (what, dtype, handle.device))
+    return t
+
+
+def _rows_of(t, rows, channels, what):
+    """Row stride of a [rows, channels] tensor whose channels lie side by side."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != channels or (channels > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be [%d, %d] with channels side by side" % (what, rows, channels))
+    return t.stride(0) if rows > 1 else max(channels, t.stride(0))
+
+
+def _layer_stream(stream, device):
+    if stream is None:
+        import torch
+        return C.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+    return _stream(stream)
+
+
+class Projection:
+    """Handle of an iodf_proj; destroyed when garbage collected."""
+
+    def __init__(self, handle, device, c_in, c_out, max_rows, x_dtype, y_dtype):
+        self.handle, self.device, self.c_in, self.c_out, self.max_rows = handle, device, c_in, c_out, max_rows
+        self.x_dtype, self.y_dtype = x_dtype, y_dtype
+
+    def __del__(self):
+        h, self.handle = getattr(self, "handle", None), None
+        if h and _lib is not None:
+            _lib.iodf_proj_destroy(h)
+
+
+def iodf_proj_create(layer, max_rows, max_adapters=0, max_rank=0, x_dtype=None, y_dtype=None, device=0):
+    """layer: a layer dict with k = 1 (w, bias, m0, s, relu, clamp), as in a model's couplings. x_dtype int8
+    (default) or uint8; y_dtype int32 (default), int8 or uint8. Adapters are put into their slots by
+    iodf_proj_set_adapter."""
+    import torch
+    L = load_library()
+    x_dtype, y_dtype = x_dtype or torch.int8, y_dtype or torch.int32
+    if layer.get("gate") is not None:
+        raise ValueError("gated (masked-dense) layers must be compacted before deployment")
+    w = np.ascontiguousarray(layer["w"], dtype=np.int8).reshape(-1)
+    par = np.concatenate([np.asarray(layer[k], dtype=np.int32).reshape(-1) for k in ("bias", "m0", "s")])
+    cl = layer["clamp"]
+    lay = LayerDesc(layer["k"], layer["c_in"], layer["c_out"], int(layer["relu"]), int(cl is not None),
+                    cl[0] if cl else 0, cl[1] if cl else 0, 0, 0)
+    desc = ProjDesc(IODF_ABI_VERSION, lay, _type_code(x_dtype, (IODF_I8, IODF_U8)),
+                    _type_code(y_dtype, (IODF_I8, IODF_U8, IODF_I32)), int(max_rows), int(max_adapters), int(max_rank))
+    out = C.c_void_p()
+    rc = L.iodf_proj_create(C.byref(desc), w.ctypes.data, w.size, par.ctypes.data, par.size, int(device), C.byref(out))
+    if rc != 0:
+        raise IodfError(rc, "iodf_proj_create")
+    return Projection(out, int(device), int(layer["c_in"]), int(layer["c_out"]), int(max_rows), x_dtype, y_dtype)
+
+
+def iodf_proj_set_adapter(proj, slot, adapter, stream=None):
+    """adapter: dict rank, down int8 [rank, c_in], m0 and s int32 [rank], up int8 [c_out, rank]; None empties the slot."""
+    rank = int(adapter["rank"]) if adapter else 0
+    down = rq = up = None
+    if rank:
+        down = np.ascontiguousarray(adapter["down"], dtype=np.int8)
+        up = np.ascontiguousarray(adapter["up"], dtype=np.int8)
+        rq = np.concatenate([np.asarray(adapter[k], dtype=np.int32).reshape(-1) for k in ("m0", "s")])
+        if down.shape != (rank, proj.c_in) or up.shape != (proj.c_out, rank) or rq.size != 2 * rank:
+            raise ValueError("adapter arrays do not match its rank and the layer's channels")
+    ptr = [None if a is None else a.ctypes.data for a in (down, rq, up)]
+    rc = load_library().iodf_proj_set_adapter(proj.handle, int(slot), rank, ptr[0], ptr[1], ptr[2],
+                                              _layer_stream(stream, proj.device))
+    if rc != 0:
+        raise IodfError(rc, "iodf_proj_set_adapter")
+
+
+def iodf_proj_forward(proj, x, seg_start=None, seg_adapter=None, y=None, stream=None):
+    """x: cuda [rows, c_in] of the handle's type, row stride a multiple of 16 bytes. seg_start int32 [n + 1] and
+    seg_adapter int32 [n] on the device: the rows and the slot of each request. Returns y [rows, c_out]; rows in no
+    request keep what y held (zero where y is made here)."""
+    import torch
+    rows = x.shape[0]
+    _on(x, proj, proj.x_dtype, "x")
+    ldx = _rows_of(x, rows, proj.c_in, "x")
+    if rows == 1:
+        ldx = (ldx + 15) // 16 * 16          # a single row has no stride of its own
+    n_seg = 0
+    if seg_start is not None:
+        n_seg = seg_adapter.numel()
+        for t, n, what in ((seg_start, n_seg + 1, "seg_start"), (seg_adapter, n_seg, "seg_adapter")):
+            _on(t, proj, torch.int32, what)
+            if t.numel() != n or not t.is_contiguous():
+                raise ValueError("%s must hold %d contiguous values" % (what, n))
+    if y is None:
+        y = (torch.zeros if n_seg else torch.empty)((rows, proj.c_out), dtype=proj.y_dtype, device=x.device)
+    _on(y, proj, proj.y_dtype, "y")
+    ldy = _rows_of(y, rows, proj.c_out, "y")
+    rc = load_library().iodf_proj_forward(proj.handle, _ptr(x), ldx, rows, _ptr(seg_start), _ptr(seg_adapter), n_seg,
+                                          _ptr(y), ldy, _layer_stream(stream, proj.device))
+    if rc != 0:
+        raise IodfError(rc, "iodf_proj_forward")
+    return y
+
+
+def iodf_proj_check(proj, stream=None):
+    n = C.c_uint32(0)
+    rc = load_library().iodf_proj_check(proj.handle, _layer_stream(stream, proj.device), C.byref(n))
+    if rc != 0:
+        raise IodfError(rc, "iodf_proj_check (%d requests)" % n.value)
+
+
+class Norm:
+    """Handle of an iodf_norm; destroyed when garbage collected."""
+
+    def __init__(self, handle, device, channels, res_dtype, block_dtype, n_dtype):
+        self.handle, self.device, self.channels = handle, device, channels
+        self.res_dtype, self.block_dtype, self.n_dtype = res_dtype, block_dtype, n_dtype
+
+    def __del__(self):
+        h, self.handle = getattr(self, "handle", None), None
+        if h and _lib is not None:
+            _lib.iodf_norm_destroy(h)
+
+
+_NORMS = {None: 0, "rms": IODF_NORM_RMS, "centred": IODF_NORM_CENTRED}
+
+
+def iodf_norm_create(desc, device=0):
+    """desc: dict with c, res_dtype (int16 | int32) and, as far as used, eps, block_dtype (int8 | int32 | None),
+    res_range (lo, hi), post {norm: None | "rms" | "centred", mult int32 [c], shift} and
+    pre {norm, mult int32 [c], shift, bias int32 [c], clamp (lo, hi), dtype int8 | uint8}."""
+    L = load_library()
+    c, post, pre = int(desc["c"]), desc.get("post"), desc.get("pre")
+    tabs = {}
+    for name, part, key in (("mult", post, "mult"), ("n_mult", pre, "mult"), ("n_bias", pre, "bias")):
+        if part is not None:
+            tabs[name] = np.ascontiguousarray(part[key], dtype=np.int32).reshape(-1)
+            if tabs[name].size != c:
+                raise ValueError("%s must hold one value per channel" % name)
+    ptr = {k: tabs[k].ctypes.data if k in tabs else None for k in ("mult", "n_mult", "n_bias")}
+    block, (lo, hi) = desc.get("block_dtype"), desc.get("res_range", (0, 0))
+    n_dtype = pre["dtype"] if pre else None
+    d = NormDesc(IODF_ABI_VERSION, c, _type_code(desc["res_dtype"], (IODF_I16, IODF_I32)),
+                 _type_code(block, (IODF_I8, IODF_I32)) if block else 0,
+                 _NORMS[post["norm"]] if post else 0, _NORMS[pre["norm"]] if pre else 0,
+                 _type_code(n_dtype, (IODF_I8, IODF_U8)) if pre else 0,
+                 int(post["shift"]) if post else 0, int(pre["shift"]) if pre else 0, int(lo), int(hi),
+                 int(pre["clamp"][0]) if pre else 0, int(pre["clamp"][1]) if pre else 0, int(desc.get("eps", 0)),
+                 ptr["mult"], ptr["n_mult"], ptr["n_bias"])
+    out = C.c_void_p()
+    rc = L.iodf_norm_create(C.byref(d), int(device), C.byref(out))
+    if rc != 0:
+        raise IodfError(rc, "iodf_norm_create")
+    return Norm(out, int(device), c, desc["res_dtype"], block, n_dtype)
+
+
+def _view(t, channels, what):
+    """rows and strides of a residual stream: [rows, c] or planes [images, c, pixels]."""
+    if t.dim() == 2 and t.shape[1] == channels and (channels == 1 or t.stride(1) == 1):
+        return t.shape[0], View(max(1, t.shape[0]), 0, 1, t.stride(0))
+    if t.dim() == 3 and t.shape[1] == channels and (t.shape[2] == 1 or t.stride(2) == 1):
+        return t.shape[0] * t.shape[2], View(max(1, t.shape[2]), t.stride(0), t.stride(1), 1)
+    raise ValueError("%s must be [rows, %d] or [images, %d, pixels] with the last axis contiguous" % (what, channels, channels))
+
+
+def iodf_norm_forward(norm, r, b=None, gate=None, r_out=None, n=None, stream=None):
+    """r: the residual stream, cuda [rows, c] or planes [images, c, pixels] (any outer strides); b [rows, c] the
+    block's output; gate uint8 [rows, c] or [c]. Returns (r_out, n), None where the handle has no such part.
+    r_out may be r."""
+    import torch
+    c = norm.channels
+    _on(r, norm, norm.res_dtype, "r")
+    rows, rv = _view(r, c, "r")
+    if (b is not None) != (norm.block_dtype is not None):
+        raise ValueError("b is given exactly if the handle has a block")
+    ldb = ldg = ldn = 0
+    ov = None
+    if b is not None:
+        ldb = _rows_of(_on(b, norm, norm.block_dtype, "b"), rows, c, "b")
+        if r_out is None:
+            r_out = torch.empty(r.shape, dtype=r.dtype, device=r.device)
+        if _on(r_out, norm, norm.res_dtype, "r_out").shape != r.shape:
+            raise ValueError("r_out must have the shape of r")
+        _, ov = _view(r_out, c, "r_out")
+    if gate is not None:
+        _on(gate, norm, torch.uint8, "gate")
+        if gate.dim() == 1:
+            if gate.shape[0] != c or (c > 1 and gate.stride(0) != 1):
+                raise ValueError("gate must be [%d] or [%d, %d]" % (c, rows, c))
+        else:
+            ldg = _rows_of(gate, rows, c, "gate")
+    if norm.n_dtype is not None:
+        if n is None:
+            n = torch.empty((rows, c), dtype=norm.n_dtype, device=r.device)
+        ldn = _rows_of(_on(n, norm, norm.n_dtype, "n"), rows, c, "n")
+    rc = load_library().iodf_norm_forward(norm.handle, rows, _ptr(r), C.byref(rv), _ptr(b), ldb, _ptr(gate), ldg,
+                                          _ptr(r_out), C.byref(ov) if ov is not None else None, _ptr(n), ldn,
+                                          _layer_stream(stream, norm.device))
+    if rc != 0:
+        raise IodfError(rc, "iodf_norm_forward")
+    return r_out, n
