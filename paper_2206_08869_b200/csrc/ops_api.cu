@@ -1,5 +1,6 @@
 // C ABI of the single integer layers (include/iodf.h): the projection with low-rank adapters and the norms
 // before and after a block. Host side only: checks, packing, device buffers, launches.
+#include <cuda.h>
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -14,8 +15,13 @@
 
 using namespace iodf;
 
+typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
 struct iodf_proj {
   int device = 0;
+  EncodeTiled encode = nullptr;
   uint32_t max_rows = 0, max_adapters = 0, max_rank = 0;
   int amax = 128;                            // largest |x|
   ProjArgs args{};
@@ -65,6 +71,21 @@ bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) &
 
 size_t up_to(size_t n, size_t m) { return (n + m - 1) / m * m; }
 
+// A row of K channels of an operand of `rows` rows, cut into stages.
+void pack_row(uint8_t* dst, size_t rows, size_t row, const int8_t* src, size_t K) {
+  for (size_t k = 0; k < K; k += 16)
+    std::memcpy(dst + k / kProjStage * rows * kProjStage + core_offset(row, k % kProjStage, kProjStage), src + k, std::min<size_t>(16, K - k));
+}
+
+// x [rows][k] with a box of one stage x box_rows rows
+bool x_map(const iodf_proj& p, const ProjArgs& a, int box_rows, CUtensorMap* out) {
+  const cuuint64_t dims[2] = {(cuuint64_t)a.k, (cuuint64_t)a.rows}, strides[1] = {(cuuint64_t)a.ldx};
+  const cuuint32_t box[2] = {(cuuint32_t)kProjStage, (cuuint32_t)box_rows}, steps[2] = {1, 1};
+  return p.encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(a.x), dims, strides, box, steps,
+                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                  CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 constexpr uint32_t kMaxChannels = 32768, kMaxRank = 128, kMaxSlots = 65536, kMaxNormChannels = 8192, kMaxPlanes = 256;
 
 int create_proj(const iodf_proj_desc& d, const int8_t* weights, size_t wn, const int32_t* requant, size_t rn, int device,
@@ -101,11 +122,13 @@ int create_proj(const iodf_proj_desc& d, const int8_t* weights, size_t wn, const
     if (p.room[n] < 0) return IODF_EOVERFLOW;
   }
 
-  const size_t kp = up_to(K, 16), slots = d.max_adapters, R = slots ? d.max_rank : 0;
-  std::vector<int8_t> wp(N * kp, 0);
-  std::vector<int4> rq(N);
+  const size_t S = kProjStage, stages = (K + S - 1) / S, tiles = (N + kProjTileN - 1) / kProjTileN, slots = d.max_adapters;
+  const size_t R = d.max_rank <= 32 ? 32 : d.max_rank <= 64 ? 64 : 128;
+  std::vector<uint8_t> wp(tiles * stages * kProjTileN * S, 0);
+  std::vector<int4> rq(tiles * kProjTileN, make_int4(1 << 30, 1, 0, 0));
   for (size_t n = 0; n < N; ++n) {
-    std::memcpy(&wp[n * kp], w + n * K, K);
+    pack_row(&wp[n / kProjTileN * stages * kProjTileN * S], kProjTileN, n % kProjTileN, w + n * K, K);
+    p.args.any_shift |= s[n] == 0;
     const int64_t add = (int64_t)bias[n] * m0[n] + (1ll << (30 + s[n]));
     rq[n] = make_int4(m0[n], s[n], (int)(uint32_t)add, (int)(uint32_t)((uint64_t)add >> 32));
   }
@@ -117,8 +140,8 @@ int create_proj(const iodf_proj_desc& d, const int8_t* weights, size_t wn, const
     total += up_to(std::max<size_t>(bytes, 1), 256);
     return at;
   };
-  const size_t o_w = part(wp.size()), o_rq = part(16 * N), o_down = part(slots * R * kp), o_drq = part(8 * slots * R),
-               o_up = part(slots * N * R), o_rank = part(4 * slots), o_h = part(slots ? d.max_rows * R : 0),
+  const size_t o_w = part(wp.size()), o_rq = part(16 * rq.size()), o_down = part(slots * R * stages * S), o_drq = part(8 * slots * R),
+               o_up = part(slots * tiles * kProjTileN * R), o_rank = part(4 * slots), o_h = part(slots ? d.max_rows * R : 0),
                o_slot = part(4 * (size_t)d.max_rows), o_status = part(8);
   p.device = device;
   p.max_rows = d.max_rows;
@@ -126,11 +149,18 @@ int create_proj(const iodf_proj_desc& d, const int8_t* weights, size_t wn, const
   p.max_rank = d.max_rank;
   OnDevice on(device);
   if (on.error() != cudaSuccess) return IODF_ECUDA;
-  cudaError_t e = cudaMalloc(&p.d_mem, total);
+  cudaDriverEntryPointQueryResult found;
+  void* entry = nullptr;
+  cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &entry, 12000, cudaEnableDefault, &found);
+  if (e != cudaSuccess || found != cudaDriverEntryPointSuccess) return IODF_ECUDA;
+  p.encode = reinterpret_cast<EncodeTiled>(entry);
+  e = configure_proj_kernels();
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&p.args.sms, cudaDevAttrMultiProcessorCount, device);
+  if (e == cudaSuccess) e = cudaMalloc(&p.d_mem, total);
   if (e != cudaSuccess) return status_of(e);
   uint8_t* m = static_cast<uint8_t*>(p.d_mem);
   e = cudaMemcpy(m + o_w, wp.data(), wp.size(), cudaMemcpyHostToDevice);
-  if (e == cudaSuccess) e = cudaMemcpy(m + o_rq, rq.data(), 16 * N, cudaMemcpyHostToDevice);
+  if (e == cudaSuccess) e = cudaMemcpy(m + o_rq, rq.data(), 16 * rq.size(), cudaMemcpyHostToDevice);
   if (e == cudaSuccess) e = cudaMemset(m + o_rank, 0, std::max<size_t>(4 * slots, 1));
   if (e == cudaSuccess) e = cudaMemset(m + o_status, 0, 8);
   if (e == cudaSuccess) e = cudaStreamSynchronize(0);        // the first call may be on a stream that does not wait for it
@@ -138,18 +168,19 @@ int create_proj(const iodf_proj_desc& d, const int8_t* weights, size_t wn, const
   ProjArgs& a = p.args;
   a.k = (int)K;
   a.n = (int)N;
-  a.kp = (int)kp;
+  a.stages = (int)stages;
+  a.tiles_n = (int)tiles;
   a.x_unsigned = d.x_type == IODF_U8;
   a.y_bytes = d.y_type == IODF_I32 ? 4 : 1;
   a.lo = lo;
   a.hi = hi;
   a.max_adapters = (int)slots;
-  a.max_rank = (int)R;
-  a.w = reinterpret_cast<const int8_t*>(m + o_w);
+  a.rp = (int)R;
+  a.w = m + o_w;
   a.rq = reinterpret_cast<const int4*>(m + o_rq);
-  a.down = reinterpret_cast<const int8_t*>(m + o_down);
+  a.down = m + o_down;
   a.down_rq = reinterpret_cast<const int2*>(m + o_drq);
-  a.up = reinterpret_cast<const int8_t*>(m + o_up);
+  a.up = m + o_up;
   a.rank = reinterpret_cast<const int*>(m + o_rank);
   a.h = reinterpret_cast<int8_t*>(m + o_h);
   a.row_slot = reinterpret_cast<int*>(m + o_slot);
@@ -159,7 +190,8 @@ int create_proj(const iodf_proj_desc& d, const int8_t* weights, size_t wn, const
 
 int set_adapter(iodf_proj& p, uint32_t slot, uint32_t rank, const int8_t* down, const int32_t* rq, const int8_t* up,
                 cudaStream_t stream) {
-  const size_t K = p.args.k, N = p.args.n, R = p.args.max_rank, kp = p.args.kp;
+  const size_t K = p.args.k, N = p.args.n, R = p.args.rp, S = kProjStage;
+  const size_t dbytes = R * p.args.stages * S, ubytes = (size_t)p.args.tiles_n * kProjTileN * R;
   for (uint32_t j = 0; j < rank; ++j) {
     if (rq[j] < (1 << 30) || rq[rank + j] < 0 || rq[rank + j] > 31) return IODF_EINVAL;
     int64_t sum = 0;
@@ -171,22 +203,23 @@ int set_adapter(iodf_proj& p, uint32_t slot, uint32_t rank, const int8_t* down, 
     for (uint32_t j = 0; j < rank; ++j) sum += std::abs((int)up[n * rank + j]);
     if (sum * 128 > p.room[n]) return IODF_EOVERFLOW;
   }
-  std::vector<int8_t> dp(R * kp, 0), upp(N * R, 0);
+  std::vector<uint8_t> dp(dbytes, 0), upp(ubytes, 0);
   std::vector<int2> q(R, make_int2(1 << 30, 0));
   for (uint32_t j = 0; j < rank; ++j) {
-    std::memcpy(&dp[j * kp], down + j * K, K);
+    pack_row(dp.data(), R, j, down + j * K, K);
     q[j] = make_int2(rq[j], rq[rank + j]);
   }
   for (size_t n = 0; n < N; ++n)
-    for (uint32_t j = 0; j < rank; ++j) upp[n * R + j] = up[n * rank + j];
+    for (uint32_t j = 0; j < rank; ++j)
+      upp[n / kProjTileN * kProjTileN * R + core_offset(n % kProjTileN, j, R)] = (uint8_t)up[n * rank + j];
   const int rk = (int)rank;
   OnDevice on(p.device);
   if (on.error() != cudaSuccess) return IODF_ECUDA;
   if (capturing(stream)) return IODF_EINVAL;
   const ProjArgs& a = p.args;
-  cudaError_t e = cudaMemcpyAsync(const_cast<int8_t*>(a.down) + slot * R * kp, dp.data(), dp.size(), cudaMemcpyHostToDevice, stream);
+  cudaError_t e = cudaMemcpyAsync(const_cast<uint8_t*>(a.down) + slot * dbytes, dp.data(), dbytes, cudaMemcpyHostToDevice, stream);
   if (e == cudaSuccess) e = cudaMemcpyAsync(const_cast<int2*>(a.down_rq) + slot * R, q.data(), 8 * R, cudaMemcpyHostToDevice, stream);
-  if (e == cudaSuccess) e = cudaMemcpyAsync(const_cast<int8_t*>(a.up) + slot * N * R, upp.data(), upp.size(), cudaMemcpyHostToDevice, stream);
+  if (e == cudaSuccess) e = cudaMemcpyAsync(const_cast<uint8_t*>(a.up) + slot * ubytes, upp.data(), ubytes, cudaMemcpyHostToDevice, stream);
   if (e == cudaSuccess) e = cudaMemcpyAsync(const_cast<int*>(a.rank) + slot, &rk, 4, cudaMemcpyHostToDevice, stream);
   const cudaError_t e2 = cudaStreamSynchronize(stream);      // the arrays above live until here
   return status_of(e != cudaSuccess ? e : e2);
@@ -324,7 +357,9 @@ int iodf_proj_forward(iodf_proj* p, const void* x, size_t ldx, int rows, const i
   a.rows = rows;
   OnDevice on(p->device);
   if (on.error() != cudaSuccess) return IODF_ECUDA;
-  return status_of(launch_proj(a, (cudaStream_t)cuda_stream));
+  CUtensorMap map, map_down;
+  if (!x_map(*p, a, proj_row_tile(a), &map) || !x_map(*p, a, kProjDownRows, &map_down)) return IODF_ECUDA;
+  return status_of(launch_proj(a, &map, &map_down, (cudaStream_t)cuda_stream));
 }
 
 int iodf_proj_check(iodf_proj* p, void* cuda_stream, uint32_t* bad_requests) {

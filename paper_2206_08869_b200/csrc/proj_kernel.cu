@@ -1,36 +1,63 @@
 // Projection with low-rank adapters of many requests (include/iodf.h: iodf_proj_forward).
+//
+// Two kernels. The first finds the adapter of every row and computes h, the 8-bit rank channels; the second multiplies
+//   D[128 output channels][rows of a tile] = W x^T + up h^T     (tcgen05 kind::i8, int32 sums in tensor memory)
+// and requantises. The output channels are the MMA's M, so a thread of the epilogue owns one channel and keeps its
+// constants in registers. An adapter is one more step along K with its own operands: `up`, and h with
+// zeros in the rows of other adapters, so a tile may mix any number of them in one accumulator. The second kernel is
+// launched while the first runs (programmatic dependent launch) and waits for it only where it needs h.
 #include "proj_kernel.h"
+
+#include <cuda.h>
+
+#include <limits.h>
+
+#include <algorithm>
+
+#include "iodf_dev.h"
+#include "ptx.cuh"
 
 namespace iodf {
 namespace {
 
-// sum over 16 products of 8-bit integers
+constexpr int kMainThreads = 512;        // warp 0 copies, 1 MMAs, 2 tensor memory, 4-7 h tiles, 8-15 epilogue
+constexpr int kFill = 128;
+constexpr int kEpiWarps = 8;
+constexpr int kMaxRing = 6;
+constexpr int kBytesW = kProjTileN * kProjStage;
+constexpr int kDownRows = kProjDownRows;
+constexpr int kDownRing = 4;
+constexpr int kDownThreads = 256;        // warp 0 copies, 1 MMAs, 2 tensor memory, 4-7 epilogue
+
+// D = s32; A int8 (weights), B int8 or uint8, both K-major, M = 128, N = n
+__device__ __forceinline__ uint32_t idesc(uint32_t n, bool b_unsigned) {
+  return (2u << 4) | (1u << 7) | ((b_unsigned ? 0u : 1u) << 10) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+}
+// operand words: core matrices 128 bytes apart along K, groups of eight rows sbo apart
+__device__ __forceinline__ uint32_t core_lo(uint32_t saddr) { return ptx::umma_desc_lo(saddr, 128u); }
+__device__ __forceinline__ uint32_t core_hi(uint32_t sbo) { return (sbo >> 4) | (1u << 14); }
+constexpr uint32_t kSwizzledHi = (1024u >> 4) | (1u << 14) | (2u << 29);   // rows of 128 bytes, 128-byte swizzle
+
 template <bool kUnsigned>
 __device__ __forceinline__ int dot4(int w, int x, int acc) {
   if (kUnsigned) asm("dp4a.s32.u32 %0, %1, %2, %3;" : "=r"(acc) : "r"(w), "r"(x), "r"(acc));
   else asm("dp4a.s32.s32 %0, %1, %2, %3;" : "=r"(acc) : "r"(w), "r"(x), "r"(acc));
   return acc;
 }
+template <bool kUnsigned>
+__device__ __forceinline__ int dot16(int4 w, int4 x, int acc) {
+  acc = dot4<kUnsigned>(w.x, x.x, acc);
+  acc = dot4<kUnsigned>(w.y, x.y, acc);
+  acc = dot4<kUnsigned>(w.z, x.z, acc);
+  return dot4<kUnsigned>(w.w, x.w, acc);
+}
 
 // 16 bytes of a row of x from channel k0 on; channels beyond the last are zero and not read
 __device__ __forceinline__ int4 load_x16(const uint8_t* row, int k0, int K) {
   if (k0 + 16 <= K) return *reinterpret_cast<const int4*>(row + k0);
   int w[4] = {0, 0, 0, 0};
-  for (int i = 0; k0 + i < K; ++i) w[i >> 2] |= (int)row[k0 + i] << (8 * (i & 3));
+  for (int i = 0; k0 + i < K && i < 16; ++i) w[i >> 2] |= (int)row[k0 + i] << (8 * (i & 3));
   return make_int4(w[0], w[1], w[2], w[3]);
-}
-
-template <bool kUnsigned>
-__device__ __forceinline__ int dot_row(const int8_t* w, const uint8_t* x, int K, int k0, int step) {
-  int acc = 0;
-  for (int k = k0; k < K; k += step) {
-    const int4 a = *reinterpret_cast<const int4*>(w + k), b = load_x16(x, k, K);
-    acc = dot4<kUnsigned>(a.x, b.x, acc);
-    acc = dot4<kUnsigned>(a.y, b.y, acc);
-    acc = dot4<kUnsigned>(a.z, b.z, acc);
-    acc = dot4<kUnsigned>(a.w, b.w, acc);
-  }
-  return acc;
 }
 
 // Which adapter a row uses: the last request that starts at or before it, found by halving. Any content of
@@ -47,73 +74,409 @@ __device__ __forceinline__ int slot_of_row(const ProjArgs& a, int row) {
   return s >= 0 && s < a.max_adapters && a.rank[s] > 0 ? s : -1;
 }
 
-// h of every row, a warp per row; block 0 looks the requests over
+__device__ __forceinline__ void look_over_requests(const ProjArgs& a) {
+  for (int q = threadIdx.x; q < a.n_seg; q += blockDim.x) {
+    const int s0 = a.seg_start[q], s1 = a.seg_start[q + 1], ad = a.seg_adapter[q];
+    if (s0 < 0 || s1 < s0 || s1 > a.rows || ad < -1 || ad >= a.max_adapters) atomicAdd(a.status + 1, 1u);
+  }
+}
+
+__device__ __forceinline__ int8_t rank_value(int acc, int2 q) {
+  const int v = (int)(((long long)acc * q.x + (1ll << (30 + q.y))) >> (31 + q.y));
+  return (int8_t)min(max(v, -128), 127);
+}
+
+// ---- h for few rows: a block per row and eight rank channels, a quarter of K per warp ----------------------
 template <bool kUnsigned>
-__global__ void __launch_bounds__(128) down_kernel(const ProjArgs a) {
-  if (blockIdx.x == 0)
-    for (int q = threadIdx.x; q < a.n_seg; q += blockDim.x) {
-      const int s0 = a.seg_start[q], s1 = a.seg_start[q + 1], ad = a.seg_adapter[q];
-      if (s0 < 0 || s1 < s0 || s1 > a.rows || ad < -1 || ad >= a.max_adapters) atomicAdd(a.status + 1, 1u);
+__global__ void __launch_bounds__(128) down_rows_kernel(const ProjArgs a) {
+  __shared__ int part[4][8];
+  ptx::grid_launch_dependents();
+  const int row = blockIdx.x, g = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  if (row == 0 && g == 0) look_over_requests(a);
+  const int slot = slot_of_row(a, row);
+  if (g == 0 && threadIdx.x == 0) a.row_slot[row] = slot;
+  if (slot < 0 || g * 8 >= a.rank[slot]) return;
+  // 32 lanes: four chunks of 16 channels x eight rank channels, 512 contiguous bytes of `down`
+  const int chunk = lane >> 3, j = lane & 7;
+  const uint8_t* d = a.down + ((size_t)slot * a.stages * a.rp + g * 8) * kProjStage + j * 16;
+  const uint8_t* x = a.x + (size_t)row * a.ldx;
+  int acc = 0;
+#pragma unroll 4
+  for (int c = warp * 4 + chunk; c * 16 < a.k; c += 16)
+    acc = dot16<kUnsigned>(*reinterpret_cast<const int4*>(d + (size_t)(c >> 3) * a.rp * kProjStage + (c & 7) * 128), load_x16(x, c * 16, a.k), acc);
+  acc += __shfl_xor_sync(0xFFFFFFFFu, acc, 8);
+  acc += __shfl_xor_sync(0xFFFFFFFFu, acc, 16);
+  if (lane < 8) part[warp][lane] = acc;
+  __syncthreads();
+  if (threadIdx.x < 8) {
+    acc = part[0][threadIdx.x] + part[1][threadIdx.x] + part[2][threadIdx.x] + part[3][threadIdx.x];
+    a.h[(size_t)row * a.rp + g * 8 + threadIdx.x] = rank_value(acc, a.down_rq[slot * a.rp + g * 8 + threadIdx.x]);
+  }
+}
+
+// ---- h for many rows: the same product as the main kernel's, M = the rank channels of 128 / rp adapters --------
+struct DownShared {
+  uint64_t full[kDownRing], empty[kDownRing], dfull[2], dempty[2];
+  uint32_t abort_flag, tmem;
+  int n_slots;
+  int slot[kDownRows], list[kDownRows];
+};
+
+__global__ void __launch_bounds__(kDownThreads, 1) down_tile_kernel(const __grid_constant__ CUtensorMap xmap, const ProjArgs a) {
+  extern __shared__ uint8_t raw[];
+  uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  __shared__ DownShared sh;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int row0 = blockIdx.x * kDownRows, per = kProjTileN / a.rp;      // adapters per MMA
+  constexpr int kStageBytes = kDownRows * kProjStage + kBytesW;
+  if (blockIdx.x == 0) look_over_requests(a);
+  if (tid == 0) {
+    for (int i = 0; i < kDownRing; ++i) {
+      ptx::mbar_init(ptx::smem_u32(&sh.full[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&sh.empty[i]), 1);
     }
-  const int lane = threadIdx.x & 31;
-  for (int row = blockIdx.x * 4 + (threadIdx.x >> 5); row < a.rows; row += gridDim.x * 4) {
-    const int slot = slot_of_row(a, row);
-    if (lane == 0) a.row_slot[row] = slot;
-    if (slot < 0) continue;
-    const int R = a.rank[slot];
-    for (int j = 0; j < R; ++j) {
-      const size_t i = (size_t)slot * a.max_rank + j;
-      int acc = dot_row<kUnsigned>(a.down + i * a.kp, a.x + (size_t)row * a.ldx, a.k, lane * 16, 512);
-      for (int o = 16; o; o >>= 1) acc += __shfl_xor_sync(0xFFFFFFFFu, acc, o);
-      if (lane == 0) {
-        const int2 q = a.down_rq[i];
-        const int v = (int)(((long long)acc * q.x + (1ll << (30 + q.y))) >> (31 + q.y));
-        a.h[(size_t)row * a.max_rank + j] = (int8_t)min(max(v, -128), 127);
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(ptx::smem_u32(&sh.dfull[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&sh.dempty[i]), 4);
+    }
+    ptx::mbar_init_fence();
+    sh.abort_flag = 0;
+    sh.n_slots = 0;
+  }
+  if (warp == 2) ptx::tmem_alloc(ptx::smem_u32(&sh.tmem), 256u);
+  if (tid < kDownRows) {
+    const int row = row0 + tid;
+    const int s = row < a.rows ? slot_of_row(a, row) : -2;
+    if (row < a.rows) a.row_slot[row] = s;
+    sh.slot[tid] = s;
+  }
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  // Only now: a block of the main kernel on this SM could otherwise take the tensor memory first and wait for this kernel.
+  ptx::grid_launch_dependents();
+  if (tid < kDownRows) {                              // the adapters of the tile, each once, in any order
+    const int s = sh.slot[tid];
+    bool first = s >= 0 && (tid == 0 || sh.slot[tid - 1] != s);
+    for (int i = 0; first && i < tid; ++i) first = sh.slot[i] != s;
+    if (first) sh.list[atomicAdd(&sh.n_slots, 1)] = s;
+  }
+  __syncthreads();
+  const int n_slots = sh.n_slots, groups = (n_slots + per - 1) / per;
+  const uint32_t base = ptx::smem_u32(smem), tmem = sh.tmem;
+  volatile uint32_t* abort_flag = &sh.abort_flag;
+
+  if (warp == 0 && lane == 0) {
+    int it = 0;
+    for (int g = 0; g < groups; ++g) {
+      const int n = min(per, n_slots - g * per);
+      for (int ks = 0; ks < a.stages; ++ks, ++it) {
+        const int s = it % kDownRing;
+        if (!ptx::bounded_wait(abort_flag, a.status, &sh.empty[s], ((it / kDownRing) & 1) ^ 1, kSpinLimit)) { g = groups; break; }
+        const uint32_t st = base + s * kStageBytes, bar = ptx::smem_u32(&sh.full[s]);
+        ptx::mbar_expect_tx(bar, (uint32_t)(kDownRows * kProjStage + n * a.rp * kProjStage));
+        ptx::tile_g2s(st, &xmap, ks * kProjStage, row0, bar);
+        for (int i = 0; i < n; ++i)
+          ptx::bulk_g2s(st + kDownRows * kProjStage + i * a.rp * kProjStage,
+                        a.down + ((size_t)sh.list[g * per + i] * a.stages + ks) * a.rp * kProjStage, (uint32_t)(a.rp * kProjStage), bar);
       }
     }
-  }
-}
-
-template <bool kUnsigned>
-__global__ void __launch_bounds__(128) proj_rows_kernel(const ProjArgs a) {
-  const long long total = (long long)a.rows * a.n;
-  for (long long i = (long long)blockIdx.x * 128 + threadIdx.x; i < total; i += (long long)gridDim.x * 128) {
-    const int row = (int)(i / a.n), n = (int)(i % a.n);
-    const int slot = a.n_seg ? a.row_slot[row] : -1;
-    if (slot == -2) continue;
-    int acc = dot_row<kUnsigned>(a.w + (size_t)n * a.kp, a.x + (size_t)row * a.ldx, a.k, 0, 16);
-    if (slot >= 0) {
-      const int R = a.rank[slot];
-      const int8_t* up = a.up + ((size_t)slot * a.n + n) * a.max_rank;
-      const int8_t* h = a.h + (size_t)row * a.max_rank;
-      for (int j = 0; j < R; ++j) acc += (int)up[j] * h[j];
+  } else if (warp == 1 && lane == 0) {
+    const uint32_t id = idesc(kDownRows, a.x_unsigned);
+    int it = 0;
+    for (int g = 0; g < groups; ++g) {
+      if (!ptx::bounded_wait(abort_flag, a.status, &sh.dempty[g & 1], ((g >> 1) & 1) ^ 1, kSpinLimit)) break;
+      ptx::tc_fence_after();
+      for (int ks = 0; ks < a.stages; ++ks, ++it) {
+        const int s = it % kDownRing;
+        if (!ptx::bounded_wait(abort_flag, a.status, &sh.full[s], (it / kDownRing) & 1, kSpinLimit)) { g = groups; break; }
+        ptx::tc_fence_after();
+        const uint32_t st = base + s * kStageBytes, alo = core_lo(st + kDownRows * kProjStage), blo = ptx::umma_desc_lo(st, 16u);
+        const int steps = min(4, (a.k - ks * kProjStage + 31) / 32);
+        for (int k = 0; k < steps; ++k)
+          ptx::umma_i8_hl(tmem + (g & 1) * kDownRows, alo + k * 16, core_hi(1024u), blo + k * 2, kSwizzledHi, id, ks | k);
+        ptx::umma_commit(ptx::smem_u32(&sh.empty[s]));
+      }
+      ptx::umma_commit(ptx::smem_u32(&sh.dfull[g & 1]));
     }
-    const int4 q = a.rq[n];
-    const long long add = (long long)(((unsigned long long)(uint32_t)q.w << 32) | (uint32_t)q.z);
-    const int v = min(max((int)(((long long)acc * q.x + add) >> (31 + q.y)), a.lo), a.hi);
-    const size_t o = (size_t)row * a.ldy + n;
-    if (a.y_bytes == 1) ((uint8_t*)a.y)[o] = (uint8_t)v;
-    else ((int*)a.y)[o] = v;
+  } else if (warp >= 4) {
+    const int q = warp - 4, m = q * 32 + lane, j = m % a.rp;
+    for (int g = 0; g < groups; ++g) {
+      const int i = g * per + m / a.rp;
+      const int slot = i < n_slots ? sh.list[i] : -3;
+      const bool used = slot >= 0 && j < a.rank[slot];
+      const int2 rq = used ? a.down_rq[slot * a.rp + j] : make_int2(1 << 30, 0);
+      if (!__all_sync(0xFFFFFFFFu, ptx::bounded_wait(abort_flag, a.status, &sh.dfull[g & 1], (g >> 1) & 1, kSpinLimit))) break;
+      ptx::tc_fence_after();
+      for (int c = 0; c < kDownRows; c += 16) {
+        uint32_t v[16];
+        ptx::tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + (g & 1) * kDownRows + c, v);
+        ptx::tmem_ld_wait16(v);
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (used && sh.slot[c + e] == slot) a.h[(size_t)(row0 + c + e) * a.rp + j] = rank_value((int)v[e], rq);
+      }
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.dempty[g & 1]));
+    }
   }
+  __syncwarp();
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (warp == 2) ptx::tmem_dealloc(tmem, 256u);
 }
 
-template <bool kUnsigned>
-cudaError_t launch(const ProjArgs& a, cudaStream_t stream) {
-  if (a.n_seg) {
-    const int grid = (a.rows + 3) / 4 < 148 * 16 ? (a.rows + 3) / 4 : 148 * 16;
-    down_kernel<kUnsigned><<<grid, 128, 0, stream>>>(a);
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
+// ---- the projection ----------------------------------------------------------------------------------------------
+struct MainShared {
+  uint64_t full[kMaxRing], empty[kMaxRing], afull[2], aempty[2], tfull[2], tempty[2];
+  uint32_t abort_flag, tmem;
+  int message[2];                        // an adapter step: 32-channel steps, 256: the tile's last
+  int least[2][4];
+};
+
+struct MainShape {
+  int tile;                              // rows per tile: 16 .. 256
+  int ring;                              // stages
+  int tmem_cols;
+};
+
+template <class YT, bool kAnyShift>
+__global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid_constant__ CUtensorMap xmap, const ProjArgs a, const MainShape shp) {
+  extern __shared__ uint8_t raw[];
+  uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  __shared__ MainShared sh;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int RT = shp.tile, ring = shp.ring;
+  const int tiles = a.tiles_n * ((a.rows + RT - 1) / RT);
+  const uint32_t stage_bytes = (uint32_t)(RT * kProjStage + kBytesW);
+  const uint32_t abytes = (uint32_t)(kProjTileN + RT) * a.rp;
+  if (tid == 0) {
+    for (int i = 0; i < ring; ++i) {
+      ptx::mbar_init(ptx::smem_u32(&sh.full[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&sh.empty[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      ptx::mbar_init(ptx::smem_u32(&sh.afull[i]), kFill + 1);
+      ptx::mbar_init(ptx::smem_u32(&sh.aempty[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&sh.tfull[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&sh.tempty[i]), kEpiWarps);
+    }
+    ptx::mbar_init_fence();
+    sh.abort_flag = 0;
   }
-  const long long blocks = ((long long)a.rows * a.n + 127) / 128;
-  proj_rows_kernel<kUnsigned><<<(int)(blocks < 148 * 64 ? blocks : 148 * 64), 128, 0, stream>>>(a);
-  return cudaGetLastError();
+  if (warp == 2) ptx::tmem_alloc(ptx::smem_u32(&sh.tmem), (uint32_t)shp.tmem_cols);
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t base = ptx::smem_u32(smem), abase = base + ring * stage_bytes, tmem = sh.tmem;
+  volatile uint32_t* abort_flag = &sh.abort_flag;
+
+  if (warp == 0 && lane == 0) {
+    int it = 0;
+    for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
+      const int tn = t % a.tiles_n, row0 = t / a.tiles_n * RT;
+      const uint8_t* w = a.w + (size_t)tn * a.stages * kBytesW;
+      for (int ks = 0; ks < a.stages; ++ks, ++it) {
+        const int s = it % ring;
+        if (!ptx::bounded_wait(abort_flag, a.status, &sh.empty[s], ((it / ring) & 1) ^ 1, kSpinLimit)) { t = tiles; break; }
+        const uint32_t st = base + s * stage_bytes, bar = ptx::smem_u32(&sh.full[s]);
+        ptx::mbar_expect_tx(bar, stage_bytes);
+        ptx::tile_g2s(st, &xmap, ks * kProjStage, row0, bar);
+        ptx::bulk_g2s(st + RT * kProjStage, w + (size_t)ks * kBytesW, kBytesW, bar);
+      }
+    }
+  } else if (warp == 1 && lane == 0) {
+    const uint32_t id = idesc((uint32_t)RT, a.x_unsigned), ida = idesc((uint32_t)RT, false);
+    const uint32_t hhi = core_hi(128u);
+    int it = 0, ai = 0, ti = 0;
+    for (int t = blockIdx.x; t < tiles; t += gridDim.x, ++ti) {
+      if (!ptx::bounded_wait(abort_flag, a.status, &sh.tempty[ti & 1], ((ti >> 1) & 1) ^ 1, kSpinLimit)) break;
+      ptx::tc_fence_after();
+      const uint32_t d = tmem + (ti & 1) * RT;
+      bool ok = true;
+      for (int ks = 0; ks < a.stages; ++ks, ++it) {
+        const int s = it % ring;
+        if (!(ok = ptx::bounded_wait(abort_flag, a.status, &sh.full[s], (it / ring) & 1, kSpinLimit))) break;
+        ptx::tc_fence_after();
+        const uint32_t st = base + s * stage_bytes, alo = core_lo(st + RT * kProjStage), blo = ptx::umma_desc_lo(st, 16u);
+        const int steps = min(4, (a.k - ks * kProjStage + 31) / 32);
+        for (int k = 0; k < steps; ++k) ptx::umma_i8_hl(d, alo + k * 16, core_hi(1024u), blo + k * 2, kSwizzledHi, id, ks | k);
+        ptx::umma_commit(ptx::smem_u32(&sh.empty[s]));
+      }
+      if (a.n_seg) {
+        for (int last = 0; ok && !last; ++ai) {
+          if (!(ok = ptx::bounded_wait(abort_flag, a.status, &sh.afull[ai & 1], (ai >> 1) & 1, kSpinLimit))) break;
+          ptx::tc_fence_after();
+          const int msg = sh.message[ai & 1], steps = msg & 255;
+          last = msg & 256;
+          const uint32_t up = abase + (ai & 1) * abytes, h = up + kProjTileN * a.rp;
+          const uint32_t alo = core_lo(up), blo = ptx::umma_desc_lo(h, (uint32_t)RT * 16u);
+          for (int k = 0; k < steps; ++k) ptx::umma_i8_hl(d, alo + k * 16, core_hi(8u * a.rp), blo + k * 2 * RT, hhi, ida, 1u);
+          ptx::umma_commit(ptx::smem_u32(&sh.aempty[ai & 1]));
+        }
+      }
+      if (!ok) break;
+      ptx::umma_commit(ptx::smem_u32(&sh.tfull[ti & 1]));
+    }
+  } else if (warp >= 4 && warp < 8 && a.n_seg) {
+    // one message per adapter of the tile, in ascending order of slots; an empty one where there is none
+    const int f = tid - 128;
+    ptx::grid_dependency_wait();
+    int ai = 0, turn = 0;
+    bool ok = true;
+    for (int t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
+      const int tn = t % a.tiles_n, row0 = t / a.tiles_n * RT;
+      int slot[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = f + i * kFill;
+        slot[i] = r < RT && row0 + r < a.rows ? a.row_slot[row0 + r] : -1;
+      }
+      // the least slot above prev among the tile's rows; -2 for all threads if a wait of any of them gave up
+      auto next_slot = [&](int prev, bool fine) {
+        int m = fine ? INT_MAX : -2;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (fine && slot[i] > prev) m = min(m, slot[i]);
+        m = __reduce_min_sync(0xFFFFFFFFu, m);
+        if (lane == 0) sh.least[turn][warp - 4] = m;
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        m = min(min(sh.least[turn][0], sh.least[turn][1]), min(sh.least[turn][2], sh.least[turn][3]));
+        turn ^= 1;
+        return m;
+      };
+      int cur = next_slot(-1, true);
+      for (bool last = false; !last; ++ai) {
+        const int ab = ai & 1, steps = cur == INT_MAX ? 0 : (a.rank[cur] + 31) / 32;
+        const int nxt = next_slot(cur, ptx::bounded_wait(abort_flag, a.status, &sh.aempty[ab], ((ai >> 1) & 1) ^ 1, kSpinLimit));
+        ok = nxt != -2;
+        if (!ok) break;
+        last = nxt == INT_MAX;
+        const uint32_t bar = ptx::smem_u32(&sh.afull[ab]), up = abase + ab * abytes, h = up + kProjTileN * a.rp;
+        if (f == 0) {
+          sh.message[ab] = steps | (last ? 256 : 0);
+          if (steps) {
+            ptx::mbar_expect_tx(bar, (uint32_t)(kProjTileN * a.rp));
+            ptx::bulk_g2s(up, a.up + ((size_t)cur * a.tiles_n + tn) * kProjTileN * a.rp, (uint32_t)(kProjTileN * a.rp), bar);
+          } else {
+            ptx::mbar_arrive(bar);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int r = f + i * kFill;
+          if (r < RT && steps) {
+            const int4* src = reinterpret_cast<const int4*>(a.h + (size_t)(row0 + r) * a.rp);
+            for (int c = 0; c < 2 * steps; ++c) {
+              const int4 v = slot[i] == cur ? src[c] : make_int4(0, 0, 0, 0);
+              *reinterpret_cast<int4*>(smem + (h - base) + (c * RT + r) * 16) = v;
+            }
+          }
+        }
+        ptx::fence_async_smem();
+        ptx::mbar_arrive(bar);
+        cur = nxt;
+      }
+    }
+  } else if (warp >= 8) {
+    const int q = warp & 3, half = (warp - 8) >> 2;
+    const int cols = RT >= 32 ? RT / 2 : (half == 0 ? RT : 0), c0 = RT >= 32 ? half * cols : 0;
+    if (a.n_seg) ptx::grid_dependency_wait();
+    int ti = 0;
+    for (int t = blockIdx.x; t < tiles; t += gridDim.x, ++ti) {
+      const int n = t % a.tiles_n * kProjTileN + q * 32 + lane, row0 = t / a.tiles_n * RT + c0;
+      const int4 rq = a.rq[n];
+      const long long add = (long long)(((unsigned long long)(uint32_t)rq.w << 32) | (uint32_t)rq.z);
+      const int shift = max(rq.y - 1, 0);
+      if (!__all_sync(0xFFFFFFFFu, ptx::bounded_wait(abort_flag, a.status, &sh.tfull[ti & 1], (ti >> 1) & 1, kSpinLimit))) break;
+      ptx::tc_fence_after();
+      for (int c = 0; c < cols; c += 16) {
+        uint32_t v[16];
+        ptx::tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + (ti & 1) * RT + c0 + c, v);
+        const int row = row0 + c + (lane & 15);
+        const uint32_t live = __ballot_sync(0xFFFFFFFFu, row < a.rows && (!a.n_seg || a.row_slot[row] != -2));
+        YT* y = (YT*)a.y + (long long)(row0 + c) * a.ldy + n;
+        ptx::tmem_ld_wait16(v);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const long long p = (long long)(int)v[e] * rq.x + add;
+          int o = (int)(p >> 32) >> shift;
+          if (kAnyShift && rq.y == 0) o = (int)(p >> 31);
+          o = min(max(o, a.lo), a.hi);
+          if ((live >> e & 1) && n < a.n) y[e * a.ldy] = (YT)o;
+        }
+      }
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.tempty[ti & 1]));
+    }
+  }
+  __syncwarp();
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (warp == 2) ptx::tmem_dealloc(tmem, (uint32_t)shp.tmem_cols);
+}
+
+constexpr int kMaxSmem = 225 * 1024;      // beside 1 KB of alignment and the static part
+constexpr int kDownSmem = kDownRing * (kDownRows * kProjStage + kBytesW) + 1024;
+
+template <class YT, bool kAnyShift>
+cudaError_t launch_main(const ProjArgs& a, const CUtensorMap& map, cudaStream_t stream) {
+  MainShape s;
+  s.tile = proj_row_tile(a);
+  s.tmem_cols = std::max(32, 2 * s.tile);
+  const int stage = s.tile * kProjStage + kBytesW, ab = a.n_seg ? 2 * (kProjTileN + s.tile) * a.rp : 0;
+  s.ring = std::min(kMaxRing, (kMaxSmem - ab) / stage);
+  const int tiles = a.tiles_n * ((a.rows + s.tile - 1) / s.tile);
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)std::min(tiles, a.sms));
+  cfg.blockDim = dim3(kMainThreads);
+  cfg.dynamicSmemBytes = (size_t)(s.ring * stage + ab + 1024);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = a.n_seg ? 1 : 0;
+  return cudaLaunchKernelEx(&cfg, proj_tile_kernel<YT, kAnyShift>, map, a, s);
 }
 
 }  // namespace
 
-cudaError_t launch_proj(const ProjArgs& a, cudaStream_t stream) {
-  return a.x_unsigned ? launch<true>(a, stream) : launch<false>(a, stream);
+cudaError_t configure_proj_kernels() {
+  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  cudaError_t e = cudaFuncSetAttribute(down_tile_kernel, attr, kDownSmem);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(proj_tile_kernel<uint8_t, false>, attr, kMaxSmem + 1024);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(proj_tile_kernel<uint8_t, true>, attr, kMaxSmem + 1024);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(proj_tile_kernel<int, false>, attr, kMaxSmem + 1024);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(proj_tile_kernel<int, true>, attr, kMaxSmem + 1024);
+  return e;
+}
+
+// The widest tile that still gives every SM one, and no wider than the rows.
+int proj_row_tile(const ProjArgs& a) {
+  int t = 256;
+  while (t > 16 && (t / 2 >= a.rows || (t > 64 && (long long)a.tiles_n * ((a.rows + t - 1) / t) < a.sms))) t /= 2;
+  return t;
+}
+
+cudaError_t launch_proj(const ProjArgs& a, const void* x_map, const void* x_map_down, cudaStream_t stream) {
+  if (a.n_seg) {
+    if ((long long)a.rows * a.rp <= 16384) {
+      const dim3 grid((unsigned)a.rows, (unsigned)(a.rp / 8));
+      if (a.x_unsigned) down_rows_kernel<true><<<grid, 128, 0, stream>>>(a);
+      else down_rows_kernel<false><<<grid, 128, 0, stream>>>(a);
+    } else {
+      down_tile_kernel<<<(a.rows + kDownRows - 1) / kDownRows, kDownThreads, kDownSmem, stream>>>(
+          *static_cast<const CUtensorMap*>(x_map_down), a);
+    }
+    const cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+  }
+  const CUtensorMap& map = *static_cast<const CUtensorMap*>(x_map);
+  if (a.y_bytes == 1) return a.any_shift ? launch_main<uint8_t, true>(a, map, stream) : launch_main<uint8_t, false>(a, map, stream);
+  return a.any_shift ? launch_main<int, true>(a, map, stream) : launch_main<int, false>(a, map, stream);
 }
 
 }  // namespace iodf

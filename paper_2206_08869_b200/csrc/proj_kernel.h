@@ -1,9 +1,17 @@
-// Projection with low-rank adapters of many requests: launch arguments.
+// Projection with low-rank adapters of many requests: launch arguments and the layout of its operands.
+//
+// Every 8-bit operand of a tcgen05.mma that is a weight is stored as the MMA reads it from shared memory (K-major, no
+// swizzle): core matrices of 8 rows x 16 bytes, 128 bytes each; [row / 8][chunk of 16 bytes][8 rows][16]. Consecutive chunks
+// are 128 bytes apart (leading-dimension offset), consecutive groups of 8 rows chunks * 128 (stride-dimension offset).
 #pragma once
 #include <cuda_runtime.h>
 #include <stdint.h>
 
 namespace iodf {
+
+constexpr int kProjTileN = 128;          // output channels per tile: the M of the MMA
+constexpr int kProjStage = 128;          // channels (bytes of K) per stage of the ring
+constexpr int kProjDownRows = 128;       // rows per tile of the kernel that computes h
 
 struct ProjArgs {
   const uint8_t* x;
@@ -11,21 +19,36 @@ struct ProjArgs {
   void* y;
   const int32_t *seg_start, *seg_adapter;
   int n_seg, rows;
-  int k, n, kp;                        // channels in, out; k rounded up to 16
+  int k, n;                            // channels in, out
+  int stages, tiles_n;                 // ceil(k / 128), ceil(n / 128)
   int x_unsigned, y_bytes;
   int lo, hi;                          // ReLU and clip of the layer
-  int max_adapters, max_rank;
-  const int8_t* w;                     // [n][kp]
-  const int4* rq;                      // [n] {M0, s, addend low, addend high}: y = (acc M0 + addend) >> (31 + s)
-  const int8_t* down;                  // [max_adapters][max_rank][kp]
-  const int2* down_rq;                 // [max_adapters][max_rank] {M, s}
-  const int8_t* up;                    // [max_adapters][n][max_rank]
+  int any_shift;                       // some s is 0
+  int max_adapters;
+  int rp;                              // ranks padded: 32, 64 or 128
+  const uint8_t* w;                    // [tiles_n][stages][128 x 128 as above]
+  const int4* rq;                      // [tiles_n * 128] {M0, s, addend low, addend high}: y = (acc M0 + addend) >> (31 + s)
+  const uint8_t* down;                 // [max_adapters][stages][rp x 128 as above]
+  const int2* down_rq;                 // [max_adapters][rp] {M, s}
+  const uint8_t* up;                   // [max_adapters][tiles_n][128 x rp as above]
   const int* rank;                     // [max_adapters]
-  int8_t* h;                           // workspace [max_rows][max_rank]
+  int8_t* h;                           // workspace [max_rows][rp]
   int* row_slot;                       // workspace [max_rows]: adapter slot, -1 none, -2 in no request
   uint32_t* status;                    // [0] a bounded wait gave up, [1] bad requests
+  int sms;
 };
 
-cudaError_t launch_proj(const ProjArgs& a, cudaStream_t stream);
+// Where element (row, k) of an operand of `width` bytes per row lies.
+inline size_t core_offset(size_t row, size_t k, size_t width) {
+  return (row / 8) * (width / 16) * 128 + (k / 16) * 128 + (row % 8) * 16 + k % 16;
+}
+
+// Once per device, before the first launch.
+cudaError_t configure_proj_kernels();
+
+// x_map, x_map_down: CUtensorMaps of x [rows][k] with boxes of 128 bytes x proj_row_tile(a) or kProjDownRows rows and
+// the 128-byte swizzle.
+int proj_row_tile(const ProjArgs& a);
+cudaError_t launch_proj(const ProjArgs& a, const void* x_map, const void* x_map_down, cudaStream_t stream);
 
 }  // namespace iodf
