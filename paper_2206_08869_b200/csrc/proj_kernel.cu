@@ -26,8 +26,11 @@ constexpr int kEpiWarps = 8;
 constexpr int kMaxRing = 6;
 constexpr int kBytesW = kProjTileN * kProjStage;
 constexpr int kDownRows = kProjDownRows;
-constexpr int kDownRing = 4;
-constexpr int kDownThreads = 256;        // warp 0 copies, 1 MMAs, 2 tensor memory, 4-7 epilogue
+constexpr int kDownRing = 6;             // stages at most
+constexpr int kDownEpiWarps = 8;
+constexpr int kDownThreads = 128 + 32 * kDownEpiWarps;   // warp 0 copies, 1 MMAs, 2 tensor memory, 4-11 epilogue
+constexpr int kDownStageBytes = kDownRows * kProjStage + kBytesW;
+constexpr int kScanRequests = 2048;      // up to here a tile reads every request, above it halves for each row
 
 // D = s32; A int8 (weights), B int8 or uint8, both K-major, M = 128, N = n
 __device__ __forceinline__ uint32_t idesc(uint32_t n, bool b_unsigned) {
@@ -115,48 +118,54 @@ __global__ void __launch_bounds__(128) down_rows_kernel(const ProjArgs a) {
 }
 
 // ---- h for many rows: the same product as the main kernel's, M = the rank channels of 128 / rp adapters --------
+// Tiles of 128 rows; each reads x once per group of 128 / rp adapters that its rows use (mostly one group). A block's time is
+// mostly latency (requests, x, sums, h), so up to three blocks share an SM when there are more tiles than SMs.
 struct DownShared {
-  uint64_t full[kDownRing], empty[kDownRing], dfull[2], dempty[2];
+  uint64_t full[kDownRing], empty[kDownRing], dfull, dempty;
   uint32_t abort_flag, tmem;
   int n_slots;
   int slot[kDownRows], list[kDownRows];
 };
 
-__global__ void __launch_bounds__(kDownThreads, 1) down_tile_kernel(const __grid_constant__ CUtensorMap xmap, const ProjArgs a) {
+__global__ void __launch_bounds__(kDownThreads) down_tile_kernel(const __grid_constant__ CUtensorMap xmap, const ProjArgs a, const int ring) {
   extern __shared__ uint8_t raw[];
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   __shared__ DownShared sh;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int row0 = blockIdx.x * kDownRows, per = kProjTileN / a.rp;      // adapters per MMA
-  constexpr int kStageBytes = kDownRows * kProjStage + kBytesW;
-  if (blockIdx.x == 0) look_over_requests(a);
   if (tid == 0) {
-    for (int i = 0; i < kDownRing; ++i) {
+    for (int i = 0; i < ring; ++i) {
       ptx::mbar_init(ptx::smem_u32(&sh.full[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&sh.empty[i]), 1);
     }
-    for (int i = 0; i < 2; ++i) {
-      ptx::mbar_init(ptx::smem_u32(&sh.dfull[i]), 1);
-      ptx::mbar_init(ptx::smem_u32(&sh.dempty[i]), 4);
-    }
+    ptx::mbar_init(ptx::smem_u32(&sh.dfull), 1);
+    ptx::mbar_init(ptx::smem_u32(&sh.dempty), kDownEpiWarps);
     ptx::mbar_init_fence();
     sh.abort_flag = 0;
     sh.n_slots = 0;
   }
-  if (warp == 2) ptx::tmem_alloc(ptx::smem_u32(&sh.tmem), 256u);
-  if (tid < kDownRows) {
-    const int row = row0 + tid;
-    const int s = row < a.rows ? slot_of_row(a, row) : -2;
-    if (row < a.rows) a.row_slot[row] = s;
-    sh.slot[tid] = s;
-  }
+  if (warp == 2) ptx::tmem_alloc(ptx::smem_u32(&sh.tmem), (uint32_t)kDownRows);
+  const bool scan = a.n_seg <= kScanRequests;
+  if (tid < kDownRows) sh.slot[tid] = scan || row0 + tid >= a.rows ? -2 : slot_of_row(a, row0 + tid);
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
   // Only now: a block of the main kernel on this SM could otherwise take the tensor memory first and wait for this kernel.
   ptx::grid_launch_dependents();
+  if (scan) {                                         // each request writes its rows of the tile: one trip to memory
+    for (int q = tid; q < a.n_seg; q += kDownThreads) {
+      const int s0 = a.seg_start[q], s1 = a.seg_start[q + 1], ad = a.seg_adapter[q];
+      const int lo = max(s0, row0), hi = min(min(s1, row0 + kDownRows), a.rows);
+      if (lo >= hi) continue;
+      const int s = ad >= 0 && ad < a.max_adapters && a.rank[ad] > 0 ? ad : -1;
+      for (int r = lo; r < hi; ++r) sh.slot[r - row0] = s;
+    }
+    __syncthreads();
+  }
+  if (blockIdx.x == 0) look_over_requests(a);
   if (tid < kDownRows) {                              // the adapters of the tile, each once, in any order
     const int s = sh.slot[tid];
+    if (row0 + tid < a.rows) a.row_slot[row0 + tid] = s;
     bool first = s >= 0 && (tid == 0 || sh.slot[tid - 1] != s);
     for (int i = 0; first && i < tid; ++i) first = sh.slot[i] != s;
     if (first) sh.list[atomicAdd(&sh.n_slots, 1)] = s;
@@ -171,9 +180,9 @@ __global__ void __launch_bounds__(kDownThreads, 1) down_tile_kernel(const __grid
     for (int g = 0; g < groups; ++g) {
       const int n = min(per, n_slots - g * per);
       for (int ks = 0; ks < a.stages; ++ks, ++it) {
-        const int s = it % kDownRing;
-        if (!ptx::bounded_wait(abort_flag, a.status, &sh.empty[s], ((it / kDownRing) & 1) ^ 1, kSpinLimit)) { g = groups; break; }
-        const uint32_t st = base + s * kStageBytes, bar = ptx::smem_u32(&sh.full[s]);
+        const int s = it % ring;
+        if (!ptx::bounded_wait(abort_flag, a.status, &sh.empty[s], ((it / ring) & 1) ^ 1, kSpinLimit)) { g = groups; break; }
+        const uint32_t st = base + s * kDownStageBytes, bar = ptx::smem_u32(&sh.full[s]);
         ptx::mbar_expect_tx(bar, (uint32_t)(kDownRows * kProjStage + n * a.rp * kProjStage));
         ptx::tile_g2s(st, &xmap, ks * kProjStage, row0, bar);
         for (int i = 0; i < n; ++i)
@@ -185,46 +194,48 @@ __global__ void __launch_bounds__(kDownThreads, 1) down_tile_kernel(const __grid
     const uint32_t id = idesc(kDownRows, a.x_unsigned);
     int it = 0;
     for (int g = 0; g < groups; ++g) {
-      if (!ptx::bounded_wait(abort_flag, a.status, &sh.dempty[g & 1], ((g >> 1) & 1) ^ 1, kSpinLimit)) break;
+      if (!ptx::bounded_wait(abort_flag, a.status, &sh.dempty, (g & 1) ^ 1, kSpinLimit)) break;
       ptx::tc_fence_after();
       for (int ks = 0; ks < a.stages; ++ks, ++it) {
-        const int s = it % kDownRing;
-        if (!ptx::bounded_wait(abort_flag, a.status, &sh.full[s], (it / kDownRing) & 1, kSpinLimit)) { g = groups; break; }
+        const int s = it % ring;
+        if (!ptx::bounded_wait(abort_flag, a.status, &sh.full[s], (it / ring) & 1, kSpinLimit)) { g = groups; break; }
         ptx::tc_fence_after();
-        const uint32_t st = base + s * kStageBytes, alo = core_lo(st + kDownRows * kProjStage), blo = ptx::umma_desc_lo(st, 16u);
+        const uint32_t st = base + s * kDownStageBytes, alo = core_lo(st + kDownRows * kProjStage), blo = ptx::umma_desc_lo(st, 16u);
         const int steps = min(4, (a.k - ks * kProjStage + 31) / 32);
         for (int k = 0; k < steps; ++k)
-          ptx::umma_i8_hl(tmem + (g & 1) * kDownRows, alo + k * 16, core_hi(1024u), blo + k * 2, kSwizzledHi, id, ks | k);
+          ptx::umma_i8_hl(tmem, alo + k * 16, core_hi(1024u), blo + k * 2, kSwizzledHi, id, ks | k);
         ptx::umma_commit(ptx::smem_u32(&sh.empty[s]));
       }
-      ptx::umma_commit(ptx::smem_u32(&sh.dfull[g & 1]));
+      ptx::umma_commit(ptx::smem_u32(&sh.dfull));
     }
   } else if (warp >= 4) {
-    const int q = warp - 4, m = q * 32 + lane, j = m % a.rp;
+    const int q = warp & 3, half = (warp - 4) >> 2, m = q * 32 + lane, j = m % a.rp;
     for (int g = 0; g < groups; ++g) {
       const int i = g * per + m / a.rp;
       const int slot = i < n_slots ? sh.list[i] : -3;
       const bool used = slot >= 0 && j < a.rank[slot];
       const int2 rq = used ? a.down_rq[slot * a.rp + j] : make_int2(1 << 30, 0);
-      if (!__all_sync(0xFFFFFFFFu, ptx::bounded_wait(abort_flag, a.status, &sh.dfull[g & 1], (g >> 1) & 1, kSpinLimit))) break;
+      if (!__all_sync(0xFFFFFFFFu, ptx::bounded_wait(abort_flag, a.status, &sh.dfull, g & 1, kSpinLimit))) break;
       ptx::tc_fence_after();
-      for (int c = 0; c < kDownRows; c += 16) {
-        uint32_t v[16];
-        ptx::tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + (g & 1) * kDownRows + c, v);
-        ptx::tmem_ld_wait16(v);
+      if (__any_sync(0xFFFFFFFFu, used)) {
+        for (int c = half * (kDownRows / 2); c < (half + 1) * (kDownRows / 2); c += 16) {
+          uint32_t v[16];
+          ptx::tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + c, v);
+          ptx::tmem_ld_wait16(v);
 #pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (used && sh.slot[c + e] == slot) a.h[(size_t)(row0 + c + e) * a.rp + j] = rank_value((int)v[e], rq);
+          for (int e = 0; e < 16; ++e)
+            if (used && sh.slot[c + e] == slot) a.h[(size_t)(row0 + c + e) * a.rp + j] = rank_value((int)v[e], rq);
+        }
       }
       ptx::tc_fence_before();
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.dempty[g & 1]));
+      if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.dempty));
     }
   }
   __syncwarp();
   ptx::tc_fence_before();
   __syncthreads();
-  if (warp == 2) ptx::tmem_dealloc(tmem, 256u);
+  if (warp == 2) ptx::tmem_dealloc(tmem, (uint32_t)kDownRows);
 }
 
 // ---- the projection ----------------------------------------------------------------------------------------------
@@ -233,13 +244,24 @@ struct MainShared {
   uint32_t abort_flag, tmem;
   int message[2];                        // an adapter step: 32-channel steps, 256: the tile's last
   int least[2][4];
+  alignas(16) uint8_t out[kEpiWarps][512];
 };
 
 struct MainShape {
   int tile;                              // rows per tile: 16 .. 256
   int ring;                              // stages
   int tmem_cols;
+  int vector_y;                          // 8-bit rows of y lie on 16-byte boundaries
 };
+
+// clip((acc M0 + addend) >> (31 + s)): the high word of a multiply-add, shifted; s = 0 (shift is 0 then too) needs one bit below it
+template <bool kAnyShift>
+__device__ __forceinline__ int out_value(int acc, int4 rq, long long add, int shift, int lo, int hi) {
+  const long long p = (long long)acc * rq.x + add;
+  int o = (int)(p >> 32) >> shift;
+  if (kAnyShift && rq.y == 0) o = (int)(p >> 31);
+  return min(max(o, lo), hi);
+}
 
 template <class YT, bool kAnyShift>
 __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid_constant__ CUtensorMap xmap, const ProjArgs a, const MainShape shp) {
@@ -380,31 +402,52 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
       }
     }
   } else if (warp >= 8) {
+    // A thread owns an output channel and walks over the rows. 8-bit results of 16 rows x 32 channels go through
+    // 512 bytes of shared memory per warp, so that a row's 32 bytes leave in two 16-byte stores instead of 32.
     const int q = warp & 3, half = (warp - 8) >> 2;
     const int cols = RT >= 32 ? RT / 2 : (half == 0 ? RT : 0), c0 = RT >= 32 ? half * cols : 0;
+    uint8_t* const stage = sh.out[warp - 8];
     if (a.n_seg) ptx::grid_dependency_wait();
     int ti = 0;
     for (int t = blockIdx.x; t < tiles; t += gridDim.x, ++ti) {
-      const int n = t % a.tiles_n * kProjTileN + q * 32 + lane, row0 = t / a.tiles_n * RT + c0;
+      const int n0 = t % a.tiles_n * kProjTileN + q * 32, n = n0 + lane, row0 = t / a.tiles_n * RT + c0;
       const int4 rq = a.rq[n];
       const long long add = (long long)(((unsigned long long)(uint32_t)rq.w << 32) | (uint32_t)rq.z);
       const int shift = max(rq.y - 1, 0);
+      uint32_t live[4] = {0, 0, 0, 0};               // the rows that are written, a bit each
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int row = row0 + i * 32 + lane;
+        const bool w = i * 32 + lane < cols && row < a.rows && (!a.n_seg || a.row_slot[row] != -2);
+        live[i] = __ballot_sync(0xFFFFFFFFu, w);
+      }
       if (!__all_sync(0xFFFFFFFFu, ptx::bounded_wait(abort_flag, a.status, &sh.tfull[ti & 1], (ti >> 1) & 1, kSpinLimit))) break;
       ptx::tc_fence_after();
-      for (int c = 0; c < cols; c += 16) {
-        uint32_t v[16];
-        ptx::tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + (ti & 1) * RT + c0 + c, v);
-        const int row = row0 + c + (lane & 15);
-        const uint32_t live = __ballot_sync(0xFFFFFFFFu, row < a.rows && (!a.n_seg || a.row_slot[row] != -2));
-        YT* y = (YT*)a.y + (long long)(row0 + c) * a.ldy + n;
+      const uint32_t d = tmem + ((uint32_t)(q * 32) << 16) + (ti & 1) * RT + c0;
+      YT* y = (YT*)a.y + (long long)row0 * a.ldy;
+      uint32_t v[16], w[16];
+      if (cols) ptx::tmem_ld16(d, v);
+#pragma unroll 2
+      for (int c = 0; c < cols; c += 16, y += 16 * a.ldy) {
         ptx::tmem_ld_wait16(v);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const long long p = (long long)(int)v[e] * rq.x + add;
-          int o = (int)(p >> 32) >> shift;
-          if (kAnyShift && rq.y == 0) o = (int)(p >> 31);
-          o = min(max(o, a.lo), a.hi);
-          if ((live >> e & 1) && n < a.n) y[e * a.ldy] = (YT)o;
+        for (int e = 0; e < 16; ++e) w[e] = v[e];
+        if (c + 16 < cols) ptx::tmem_ld16(d + c + 16, v);
+        const uint32_t rows16 = live[c >> 5] >> (c & 16);
+        if (sizeof(YT) == 1 && shp.vector_y && n0 + 32 <= a.n) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) stage[e * 32 + lane] = (uint8_t)out_value<kAnyShift>((int)w[e], rq, add, shift, a.lo, a.hi);
+          __syncwarp();
+          const int4 o = *reinterpret_cast<const int4*>(stage + lane * 16);
+          if (rows16 >> (lane >> 1) & 1) *reinterpret_cast<int4*>(y + (lane >> 1) * a.ldy + n0 + (lane & 1) * 16) = o;
+          __syncwarp();
+        } else {
+          YT* p = y + n;
+#pragma unroll
+          for (int e = 0; e < 16; ++e, p += a.ldy) {
+            const int o = out_value<kAnyShift>((int)w[e], rq, add, shift, a.lo, a.hi);
+            if ((rows16 >> e & 1) && n < a.n) *p = (YT)o;
+          }
         }
       }
       ptx::tc_fence_before();
@@ -418,14 +461,14 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
   if (warp == 2) ptx::tmem_dealloc(tmem, (uint32_t)shp.tmem_cols);
 }
 
-constexpr int kMaxSmem = 225 * 1024;      // beside 1 KB of alignment and the static part
-constexpr int kDownSmem = kDownRing * (kDownRows * kProjStage + kBytesW) + 1024;
+constexpr int kMaxSmem = 221 * 1024;      // beside 1 KB of alignment and the static part
 
 template <class YT, bool kAnyShift>
 cudaError_t launch_main(const ProjArgs& a, const CUtensorMap& map, cudaStream_t stream) {
   MainShape s;
   s.tile = proj_row_tile(a);
   s.tmem_cols = std::max(32, 2 * s.tile);
+  s.vector_y = a.y_bytes == 1 && a.ldy % 16 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
   const int stage = s.tile * kProjStage + kBytesW, ab = a.n_seg ? 2 * (kProjTileN + s.tile) * a.rp : 0;
   s.ring = std::min(kMaxRing, (kMaxSmem - ab) / stage);
   const int tiles = a.tiles_n * ((a.rows + s.tile - 1) / s.tile);
@@ -446,7 +489,7 @@ cudaError_t launch_main(const ProjArgs& a, const CUtensorMap& map, cudaStream_t 
 
 cudaError_t configure_proj_kernels() {
   const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  cudaError_t e = cudaFuncSetAttribute(down_tile_kernel, attr, kDownSmem);
+  cudaError_t e = cudaFuncSetAttribute(down_tile_kernel, attr, kDownRing * kDownStageBytes + 1024);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(proj_tile_kernel<uint8_t, false>, attr, kMaxSmem + 1024);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(proj_tile_kernel<uint8_t, true>, attr, kMaxSmem + 1024);
   if (e == cudaSuccess) e = cudaFuncSetAttribute(proj_tile_kernel<int, false>, attr, kMaxSmem + 1024);
@@ -468,8 +511,8 @@ cudaError_t launch_proj(const ProjArgs& a, const void* x_map, const void* x_map_
       if (a.x_unsigned) down_rows_kernel<true><<<grid, 128, 0, stream>>>(a);
       else down_rows_kernel<false><<<grid, 128, 0, stream>>>(a);
     } else {
-      down_tile_kernel<<<(a.rows + kDownRows - 1) / kDownRows, kDownThreads, kDownSmem, stream>>>(
-          *static_cast<const CUtensorMap*>(x_map_down), a);
+      const int tiles = (a.rows + kDownRows - 1) / kDownRows, ring = tiles > a.sms ? 2 : kDownRing;
+      down_tile_kernel<<<tiles, kDownThreads, ring * kDownStageBytes + 1024, stream>>>(*static_cast<const CUtensorMap*>(x_map_down), a, ring);
     }
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
