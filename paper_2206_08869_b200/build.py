@@ -9,7 +9,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libiodf_b200.so")
 STAMP = LIB + ".sha256"      # hash of the sources the library was built from
 NVCC_FLAGS = ["-shared", "-Xcompiler", "-fPIC", "-O3", "-std=c++17", "-gencode",
-              "arch=compute_100a,code=sm_100a", "-lineinfo"]
+              "arch=compute_100a,code=sm_100a", "-lineinfo", "--threads", "0"]
 
 
 def sources():

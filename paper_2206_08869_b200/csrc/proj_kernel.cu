@@ -461,44 +461,225 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
   if (warp == 2) ptx::tmem_dealloc(tmem, (uint32_t)shp.tmem_cols);
 }
 
+// ---- the projection of few rows ------------------------------------------------------------------------------------
+// Where a tile per SM is not reached, the CTAs of a cluster share a tile: each multiplies a part of K, sends its int32
+// sums to the CTA that owns the row (shared memory of the cluster) and finishes RT / S rows itself. There are few
+// rows, mostly of different requests, so the adapters' products are dot products of 16 bytes here: an adapter
+// step of the main kernel costs a tile's time whatever the number of rows that use it.
+constexpr int kSplitThreads = 256;       // warp 0 copies, 1 MMAs, 2 tensor memory, 4-7 send the sums; all finish rows
+constexpr int kSplitRing = 8;
+constexpr int kSplitRows = 128;          // rows of a tile at most
+
+struct SplitShared {
+  uint64_t full[kSplitRing], empty[kSplitRing], tfull;
+  uint32_t abort_flag, tmem;
+};
+
+struct SplitShape {
+  int tile, ring, parts;                 // rows of a tile, stages of the ring, CTAs of a cluster (powers of two: tile, parts)
+  int vector_y;                          // four neighbouring outputs lie on a 4 or 16-byte boundary
+};
+
+template <class YT, bool kAnyShift>
+__global__ void __launch_bounds__(kSplitThreads, 1) proj_split_kernel(const __grid_constant__ CUtensorMap xmap, const ProjArgs a, const SplitShape shp) {
+  extern __shared__ uint8_t raw[];
+  uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
+  __shared__ SplitShared sh;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int RT = shp.tile, ring = shp.ring, own = RT / shp.parts;       // rows that this CTA finishes
+  const int part = (int)ptx::cluster_rank(), t = blockIdx.x / shp.parts;
+  const int tn = t % a.tiles_n, row0 = t / a.tiles_n * RT;
+  const int k0 = part * a.stages / shp.parts, k1 = (part + 1) * a.stages / shp.parts;
+  const uint32_t stage_bytes = (uint32_t)(RT * kProjStage + kBytesW);
+  if (tid == 0) {
+    for (int i = 0; i < ring; ++i) {
+      ptx::mbar_init(ptx::smem_u32(&sh.full[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&sh.empty[i]), 1);
+    }
+    ptx::mbar_init(ptx::smem_u32(&sh.tfull), 1);
+    ptx::mbar_init_fence();
+    sh.abort_flag = 0;
+  }
+  // First phase of the cluster's barrier: every CTA runs before any of them writes into another. Tensor memory is given
+  // back before the second: a CTA that kept it while another CTA of its cluster waits for tensor memory on its own SM
+  // could lock up with another kernel's cluster.
+  ptx::cluster_arrive();
+  const uint32_t tmem_cols = (uint32_t)max(32, RT);
+  if (warp == 2) ptx::tmem_alloc(ptx::smem_u32(&sh.tmem), tmem_cols);
+  ptx::tc_fence_before();
+  __syncthreads();
+  ptx::tc_fence_after();
+  const uint32_t base = ptx::smem_u32(smem), tmem = sh.tmem;
+  const int* const sums = reinterpret_cast<const int*>(smem + ring * stage_bytes);   // [parts][own][128]
+  volatile uint32_t* abort_flag = &sh.abort_flag;
+
+  if (warp == 0 && lane == 0) {
+    const uint8_t* w = a.w + (size_t)tn * a.stages * kBytesW;
+    for (int ks = k0; ks < k1; ++ks) {
+      const int it = ks - k0, s = it % ring;
+      if (!ptx::bounded_wait(abort_flag, a.status, &sh.empty[s], ((it / ring) & 1) ^ 1, kSpinLimit)) break;
+      const uint32_t st = base + s * stage_bytes, bar = ptx::smem_u32(&sh.full[s]);
+      ptx::mbar_expect_tx(bar, stage_bytes);
+      ptx::bulk_g2s(st + RT * kProjStage, w + (size_t)ks * kBytesW, kBytesW, bar);
+      ptx::tile_g2s(st, &xmap, ks * kProjStage, row0, bar);
+    }
+  } else if (warp == 1 && lane == 0) {
+    const uint32_t id = idesc((uint32_t)RT, a.x_unsigned);
+    for (int ks = k0; ks < k1; ++ks) {
+      const int it = ks - k0, s = it % ring;
+      if (!ptx::bounded_wait(abort_flag, a.status, &sh.full[s], (it / ring) & 1, kSpinLimit)) break;
+      ptx::tc_fence_after();
+      const uint32_t st = base + s * stage_bytes, alo = core_lo(st + RT * kProjStage), blo = ptx::umma_desc_lo(st, 16u);
+      const int steps = min(4, (a.k - ks * kProjStage + 31) / 32);
+      for (int k = 0; k < steps; ++k) ptx::umma_i8_hl(tmem, alo + k * 16, core_hi(1024u), blo + k * 2, kSwizzledHi, id, it | k);
+      ptx::umma_commit(ptx::smem_u32(&sh.empty[s]));
+    }
+    ptx::umma_commit(ptx::smem_u32(&sh.tfull));
+  } else if (warp >= 4) {
+    const int q = warp & 3;
+    ptx::cluster_wait();
+    const uint32_t dst = ptx::smem_u32(sums) + (uint32_t)(part * own * kProjTileN + q * 32 + lane) * 4u;
+    if (__all_sync(0xFFFFFFFFu, ptx::bounded_wait(abort_flag, a.status, &sh.tfull, 0u, kSpinLimit))) {
+      ptx::tc_fence_after();
+      for (int c = 0; c < RT; c += 16) {
+        uint32_t v[16];
+        ptx::tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + c, v);
+        ptx::tmem_ld_wait16(v);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int r = c + e;
+          ptx::st_cluster(ptx::cluster_addr(dst + (uint32_t)((r & (own - 1)) * kProjTileN * 4), (uint32_t)(r / own)), v[e]);
+        }
+      }
+      ptx::tc_fence_before();
+    }
+  }
+  __syncwarp();
+  if (warp < 4) ptx::cluster_wait();
+  ptx::tc_fence_before();
+  __syncthreads();
+  if (warp == 2) ptx::tmem_dealloc(tmem, tmem_cols);
+  __syncwarp();
+  ptx::cluster_arrive();
+  const int n = tn * kProjTileN + lane * 4;                   // from here on a thread owns four neighbouring channels
+  int4 rq[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) rq[i] = a.rq[n + i];
+  if (a.n_seg) ptx::grid_dependency_wait();
+  ptx::cluster_wait();
+  for (int r = warp; r < own; r += kSplitThreads / 32) {
+    const int row = row0 + part * own + r;
+    if (row >= a.rows) break;
+    const int slot = a.n_seg ? a.row_slot[row] : -1;
+    if (slot == -2) continue;
+    int4 v = make_int4(0, 0, 0, 0);
+    for (int p = 0; p < shp.parts; ++p) {
+      const int4 u = *reinterpret_cast<const int4*>(sums + (p * own + r) * kProjTileN + lane * 4);
+      v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+    }
+    int acc[4] = {v.x, v.y, v.z, v.w};
+    if (slot >= 0) {
+      const int chunks = (a.rank[slot] + 15) >> 4;
+      const int4* h = reinterpret_cast<const int4*>(a.h + (size_t)row * a.rp);
+      const uint8_t* up = a.up + ((size_t)slot * a.tiles_n + tn) * kProjTileN * a.rp + (lane >> 1) * a.rp * 8 + (lane & 1) * 64;
+      for (int c = 0; c < chunks; ++c) {
+        const int4 hv = h[c];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = dot16<false>(*reinterpret_cast<const int4*>(up + c * 128 + i * 16), hv, acc[i]);
+      }
+    }
+    int o[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const long long add = (long long)(((unsigned long long)(uint32_t)rq[i].w << 32) | (uint32_t)rq[i].z);
+      o[i] = out_value<kAnyShift>(acc[i], rq[i], add, max(rq[i].y - 1, 0), a.lo, a.hi);
+    }
+    YT* y = (YT*)a.y + (long long)row * a.ldy + n;
+    if (shp.vector_y && n + 4 <= a.n) {
+      if (sizeof(YT) == 1)
+        *reinterpret_cast<int*>(y) = __byte_perm(__byte_perm(o[0], o[1], 0x0040), __byte_perm(o[2], o[3], 0x0040), 0x5410);
+      else
+        *reinterpret_cast<int4*>(y) = make_int4(o[0], o[1], o[2], o[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (n + i < a.n) y[i] = (YT)o[i];
+    }
+  }
+}
+
 constexpr int kMaxSmem = 221 * 1024;      // beside 1 KB of alignment and the static part
+
+// Rows of a tile of the kernel for few rows: 0 where its tiles would be more than the SMs.
+int split_tile(const ProjArgs& a) {
+  int t = 16;
+  while (t < kSplitRows && t < a.rows) t *= 2;
+  return (long long)a.tiles_n * ((a.rows + t - 1) / t) <= a.sms ? t : 0;
+}
+
+template <class Shape>
+cudaError_t launch_tiles(void (*kernel)(CUtensorMap, ProjArgs, Shape), const ProjArgs& a, const CUtensorMap& map, const Shape& s, int grid,
+                         int cluster, int threads, size_t smem, cudaStream_t stream) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)grid);
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = (unsigned)cluster;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = a.n_seg ? 2 : 1;                   // follows the kernel that computes h
+  return cudaLaunchKernelEx(&cfg, kernel, map, a, s);
+}
 
 template <class YT, bool kAnyShift>
 cudaError_t launch_main(const ProjArgs& a, const CUtensorMap& map, cudaStream_t stream) {
+  const int tile = proj_row_tile(a), tiles = a.tiles_n * ((a.rows + tile - 1) / tile), stage = tile * kProjStage + kBytesW;
+  const uintptr_t y = reinterpret_cast<uintptr_t>(a.y);
+  if (split_tile(a)) {
+    SplitShape s;
+    s.tile = tile;
+    s.parts = 1;
+    while (s.parts < 8 && 2 * s.parts * tiles <= a.sms && 2 * s.parts <= a.stages) s.parts *= 2;
+    const int sums = tile * kProjTileN * 4, most = (a.stages + s.parts - 1) / s.parts;
+    s.ring = std::min(std::min(kSplitRing, most), (kMaxSmem - sums) / stage);
+    s.vector_y = a.ldy % 4 == 0 && y % (4 * a.y_bytes) == 0;
+    return launch_tiles(proj_split_kernel<YT, kAnyShift>, a, map, s, tiles * s.parts, s.parts, kSplitThreads, (size_t)(s.ring * stage + sums + 1024), stream);
+  }
   MainShape s;
-  s.tile = proj_row_tile(a);
-  s.tmem_cols = std::max(32, 2 * s.tile);
-  s.vector_y = a.y_bytes == 1 && a.ldy % 16 == 0 && reinterpret_cast<uintptr_t>(a.y) % 16 == 0;
-  const int stage = s.tile * kProjStage + kBytesW, ab = a.n_seg ? 2 * (kProjTileN + s.tile) * a.rp : 0;
+  s.tile = tile;
+  s.tmem_cols = std::max(32, 2 * tile);
+  s.vector_y = a.y_bytes == 1 && a.ldy % 16 == 0 && y % 16 == 0;
+  const int ab = a.n_seg ? 2 * (kProjTileN + tile) * a.rp : 0;
   s.ring = std::min(kMaxRing, (kMaxSmem - ab) / stage);
-  const int tiles = a.tiles_n * ((a.rows + s.tile - 1) / s.tile);
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)std::min(tiles, a.sms));
-  cfg.blockDim = dim3(kMainThreads);
-  cfg.dynamicSmemBytes = (size_t)(s.ring * stage + ab + 1024);
-  cfg.stream = stream;
-  cudaLaunchAttribute attr;
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = a.n_seg ? 1 : 0;
-  return cudaLaunchKernelEx(&cfg, proj_tile_kernel<YT, kAnyShift>, map, a, s);
+  return launch_tiles(proj_tile_kernel<YT, kAnyShift>, a, map, s, std::min(tiles, a.sms), 1, kMainThreads, (size_t)(s.ring * stage + ab + 1024), stream);
+}
+
+template <class YT, bool kAnyShift>
+cudaError_t configure() {
+  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
+  cudaError_t e = cudaFuncSetAttribute(proj_tile_kernel<YT, kAnyShift>, attr, kMaxSmem + 1024);
+  return e == cudaSuccess ? cudaFuncSetAttribute(proj_split_kernel<YT, kAnyShift>, attr, kMaxSmem + 1024) : e;
 }
 
 }  // namespace
 
 cudaError_t configure_proj_kernels() {
-  const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  cudaError_t e = cudaFuncSetAttribute(down_tile_kernel, attr, kDownRing * kDownStageBytes + 1024);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(proj_tile_kernel<uint8_t, false>, attr, kMaxSmem + 1024);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(proj_tile_kernel<uint8_t, true>, attr, kMaxSmem + 1024);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(proj_tile_kernel<int, false>, attr, kMaxSmem + 1024);
-  if (e == cudaSuccess) e = cudaFuncSetAttribute(proj_tile_kernel<int, true>, attr, kMaxSmem + 1024);
+  cudaError_t e = cudaFuncSetAttribute(down_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDownRing * kDownStageBytes + 1024);
+  if (e == cudaSuccess) e = configure<uint8_t, false>();
+  if (e == cudaSuccess) e = configure<uint8_t, true>();
+  if (e == cudaSuccess) e = configure<int, false>();
+  if (e == cudaSuccess) e = configure<int, true>();
   return e;
 }
 
-// The widest tile that still gives every SM one, and no wider than the rows.
+// In the persistent kernel the widest tile that still gives every SM one.
 int proj_row_tile(const ProjArgs& a) {
+  if (const int split = split_tile(a)) return split;
   int t = 256;
   while (t > 16 && (t / 2 >= a.rows || (t > 64 && (long long)a.tiles_n * ((a.rows + t - 1) / t) < a.sms))) t /= 2;
   return t;
