@@ -20,9 +20,9 @@
 namespace iodf {
 namespace {
 
-constexpr int kMainThreads = 512;        // warp 0 copies, 1 MMAs, 2 tensor memory, 4-7 h tiles, 8-15 epilogue
+constexpr int kEpiWarps = 16;
 constexpr int kFill = 128;
-constexpr int kEpiWarps = 8;
+constexpr int kMainThreads = 256 + 32 * kEpiWarps;   // warp 0 copies, 1 MMAs, 2 tensor memory, 4-7 adapter steps, 8-23 epilogue
 constexpr int kMaxRing = 6;
 constexpr int kBytesW = kProjTileN * kProjStage;
 constexpr int kDownRows = kProjDownRows;
@@ -77,11 +77,12 @@ __device__ __forceinline__ int slot_of_row(const ProjArgs& a, int row) {
   return s >= 0 && s < a.max_adapters && a.rank[s] > 0 ? s : -1;
 }
 
+__device__ __forceinline__ void look_over_request(const ProjArgs& a, int q) {
+  const int s0 = a.seg_start[q], s1 = a.seg_start[q + 1], ad = a.seg_adapter[q];
+  if (s0 < 0 || s1 < s0 || s1 > a.rows || ad < -1 || ad >= a.max_adapters) atomicAdd(a.status + 1, 1u);
+}
 __device__ __forceinline__ void look_over_requests(const ProjArgs& a) {
-  for (int q = threadIdx.x; q < a.n_seg; q += blockDim.x) {
-    const int s0 = a.seg_start[q], s1 = a.seg_start[q + 1], ad = a.seg_adapter[q];
-    if (s0 < 0 || s1 < s0 || s1 > a.rows || ad < -1 || ad >= a.max_adapters) atomicAdd(a.status + 1, 1u);
-  }
+  for (int q = threadIdx.x; q < a.n_seg; q += blockDim.x) look_over_request(a, q);
 }
 
 __device__ __forceinline__ int8_t rank_value(int acc, int2 q) {
@@ -239,18 +240,31 @@ __global__ void __launch_bounds__(kDownThreads) down_tile_kernel(const __grid_co
 }
 
 // ---- the projection ----------------------------------------------------------------------------------------------
+// Persistent: a CTA takes units of one row tile and `chunk` output tiles. Two ways to come by h:
+//   fused     the CTA computes it itself, as further items of its pipeline in front of the unit's output tiles: the
+//             sums of `down x^T` go through the same accumulators, and h through global memory to the warps that lay it out
+//   separate  down_tile_kernel has computed it before (units of one output tile)
+// Fused repeats the product for every chunk of output tiles, separate costs a launch and a wait for it.
+constexpr int kMaxTile = 256;
+
 struct MainShared {
-  uint64_t full[kMaxRing], empty[kMaxRing], afull[2], aempty[2], tfull[2], tempty[2];
+  uint64_t full[kMaxRing], empty[kMaxRing], afull[2], aempty[2], tfull[2], tempty[2], lready[2], lfree[2], hready;
   uint32_t abort_flag, tmem;
-  int message[2];                        // an adapter step: 32-channel steps, 256: the tile's last
-  int least[2][4];
+  int message[2];                        // an adapter step: adapters << 4 | 32-channel steps of each, 256: the tile's last
+  int n_list[2];
+  int slot[2][kMaxTile], list[2][kMaxTile];   // of a unit: adapter of each row, every adapter once
+  uint32_t live[2][kMaxTile / 32];       // of a unit: the rows that some request owns
   alignas(16) uint8_t out[kEpiWarps][512];
 };
 
 struct MainShape {
-  int tile;                              // rows per tile: 16 .. 256
+  int tile;                              // rows per tile: 64, 128 or 256
   int ring;                              // stages
   int tmem_cols;
+  int chunk, chunks;                     // output tiles of a unit, units of a row tile
+  int units;
+  int abytes;                            // an adapter step's operands: `up`, h
+  int step_adapters;                     // adapters of a step
   int vector_y;                          // 8-bit rows of y lie on 16-byte boundaries
 };
 
@@ -263,16 +277,26 @@ __device__ __forceinline__ int out_value(int acc, int4 rq, long long add, int sh
   return min(max(o, lo), hi);
 }
 
-template <class YT, bool kAnyShift>
+// true if it is for all 128 threads of warps 4-7 (and a barrier of theirs)
+__device__ __forceinline__ bool fill_all(bool fine) {
+  uint32_t r;
+  asm volatile(
+      "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %1, 0;\n\t"
+      "barrier.cta.red.and.pred p, 1, 128, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(r)
+      : "r"((uint32_t)fine)
+      : "memory");
+  return r != 0;
+}
+
+template <class YT, bool kAnyShift, bool kFused>
 __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid_constant__ CUtensorMap xmap, const ProjArgs a, const MainShape shp) {
   extern __shared__ uint8_t raw[];
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   __shared__ MainShared sh;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int RT = shp.tile, ring = shp.ring;
-  const int tiles = a.tiles_n * ((a.rows + RT - 1) / RT);
   const uint32_t stage_bytes = (uint32_t)(RT * kProjStage + kBytesW);
-  const uint32_t abytes = (uint32_t)(kProjTileN + RT) * a.rp;
   if (tid == 0) {
     for (int i = 0; i < ring; ++i) {
       ptx::mbar_init(ptx::smem_u32(&sh.full[i]), 1);
@@ -283,7 +307,10 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
       ptx::mbar_init(ptx::smem_u32(&sh.aempty[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&sh.tfull[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&sh.tempty[i]), kEpiWarps);
+      ptx::mbar_init(ptx::smem_u32(&sh.lready[i]), kFill);
+      ptx::mbar_init(ptx::smem_u32(&sh.lfree[i]), kEpiWarps);
     }
+    ptx::mbar_init(ptx::smem_u32(&sh.hready), kEpiWarps);
     ptx::mbar_init_fence();
     sh.abort_flag = 0;
   }
@@ -293,166 +320,272 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
   ptx::tc_fence_after();
   const uint32_t base = ptx::smem_u32(smem), abase = base + ring * stage_bytes, tmem = sh.tmem;
   volatile uint32_t* abort_flag = &sh.abort_flag;
+  auto wait = [&](uint64_t* bar, uint32_t parity) { return ptx::bounded_wait(abort_flag, a.status, bar, parity, kSpinLimit); };
+  const int per = kProjTileN / a.rp;                  // adapters of one product `down x^T`
+  const bool adapters = a.n_seg != 0;
 
   if (warp == 0 && lane == 0) {
-    int it = 0;
-    for (int t = blockIdx.x; t < tiles; t += gridDim.x) {
-      const int tn = t % a.tiles_n, row0 = t / a.tiles_n * RT;
-      const uint8_t* w = a.w + (size_t)tn * a.stages * kBytesW;
-      for (int ks = 0; ks < a.stages; ++ks, ++it) {
-        const int s = it % ring;
-        if (!ptx::bounded_wait(abort_flag, a.status, &sh.empty[s], ((it / ring) & 1) ^ 1, kSpinLimit)) { t = tiles; break; }
-        const uint32_t st = base + s * stage_bytes, bar = ptx::smem_u32(&sh.full[s]);
-        ptx::mbar_expect_tx(bar, stage_bytes);
-        ptx::tile_g2s(st, &xmap, ks * kProjStage, row0, bar);
-        ptx::bulk_g2s(st + RT * kProjStage, w + (size_t)ks * kBytesW, kBytesW, bar);
+    int it = 0, ui = 0;
+    bool ok = true;
+    // room in the ring; the stage's x is asked for, `bytes` of weights come too
+    auto stage = [&](int ks, int row0, uint32_t bytes) {
+      const int s = it % ring;
+      ok = wait(&sh.empty[s], ((it / ring) & 1) ^ 1);
+      if (!ok) return base;
+      const uint32_t st = base + s * stage_bytes, bar = ptx::smem_u32(&sh.full[s]);
+      ptx::mbar_expect_tx(bar, RT * kProjStage + bytes);
+      ptx::tile_g2s(st, &xmap, ks * kProjStage, row0, bar);
+      return st;
+    };
+    for (int u = blockIdx.x; ok && u < shp.units; u += gridDim.x, ++ui) {
+      const int row0 = u / shp.chunks * RT, t0 = u % shp.chunks * shp.chunk, t1 = min(t0 + shp.chunk, a.tiles_n);
+      if (kFused && adapters) {
+        if (!(ok = wait(&sh.lready[ui & 1], (ui >> 1) & 1))) break;
+        const int n_list = sh.n_list[ui & 1];
+        for (int g = 0; ok && g < n_list; g += per) {
+          const int n = min(per, n_list - g);
+          for (int ks = 0; ks < a.stages; ++ks, ++it) {
+            const uint32_t st = stage(ks, row0, (uint32_t)(n * a.rp * kProjStage));
+            if (!ok) break;
+            for (int i = 0; i < n; ++i)
+              ptx::bulk_g2s(st + RT * kProjStage + i * a.rp * kProjStage,
+                            a.down + ((size_t)sh.list[ui & 1][g + i] * a.stages + ks) * a.rp * kProjStage,
+                            (uint32_t)(a.rp * kProjStage), ptx::smem_u32(&sh.full[it % ring]));
+          }
+        }
       }
+      for (int tn = t0; ok && tn < t1; ++tn)
+        for (int ks = 0; ks < a.stages; ++ks, ++it) {
+          const uint32_t st = stage(ks, row0, kBytesW);
+          if (!ok) break;
+          ptx::bulk_g2s(st + RT * kProjStage, a.w + ((size_t)tn * a.stages + ks) * kBytesW, kBytesW, ptx::smem_u32(&sh.full[it % ring]));
+        }
     }
   } else if (warp == 1 && lane == 0) {
     const uint32_t id = idesc((uint32_t)RT, a.x_unsigned), ida = idesc((uint32_t)RT, false);
     const uint32_t hhi = core_hi(128u);
-    int it = 0, ai = 0, ti = 0;
-    for (int t = blockIdx.x; t < tiles; t += gridDim.x, ++ti) {
-      if (!ptx::bounded_wait(abort_flag, a.status, &sh.tempty[ti & 1], ((ti >> 1) & 1) ^ 1, kSpinLimit)) break;
+    int it = 0, ai = 0, ti = 0, ui = 0;
+    bool ok = true;
+    auto product = [&]() {                              // one accumulator: all stages of K
+      ok = wait(&sh.tempty[ti & 1], ((ti >> 1) & 1) ^ 1);
+      if (!ok) return;
       ptx::tc_fence_after();
       const uint32_t d = tmem + (ti & 1) * RT;
-      bool ok = true;
       for (int ks = 0; ks < a.stages; ++ks, ++it) {
         const int s = it % ring;
-        if (!(ok = ptx::bounded_wait(abort_flag, a.status, &sh.full[s], (it / ring) & 1, kSpinLimit))) break;
+        if (!(ok = wait(&sh.full[s], (it / ring) & 1))) return;
         ptx::tc_fence_after();
         const uint32_t st = base + s * stage_bytes, alo = core_lo(st + RT * kProjStage), blo = ptx::umma_desc_lo(st, 16u);
         const int steps = min(4, (a.k - ks * kProjStage + 31) / 32);
         for (int k = 0; k < steps; ++k) ptx::umma_i8_hl(d, alo + k * 16, core_hi(1024u), blo + k * 2, kSwizzledHi, id, ks | k);
         ptx::umma_commit(ptx::smem_u32(&sh.empty[s]));
       }
-      if (a.n_seg) {
-        for (int last = 0; ok && !last; ++ai) {
-          if (!(ok = ptx::bounded_wait(abort_flag, a.status, &sh.afull[ai & 1], (ai >> 1) & 1, kSpinLimit))) break;
+    };
+    for (int u = blockIdx.x; ok && u < shp.units; u += gridDim.x, ++ui) {
+      const int t0 = u % shp.chunks * shp.chunk, t1 = min(t0 + shp.chunk, a.tiles_n);
+      if (kFused && adapters) {
+        if (!(ok = wait(&sh.lready[ui & 1], (ui >> 1) & 1))) break;
+        const int n_list = sh.n_list[ui & 1];
+        for (int g = 0; ok && g < n_list; g += per, ++ti) {
+          product();
+          if (ok) ptx::umma_commit(ptx::smem_u32(&sh.tfull[ti & 1]));
+        }
+      }
+      for (int tn = t0; ok && tn < t1; ++tn, ++ti) {
+        product();
+        const uint32_t d = tmem + (ti & 1) * RT;
+        for (int last = !adapters; ok && !last; ++ai) {
+          if (!(ok = wait(&sh.afull[ai & 1], (ai >> 1) & 1))) break;
           ptx::tc_fence_after();
-          const int msg = sh.message[ai & 1], steps = msg & 255;
+          const int msg = sh.message[ai & 1], steps = msg & 15, slices = (msg >> 4) & 15;
           last = msg & 256;
-          const uint32_t up = abase + (ai & 1) * abytes, h = up + kProjTileN * a.rp;
-          const uint32_t alo = core_lo(up), blo = ptx::umma_desc_lo(h, (uint32_t)RT * 16u);
-          for (int k = 0; k < steps; ++k) ptx::umma_i8_hl(d, alo + k * 16, core_hi(8u * a.rp), blo + k * 2 * RT, hhi, ida, 1u);
+          const uint32_t up = abase + (ai & 1) * shp.abytes, h = up + (uint32_t)(shp.step_adapters * kProjTileN * a.rp);
+          for (int i = 0; i < slices; ++i) {
+            const uint32_t alo = core_lo(up + (uint32_t)(i * kProjTileN * a.rp));
+            const uint32_t blo = ptx::umma_desc_lo(h + (uint32_t)(i * RT * a.rp), (uint32_t)RT * 16u);
+            for (int k = 0; k < steps; ++k) ptx::umma_i8_hl(d, alo + k * 16, core_hi(8u * a.rp), blo + k * 2 * RT, hhi, ida, 1u);
+          }
           ptx::umma_commit(ptx::smem_u32(&sh.aempty[ai & 1]));
         }
+        if (ok) ptx::umma_commit(ptx::smem_u32(&sh.tfull[ti & 1]));
       }
-      if (!ok) break;
-      ptx::umma_commit(ptx::smem_u32(&sh.tfull[ti & 1]));
     }
-  } else if (warp >= 4 && warp < 8 && a.n_seg) {
-    // one message per adapter of the tile, in ascending order of slots; an empty one where there is none
+  } else if (warp >= 4 && warp < 8 && adapters) {
+    // The adapters of each unit's rows, then for each of its output tiles the operands of their steps.
     const int f = tid - 128;
-    ptx::grid_dependency_wait();
-    int ai = 0, turn = 0;
-    bool ok = true;
-    for (int t = blockIdx.x; ok && t < tiles; t += gridDim.x) {
-      const int tn = t % a.tiles_n, row0 = t / a.tiles_n * RT;
-      int slot[2];
+    if (!kFused) ptx::grid_dependency_wait();
+    else if (blockIdx.x == 0)
+      for (int q = f; q < a.n_seg; q += kFill) look_over_request(a, q);
+    auto rows_of = [&](int u, int ui) {                 // slot, live, list and n_list of unit u
+      const int ub = ui & 1, row0 = u / shp.chunks * RT;
+      if (!fill_all(wait(&sh.lfree[ub], ((ui >> 1) & 1) ^ 1))) return false;
+      const bool scan = kFused && a.n_seg <= kScanRequests;
+      if (f == 0) sh.n_list[ub] = 0;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const int r = f + i * kFill;
-        slot[i] = r < RT && row0 + r < a.rows ? a.row_slot[row0 + r] : -1;
+        const int r = f + i * kFill, row = row0 + r;
+        if (r < RT) sh.slot[ub][r] = scan || row >= a.rows ? -2 : kFused ? slot_of_row(a, row) : a.row_slot[row];
       }
-      // the least slot above prev among the tile's rows; -2 for all threads if a wait of any of them gave up
-      auto next_slot = [&](int prev, bool fine) {
-        int m = fine ? INT_MAX : -2;
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          if (fine && slot[i] > prev) m = min(m, slot[i]);
-        m = __reduce_min_sync(0xFFFFFFFFu, m);
-        if (lane == 0) sh.least[turn][warp - 4] = m;
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        m = min(min(sh.least[turn][0], sh.least[turn][1]), min(sh.least[turn][2], sh.least[turn][3]));
-        turn ^= 1;
-        return m;
-      };
-      int cur = next_slot(-1, true);
-      for (bool last = false; !last; ++ai) {
-        const int ab = ai & 1, steps = cur == INT_MAX ? 0 : (a.rank[cur] + 31) / 32;
-        const int nxt = next_slot(cur, ptx::bounded_wait(abort_flag, a.status, &sh.aempty[ab], ((ai >> 1) & 1) ^ 1, kSpinLimit));
-        ok = nxt != -2;
-        if (!ok) break;
-        last = nxt == INT_MAX;
-        const uint32_t bar = ptx::smem_u32(&sh.afull[ab]), up = abase + ab * abytes, h = up + kProjTileN * a.rp;
-        if (f == 0) {
-          sh.message[ab] = steps | (last ? 256 : 0);
-          if (steps) {
-            ptx::mbar_expect_tx(bar, (uint32_t)(kProjTileN * a.rp));
-            ptx::bulk_g2s(up, a.up + ((size_t)cur * a.tiles_n + tn) * kProjTileN * a.rp, (uint32_t)(kProjTileN * a.rp), bar);
-          } else {
-            ptx::mbar_arrive(bar);
-          }
+      fill_all(true);
+      if (scan) {                                       // each request writes its rows of the tile: one trip to memory
+        for (int q = f; q < a.n_seg; q += kFill) {
+          const int s0 = a.seg_start[q], s1 = a.seg_start[q + 1], ad = a.seg_adapter[q];
+          const int lo = max(s0, row0), hi = min(min(s1, row0 + RT), a.rows);
+          if (lo >= hi) continue;
+          const int s = ad >= 0 && ad < a.max_adapters && a.rank[ad] > 0 ? ad : -1;
+          for (int r = lo; r < hi; ++r) sh.slot[ub][r - row0] = s;
         }
+        fill_all(true);
+      }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int r = f + i * kFill;
-          if (r < RT && steps) {
-            const int4* src = reinterpret_cast<const int4*>(a.h + (size_t)(row0 + r) * a.rp);
-            for (int c = 0; c < 2 * steps; ++c) {
-              const int4 v = slot[i] == cur ? src[c] : make_int4(0, 0, 0, 0);
-              *reinterpret_cast<int4*>(smem + (h - base) + (c * RT + r) * 16) = v;
+      for (int i = 0; i < 2; ++i) {
+        const int r = f + i * kFill, s = r < RT ? sh.slot[ub][r] : -2;
+        const uint32_t live = __ballot_sync(0xFFFFFFFFu, s != -2);
+        if (lane == 0 && r < RT) sh.live[ub][r >> 5] = live;
+        bool first = s >= 0 && (r == 0 || sh.slot[ub][r - 1] != s);
+        for (int e = 0; first && e < r; ++e) first = sh.slot[ub][e] != s;
+        if (first) sh.list[ub][atomicAdd(&sh.n_list[ub], 1)] = s;
+      }
+      fill_all(true);
+      ptx::mbar_arrive(ptx::smem_u32(&sh.lready[ub]));
+      return true;
+    };
+    int ai = 0, ui = 0, hi = 0;
+    bool ok = (int)blockIdx.x >= shp.units || rows_of(blockIdx.x, 0);
+    for (int u = blockIdx.x; ok && u < shp.units; u += gridDim.x, ++ui) {
+      const int row0 = u / shp.chunks * RT, t0 = u % shp.chunks * shp.chunk, t1 = min(t0 + shp.chunk, a.tiles_n), ub = ui & 1;
+      const int n_list = sh.n_list[ub];
+      int slot[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) slot[i] = f + i * kFill < RT ? sh.slot[ub][f + i * kFill] : -2;
+      if (u + (int)gridDim.x < shp.units && !(ok = rows_of(u + gridDim.x, ui + 1))) break;   // a unit ahead
+      if (kFused && n_list && !(ok = fill_all(wait(&sh.hready, hi++ & 1)))) break;
+      for (int tn = t0; ok && tn < t1; ++tn) {
+        int at = 0;
+        do {
+          const int ab = ai & 1, slices = min(shp.step_adapters, n_list - at);
+          if (!(ok = fill_all(wait(&sh.aempty[ab], ((ai >> 1) & 1) ^ 1)))) break;
+          ++ai;
+          int steps = 0;
+          for (int i = 0; i < slices; ++i) steps = max(steps, (a.rank[sh.list[ub][at + i]] + 31) / 32);
+          const uint32_t bar = ptx::smem_u32(&sh.afull[ab]), up = abase + ab * shp.abytes;
+          uint8_t* const h = smem + (up - base) + shp.step_adapters * kProjTileN * a.rp;
+          if (f == 0) {
+            sh.message[ab] = steps | slices << 4 | (at + slices >= n_list ? 256 : 0);
+            if (slices) {
+              const uint32_t bytes = (uint32_t)(kProjTileN * a.rp);
+              ptx::mbar_expect_tx(bar, slices * bytes);
+              for (int i = 0; i < slices; ++i)
+                ptx::bulk_g2s(up + i * bytes, a.up + ((size_t)sh.list[ub][at + i] * a.tiles_n + tn) * bytes, bytes, bar);
+            } else {
+              ptx::mbar_arrive(bar);
             }
           }
-        }
-        ptx::fence_async_smem();
-        ptx::mbar_arrive(bar);
-        cur = nxt;
+#pragma unroll
+          for (int r2 = 0; r2 < 2; ++r2) {
+            const int r = f + r2 * kFill;
+            if (r >= RT) continue;
+            const int4* src = reinterpret_cast<const int4*>(a.h + (size_t)(row0 + r) * a.rp);
+            for (int i = 0; i < slices; ++i) {
+              const bool mine = slot[r2] == sh.list[ub][at + i];
+              for (int c = 0; c < 2 * steps; ++c)
+                *reinterpret_cast<int4*>(h + ((i * (a.rp / 16) + c) * RT + r) * 16) = mine ? __ldcg(src + c) : make_int4(0, 0, 0, 0);
+            }
+          }
+          ptx::fence_async_smem();
+          ptx::mbar_arrive(bar);
+          at += slices;
+        } while (at < n_list);
       }
     }
   } else if (warp >= 8) {
     // A thread owns an output channel and walks over the rows. 8-bit results of 16 rows x 32 channels go through
     // 512 bytes of shared memory per warp, so that a row's 32 bytes leave in two 16-byte stores instead of 32.
-    const int q = warp & 3, half = (warp - 8) >> 2;
-    const int cols = RT >= 32 ? RT / 2 : (half == 0 ? RT : 0), c0 = RT >= 32 ? half * cols : 0;
+    const int q = warp & 3, cols = RT / (kEpiWarps / 4), c0 = ((warp - 8) >> 2) * cols;
     uint8_t* const stage = sh.out[warp - 8];
-    if (a.n_seg) ptx::grid_dependency_wait();
-    int ti = 0;
-    for (int t = blockIdx.x; t < tiles; t += gridDim.x, ++ti) {
-      const int n0 = t % a.tiles_n * kProjTileN + q * 32, n = n0 + lane, row0 = t / a.tiles_n * RT + c0;
-      const int4 rq = a.rq[n];
-      const long long add = (long long)(((unsigned long long)(uint32_t)rq.w << 32) | (uint32_t)rq.z);
-      const int shift = max(rq.y - 1, 0);
-      uint32_t live[4] = {0, 0, 0, 0};               // the rows that are written, a bit each
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = row0 + i * 32 + lane;
-        const bool w = i * 32 + lane < cols && row < a.rows && (!a.n_seg || a.row_slot[row] != -2);
-        live[i] = __ballot_sync(0xFFFFFFFFu, w);
-      }
-      if (!__all_sync(0xFFFFFFFFu, ptx::bounded_wait(abort_flag, a.status, &sh.tfull[ti & 1], (ti >> 1) & 1, kSpinLimit))) break;
+    int ti = 0, ui = 0;
+    bool ok = true;
+    auto sums = [&]() {
+      ok = __all_sync(0xFFFFFFFFu, wait(&sh.tfull[ti & 1], (ti >> 1) & 1));
       ptx::tc_fence_after();
-      const uint32_t d = tmem + ((uint32_t)(q * 32) << 16) + (ti & 1) * RT + c0;
-      YT* y = (YT*)a.y + (long long)row0 * a.ldy;
-      uint32_t v[16], w[16];
-      if (cols) ptx::tmem_ld16(d, v);
-#pragma unroll 2
-      for (int c = 0; c < cols; c += 16, y += 16 * a.ldy) {
-        ptx::tmem_ld_wait16(v);
-#pragma unroll
-        for (int e = 0; e < 16; ++e) w[e] = v[e];
-        if (c + 16 < cols) ptx::tmem_ld16(d + c + 16, v);
-        const uint32_t rows16 = live[c >> 5] >> (c & 16);
-        if (sizeof(YT) == 1 && shp.vector_y && n0 + 32 <= a.n) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) stage[e * 32 + lane] = (uint8_t)out_value<kAnyShift>((int)w[e], rq, add, shift, a.lo, a.hi);
-          __syncwarp();
-          const int4 o = *reinterpret_cast<const int4*>(stage + lane * 16);
-          if (rows16 >> (lane >> 1) & 1) *reinterpret_cast<int4*>(y + (lane >> 1) * a.ldy + n0 + (lane & 1) * 16) = o;
-          __syncwarp();
-        } else {
-          YT* p = y + n;
-#pragma unroll
-          for (int e = 0; e < 16; ++e, p += a.ldy) {
-            const int o = out_value<kAnyShift>((int)w[e], rq, add, shift, a.lo, a.hi);
-            if ((rows16 >> e & 1) && n < a.n) *p = (YT)o;
-          }
-        }
-      }
+      return tmem + ((uint32_t)(q * 32) << 16) + (ti & 1) * RT + c0;
+    };
+    auto done = [&](uint64_t* bar) {
       ptx::tc_fence_before();
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.tempty[ti & 1]));
+      if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(bar));
+    };
+    int4 rq_next = a.rq[(int)blockIdx.x % shp.chunks * shp.chunk * kProjTileN + q * 32 + lane];
+    for (int u = blockIdx.x; ok && u < shp.units; u += gridDim.x, ++ui) {
+      const int row0 = u / shp.chunks * RT, t0 = u % shp.chunks * shp.chunk, t1 = min(t0 + shp.chunk, a.tiles_n), ub = ui & 1;
+      if (adapters && !(ok = __all_sync(0xFFFFFFFFu, wait(&sh.lready[ub], (ui >> 1) & 1)))) break;
+      if (kFused && adapters) {
+        const int n_list = sh.n_list[ub], m = q * 32 + lane, j = m % a.rp;
+        for (int g = 0; ok && g < n_list; g += per, ++ti) {
+          const int i = g + m / a.rp;
+          const int slot = i < n_list ? sh.list[ub][i] : -3;
+          const bool used = slot >= 0 && j < a.rank[slot];
+          const int2 rq = used ? a.down_rq[slot * a.rp + j] : make_int2(1 << 30, 0);
+          const uint32_t d = sums();
+          if (!ok) break;
+          if (__any_sync(0xFFFFFFFFu, used)) {
+            for (int c = 0; c < cols; c += 16) {
+              uint32_t v[16];
+              ptx::tmem_ld16(d + c, v);
+              ptx::tmem_ld_wait16(v);
+              int8_t* h = a.h + (size_t)(row0 + c0 + c) * a.rp + j;
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                if (used && sh.slot[ub][c0 + c + e] == slot) h[e * a.rp] = rank_value((int)v[e], rq);
+            }
+          }
+          done(&sh.tempty[ti & 1]);
+        }
+        if (!ok) break;
+        if (n_list) {                                   // each warp's h is written: to the warps that lay it out
+          __syncwarp();
+          if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.hready));
+        }
+      }
+      for (int tn = t0; ok && tn < t1; ++tn, ++ti) {
+        const int n0 = tn * kProjTileN + q * 32, n = n0 + lane;
+        const int4 rq = rq_next;
+        {                                               // the next tile's constants
+          const int un = u + gridDim.x;
+          const int next = tn + 1 < t1 ? tn + 1 : un < shp.units ? un % shp.chunks * shp.chunk : tn;
+          rq_next = a.rq[next * kProjTileN + q * 32 + lane];
+        }
+        const long long add = (long long)(((unsigned long long)(uint32_t)rq.w << 32) | (uint32_t)rq.z);
+        const int shift = max(rq.y - 1, 0);
+        const uint32_t d = sums();
+        if (!ok) break;
+        YT* y = (YT*)a.y + (long long)(row0 + c0) * a.ldy;
+        for (int c = 0; c < cols; c += 16, y += 16 * a.ldy) {
+          uint32_t v[16];
+          ptx::tmem_ld16(d + c, v);
+          const int r = c0 + c, rest = a.rows - row0 - r;
+          uint32_t rows16 = rest >= 16 ? 0xFFFFu : rest > 0 ? (1u << rest) - 1 : 0;    // the rows that are written, a bit each
+          if (adapters) rows16 &= sh.live[ub][r >> 5] >> (r & 31);
+          ptx::tmem_ld_wait16(v);
+          if (sizeof(YT) == 1 && shp.vector_y && n0 + 32 <= a.n) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) stage[e * 32 + lane] = (uint8_t)out_value<kAnyShift>((int)v[e], rq, add, shift, a.lo, a.hi);
+            __syncwarp();
+            const int4 o = *reinterpret_cast<const int4*>(stage + lane * 16);
+            if (rows16 >> (lane >> 1) & 1) *reinterpret_cast<int4*>(y + (lane >> 1) * a.ldy + n0 + (lane & 1) * 16) = o;
+            __syncwarp();
+          } else {
+            YT* p = y + n;
+#pragma unroll
+            for (int e = 0; e < 16; ++e, p += a.ldy) {
+              const int o = out_value<kAnyShift>((int)v[e], rq, add, shift, a.lo, a.hi);
+              if ((rows16 >> e & 1) && n < a.n) *p = (YT)o;
+            }
+          }
+        }
+        done(&sh.tempty[ti & 1]);
+      }
+      if (ok && lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.lfree[ub]));
     }
   }
   __syncwarp();
@@ -469,6 +602,7 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
 constexpr int kSplitThreads = 256;       // warp 0 copies, 1 MMAs, 2 tensor memory, 4-7 send the sums; all finish rows
 constexpr int kSplitRing = 8;
 constexpr int kSplitRows = 128;          // rows of a tile at most
+constexpr int kDownRowsMost = 65536;     // rows x padded rank
 
 struct SplitShared {
   uint64_t full[kSplitRing], empty[kSplitRing], tfull;
@@ -608,18 +742,37 @@ __global__ void __launch_bounds__(kSplitThreads, 1) proj_split_kernel(const __gr
   }
 }
 
-constexpr int kMaxSmem = 221 * 1024;      // beside 1 KB of alignment and the static part
+constexpr int kMaxSmem = 213 * 1024;      // beside 1 KB of alignment and the static part
 
-// Rows of a tile of the kernel for few rows: 0 where its tiles would be more than the SMs.
+// Rows of a tile of the kernel for few rows: 0 where its tiles would be more than the SMs, or h too much for down_rows_kernel.
 int split_tile(const ProjArgs& a) {
   int t = 16;
   while (t < kSplitRows && t < a.rows) t *= 2;
+  if (a.n_seg && (long long)a.rows * a.rp > kDownRowsMost) return 0;
   return (long long)a.tiles_n * ((a.rows + t - 1) / t) <= a.sms ? t : 0;
+}
+
+// h within the projection's own kernel, or before it.
+bool fuse_down(const ProjArgs& a) { return a.stages <= 8; }
+
+// Output tiles of a unit: the most that cost the least, in items of a whole round of the SMs (a unit has one more item with adapters).
+int fused_chunk(const ProjArgs& a, int row_tiles) {
+  int best = 1;
+  long long least = LLONG_MAX;
+  for (int c = 1; c <= a.tiles_n; ++c) {
+    const long long units = (long long)row_tiles * ((a.tiles_n + c - 1) / c);
+    const long long cost = (units + a.sms - 1) / a.sms * (c + (a.n_seg ? 1 : 0));
+    if (cost <= least) {
+      least = cost;
+      best = c;
+    }
+  }
+  return best;
 }
 
 template <class Shape>
 cudaError_t launch_tiles(void (*kernel)(CUtensorMap, ProjArgs, Shape), const ProjArgs& a, const CUtensorMap& map, const Shape& s, int grid,
-                         int cluster, int threads, size_t smem, cudaStream_t stream) {
+                         int cluster, int threads, size_t smem, bool follows_down, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3((unsigned)threads);
@@ -632,7 +785,7 @@ cudaError_t launch_tiles(void (*kernel)(CUtensorMap, ProjArgs, Shape), const Pro
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = a.n_seg ? 2 : 1;                   // follows the kernel that computes h
+  cfg.numAttrs = a.n_seg && follows_down ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kernel, map, a, s);
 }
 
@@ -648,21 +801,29 @@ cudaError_t launch_main(const ProjArgs& a, const CUtensorMap& map, cudaStream_t 
     const int sums = tile * kProjTileN * 4, most = (a.stages + s.parts - 1) / s.parts;
     s.ring = std::min(std::min(kSplitRing, most), (kMaxSmem - sums) / stage);
     s.vector_y = a.ldy % 4 == 0 && y % (4 * a.y_bytes) == 0;
-    return launch_tiles(proj_split_kernel<YT, kAnyShift>, a, map, s, tiles * s.parts, s.parts, kSplitThreads, (size_t)(s.ring * stage + sums + 1024), stream);
+    return launch_tiles(proj_split_kernel<YT, kAnyShift>, a, map, s, tiles * s.parts, s.parts, kSplitThreads, (size_t)(s.ring * stage + sums + 1024), true, stream);
   }
   MainShape s;
   s.tile = tile;
-  s.tmem_cols = std::max(32, 2 * tile);
+  s.tmem_cols = 2 * tile;
   s.vector_y = a.y_bytes == 1 && a.ldy % 16 == 0 && y % 16 == 0;
-  const int ab = a.n_seg ? 2 * (kProjTileN + tile) * a.rp : 0;
+  s.step_adapters = a.rp == 32 ? 2 : 1;
+  s.abytes = (kProjTileN + tile) * std::max(a.rp, 64);
+  const int ab = a.n_seg ? 2 * s.abytes : 0, row_tiles = (a.rows + tile - 1) / tile;
   s.ring = std::min(kMaxRing, (kMaxSmem - ab) / stage);
-  return launch_tiles(proj_tile_kernel<YT, kAnyShift>, a, map, s, std::min(tiles, a.sms), 1, kMainThreads, (size_t)(s.ring * stage + ab + 1024), stream);
+  const bool fused = fuse_down(a);
+  s.chunk = fused ? fused_chunk(a, row_tiles) : 1;
+  s.chunks = (a.tiles_n + s.chunk - 1) / s.chunk;
+  s.units = row_tiles * s.chunks;
+  return launch_tiles(fused ? proj_tile_kernel<YT, kAnyShift, true> : proj_tile_kernel<YT, kAnyShift, false>, a, map, s,
+                      std::min(s.units, a.sms), 1, kMainThreads, (size_t)(s.ring * stage + ab + 1024), !fused, stream);
 }
 
 template <class YT, bool kAnyShift>
 cudaError_t configure() {
   const auto attr = cudaFuncAttributeMaxDynamicSharedMemorySize;
-  cudaError_t e = cudaFuncSetAttribute(proj_tile_kernel<YT, kAnyShift>, attr, kMaxSmem + 1024);
+  cudaError_t e = cudaFuncSetAttribute(proj_tile_kernel<YT, kAnyShift, false>, attr, kMaxSmem + 1024);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(proj_tile_kernel<YT, kAnyShift, true>, attr, kMaxSmem + 1024);
   return e == cudaSuccess ? cudaFuncSetAttribute(proj_split_kernel<YT, kAnyShift>, attr, kMaxSmem + 1024) : e;
 }
 
@@ -680,14 +841,14 @@ cudaError_t configure_proj_kernels() {
 // In the persistent kernel the widest tile that still gives every SM one.
 int proj_row_tile(const ProjArgs& a) {
   if (const int split = split_tile(a)) return split;
-  int t = 256;
-  while (t > 16 && (t / 2 >= a.rows || (t > 64 && (long long)a.tiles_n * ((a.rows + t - 1) / t) < a.sms))) t /= 2;
+  int t = kMaxTile;
+  while (t > 64 && (t / 2 >= a.rows || (long long)a.tiles_n * ((a.rows + t - 1) / t) < a.sms)) t /= 2;
   return t;
 }
 
 cudaError_t launch_proj(const ProjArgs& a, const void* x_map, const void* x_map_down, cudaStream_t stream) {
-  if (a.n_seg) {
-    if ((long long)a.rows * a.rp <= 16384) {
+  if (a.n_seg && (split_tile(a) || !fuse_down(a))) {
+    if ((long long)a.rows * a.rp <= kDownRowsMost) {
       const dim3 grid((unsigned)a.rows, (unsigned)(a.rp / 8));
       if (a.x_unsigned) down_rows_kernel<true><<<grid, 128, 0, stream>>>(a);
       else down_rows_kernel<false><<<grid, 128, 0, stream>>>(a);
