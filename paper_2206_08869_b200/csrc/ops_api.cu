@@ -161,7 +161,7 @@ int create_proj(const iodf_proj_desc& d, const int8_t* weights, size_t wn, const
   uint8_t* m = static_cast<uint8_t*>(p.d_mem);
   e = cudaMemcpy(m + o_w, wp.data(), wp.size(), cudaMemcpyHostToDevice);
   if (e == cudaSuccess) e = cudaMemcpy(m + o_rq, rq.data(), 16 * rq.size(), cudaMemcpyHostToDevice);
-  if (e == cudaSuccess) e = cudaMemset(m + o_rank, 0, std::max<size_t>(4 * slots, 1));
+  if (e == cudaSuccess) e = cudaMemset(m + o_down, 0, o_h - o_down);     // an empty slot adds nothing: all zeros
   if (e == cudaSuccess) e = cudaMemset(m + o_status, 0, 8);
   if (e == cudaSuccess) e = cudaStreamSynchronize(0);        // the first call may be on a stream that does not wait for it
   if (e != cudaSuccess) return status_of(e);

@@ -41,6 +41,29 @@ __device__ __forceinline__ uint32_t core_lo(uint32_t saddr) { return ptx::umma_d
 __device__ __forceinline__ uint32_t core_hi(uint32_t sbo) { return (sbo >> 4) | (1u << 14); }
 constexpr uint32_t kSwizzledHi = (1024u >> 4) | (1u << 14) | (2u << 29);   // rows of 128 bytes, 128-byte swizzle
 
+// Slot and phase of a ring of barriers, counted (a modulus costs some 70 ns).
+struct Turn {
+  int slot = 0;
+  uint32_t phase = 0;
+  __device__ __forceinline__ void next(int size) {
+    if (++slot == size) {
+      slot = 0;
+      phase ^= 1u;
+    }
+  }
+};
+
+// The MMAs of a stage: up to four steps of 32 channels, both operands K-major (x with the 128-byte swizzle).
+__device__ __forceinline__ void stage_mmas(uint32_t d, uint32_t alo, uint32_t blo, uint32_t id, int steps, bool first) {
+  ptx::umma_i8_hl(d, alo, core_hi(1024u), blo, kSwizzledHi, id, first ? 0u : 1u);
+  if (steps == 4) {
+#pragma unroll
+    for (int k = 1; k < 4; ++k) ptx::umma_i8_hl(d, alo + k * 16, core_hi(1024u), blo + k * 2, kSwizzledHi, id, 1u);
+  } else {
+    for (int k = 1; k < steps; ++k) ptx::umma_i8_hl(d, alo + k * 16, core_hi(1024u), blo + k * 2, kSwizzledHi, id, 1u);
+  }
+}
+
 template <bool kUnsigned>
 __device__ __forceinline__ int dot4(int w, int x, int acc) {
   if (kUnsigned) asm("dp4a.s32.u32 %0, %1, %2, %3;" : "=r"(acc) : "r"(w), "r"(x), "r"(acc));
@@ -74,7 +97,7 @@ __device__ __forceinline__ int slot_of_row(const ProjArgs& a, int row) {
   }
   if (row < a.seg_start[lo] || row >= a.seg_start[lo + 1]) return -2;
   const int s = a.seg_adapter[lo];
-  return s >= 0 && s < a.max_adapters && a.rank[s] > 0 ? s : -1;
+  return s >= 0 && s < a.max_adapters ? s : -1;
 }
 
 __device__ __forceinline__ void look_over_request(const ProjArgs& a, int q) {
@@ -88,6 +111,22 @@ __device__ __forceinline__ void look_over_requests(const ProjArgs& a) {
 __device__ __forceinline__ int8_t rank_value(int acc, int2 q) {
   const int v = (int)(((long long)acc * q.x + (1ll << (30 + q.y))) >> (31 + q.y));
   return (int8_t)min(max(v, -128), 127);
+}
+
+// h of 16 rows for one rank channel of adapter `slot`, in the rows that use it. slots: 16-byte aligned, shared memory.
+__device__ __forceinline__ void store_rank(int8_t* h, int rp, const uint32_t (&v)[16], int2 q, int slot, const int* slots) {
+  int s[16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int4 t = reinterpret_cast<const int4*>(slots)[i];
+    s[4 * i] = t.x; s[4 * i + 1] = t.y; s[4 * i + 2] = t.z; s[4 * i + 3] = t.w;
+  }
+  const long long round = 1ll << (30 + q.y);
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const int o = min(max((int)(((long long)(int)v[e] * q.x + round) >> (31 + q.y)), -128), 127);
+    if (s[e] == slot) h[e * rp] = (int8_t)o;
+  }
 }
 
 // ---- h for few rows: a block per row and eight rank channels, a quarter of K per warp ----------------------
@@ -125,7 +164,8 @@ struct DownShared {
   uint64_t full[kDownRing], empty[kDownRing], dfull, dempty;
   uint32_t abort_flag, tmem;
   int n_slots;
-  int slot[kDownRows], list[kDownRows];
+  alignas(16) int slot[kDownRows];
+  int list[kDownRows];
 };
 
 __global__ void __launch_bounds__(kDownThreads) down_tile_kernel(const __grid_constant__ CUtensorMap xmap, const ProjArgs a, const int ring) {
@@ -158,7 +198,7 @@ __global__ void __launch_bounds__(kDownThreads) down_tile_kernel(const __grid_co
       const int s0 = a.seg_start[q], s1 = a.seg_start[q + 1], ad = a.seg_adapter[q];
       const int lo = max(s0, row0), hi = min(min(s1, row0 + kDownRows), a.rows);
       if (lo >= hi) continue;
-      const int s = ad >= 0 && ad < a.max_adapters && a.rank[ad] > 0 ? ad : -1;
+      const int s = ad >= 0 && ad < a.max_adapters ? ad : -1;
       for (int r = lo; r < hi; ++r) sh.slot[r - row0] = s;
     }
     __syncthreads();
@@ -176,13 +216,13 @@ __global__ void __launch_bounds__(kDownThreads) down_tile_kernel(const __grid_co
   const uint32_t base = ptx::smem_u32(smem), tmem = sh.tmem;
   volatile uint32_t* abort_flag = &sh.abort_flag;
 
-  if (warp == 0 && lane == 0) {
-    int it = 0;
+  if (warp == 0 && ptx::elect_one()) {
+    Turn turn;
     for (int g = 0; g < groups; ++g) {
       const int n = min(per, n_slots - g * per);
-      for (int ks = 0; ks < a.stages; ++ks, ++it) {
-        const int s = it % ring;
-        if (!ptx::bounded_wait(abort_flag, a.status, &sh.empty[s], ((it / ring) & 1) ^ 1, kSpinLimit)) { g = groups; break; }
+      for (int ks = 0; ks < a.stages; ++ks, turn.next(ring)) {
+        const int s = turn.slot;
+        if (!ptx::quick_wait(abort_flag, a.status, &sh.empty[s], turn.phase ^ 1, kSpinLimit)) { g = groups; break; }
         const uint32_t st = base + s * kDownStageBytes, bar = ptx::smem_u32(&sh.full[s]);
         ptx::mbar_expect_tx(bar, (uint32_t)(kDownRows * kProjStage + n * a.rp * kProjStage));
         ptx::tile_g2s(st, &xmap, ks * kProjStage, row0, bar);
@@ -191,20 +231,18 @@ __global__ void __launch_bounds__(kDownThreads) down_tile_kernel(const __grid_co
                         a.down + ((size_t)sh.list[g * per + i] * a.stages + ks) * a.rp * kProjStage, (uint32_t)(a.rp * kProjStage), bar);
       }
     }
-  } else if (warp == 1 && lane == 0) {
+  } else if (warp == 1 && ptx::elect_one()) {
     const uint32_t id = idesc(kDownRows, a.x_unsigned);
-    int it = 0;
+    Turn turn;
     for (int g = 0; g < groups; ++g) {
-      if (!ptx::bounded_wait(abort_flag, a.status, &sh.dempty, (g & 1) ^ 1, kSpinLimit)) break;
+      if (!ptx::quick_wait(abort_flag, a.status, &sh.dempty, (g & 1) ^ 1, kSpinLimit)) break;
       ptx::tc_fence_after();
-      for (int ks = 0; ks < a.stages; ++ks, ++it) {
-        const int s = it % ring;
-        if (!ptx::bounded_wait(abort_flag, a.status, &sh.full[s], (it / ring) & 1, kSpinLimit)) { g = groups; break; }
+      for (int ks = 0; ks < a.stages; ++ks, turn.next(ring)) {
+        const int s = turn.slot;
+        if (!ptx::quick_wait(abort_flag, a.status, &sh.full[s], turn.phase, kSpinLimit)) { g = groups; break; }
         ptx::tc_fence_after();
-        const uint32_t st = base + s * kDownStageBytes, alo = core_lo(st + kDownRows * kProjStage), blo = ptx::umma_desc_lo(st, 16u);
-        const int steps = min(4, (a.k - ks * kProjStage + 31) / 32);
-        for (int k = 0; k < steps; ++k)
-          ptx::umma_i8_hl(tmem, alo + k * 16, core_hi(1024u), blo + k * 2, kSwizzledHi, id, ks | k);
+        const uint32_t st = base + s * kDownStageBytes;
+        stage_mmas(tmem, core_lo(st + kDownRows * kProjStage), ptx::umma_desc_lo(st, 16u), id, min(4, (a.k - ks * kProjStage + 31) >> 5), ks == 0);
         ptx::umma_commit(ptx::smem_u32(&sh.empty[s]));
       }
       ptx::umma_commit(ptx::smem_u32(&sh.dfull));
@@ -214,18 +252,16 @@ __global__ void __launch_bounds__(kDownThreads) down_tile_kernel(const __grid_co
     for (int g = 0; g < groups; ++g) {
       const int i = g * per + m / a.rp;
       const int slot = i < n_slots ? sh.list[i] : -3;
-      const bool used = slot >= 0 && j < a.rank[slot];
+      const bool used = slot >= 0;
       const int2 rq = used ? a.down_rq[slot * a.rp + j] : make_int2(1 << 30, 0);
-      if (!__all_sync(0xFFFFFFFFu, ptx::bounded_wait(abort_flag, a.status, &sh.dfull, g & 1, kSpinLimit))) break;
+      if (!__all_sync(0xFFFFFFFFu, ptx::quick_wait(abort_flag, a.status, &sh.dfull, g & 1, kSpinLimit))) break;
       ptx::tc_fence_after();
       if (__any_sync(0xFFFFFFFFu, used)) {
         for (int c = half * (kDownRows / 2); c < (half + 1) * (kDownRows / 2); c += 16) {
           uint32_t v[16];
           ptx::tmem_ld16(tmem + ((uint32_t)(q * 32) << 16) + c, v);
           ptx::tmem_ld_wait16(v);
-#pragma unroll
-          for (int e = 0; e < 16; ++e)
-            if (used && sh.slot[c + e] == slot) a.h[(size_t)(row0 + c + e) * a.rp + j] = rank_value((int)v[e], rq);
+          store_rank(a.h + (size_t)(row0 + c) * a.rp + j, a.rp, v, rq, slot, sh.slot + c);
         }
       }
       ptx::tc_fence_before();
@@ -250,9 +286,10 @@ constexpr int kMaxTile = 256;
 struct MainShared {
   uint64_t full[kMaxRing], empty[kMaxRing], afull[2], aempty[2], tfull[2], tempty[2], lready[2], lfree[2], hready;
   uint32_t abort_flag, tmem;
-  int message[2];                        // an adapter step: adapters << 4 | 32-channel steps of each, 256: the tile's last
+  int message[2];                        // an adapter step: its adapters, 256: the tile's last
   int n_list[2];
-  int slot[2][kMaxTile], list[2][kMaxTile];   // of a unit: adapter of each row, every adapter once
+  alignas(16) int slot[2][kMaxTile];     // of a unit: adapter of each row
+  int list[2][kMaxTile];                 //            every adapter once
   uint32_t live[2][kMaxTile / 32];       // of a unit: the rows that some request owns
   alignas(16) uint8_t out[kEpiWarps][512];
 };
@@ -320,17 +357,18 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
   ptx::tc_fence_after();
   const uint32_t base = ptx::smem_u32(smem), abase = base + ring * stage_bytes, tmem = sh.tmem;
   volatile uint32_t* abort_flag = &sh.abort_flag;
-  auto wait = [&](uint64_t* bar, uint32_t parity) { return ptx::bounded_wait(abort_flag, a.status, bar, parity, kSpinLimit); };
+  auto wait = [&](uint64_t* bar, uint32_t parity) { return ptx::quick_wait(abort_flag, a.status, bar, parity, kSpinLimit); };
   const int per = kProjTileN / a.rp;                  // adapters of one product `down x^T`
   const bool adapters = a.n_seg != 0;
 
-  if (warp == 0 && lane == 0) {
-    int it = 0, ui = 0;
+  if (warp == 0 && ptx::elect_one()) {
+    Turn turn;
+    int ui = 0;
     bool ok = true;
     // room in the ring; the stage's x is asked for, `bytes` of weights come too
     auto stage = [&](int ks, int row0, uint32_t bytes) {
-      const int s = it % ring;
-      ok = wait(&sh.empty[s], ((it / ring) & 1) ^ 1);
+      const int s = turn.slot;
+      ok = wait(&sh.empty[s], turn.phase ^ 1);
       if (!ok) return base;
       const uint32_t st = base + s * stage_bytes, bar = ptx::smem_u32(&sh.full[s]);
       ptx::mbar_expect_tx(bar, RT * kProjStage + bytes);
@@ -344,40 +382,40 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         const int n_list = sh.n_list[ui & 1];
         for (int g = 0; ok && g < n_list; g += per) {
           const int n = min(per, n_list - g);
-          for (int ks = 0; ks < a.stages; ++ks, ++it) {
+          for (int ks = 0; ks < a.stages; ++ks, turn.next(ring)) {
             const uint32_t st = stage(ks, row0, (uint32_t)(n * a.rp * kProjStage));
             if (!ok) break;
             for (int i = 0; i < n; ++i)
               ptx::bulk_g2s(st + RT * kProjStage + i * a.rp * kProjStage,
                             a.down + ((size_t)sh.list[ui & 1][g + i] * a.stages + ks) * a.rp * kProjStage,
-                            (uint32_t)(a.rp * kProjStage), ptx::smem_u32(&sh.full[it % ring]));
+                            (uint32_t)(a.rp * kProjStage), ptx::smem_u32(&sh.full[turn.slot]));
           }
         }
       }
       for (int tn = t0; ok && tn < t1; ++tn)
-        for (int ks = 0; ks < a.stages; ++ks, ++it) {
+        for (int ks = 0; ks < a.stages; ++ks, turn.next(ring)) {
           const uint32_t st = stage(ks, row0, kBytesW);
           if (!ok) break;
-          ptx::bulk_g2s(st + RT * kProjStage, a.w + ((size_t)tn * a.stages + ks) * kBytesW, kBytesW, ptx::smem_u32(&sh.full[it % ring]));
+          ptx::bulk_g2s(st + RT * kProjStage, a.w + ((size_t)tn * a.stages + ks) * kBytesW, kBytesW, ptx::smem_u32(&sh.full[turn.slot]));
         }
     }
-  } else if (warp == 1 && lane == 0) {
+  } else if (warp == 1 && ptx::elect_one()) {
     const uint32_t id = idesc((uint32_t)RT, a.x_unsigned), ida = idesc((uint32_t)RT, false);
     const uint32_t hhi = core_hi(128u);
-    int it = 0, ai = 0, ti = 0, ui = 0;
+    Turn turn;
+    int ai = 0, ti = 0, ui = 0;
     bool ok = true;
     auto product = [&]() {                              // one accumulator: all stages of K
       ok = wait(&sh.tempty[ti & 1], ((ti >> 1) & 1) ^ 1);
       if (!ok) return;
       ptx::tc_fence_after();
       const uint32_t d = tmem + (ti & 1) * RT;
-      for (int ks = 0; ks < a.stages; ++ks, ++it) {
-        const int s = it % ring;
-        if (!(ok = wait(&sh.full[s], (it / ring) & 1))) return;
+      for (int ks = 0; ks < a.stages; ++ks, turn.next(ring)) {
+        const int s = turn.slot;
+        if (!(ok = wait(&sh.full[s], turn.phase))) return;
         ptx::tc_fence_after();
-        const uint32_t st = base + s * stage_bytes, alo = core_lo(st + RT * kProjStage), blo = ptx::umma_desc_lo(st, 16u);
-        const int steps = min(4, (a.k - ks * kProjStage + 31) / 32);
-        for (int k = 0; k < steps; ++k) ptx::umma_i8_hl(d, alo + k * 16, core_hi(1024u), blo + k * 2, kSwizzledHi, id, ks | k);
+        const uint32_t st = base + s * stage_bytes;
+        stage_mmas(d, core_lo(st + RT * kProjStage), ptx::umma_desc_lo(st, 16u), id, min(4, (a.k - ks * kProjStage + 31) >> 5), ks == 0);
         ptx::umma_commit(ptx::smem_u32(&sh.empty[s]));
       }
     };
@@ -397,13 +435,13 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         for (int last = !adapters; ok && !last; ++ai) {
           if (!(ok = wait(&sh.afull[ai & 1], (ai >> 1) & 1))) break;
           ptx::tc_fence_after();
-          const int msg = sh.message[ai & 1], steps = msg & 15, slices = (msg >> 4) & 15;
+          const int msg = sh.message[ai & 1], slices = msg & 15;
           last = msg & 256;
           const uint32_t up = abase + (ai & 1) * shp.abytes, h = up + (uint32_t)(shp.step_adapters * kProjTileN * a.rp);
           for (int i = 0; i < slices; ++i) {
             const uint32_t alo = core_lo(up + (uint32_t)(i * kProjTileN * a.rp));
             const uint32_t blo = ptx::umma_desc_lo(h + (uint32_t)(i * RT * a.rp), (uint32_t)RT * 16u);
-            for (int k = 0; k < steps; ++k) ptx::umma_i8_hl(d, alo + k * 16, core_hi(8u * a.rp), blo + k * 2 * RT, hhi, ida, 1u);
+            for (int k = 0; k < a.rp / 32; ++k) ptx::umma_i8_hl(d, alo + k * 16, core_hi(8u * a.rp), blo + k * 2 * RT, hhi, ida, 1u);
           }
           ptx::umma_commit(ptx::smem_u32(&sh.aempty[ai & 1]));
         }
@@ -432,7 +470,7 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
           const int s0 = a.seg_start[q], s1 = a.seg_start[q + 1], ad = a.seg_adapter[q];
           const int lo = max(s0, row0), hi = min(min(s1, row0 + RT), a.rows);
           if (lo >= hi) continue;
-          const int s = ad >= 0 && ad < a.max_adapters && a.rank[ad] > 0 ? ad : -1;
+          const int s = ad >= 0 && ad < a.max_adapters ? ad : -1;
           for (int r = lo; r < hi; ++r) sh.slot[ub][r - row0] = s;
         }
         fill_all(true);
@@ -466,12 +504,10 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
           const int ab = ai & 1, slices = min(shp.step_adapters, n_list - at);
           if (!(ok = fill_all(wait(&sh.aempty[ab], ((ai >> 1) & 1) ^ 1)))) break;
           ++ai;
-          int steps = 0;
-          for (int i = 0; i < slices; ++i) steps = max(steps, (a.rank[sh.list[ub][at + i]] + 31) / 32);
           const uint32_t bar = ptx::smem_u32(&sh.afull[ab]), up = abase + ab * shp.abytes;
           uint8_t* const h = smem + (up - base) + shp.step_adapters * kProjTileN * a.rp;
           if (f == 0) {
-            sh.message[ab] = steps | slices << 4 | (at + slices >= n_list ? 256 : 0);
+            sh.message[ab] = slices | (at + slices >= n_list ? 256 : 0);
             if (slices) {
               const uint32_t bytes = (uint32_t)(kProjTileN * a.rp);
               ptx::mbar_expect_tx(bar, slices * bytes);
@@ -488,7 +524,7 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
             const int4* src = reinterpret_cast<const int4*>(a.h + (size_t)(row0 + r) * a.rp);
             for (int i = 0; i < slices; ++i) {
               const bool mine = slot[r2] == sh.list[ub][at + i];
-              for (int c = 0; c < 2 * steps; ++c)
+              for (int c = 0; c < a.rp / 16; ++c)
                 *reinterpret_cast<int4*>(h + ((i * (a.rp / 16) + c) * RT + r) * 16) = mine ? __ldcg(src + c) : make_int4(0, 0, 0, 0);
             }
           }
@@ -524,7 +560,7 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         for (int g = 0; ok && g < n_list; g += per, ++ti) {
           const int i = g + m / a.rp;
           const int slot = i < n_list ? sh.list[ub][i] : -3;
-          const bool used = slot >= 0 && j < a.rank[slot];
+          const bool used = slot >= 0;
           const int2 rq = used ? a.down_rq[slot * a.rp + j] : make_int2(1 << 30, 0);
           const uint32_t d = sums();
           if (!ok) break;
@@ -533,10 +569,7 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
               uint32_t v[16];
               ptx::tmem_ld16(d + c, v);
               ptx::tmem_ld_wait16(v);
-              int8_t* h = a.h + (size_t)(row0 + c0 + c) * a.rp + j;
-#pragma unroll
-              for (int e = 0; e < 16; ++e)
-                if (used && sh.slot[ub][c0 + c + e] == slot) h[e * a.rp] = rank_value((int)v[e], rq);
+              store_rank(a.h + (size_t)(row0 + c0 + c) * a.rp + j, a.rp, v, rq, slot, sh.slot[ub] + c0 + c);
             }
           }
           done(&sh.tempty[ti & 1]);
@@ -647,25 +680,26 @@ __global__ void __launch_bounds__(kSplitThreads, 1) proj_split_kernel(const __gr
   const int* const sums = reinterpret_cast<const int*>(smem + ring * stage_bytes);   // [parts][own][128]
   volatile uint32_t* abort_flag = &sh.abort_flag;
 
-  if (warp == 0 && lane == 0) {
+  if (warp == 0 && ptx::elect_one()) {
     const uint8_t* w = a.w + (size_t)tn * a.stages * kBytesW;
-    for (int ks = k0; ks < k1; ++ks) {
-      const int it = ks - k0, s = it % ring;
-      if (!ptx::bounded_wait(abort_flag, a.status, &sh.empty[s], ((it / ring) & 1) ^ 1, kSpinLimit)) break;
+    Turn turn;
+    for (int ks = k0; ks < k1; ++ks, turn.next(ring)) {
+      const int s = turn.slot;
+      if (!ptx::quick_wait(abort_flag, a.status, &sh.empty[s], turn.phase ^ 1, kSpinLimit)) break;
       const uint32_t st = base + s * stage_bytes, bar = ptx::smem_u32(&sh.full[s]);
       ptx::mbar_expect_tx(bar, stage_bytes);
       ptx::bulk_g2s(st + RT * kProjStage, w + (size_t)ks * kBytesW, kBytesW, bar);
       ptx::tile_g2s(st, &xmap, ks * kProjStage, row0, bar);
     }
-  } else if (warp == 1 && lane == 0) {
+  } else if (warp == 1 && ptx::elect_one()) {
     const uint32_t id = idesc((uint32_t)RT, a.x_unsigned);
-    for (int ks = k0; ks < k1; ++ks) {
-      const int it = ks - k0, s = it % ring;
-      if (!ptx::bounded_wait(abort_flag, a.status, &sh.full[s], (it / ring) & 1, kSpinLimit)) break;
+    Turn turn;
+    for (int ks = k0; ks < k1; ++ks, turn.next(ring)) {
+      const int s = turn.slot;
+      if (!ptx::quick_wait(abort_flag, a.status, &sh.full[s], turn.phase, kSpinLimit)) break;
       ptx::tc_fence_after();
-      const uint32_t st = base + s * stage_bytes, alo = core_lo(st + RT * kProjStage), blo = ptx::umma_desc_lo(st, 16u);
-      const int steps = min(4, (a.k - ks * kProjStage + 31) / 32);
-      for (int k = 0; k < steps; ++k) ptx::umma_i8_hl(tmem, alo + k * 16, core_hi(1024u), blo + k * 2, kSwizzledHi, id, it | k);
+      const uint32_t st = base + s * stage_bytes;
+      stage_mmas(tmem, core_lo(st + RT * kProjStage), ptx::umma_desc_lo(st, 16u), id, min(4, (a.k - ks * kProjStage + 31) >> 5), ks == k0);
       ptx::umma_commit(ptx::smem_u32(&sh.empty[s]));
     }
     ptx::umma_commit(ptx::smem_u32(&sh.tfull));
@@ -673,7 +707,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) proj_split_kernel(const __gr
     const int q = warp & 3;
     ptx::cluster_wait();
     const uint32_t dst = ptx::smem_u32(sums) + (uint32_t)(part * own * kProjTileN + q * 32 + lane) * 4u;
-    if (__all_sync(0xFFFFFFFFu, ptx::bounded_wait(abort_flag, a.status, &sh.tfull, 0u, kSpinLimit))) {
+    if (__all_sync(0xFFFFFFFFu, ptx::quick_wait(abort_flag, a.status, &sh.tfull, 0u, kSpinLimit))) {
       ptx::tc_fence_after();
       for (int c = 0; c < RT; c += 16) {
         uint32_t v[16];
