@@ -171,6 +171,7 @@ int create_proj(const iodf_proj_desc& d, const int8_t* weights, size_t wn, const
   a.stages = (int)stages;
   a.tiles_n = (int)tiles;
   a.x_unsigned = d.x_type == IODF_U8;
+  a.y_type = (int)d.y_type;
   a.y_bytes = d.y_type == IODF_I32 ? 4 : 1;
   a.lo = lo;
   a.hi = hi;

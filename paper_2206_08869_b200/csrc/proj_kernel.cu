@@ -14,6 +14,7 @@
 
 #include <algorithm>
 
+#include "../../include/iodf.h"
 #include "iodf_dev.h"
 #include "ptx.cuh"
 
@@ -291,7 +292,7 @@ struct MainShared {
   alignas(16) int slot[2][kMaxTile];     // of a unit: adapter of each row
   int list[2][kMaxTile];                 //            every adapter once
   uint32_t live[2][kMaxTile / 32];       // of a unit: the rows that some request owns
-  alignas(16) uint8_t out[kEpiWarps][512];
+  alignas(16) uint32_t out[kEpiWarps][128];
 };
 
 struct MainShape {
@@ -302,16 +303,30 @@ struct MainShape {
   int units;
   int abytes;                            // an adapter step's operands: `up`, h
   int step_adapters;                     // adapters of a step
-  int vector_y;                          // 8-bit rows of y lie on 16-byte boundaries
+  int vector_y;                          // 8-bit rows of y lie on 4-byte boundaries
+  int clip;                              // the clip is narrower than the output's type
 };
 
-// clip((acc M0 + addend) >> (31 + s)): the high word of a multiply-add, shifted; s = 0 (shift is 0 then too) needs one bit below it
+// (acc M0 + addend) >> (31 + s): the high word of a multiply-add, shifted; s = 0 (shift is 0 then too) needs one bit below it
 template <bool kAnyShift>
-__device__ __forceinline__ int out_value(int acc, int4 rq, long long add, int shift, int lo, int hi) {
+__device__ __forceinline__ int requantised(int acc, int4 rq, long long add, int shift) {
   const long long p = (long long)acc * rq.x + add;
-  int o = (int)(p >> 32) >> shift;
-  if (kAnyShift && rq.y == 0) o = (int)(p >> 31);
-  return min(max(o, lo), hi);
+  const int o = (int)(p >> 32) >> shift;
+  return kAnyShift && rq.y == 0 ? (int)(p >> 31) : o;
+}
+
+// {sat(y3), sat(y2), sat(y1), sat(y0)}, y0 in the lowest byte
+template <class YT>
+__device__ __forceinline__ uint32_t pack4(int y0, int y1, int y2, int y3) {
+  uint32_t t, w;
+  if (YT(-1) < YT(0)) {
+    asm("cvt.pack.sat.s8.s32.b32 %0, %1, %2, %3;" : "=r"(t) : "r"(y3), "r"(y2), "r"(0));
+    asm("cvt.pack.sat.s8.s32.b32 %0, %1, %2, %3;" : "=r"(w) : "r"(y1), "r"(y0), "r"(t));
+  } else {
+    asm("cvt.pack.sat.u8.s32.b32 %0, %1, %2, %3;" : "=r"(t) : "r"(y3), "r"(y2), "r"(0));
+    asm("cvt.pack.sat.u8.s32.b32 %0, %1, %2, %3;" : "=r"(w) : "r"(y1), "r"(y0), "r"(t));
+  }
+  return w;
 }
 
 // true if it is for all 128 threads of warps 4-7 (and a barrier of theirs)
@@ -381,13 +396,13 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         if (!(ok = wait(&sh.lready[ui & 1], (ui >> 1) & 1))) break;
         const int n_list = sh.n_list[ui & 1];
         for (int g = 0; ok && g < n_list; g += per) {
-          const int n = min(per, n_list - g);
+          const int n = min(per, n_list - g), parts = per / n * n;     // fewer adapters: copies, see the epilogue
           for (int ks = 0; ks < a.stages; ++ks, turn.next(ring)) {
-            const uint32_t st = stage(ks, row0, (uint32_t)(n * a.rp * kProjStage));
+            const uint32_t st = stage(ks, row0, (uint32_t)(parts * a.rp * kProjStage));
             if (!ok) break;
-            for (int i = 0; i < n; ++i)
+            for (int i = 0; i < parts; ++i)
               ptx::bulk_g2s(st + RT * kProjStage + i * a.rp * kProjStage,
-                            a.down + ((size_t)sh.list[ui & 1][g + i] * a.stages + ks) * a.rp * kProjStage,
+                            a.down + ((size_t)sh.list[ui & 1][g + i % n] * a.stages + ks) * a.rp * kProjStage,
                             (uint32_t)(a.rp * kProjStage), ptx::smem_u32(&sh.full[turn.slot]));
           }
         }
@@ -535,10 +550,11 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
       }
     }
   } else if (warp >= 8) {
-    // A thread owns an output channel and walks over the rows. 8-bit results of 16 rows x 32 channels go through
-    // 512 bytes of shared memory per warp, so that a row's 32 bytes leave in two 16-byte stores instead of 32.
+    // A thread owns an output channel and walks over the rows. The exact requantisation runs on the half-rate integer
+    // pipes (17 to 20 outputs per clock and SM with 16 warps, see the requantisation microbenchmark), so what is added to
+    // it is kept small: the clip of an 8-bit type is the saturating pack, rows leave as words of four channels.
     const int q = warp & 3, cols = RT / (kEpiWarps / 4), c0 = ((warp - 8) >> 2) * cols;
-    uint8_t* const stage = sh.out[warp - 8];
+    uint32_t* const stage = sh.out[warp - 8];
     int ti = 0, ui = 0;
     bool ok = true;
     auto sums = [&]() {
@@ -556,21 +572,20 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
       const int row0 = u / shp.chunks * RT, t0 = u % shp.chunks * shp.chunk, t1 = min(t0 + shp.chunk, a.tiles_n), ub = ui & 1;
       if (adapters && !(ok = __all_sync(0xFFFFFFFFu, wait(&sh.lready[ub], (ui >> 1) & 1)))) break;
       if (kFused && adapters) {
+        // The product's lanes are rank channels: those of one adapter would be work for a quarter of the warps (tensor
+        // memory shows a warp 32 lanes), so copies of them stand in the other lanes, a share of the rows each.
         const int n_list = sh.n_list[ub], m = q * 32 + lane, j = m % a.rp;
         for (int g = 0; ok && g < n_list; g += per, ++ti) {
-          const int i = g + m / a.rp;
-          const int slot = i < n_list ? sh.list[ub][i] : -3;
-          const bool used = slot >= 0;
-          const int2 rq = used ? a.down_rq[slot * a.rp + j] : make_int2(1 << 30, 0);
+          const int n = min(per, n_list - g), copies = per / n, i = m / a.rp % n, copy = m / a.rp / n;
+          const int slot = sh.list[ub][g + i];
+          const int2 rq = a.down_rq[slot * a.rp + j];
           const uint32_t d = sums();
           if (!ok) break;
-          if (__any_sync(0xFFFFFFFFu, used)) {
-            for (int c = 0; c < cols; c += 16) {
-              uint32_t v[16];
-              ptx::tmem_ld16(d + c, v);
-              ptx::tmem_ld_wait16(v);
-              store_rank(a.h + (size_t)(row0 + c0 + c) * a.rp + j, a.rp, v, rq, slot, sh.slot[ub] + c0 + c);
-            }
+          for (int c = copy < copies ? copy * 16 : cols; c < cols; c += copies * 16) {
+            uint32_t v[16];
+            ptx::tmem_ld16(d + c, v);
+            ptx::tmem_ld_wait16(v);
+            store_rank(a.h + (size_t)(row0 + c0 + c) * a.rp + j, a.rp, v, rq, slot, sh.slot[ub] + c0 + c);
           }
           done(&sh.tempty[ti & 1]);
         }
@@ -590,9 +605,11 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         }
         const long long add = (long long)(((unsigned long long)(uint32_t)rq.w << 32) | (uint32_t)rq.z);
         const int shift = max(rq.y - 1, 0);
+        const bool words = sizeof(YT) == 1 && shp.vector_y && n0 + 32 <= a.n;
+        const int first = words ? lane >> 3 << 2 : 0;  // rows first .. first + 3 of 16 are this lane's, channels n0 + 4 (lane & 7) ..
+        YT* y = (YT*)a.y + (long long)(row0 + c0 + first) * a.ldy + (words ? n0 + (lane & 7) * 4 : n);
         const uint32_t d = sums();
         if (!ok) break;
-        YT* y = (YT*)a.y + (long long)(row0 + c0) * a.ldy;
         for (int c = 0; c < cols; c += 16, y += 16 * a.ldy) {
           uint32_t v[16];
           ptx::tmem_ld16(d + c, v);
@@ -600,20 +617,31 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
           uint32_t rows16 = rest >= 16 ? 0xFFFFu : rest > 0 ? (1u << rest) - 1 : 0;    // the rows that are written, a bit each
           if (adapters) rows16 &= sh.live[ub][r >> 5] >> (r & 31);
           ptx::tmem_ld_wait16(v);
-          if (sizeof(YT) == 1 && shp.vector_y && n0 + 32 <= a.n) {
+          int o[16];
 #pragma unroll
-            for (int e = 0; e < 16; ++e) stage[e * 32 + lane] = (uint8_t)out_value<kAnyShift>((int)v[e], rq, add, shift, a.lo, a.hi);
+          for (int e = 0; e < 16; ++e) o[e] = requantised<kAnyShift>((int)v[e], rq, add, shift);
+          if (shp.clip) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[e] = min(max(o[e], a.lo), a.hi);
+          }
+          YT* p = y;
+          if (words) {                                  // four rows to a word, 16 x 32 of them transposed through shared memory
+#pragma unroll
+            for (int i = 0; i < 4; ++i) stage[i * 32 + lane] = pack4<YT>(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
             __syncwarp();
-            const int4 o = *reinterpret_cast<const int4*>(stage + lane * 16);
-            if (rows16 >> (lane >> 1) & 1) *reinterpret_cast<int4*>(y + (lane >> 1) * a.ldy + n0 + (lane & 1) * 16) = o;
+            const int4 t = *reinterpret_cast<const int4*>(stage + (lane >> 3) * 32 + (lane & 7) * 4);
             __syncwarp();
+            const uint32_t ab = __byte_perm(t.x, t.y, 0x5140), cd = __byte_perm(t.z, t.w, 0x5140);      // rows 0 and 1 of channels 0, 1 and 2, 3
+            const uint32_t ef = __byte_perm(t.x, t.y, 0x7362), gh = __byte_perm(t.z, t.w, 0x7362);
+            const uint32_t w[4] = {__byte_perm(ab, cd, 0x5410), __byte_perm(ab, cd, 0x7632), __byte_perm(ef, gh, 0x5410), __byte_perm(ef, gh, 0x7632)};
+#pragma unroll
+            for (int i = 0; i < 4; ++i, p += a.ldy)
+              if (rows16 >> (first + i) & 1) *reinterpret_cast<uint32_t*>(p) = w[i];
           } else {
-            YT* p = y + n;
 #pragma unroll
-            for (int e = 0; e < 16; ++e, p += a.ldy) {
-              const int o = out_value<kAnyShift>((int)v[e], rq, add, shift, a.lo, a.hi);
-              if ((rows16 >> e & 1) && n < a.n) *p = (YT)o;
-            }
+            for (int e = 0; e < 16; ++e, p += a.ldy)
+              if ((rows16 >> e & 1) && n < a.n)
+                *p = sizeof(YT) == 4 ? (YT)o[e] : (YT)min(max(o[e], YT(-1) < YT(0) ? -128 : 0), YT(-1) < YT(0) ? 127 : 255);
           }
         }
         done(&sh.tempty[ti & 1]);
@@ -760,12 +788,12 @@ __global__ void __launch_bounds__(kSplitThreads, 1) proj_split_kernel(const __gr
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const long long add = (long long)(((unsigned long long)(uint32_t)rq[i].w << 32) | (uint32_t)rq[i].z);
-      o[i] = out_value<kAnyShift>(acc[i], rq[i], add, max(rq[i].y - 1, 0), a.lo, a.hi);
+      o[i] = min(max(requantised<kAnyShift>(acc[i], rq[i], add, max(rq[i].y - 1, 0)), a.lo), a.hi);
     }
     YT* y = (YT*)a.y + (long long)row * a.ldy + n;
     if (shp.vector_y && n + 4 <= a.n) {
       if (sizeof(YT) == 1)
-        *reinterpret_cast<int*>(y) = __byte_perm(__byte_perm(o[0], o[1], 0x0040), __byte_perm(o[2], o[3], 0x0040), 0x5410);
+        *reinterpret_cast<uint32_t*>(y) = pack4<YT>(o[0], o[1], o[2], o[3]);
       else
         *reinterpret_cast<int4*>(y) = make_int4(o[0], o[1], o[2], o[3]);
     } else {
@@ -840,7 +868,9 @@ cudaError_t launch_main(const ProjArgs& a, const CUtensorMap& map, cudaStream_t 
   MainShape s;
   s.tile = tile;
   s.tmem_cols = 2 * tile;
-  s.vector_y = a.y_bytes == 1 && a.ldy % 16 == 0 && y % 16 == 0;
+  s.vector_y = a.y_bytes == 1 && a.ldy % 4 == 0 && y % 4 == 0;
+  const int lo = a.y_type == IODF_I8 ? -128 : a.y_type == IODF_U8 ? 0 : INT_MIN, hi = a.y_type == IODF_I8 ? 127 : a.y_type == IODF_U8 ? 255 : INT_MAX;
+  s.clip = a.lo > lo || a.hi < hi;
   s.step_adapters = a.rp == 32 ? 2 : 1;
   s.abytes = (kProjTileN + tile) * std::max(a.rp, 64);
   const int ab = a.n_seg ? 2 * s.abytes : 0, row_tiles = (a.rows + tile - 1) / tile;
@@ -865,6 +895,8 @@ cudaError_t configure() {
 
 cudaError_t configure_proj_kernels() {
   cudaError_t e = cudaFuncSetAttribute(down_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDownRing * kDownStageBytes + 1024);
+  if (e == cudaSuccess) e = configure<int8_t, false>();
+  if (e == cudaSuccess) e = configure<int8_t, true>();
   if (e == cudaSuccess) e = configure<uint8_t, false>();
   if (e == cudaSuccess) e = configure<uint8_t, true>();
   if (e == cudaSuccess) e = configure<int, false>();
@@ -894,7 +926,8 @@ cudaError_t launch_proj(const ProjArgs& a, const void* x_map, const void* x_map_
     if (e != cudaSuccess) return e;
   }
   const CUtensorMap& map = *static_cast<const CUtensorMap*>(x_map);
-  if (a.y_bytes == 1) return a.any_shift ? launch_main<uint8_t, true>(a, map, stream) : launch_main<uint8_t, false>(a, map, stream);
+  if (a.y_type == IODF_I8) return a.any_shift ? launch_main<int8_t, true>(a, map, stream) : launch_main<int8_t, false>(a, map, stream);
+  if (a.y_type == IODF_U8) return a.any_shift ? launch_main<uint8_t, true>(a, map, stream) : launch_main<uint8_t, false>(a, map, stream);
   return a.any_shift ? launch_main<int, true>(a, map, stream) : launch_main<int, false>(a, map, stream);
 }
 

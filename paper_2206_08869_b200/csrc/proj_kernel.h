@@ -21,7 +21,7 @@ struct ProjArgs {
   int n_seg, rows;
   int k, n;                            // channels in, out
   int stages, tiles_n;                 // ceil(k / 128), ceil(n / 128)
-  int x_unsigned, y_bytes;
+  int x_unsigned, y_type, y_bytes;     // y_type: IODF_I8, IODF_U8 or IODF_I32
   int lo, hi;                          // ReLU and clip of the layer
   int any_shift;                       // some s is 0
   int max_adapters;
