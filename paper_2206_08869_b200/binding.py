@@ -597,14 +597,14 @@ def _type_code(dtype, allowed):
 
 
 def _on(t, handle, dtype, what):
-    if not t.is_cuda or t.device.index != handle.device or t.dtype != dtype:
+    if t.get_device() != handle.device or t.dtype != dtype:        # -1: not on a GPU
         raise ValueError("%s must be a %s tensor on cuda:%d" % (what, dtype, handle.device))
     return t
 
 
 def _rows_of(t, rows, channels, what):
     """Row stride of a [rows, channels] tensor whose channels lie side by side."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != channels or (channels > 1 and t.stride(1) != 1):
+    if t.shape != (rows, channels) or (channels > 1 and t.stride(1) != 1):
         raise ValueError("%s must be [%d, %d] with channels side by side" % (what, rows, channels))
     return t.stride(0) if rows > 1 else max(channels, t.stride(0))
 
@@ -612,8 +612,12 @@ def _rows_of(t, rows, channels, what):
 def _layer_stream(stream, device):
     if stream is None:
         import torch
-        return C.c_void_p(torch.cuda.current_stream(device).cuda_stream)
-    return _stream(stream)
+        return torch._C._cuda_getCurrentRawStream(device)
+    return int(getattr(stream, "cuda_stream", stream))
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
 
 
 class Projection:
@@ -622,6 +626,8 @@ class Projection:
     def __init__(self, handle, device, c_in, c_out, max_rows, x_dtype, y_dtype):
         self.handle, self.device, self.c_in, self.c_out, self.max_rows = handle, device, c_in, c_out, max_rows
         self.x_dtype, self.y_dtype = x_dtype, y_dtype
+        import torch
+        self.int32 = torch.int32
 
     def __del__(self):
         h, self.handle = getattr(self, "handle", None), None
@@ -673,7 +679,6 @@ def iodf_proj_forward(proj, x, seg_start=None, seg_adapter=None, y=None, stream=
     """x: cuda [rows, c_in] of the handle's type, row stride a multiple of 16 bytes. seg_start int32 [n + 1] and
     seg_adapter int32 [n] on the device: the rows and the slot of each request. Returns y [rows, c_out]; rows in no
     request keep what y held (zero where y is made here)."""
-    import torch
     rows = x.shape[0]
     _on(x, proj, proj.x_dtype, "x")
     ldx = _rows_of(x, rows, proj.c_in, "x")
@@ -683,15 +688,17 @@ def iodf_proj_forward(proj, x, seg_start=None, seg_adapter=None, y=None, stream=
     if seg_start is not None:
         n_seg = seg_adapter.numel()
         for t, n, what in ((seg_start, n_seg + 1, "seg_start"), (seg_adapter, n_seg, "seg_adapter")):
-            _on(t, proj, torch.int32, what)
+            _on(t, proj, proj.int32, what)
             if t.numel() != n or not t.is_contiguous():
                 raise ValueError("%s must hold %d contiguous values" % (what, n))
     if y is None:
+        import torch
         y = (torch.zeros if n_seg else torch.empty)((rows, proj.c_out), dtype=proj.y_dtype, device=x.device)
     _on(y, proj, proj.y_dtype, "y")
     ldy = _rows_of(y, rows, proj.c_out, "y")
-    rc = load_library().iodf_proj_forward(proj.handle, _ptr(x), ldx, rows, _ptr(seg_start), _ptr(seg_adapter), n_seg,
-                                          _ptr(y), ldy, _layer_stream(stream, proj.device))
+    rc = (_lib or load_library()).iodf_proj_forward(proj.handle, x.data_ptr(), ldx, rows, _addr(seg_start),
+                                                    _addr(seg_adapter), n_seg, y.data_ptr(), ldy,
+                                                    _layer_stream(stream, proj.device))
     if rc != 0:
         raise IodfError(rc, "iodf_proj_forward")
     return y
@@ -710,6 +717,8 @@ class Norm:
     def __init__(self, handle, device, channels, res_dtype, block_dtype, n_dtype):
         self.handle, self.device, self.channels = handle, device, channels
         self.res_dtype, self.block_dtype, self.n_dtype = res_dtype, block_dtype, n_dtype
+        import torch
+        self.uint8 = torch.uint8
 
     def __del__(self):
         h, self.handle = getattr(self, "handle", None), None
@@ -751,10 +760,11 @@ def iodf_norm_create(desc, device=0):
 
 def _view(t, channels, what):
     """rows and strides of a residual stream: [rows, c] or planes [images, c, pixels]."""
-    if t.dim() == 2 and t.shape[1] == channels and (channels == 1 or t.stride(1) == 1):
-        return t.shape[0], View(max(1, t.shape[0]), 0, 1, t.stride(0))
-    if t.dim() == 3 and t.shape[1] == channels and (t.shape[2] == 1 or t.stride(2) == 1):
-        return t.shape[0] * t.shape[2], View(max(1, t.shape[2]), t.stride(0), t.stride(1), 1)
+    shape = t.shape
+    if len(shape) == 2 and shape[1] == channels and (channels == 1 or t.stride(1) == 1):
+        return shape[0], View(max(1, shape[0]), 0, 1, t.stride(0))
+    if len(shape) == 3 and shape[1] == channels and (shape[2] == 1 or t.stride(2) == 1):
+        return shape[0] * shape[2], View(max(1, shape[2]), t.stride(0), t.stride(1), 1)
     raise ValueError("%s must be [rows, %d] or [images, %d, pixels] with the last axis contiguous" % (what, channels, channels))
 
 
@@ -762,7 +772,6 @@ def iodf_norm_forward(norm, r, b=None, gate=None, r_out=None, n=None, stream=Non
     """r: the residual stream, cuda [rows, c] or planes [images, c, pixels] (any outer strides); b [rows, c] the
     block's output; gate uint8 [rows, c] or [c]. Returns (r_out, n), None where the handle has no such part.
     r_out may be r."""
-    import torch
     c = norm.channels
     _on(r, norm, norm.res_dtype, "r")
     rows, rv = _view(r, c, "r")
@@ -772,13 +781,17 @@ def iodf_norm_forward(norm, r, b=None, gate=None, r_out=None, n=None, stream=Non
     ov = None
     if b is not None:
         ldb = _rows_of(_on(b, norm, norm.block_dtype, "b"), rows, c, "b")
-        if r_out is None:
-            r_out = torch.empty(r.shape, dtype=r.dtype, device=r.device)
-        if _on(r_out, norm, norm.res_dtype, "r_out").shape != r.shape:
-            raise ValueError("r_out must have the shape of r")
-        _, ov = _view(r_out, c, "r_out")
+        if r_out is r:
+            ov = rv
+        else:
+            if r_out is None:
+                import torch
+                r_out = torch.empty(r.shape, dtype=r.dtype, device=r.device)
+            if _on(r_out, norm, norm.res_dtype, "r_out").shape != r.shape:
+                raise ValueError("r_out must have the shape of r")
+            _, ov = _view(r_out, c, "r_out")
     if gate is not None:
-        _on(gate, norm, torch.uint8, "gate")
+        _on(gate, norm, norm.uint8, "gate")
         if gate.dim() == 1:
             if gate.shape[0] != c or (c > 1 and gate.stride(0) != 1):
                 raise ValueError("gate must be [%d] or [%d, %d]" % (c, rows, c))
@@ -786,11 +799,11 @@ def iodf_norm_forward(norm, r, b=None, gate=None, r_out=None, n=None, stream=Non
             ldg = _rows_of(gate, rows, c, "gate")
     if norm.n_dtype is not None:
         if n is None:
+            import torch
             n = torch.empty((rows, c), dtype=norm.n_dtype, device=r.device)
         ldn = _rows_of(_on(n, norm, norm.n_dtype, "n"), rows, c, "n")
-    rc = load_library().iodf_norm_forward(norm.handle, rows, _ptr(r), C.byref(rv), _ptr(b), ldb, _ptr(gate), ldg,
-                                          _ptr(r_out), C.byref(ov) if ov is not None else None, _ptr(n), ldn,
-                                          _layer_stream(stream, norm.device))
+    rc = (_lib or load_library()).iodf_norm_forward(norm.handle, rows, r.data_ptr(), rv, _addr(b), ldb, _addr(gate), ldg,
+                                                    _addr(r_out), ov, _addr(n), ldn, _layer_stream(stream, norm.device))
     if rc != 0:
         raise IodfError(rc, "iodf_norm_forward")
     return r_out, n

@@ -27,37 +27,41 @@ __device__ __forceinline__ int clip24(int v) { return min(max(v, -(1 << 23)), (1
 // a b + c, its high word
 __device__ __forceinline__ int mad_hi(int a, int b, long long c) { return (int)(((long long)a * b + c) >> 32); }
 
-// What scales a row: N(v) = (v rho + 2^(sh-1)) >> sh, rho / 2^sh ~ 2^22 / sqrt(D), 1 <= D < 2^62, 9 <= sh <= 39. Where
-// sh < 32 the values are small (|v| <= sqrt(D)): they are shifted up by 32 - sh first and stay below
-// 2^24, so that the result is always the high word, shifted.
+// What scales a row: N(v) = (v rho + 2^(sh-1)) >> sh, rho / 2^sh ~ 2^22 / sqrt(D), 1 <= D < 2^62, 9 <= sh <= 39.
 struct RowScale {
-  int rho, up, down;
+  int rho, sh;
   long long round;
-  __device__ __forceinline__ int operator()(int v) const { return mad_hi(v << up, rho, round) >> down; }
 };
 
 // sigma = floor(sqrt(m)) and rho = floor((2^61 - 1) / sigma) for m = D 2^t in [2^60, 2^62). Both come from one
-// reciprocal root y in double precision. m y is off by less than 2^-19, so sigma is off by one at most;
-// 1 / sigma = y (1 + e + e^2 ..) with e = (sqrt(m) - sigma) / sigma < 2^-30, whose square moves rho by less than 2^-28, so
-// rho is off by one at most too. Both are put right in integers.
+// reciprocal root y of m: the hardware's estimate (more than 20 bits) and one step of third order, whose error (5/16 e^3 and
+// roundings, together below 2^-50) puts m y and 2^61 y (1 + e') within 2^-18 of the root and the quotient; e' = (root - sigma) y
+// < 2^-30 and its square, below 2^-60, moves rho by less than 2^-28. Rounded to integers by adding 1.5 * 2^52, each is
+// off by one at most, and put right by its exact remainder.
 __device__ __forceinline__ RowScale row_scale(unsigned long long D) {
+  constexpr double kMagic = 6755399441055744.0;         // 1.5 * 2^52: the low word of the sum is the nearest integer
   const int t = (__clzll((long long)D) - 2) & ~1;
   const unsigned long long m = D << t;
-  const double md = (double)m, y = rsqrt(md), root = md * y;
-  unsigned int s = (unsigned int)fmin(root, 2147483647.0);
-  if ((unsigned long long)s * s > m) --s;
-  if ((unsigned long long)(s + 1) * (s + 1) <= m) ++s;
-  const double e = (root - (double)s) * y;
-  const unsigned long long top = (1ull << 61) - 1;
-  unsigned int q = (unsigned int)fmin((y + y * e) * 2305843009213693952.0, 2147483647.0);
-  if ((unsigned long long)q * s > top) --q;
-  if ((unsigned long long)(q + 1) * s <= top) ++q;
-  const int sh = 39 - (t >> 1);
+  const double md = (double)m;
+  double y;
+  asm("rsqrt.approx.ftz.f64 %0, %1;" : "=d"(y) : "d"(md));
+  const double h = fma(-md * y, y, 1.0);
+  y = fma(y * h, fma(h, 0.375, 0.5), y);
+  const double root = md * y, rs = root + kMagic;
+  unsigned int s = (unsigned int)__double2loint(rs);
+  long long rem = (long long)(m - (unsigned long long)s * s);          // 0 .. 2 s if s is the floor
+  const double e = (root - (rs - kMagic)) * y;
+  unsigned int q = (unsigned int)__double2loint(fma(fma(y, e, y), 2305843009213693952.0, kMagic));
+  // s too large by one: rem < 0; too small: rem > 2 s. The quotient by the nearest integer is one by the floor, or the next.
+  const int ds = rem < 0 ? -1 : rem > 2ll * s ? 1 : 0;
+  s += ds;
+  rem = (long long)(((1ull << 61) - 1) - (unsigned long long)q * s);   // 0 .. s - 1 if q is the floor
+  while (rem < 0) { --q; rem += s; }
+  while (rem >= (long long)s) { ++q; rem -= s; }
   RowScale r;
   r.rho = (int)q;
-  r.up = max(32 - sh, 0);
-  r.down = max(sh - 32, 0);
-  r.round = 1ll << (31 + r.down);
+  r.sh = 39 - (t >> 1);
+  r.round = 1ll << (r.sh - 1);
   return r;
 }
 
@@ -78,9 +82,9 @@ __device__ __forceinline__ long long row_sum(long long v, long long* red) {
     if constexpr (T > 32) {
       if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = s;
       __syncthreads();
-      s = 0;
+      s = red[threadIdx.x & (T / 32 - 1)];
 #pragma unroll
-      for (int w = 0; w < T / 32; ++w) s += red[w];
+      for (int o = T / 64; o; o >>= 1) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
     }
     return s;
   }
@@ -103,41 +107,46 @@ __device__ __forceinline__ void norm_row(int (&v)[E], int C, int kind, unsigned 
   long long q = 0;
 #pragma unroll
   for (int e = 0; e < E; ++e) q += (long long)v[e] * v[e];
-  const RowScale scale = row_scale((unsigned long long)row_sum<T, false>(q, red + 16) + eps);
+  const RowScale s = row_scale((unsigned long long)row_sum<T, false>(q, red + 16) + eps);
+  if (s.sh < 32) {                                      // sqrt(D) below 2^24: a funnel shift of the two words
 #pragma unroll
-  for (int e = 0; e < E; ++e) v[e] = scale(v[e]);
+    for (int e = 0; e < E; ++e) {
+      const long long p = (long long)v[e] * s.rho + s.round;
+      v[e] = (int)__funnelshift_r((unsigned int)p, (unsigned int)(p >> 32), s.sh);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = mad_hi(v[e], s.rho, s.round) >> (s.sh - 32);
+  }
 }
 
-// ---- eight neighbouring elements --------------------------------------------------------------------------
-__device__ __forceinline__ void load8(const int* p, int (&v)[8]) {
-  const int4 a = reinterpret_cast<const int4*>(p)[0], b = reinterpret_cast<const int4*>(p)[1];
-  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-__device__ __forceinline__ void load8(const int16_t* p, int (&v)[8]) {
-  const int4 a = *reinterpret_cast<const int4*>(p);
-  const int w[4] = {a.x, a.y, a.z, a.w};
+// ---- eight neighbouring elements, as they lie in memory until they are used --------------------------------------
+template <class Q>
+struct Raw8 {
+  uint32_t w[2 * sizeof(Q)];
+  __device__ __forceinline__ void zero() {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[2 * i] = (int16_t)w[i];
-    v[2 * i + 1] = w[i] >> 16;
+    for (int i = 0; i < (int)(2 * sizeof(Q)); ++i) w[i] = 0;
   }
-}
-__device__ __forceinline__ void load8(const int8_t* p, int (&v)[8]) {
-  const int2 a = *reinterpret_cast<const int2*>(p);
+  __device__ __forceinline__ void load(const Q* p) {
+    if (sizeof(Q) == 1) {
+      const uint2 a = *reinterpret_cast<const uint2*>(p);
+      w[0] = a.x; w[1] = a.y;
+    } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[i] = (int8_t)(a.x >> (8 * i));
-    v[4 + i] = (int8_t)(a.y >> (8 * i));
+      for (int i = 0; i < (int)sizeof(Q) / 2; ++i) {
+        const uint4 a = reinterpret_cast<const uint4*>(p)[i];
+        w[4 * i] = a.x; w[4 * i + 1] = a.y; w[4 * i + 2] = a.z; w[4 * i + 3] = a.w;
+      }
+    }
   }
-}
-__device__ __forceinline__ void load8(const uint8_t* p, int (&v)[8]) {
-  const uint2 a = *reinterpret_cast<const uint2*>(p);
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    v[i] = (a.x >> (8 * i)) & 255;
-    v[4 + i] = (a.y >> (8 * i)) & 255;
+  __device__ __forceinline__ int at(int e) const {
+    if (sizeof(Q) == 4) return (int)w[e];
+    if (sizeof(Q) == 2) return e & 1 ? (int)w[e / 2] >> 16 : (int)(int16_t)w[e / 2];
+    if (Q(-1) < Q(0)) return (int)(int8_t)(w[e / 4] >> (8 * (e & 3)));
+    return (int)((w[e / 4] >> (8 * (e & 3))) & 255u);
   }
-}
+};
 __device__ __forceinline__ void store8(int* p, const int (&v)[8]) {
   reinterpret_cast<int4*>(p)[0] = make_int4(v[0], v[1], v[2], v[3]);
   reinterpret_cast<int4*>(p)[1] = make_int4(v[4], v[5], v[6], v[7]);
@@ -148,18 +157,34 @@ __device__ __forceinline__ void store8(int16_t* p, const int (&v)[8]) {
   for (int i = 0; i < 4; ++i) w[i] = __byte_perm(v[2 * i], v[2 * i + 1], 0x5410);
   *reinterpret_cast<int4*>(p) = make_int4(w[0], w[1], w[2], w[3]);
 }
-__device__ __forceinline__ void store8(uint8_t* p, const int (&v)[8]) {
-  int2 a;
-  a.x = __byte_perm(__byte_perm(v[0], v[1], 0x0040), __byte_perm(v[2], v[3], 0x0040), 0x5410);
-  a.y = __byte_perm(__byte_perm(v[4], v[5], 0x0040), __byte_perm(v[6], v[7], 0x0040), 0x5410);
-  *reinterpret_cast<int2*>(p) = a;
+// clip to the whole range of int8 or uint8
+__device__ __forceinline__ void store8_sat(uint8_t* p, const int (&v)[8], bool is_signed) {
+  uint32_t w[2], t;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (is_signed) {
+      asm("cvt.pack.sat.s8.s32.b32 %0, %1, %2, %3;" : "=r"(t) : "r"(v[4 * i + 3]), "r"(v[4 * i + 2]), "r"(0));
+      asm("cvt.pack.sat.s8.s32.b32 %0, %1, %2, %3;" : "=r"(w[i]) : "r"(v[4 * i + 1]), "r"(v[4 * i]), "r"(t));
+    } else {
+      asm("cvt.pack.sat.u8.s32.b32 %0, %1, %2, %3;" : "=r"(t) : "r"(v[4 * i + 3]), "r"(v[4 * i + 2]), "r"(0));
+      asm("cvt.pack.sat.u8.s32.b32 %0, %1, %2, %3;" : "=r"(w[i]) : "r"(v[4 * i + 1]), "r"(v[4 * i]), "r"(t));
+    }
+  }
+  *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
 }
 
 template <int T>
 struct Block { static constexpr int threads = T <= 32 ? 128 : T, rows = threads / T; };
 
-template <class RT, class BT, int T, int E, int MODE>
-__global__ void __launch_bounds__(Block<T>::threads) norm_kernel(const NormArgs a) {
+// Blocks per SM that the registers have to leave room for: what measured best (32 to 40 warps; 16384 x 4096 int16 with
+// int32 blocks and gates 152 us without the bound, 134 with it).
+template <int T, int E, int MODE>
+__host__ __device__ constexpr int min_blocks() {
+  return MODE != kVector ? 1 : T == 512 ? 2 : T == 256 ? 5 : T == 128 ? 9 : T == 64 ? 16 : E <= 8 ? 10 : 8;
+}
+
+template <class RT, class BT, int T, int E, int MODE, bool kFull>
+__global__ void __launch_bounds__(Block<T>::threads, min_blocks<T, E, MODE>()) norm_kernel(const NormArgs a) {
   constexpr bool kBlock = !std::is_same<BT, None>::value;
   using B = typename std::conditional<kBlock, BT, int8_t>::type;
   __shared__ long long red[64];
@@ -171,7 +196,10 @@ __global__ void __launch_bounds__(Block<T>::threads) norm_kernel(const NormArgs 
   const unsigned int row = live ? row0 : rows - 1;
   const int C = a.channels;
   auto channel = [&](int e) { return MODE == kVector ? ((e / 8) * T + t) * 8 + e % 8 : e * T + t; };
-  auto valid = [&](int e) { return channel(e) < C; };
+  auto valid = [&](int e) {
+    if (kFull) return MODE == kVector || e < E - 1 || channel(e) < C;
+    return channel(e) < C;
+  };
 
   const RT* rp;
   RT* op = nullptr;
@@ -188,28 +216,32 @@ __global__ void __launch_bounds__(Block<T>::threads) norm_kernel(const NormArgs 
   const uint8_t* gp = a.gate + (long long)row * a.ldg;
   uint8_t* np = (uint8_t*)a.n + (long long)row * a.ldn;
 
-  int v[E], r[E];
-  if (MODE == kVector) {
+  // Every operand of the row is asked for here, before the first is used. kVector has whole vectors only (C is a
+  // multiple of 8), and with kFull every thread has its E channels (kScalar: all but the last), so that no guard stands between
+  // the tables' loads either: a guarded load waits by itself (measured: a gate of 67 MB cost 50 us so, 8 us now).
+  int v[E], r[MODE == kVector ? 1 : E];
+  Raw8<RT> rr[MODE == kVector ? E / 8 : 1];
+  Raw8<uint8_t> gr[MODE == kVector ? E / 8 : 1];
+  int g[MODE == kVector ? 1 : E];
+  const bool gated = kBlock && a.gate != nullptr;
+  if constexpr (MODE == kVector) {
+    Raw8<B> br[E / 8];
 #pragma unroll
     for (int i = 0; i < E / 8; ++i) {
       const int c = channel(8 * i);
-      int x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, y[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-      if (c + 8 <= C) {
-        load8(rp + c, x);
-        if (kBlock) load8(bp + c, y);
-      } else if (c < C) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (c + e < C) {
-            x[e] = rp[c + e];
-            if (kBlock) y[e] = bp[c + e];
-          }
+      if (!kFull) {
+        rr[i].zero();
+        br[i].zero();
       }
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        r[8 * i + e] = x[e];
-        v[8 * i + e] = y[e];
+      if (kFull || c < C) {
+        rr[i].load(rp + c);
+        if (kBlock) br[i].load(bp + c);
+        if (gated) gr[i].load(gp + c);
       }
+    }
+    if (kBlock) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = sizeof(B) == 4 ? clip24(br[e / 8].at(e % 8)) : br[e / 8].at(e % 8);
     }
   } else {
 #pragma unroll
@@ -217,82 +249,81 @@ __global__ void __launch_bounds__(Block<T>::threads) norm_kernel(const NormArgs 
       r[e] = valid(e) ? rp[channel(e) * rc] : 0;
       v[e] = kBlock && valid(e) ? bp[channel(e)] : 0;
     }
-  }
-  if (sizeof(RT) == 4)
+    if (gated) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) r[e] = clip24(r[e]);
+      for (int e = 0; e < E; ++e) g[e] = valid(e) ? gp[channel(e)] : 0;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if (sizeof(RT) == 4) r[e] = clip24(r[e]);
+      if (kBlock && sizeof(B) == 4) v[e] = clip24(v[e]);
+    }
+  }
+  auto residual = [&](int e) {
+    if constexpr (MODE != kVector) {
+      return r[e];
+    } else {
+      const int x = rr[e / 8].at(e % 8);
+      return sizeof(RT) == 4 ? clip24(x) : x;
+    }
+  };
 
   if constexpr (kBlock) {
-    if (sizeof(B) == 4)
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = clip24(v[e]);
     if (a.post) norm_row<T>(v, C, a.post, a.eps, red, valid);
     const long long round = 1ll << (30 + a.shift);
-    if (MODE == kVector) {
+    if constexpr (MODE == kVector) {
 #pragma unroll
       for (int i = 0; i < E / 8; ++i) {
         const int c = channel(8 * i);
-        if (c >= C) continue;
-        int m[8], g[8], o[8];
-        load8(a.mult + c, m);
-        if (a.gate) {
-          if (c + 8 <= C) {
-            load8(gp + c, g);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) g[e] = c + e < C ? gp[c + e] : 0;
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[8 * i + e] *= g[e];
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          o[e] = min(max(r[8 * i + e] + (mad_hi(v[8 * i + e], m[e], round) >> (a.shift - 1)), a.res_lo), a.res_hi);
-        if (c + 8 <= C) {
-          if (live) store8(op + c, o);
-        } else {
+        if (kFull || c < C) {
+          Raw8<int> m;
+          m.load(a.mult + c);
+          int o[8];
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            if (live && c + e < C) op[c + e] = (RT)o[e];
-            if (c + e >= C) o[e] = 0;                   // the clip's range need not hold zero
+            const int u = gated ? v[8 * i + e] * gr[i].at(e) : v[8 * i + e];
+            o[e] = min(max(residual(8 * i + e) + (mad_hi(u, m.at(e), round) >> (a.shift - 1)), a.res_lo), a.res_hi);
           }
-        }
+          if (live) store8(op + c, o);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) r[8 * i + e] = o[e];
+          for (int e = 0; e < 8; ++e) v[8 * i + e] = o[e];
+        }
       }
     } else {
 #pragma unroll
       for (int e = 0; e < E; ++e)
         if (valid(e)) {
           const int c = channel(e);
-          if (a.gate) v[e] *= gp[c];
-          r[e] = min(max(r[e] + (mad_hi(v[e], a.mult[c], round) >> (a.shift - 1)), a.res_lo), a.res_hi);
-          if (live) op[c * oc] = (RT)r[e];
+          if (gated) v[e] *= g[e];
+          const int o = min(max(r[e] + (mad_hi(v[e], a.mult[c], round) >> (a.shift - 1)), a.res_lo), a.res_hi);
+          if (live) op[c * oc] = (RT)o;
+          v[e] = o;
         }
     }
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = residual(e);
   }
 
   if (a.pre) {
-    norm_row<T>(r, C, a.pre, a.eps, red + 32, valid);
+    norm_row<T>(v, C, a.pre, a.eps, red + 32, valid);
     const long long round = 1ll << (30 + a.n_shift);
-    if (MODE == kVector) {
+    if constexpr (MODE == kVector) {
 #pragma unroll
       for (int i = 0; i < E / 8; ++i) {
         const int c = channel(8 * i);
-        if (c >= C) continue;
-        int m[8], o[8], d[8];
-        load8(a.n_mult + c, m);
-        load8(a.n_bias + c, d);
+        if (kFull || c < C) {
+          Raw8<int> m, d;
+          m.load(a.n_mult + c);
+          d.load(a.n_bias + c);
+          int o[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          o[e] = min(max((mad_hi(r[8 * i + e], m[e], round) >> (a.n_shift - 1)) + d[e], a.n_lo), a.n_hi);
-        if (!live) continue;
-        if (c + 8 <= C) {
-          store8(np + c, o);
-        } else {
+          for (int e = 0; e < 8; ++e) o[e] = (mad_hi(v[8 * i + e], m.at(e), round) >> (a.n_shift - 1)) + d.at(e);
+          if (!a.n_full) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (c + e < C) np[c + e] = (uint8_t)o[e];
+            for (int e = 0; e < 8; ++e) o[e] = min(max(o[e], a.n_lo), a.n_hi);
+          }
+          if (live) store8_sat(np + c, o, a.n_lo < 0);
         }
       }
     } else {
@@ -300,7 +331,7 @@ __global__ void __launch_bounds__(Block<T>::threads) norm_kernel(const NormArgs 
       for (int e = 0; e < E; ++e)
         if (live && valid(e)) {
           const int c = channel(e);
-          np[c] = (uint8_t)min(max((mad_hi(r[e], a.n_mult[c], round) >> (a.n_shift - 1)) + a.n_bias[c], a.n_lo), a.n_hi);
+          np[c] = (uint8_t)min(max((mad_hi(v[e], a.n_mult[c], round) >> (a.n_shift - 1)) + a.n_bias[c], a.n_lo), a.n_hi);
         }
     }
   }
@@ -309,7 +340,11 @@ __global__ void __launch_bounds__(Block<T>::threads) norm_kernel(const NormArgs 
 template <class RT, class BT, int T, int E, int MODE>
 cudaError_t run(const NormArgs& a, cudaStream_t stream) {
   constexpr int kRows = Block<T>::rows;
-  norm_kernel<RT, BT, T, E, MODE><<<(unsigned int)((a.rows + kRows - 1) / kRows), Block<T>::threads, 0, stream>>>(a);
+  const unsigned int grid = (unsigned int)((a.rows + kRows - 1) / kRows);
+  // every thread has E channels (kScalar: E - 1 and perhaps one more)
+  const bool full = MODE == kVector ? a.channels == T * E : MODE == kScalar && a.channels > T * (E - 1);
+  if (full) norm_kernel<RT, BT, T, E, MODE, MODE != kPlanes><<<grid, Block<T>::threads, 0, stream>>>(a);
+  else norm_kernel<RT, BT, T, E, MODE, false><<<grid, Block<T>::threads, 0, stream>>>(a);
   return cudaGetLastError();
 }
 
@@ -326,7 +361,7 @@ cudaError_t pick(NormArgs a, cudaStream_t stream) {
   const bool rows = a.rv.chan == 1 && (!a.has_block || a.ov.chan == 1) && a.rv.pixels >= a.rows && (!a.has_block || a.ov.pixels >= a.rows);
   if (!rows) {
     a.rv.pixels = std::min(a.rv.pixels, 0xFFFFFFFFll);
-    a.ov.pixels = a.has_block ? min(a.ov.pixels, 0xFFFFFFFFll) : 1;
+    a.ov.pixels = a.has_block ? std::min(a.ov.pixels, 0xFFFFFFFFll) : 1;
     if (C <= 8) return run<RT, BT, 1, 8, kPlanes>(a, stream);
     if (C <= 32) return run<RT, BT, 1, 32, kPlanes>(a, stream);
     if (C <= 128) return run<RT, BT, 8, 16, kPlanes>(a, stream);
@@ -334,11 +369,11 @@ cudaError_t pick(NormArgs a, cudaStream_t stream) {
     if (C <= 2048) return run<RT, BT, 128, 16, kPlanes>(a, stream);
     return run<RT, BT, 512, 16, kPlanes>(a, stream);
   }
-  if (vectors(a.r, a.rv.pix, sizeof(RT)) && vectors(a.r_out, a.ov.pix, sizeof(RT)) && vectors(a.b, a.ldb, kB) &&
+  if (C % 8 == 0 && vectors(a.r, a.rv.pix, sizeof(RT)) && vectors(a.r_out, a.ov.pix, sizeof(RT)) && vectors(a.b, a.ldb, kB) &&
       vectors(a.gate, a.ldg, 1) && vectors(a.n, a.ldn, 1)) {
     if (C <= 64) return run<RT, BT, 8, 8, kVector>(a, stream);
     if (C <= 128) return run<RT, BT, 16, 8, kVector>(a, stream);
-    if (C <= 256) return run<RT, BT, 32, 8, kVector>(a, stream);
+    if (C <= 256) return run<RT, BT, 16, 16, kVector>(a, stream);
     if (C <= 512) return run<RT, BT, 32, 16, kVector>(a, stream);
     if (C <= 1024) return run<RT, BT, 64, 16, kVector>(a, stream);
     if (C <= 2048) return run<RT, BT, 128, 16, kVector>(a, stream);
@@ -346,7 +381,14 @@ cudaError_t pick(NormArgs a, cudaStream_t stream) {
     return run<RT, BT, 512, 16, kVector>(a, stream);
   }
   if (C <= 64) return run<RT, BT, 8, 8, kScalar>(a, stream);
-  if (C <= 256) return run<RT, BT, 32, 8, kScalar>(a, stream);
+  switch ((C + 31) / 32) {                              // of the widths that pruning leaves: only the last element is guarded
+    case 3: return run<RT, BT, 32, 3, kScalar>(a, stream);
+    case 4: return run<RT, BT, 32, 4, kScalar>(a, stream);
+    case 5: return run<RT, BT, 32, 5, kScalar>(a, stream);
+    case 6: return run<RT, BT, 32, 6, kScalar>(a, stream);
+    case 7: return run<RT, BT, 32, 7, kScalar>(a, stream);
+    case 8: return run<RT, BT, 32, 8, kScalar>(a, stream);
+  }
   if (C <= 512) return run<RT, BT, 32, 16, kScalar>(a, stream);
   if (C <= 2048) return run<RT, BT, 128, 16, kScalar>(a, stream);
   return run<RT, BT, 512, 16, kScalar>(a, stream);

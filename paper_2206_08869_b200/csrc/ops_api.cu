@@ -277,6 +277,7 @@ int create_norm(const iodf_norm_desc& d, int device, iodf_norm& nm) {
   a.res_hi = d.res_hi;
   a.n_lo = d.n_lo;
   a.n_hi = d.n_hi;
+  a.n_full = d.n_type == IODF_I8 ? d.n_lo == -128 && d.n_hi == 127 : d.n_lo == 0 && d.n_hi == 255;
   a.eps = d.eps;
   a.mult = nm.d_consts;
   a.n_mult = nm.d_consts + cp;
