@@ -292,11 +292,11 @@ struct MainShared {
   alignas(16) int slot[2][kMaxTile];     // of a unit: adapter of each row
   int list[2][kMaxTile];                 //            every adapter once
   uint32_t live[2][kMaxTile / 32];       // of a unit: the rows that some request owns
-  alignas(16) uint32_t out[kEpiWarps][128];
+  alignas(16) uint32_t out[kEpiWarps][256];
 };
 
 struct MainShape {
-  int tile;                              // rows per tile: 64, 128 or 256
+  int tile;                              // rows per tile: 128 or 256
   int ring;                              // stages
   int tmem_cols;
   int chunk, chunks;                     // output tiles of a unit, units of a row tile
@@ -329,6 +329,16 @@ __device__ __forceinline__ uint32_t pack4(int y0, int y1, int y2, int y3) {
   return w;
 }
 
+// Four words of four rows, one word per channel -> four words of four channels, one per row.
+__device__ __forceinline__ void transpose4(int4 t, uint32_t* w) {
+  const uint32_t ab = __byte_perm(t.x, t.y, 0x5140), cd = __byte_perm(t.z, t.w, 0x5140);    // rows 0 and 1 of channels 0, 1 and 2, 3
+  const uint32_t ef = __byte_perm(t.x, t.y, 0x7362), gh = __byte_perm(t.z, t.w, 0x7362);
+  w[0] = __byte_perm(ab, cd, 0x5410);
+  w[1] = __byte_perm(ab, cd, 0x7632);
+  w[2] = __byte_perm(ef, gh, 0x5410);
+  w[3] = __byte_perm(ef, gh, 0x7632);
+}
+
 // true if it is for all 128 threads of warps 4-7 (and a barrier of theirs)
 __device__ __forceinline__ bool fill_all(bool fine) {
   uint32_t r;
@@ -351,7 +361,7 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
   const uint32_t stage_bytes = (uint32_t)(RT * kProjStage + kBytesW);
   if (tid == 0) {
     for (int i = 0; i < ring; ++i) {
-      ptx::mbar_init(ptx::smem_u32(&sh.full[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&sh.full[i]), 2);            // x, weights
       ptx::mbar_init(ptx::smem_u32(&sh.empty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
@@ -377,41 +387,47 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
   const bool adapters = a.n_seg != 0;
 
   if (warp == 0 && ptx::elect_one()) {
-    Turn turn;
+    Turn turn;                                          // of x; the weights of a stage follow, at most a ring behind
+    Turn wturn;
     int ui = 0;
     bool ok = true;
-    // room in the ring; the stage's x is asked for, `bytes` of weights come too
-    auto stage = [&](int ks, int row0, uint32_t bytes) {
-      const int s = turn.slot;
-      ok = wait(&sh.empty[s], turn.phase ^ 1);
-      if (!ok) return base;
-      const uint32_t st = base + s * stage_bytes, bar = ptx::smem_u32(&sh.full[s]);
-      ptx::mbar_expect_tx(bar, RT * kProjStage + bytes);
-      ptx::tile_g2s(st, &xmap, ks * kProjStage, row0, bar);
-      return st;
+    auto ask_x = [&](int ks, int row0) {
+      ok = wait(&sh.empty[turn.slot], turn.phase ^ 1);
+      if (!ok) return;
+      const uint32_t bar = ptx::smem_u32(&sh.full[turn.slot]);
+      ptx::mbar_expect_tx(bar, RT * kProjStage);
+      ptx::tile_g2s(base + turn.slot * stage_bytes, &xmap, ks * kProjStage, row0, bar);
+      turn.next(ring);
     };
     for (int u = blockIdx.x; ok && u < shp.units; u += gridDim.x, ++ui) {
       const int row0 = u / shp.chunks * RT, t0 = u % shp.chunks * shp.chunk, t1 = min(t0 + shp.chunk, a.tiles_n);
       if (kFused && adapters) {
-        if (!(ok = wait(&sh.lready[ui & 1], (ui >> 1) & 1))) break;
+        // x of the first product does not depend on the rows' adapters: it is asked for before they are known
+        const int ahead = min(ring, a.stages);
+        for (int ks = 0; ok && ks < ahead; ++ks) ask_x(ks, row0);
+        if (!ok || !(ok = wait(&sh.lready[ui & 1], (ui >> 1) & 1))) break;
         const int n_list = sh.n_list[ui & 1];
         for (int g = 0; ok && g < n_list; g += per) {
           const int n = min(per, n_list - g), parts = per / n * n;     // fewer adapters: copies, see the epilogue
-          for (int ks = 0; ks < a.stages; ++ks, turn.next(ring)) {
-            const uint32_t st = stage(ks, row0, (uint32_t)(parts * a.rp * kProjStage));
+          for (int ks = 0; ks < a.stages; ++ks, wturn.next(ring)) {
+            if (g > 0 || ks >= ahead) ask_x(ks, row0);
             if (!ok) break;
+            const uint32_t bar = ptx::smem_u32(&sh.full[wturn.slot]), dst = base + wturn.slot * stage_bytes + RT * kProjStage;
+            ptx::mbar_expect_tx(bar, (uint32_t)(parts * a.rp * kProjStage));
             for (int i = 0; i < parts; ++i)
-              ptx::bulk_g2s(st + RT * kProjStage + i * a.rp * kProjStage,
-                            a.down + ((size_t)sh.list[ui & 1][g + i % n] * a.stages + ks) * a.rp * kProjStage,
-                            (uint32_t)(a.rp * kProjStage), ptx::smem_u32(&sh.full[turn.slot]));
+              ptx::bulk_g2s(dst + i * a.rp * kProjStage, a.down + ((size_t)sh.list[ui & 1][g + i % n] * a.stages + ks) * a.rp * kProjStage,
+                            (uint32_t)(a.rp * kProjStage), bar);
           }
         }
       }
       for (int tn = t0; ok && tn < t1; ++tn)
-        for (int ks = 0; ks < a.stages; ++ks, turn.next(ring)) {
-          const uint32_t st = stage(ks, row0, kBytesW);
+        for (int ks = 0; ks < a.stages; ++ks, wturn.next(ring)) {
+          // the stages asked for ahead are the first output tile's where no row has an adapter
+          if (!(kFused && adapters && tn == t0 && ks < min(ring, a.stages) && sh.n_list[ui & 1] == 0)) ask_x(ks, row0);
           if (!ok) break;
-          ptx::bulk_g2s(st + RT * kProjStage, a.w + ((size_t)tn * a.stages + ks) * kBytesW, kBytesW, ptx::smem_u32(&sh.full[turn.slot]));
+          const uint32_t bar = ptx::smem_u32(&sh.full[wturn.slot]);
+          ptx::mbar_expect_tx(bar, kBytesW);
+          ptx::bulk_g2s(base + wturn.slot * stage_bytes + RT * kProjStage, a.w + ((size_t)tn * a.stages + ks) * kBytesW, kBytesW, bar);
         }
     }
   } else if (warp == 1 && ptx::elect_one()) {
@@ -480,13 +496,21 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         if (r < RT) sh.slot[ub][r] = scan || row >= a.rows ? -2 : kFused ? slot_of_row(a, row) : a.row_slot[row];
       }
       fill_all(true);
-      if (scan) {                                       // each request writes its rows of the tile: one trip to memory
-        for (int q = f; q < a.n_seg; q += kFill) {
-          const int s0 = a.seg_start[q], s1 = a.seg_start[q + 1], ad = a.seg_adapter[q];
-          const int lo = max(s0, row0), hi = min(min(s1, row0 + RT), a.rows);
-          if (lo >= hi) continue;
-          const int s = ad >= 0 && ad < a.max_adapters ? ad : -1;
-          for (int r = lo; r < hi; ++r) sh.slot[ub][r - row0] = s;
+      if (scan) {                                       // a warp reads 32 requests and writes the rows of those in the tile
+        for (int q0 = f & ~31; q0 < a.n_seg; q0 += kFill) {
+          const int q = q0 + lane;
+          int lo = 0, hi = 0, s = -1;
+          if (q < a.n_seg) {
+            const int s0 = a.seg_start[q], s1 = a.seg_start[q + 1], ad = a.seg_adapter[q];
+            lo = max(s0, row0);
+            hi = min(min(s1, row0 + RT), a.rows);
+            if (ad >= 0 && ad < a.max_adapters) s = ad;
+          }
+          for (uint32_t in = __ballot_sync(0xFFFFFFFFu, lo < hi); in; in &= in - 1) {
+            const int from = __ffs((int)in) - 1;
+            const int rlo = __shfl_sync(0xFFFFFFFFu, lo, from), rhi = __shfl_sync(0xFFFFFFFFu, hi, from), rs = __shfl_sync(0xFFFFFFFFu, s, from);
+            for (int r = rlo + lane; r < rhi; r += 32) sh.slot[ub][r - row0] = rs;
+          }
         }
         fill_all(true);
       }
@@ -532,15 +556,20 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
               ptx::mbar_arrive(bar);
             }
           }
+          for (int i = 0; i < slices; ++i) {
+            const int s = sh.list[ub][at + i];
+            for (int c = 0; c < a.rp / 16; c += 2) {    // 32 rank channels of two rows: loads first, then stores
+              int4 t[2][2];
 #pragma unroll
-          for (int r2 = 0; r2 < 2; ++r2) {
-            const int r = f + r2 * kFill;
-            if (r >= RT) continue;
-            const int4* src = reinterpret_cast<const int4*>(a.h + (size_t)(row0 + r) * a.rp);
-            for (int i = 0; i < slices; ++i) {
-              const bool mine = slot[r2] == sh.list[ub][at + i];
-              for (int c = 0; c < a.rp / 16; ++c)
-                *reinterpret_cast<int4*>(h + ((i * (a.rp / 16) + c) * RT + r) * 16) = mine ? __ldcg(src + c) : make_int4(0, 0, 0, 0);
+              for (int e = 0; e < 4; ++e) {
+                const bool mine = slot[e >> 1] == s;
+                t[e >> 1][e & 1] = make_int4(0, 0, 0, 0);
+                if (mine) t[e >> 1][e & 1] = __ldcg(reinterpret_cast<const int4*>(a.h + (size_t)(row0 + f + (e >> 1) * kFill) * a.rp) + c + (e & 1));
+              }
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (f + (e >> 1) * kFill < RT)
+                  *reinterpret_cast<int4*>(h + ((i * (a.rp / 16) + c + (e & 1)) * RT + f + (e >> 1) * kFill) * 16) = t[e >> 1][e & 1];
             }
           }
           ptx::fence_async_smem();
@@ -606,42 +635,54 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         const long long add = (long long)(((unsigned long long)(uint32_t)rq.w << 32) | (uint32_t)rq.z);
         const int shift = max(rq.y - 1, 0);
         const bool words = sizeof(YT) == 1 && shp.vector_y && n0 + 32 <= a.n;
-        const int first = words ? lane >> 3 << 2 : 0;  // rows first .. first + 3 of 16 are this lane's, channels n0 + 4 (lane & 7) ..
+        const int first = words ? lane >> 3 << 2 : 0;  // rows first .. first + 3 of each 16 are this lane's, channels n0 + 4 (lane & 7) ..
         YT* y = (YT*)a.y + (long long)(row0 + c0 + first) * a.ldy + (words ? n0 + (lane & 7) * 4 : n);
         const uint32_t d = sums();
         if (!ok) break;
-        for (int c = 0; c < cols; c += 16, y += 16 * a.ldy) {
-          uint32_t v[16];
-          ptx::tmem_ld16(d + c, v);
+        for (int c = 0; c < cols; c += 32, y += 32 * a.ldy) {
+          uint32_t v[2][16];
+          ptx::tmem_ld16(d + c, v[0]);
+          ptx::tmem_ld16(d + c + 16, v[1]);
           const int r = c0 + c, rest = a.rows - row0 - r;
-          uint32_t rows16 = rest >= 16 ? 0xFFFFu : rest > 0 ? (1u << rest) - 1 : 0;    // the rows that are written, a bit each
-          if (adapters) rows16 &= sh.live[ub][r >> 5] >> (r & 31);
-          ptx::tmem_ld_wait16(v);
-          int o[16];
+          uint32_t rows32 = rest >= 32 ? 0xFFFFFFFFu : rest > 0 ? (1u << rest) - 1 : 0;    // the rows that are written, a bit each
+          if (adapters) rows32 &= sh.live[ub][r >> 5];
+          ptx::tmem_ld_wait16(v[0]);
+          ptx::tmem_ld_wait16_nosync(v[1]);
+          int o[32];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) o[e] = requantised<kAnyShift>((int)v[e], rq, add, shift);
+          for (int e = 0; e < 32; ++e) o[e] = requantised<kAnyShift>((int)v[e >> 4][e & 15], rq, add, shift);
           if (shp.clip) {
 #pragma unroll
-            for (int e = 0; e < 16; ++e) o[e] = min(max(o[e], a.lo), a.hi);
+            for (int e = 0; e < 32; ++e) o[e] = min(max(o[e], a.lo), a.hi);
           }
-          YT* p = y;
-          if (words) {                                  // four rows to a word, 16 x 32 of them transposed through shared memory
+          if (words) {                                  // four rows to a word, 32 x 32 of them transposed through shared memory
 #pragma unroll
-            for (int i = 0; i < 4; ++i) stage[i * 32 + lane] = pack4<YT>(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+            for (int i = 0; i < 8; ++i) stage[i * 32 + lane] = pack4<YT>(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
             __syncwarp();
-            const int4 t = *reinterpret_cast<const int4*>(stage + (lane >> 3) * 32 + (lane & 7) * 4);
+            const int4 t0 = *reinterpret_cast<const int4*>(stage + lane * 4), t1 = *reinterpret_cast<const int4*>(stage + 128 + lane * 4);
             __syncwarp();
-            const uint32_t ab = __byte_perm(t.x, t.y, 0x5140), cd = __byte_perm(t.z, t.w, 0x5140);      // rows 0 and 1 of channels 0, 1 and 2, 3
-            const uint32_t ef = __byte_perm(t.x, t.y, 0x7362), gh = __byte_perm(t.z, t.w, 0x7362);
-            const uint32_t w[4] = {__byte_perm(ab, cd, 0x5410), __byte_perm(ab, cd, 0x7632), __byte_perm(ef, gh, 0x5410), __byte_perm(ef, gh, 0x7632)};
+            uint32_t w[8];
+            transpose4(t0, w);
+            transpose4(t1, w + 4);
+            YT* p = y;
+            if (rows32 == 0xFFFFFFFFu) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i, p += a.ldy)
-              if (rows16 >> (first + i) & 1) *reinterpret_cast<uint32_t*>(p) = w[i];
-          } else {
+              for (int i = 0; i < 4; ++i, p += a.ldy) {
+                *reinterpret_cast<uint32_t*>(p) = w[i];
+                *reinterpret_cast<uint32_t*>(p + 16 * a.ldy) = w[4 + i];
+              }
+            } else {
 #pragma unroll
-            for (int e = 0; e < 16; ++e, p += a.ldy)
-              if ((rows16 >> e & 1) && n < a.n)
-                *p = sizeof(YT) == 4 ? (YT)o[e] : (YT)min(max(o[e], YT(-1) < YT(0) ? -128 : 0), YT(-1) < YT(0) ? 127 : 255);
+              for (int i = 0; i < 4; ++i, p += a.ldy) {
+                if (rows32 >> (first + i) & 1) *reinterpret_cast<uint32_t*>(p) = w[i];
+                if (rows32 >> (16 + first + i) & 1) *reinterpret_cast<uint32_t*>(p + 16 * a.ldy) = w[4 + i];
+              }
+            }
+          } else if (n < a.n) {
+            YT* p = y;
+#pragma unroll
+            for (int e = 0; e < 32; ++e, p += a.ldy)
+              if (rows32 >> e & 1) *p = sizeof(YT) == 4 ? (YT)o[e] : (YT)min(max(o[e], YT(-1) < YT(0) ? -128 : 0), YT(-1) < YT(0) ? 127 : 255);
           }
         }
         done(&sh.tempty[ti & 1]);
@@ -804,7 +845,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) proj_split_kernel(const __gr
   }
 }
 
-constexpr int kMaxSmem = 213 * 1024;      // beside 1 KB of alignment and the static part
+constexpr int kMaxSmem = 204 * 1024;      // beside 1 KB of alignment and the static part
 
 // Rows of a tile of the kernel for few rows: 0 where its tiles would be more than the SMs, or h too much for down_rows_kernel.
 int split_tile(const ProjArgs& a) {
@@ -817,19 +858,24 @@ int split_tile(const ProjArgs& a) {
 // h within the projection's own kernel, or before it.
 bool fuse_down(const ProjArgs& a) { return a.stages <= 8; }
 
-// Output tiles of a unit: the most that cost the least, in items of a whole round of the SMs (a unit has one more item with adapters).
-int fused_chunk(const ProjArgs& a, int row_tiles) {
-  int best = 1;
+// Rows of a tile and output tiles of a unit of the persistent kernel: what costs the least in rounds of the SMs. A round is a
+// unit's items (its output tiles, and one more for h with adapters), and an item costs its rows and as much as 128
+// rows more (measured on 32768 x 256 -> 256 and 65536 x 512 -> 512: 4 to 6 us with 256 rows, latencies for half of it).
+void main_tiles(const ProjArgs& a, int* tile, int* chunk) {
+  const bool fused = fuse_down(a);
   long long least = LLONG_MAX;
-  for (int c = 1; c <= a.tiles_n; ++c) {
-    const long long units = (long long)row_tiles * ((a.tiles_n + c - 1) / c);
-    const long long cost = (units + a.sms - 1) / a.sms * (c + (a.n_seg ? 1 : 0));
-    if (cost <= least) {
-      least = cost;
-      best = c;
+  for (int t = kMaxTile; t >= kMaxTile / 2; t /= 2) {
+    const long long row_tiles = (a.rows + t - 1) / t;
+    for (int c = 1; c <= (fused ? a.tiles_n : 1); ++c) {
+      const long long units = row_tiles * ((a.tiles_n + c - 1) / c);
+      const long long cost = (units + a.sms - 1) / a.sms * (c + (fused && a.n_seg ? 1 : 0)) * (t + 128);
+      if (cost < least) {
+        least = cost;
+        *tile = t;
+        *chunk = c;
+      }
     }
   }
-  return best;
 }
 
 template <class Shape>
@@ -876,7 +922,8 @@ cudaError_t launch_main(const ProjArgs& a, const CUtensorMap& map, cudaStream_t 
   const int ab = a.n_seg ? 2 * s.abytes : 0, row_tiles = (a.rows + tile - 1) / tile;
   s.ring = std::min(kMaxRing, (kMaxSmem - ab) / stage);
   const bool fused = fuse_down(a);
-  s.chunk = fused ? fused_chunk(a, row_tiles) : 1;
+  int unused;
+  main_tiles(a, &unused, &s.chunk);
   s.chunks = (a.tiles_n + s.chunk - 1) / s.chunk;
   s.units = row_tiles * s.chunks;
   return launch_tiles(fused ? proj_tile_kernel<YT, kAnyShift, true> : proj_tile_kernel<YT, kAnyShift, false>, a, map, s,
@@ -904,12 +951,10 @@ cudaError_t configure_proj_kernels() {
   return e;
 }
 
-// In the persistent kernel the widest tile that still gives every SM one.
 int proj_row_tile(const ProjArgs& a) {
-  if (const int split = split_tile(a)) return split;
-  int t = kMaxTile;
-  while (t > 64 && (t / 2 >= a.rows || (long long)a.tiles_n * ((a.rows + t - 1) / t) < a.sms)) t /= 2;
-  return t;
+  int tile = split_tile(a), chunk;
+  if (!tile) main_tiles(a, &tile, &chunk);
+  return tile;
 }
 
 cudaError_t launch_proj(const ProjArgs& a, const void* x_map, const void* x_map_down, cudaStream_t stream) {
