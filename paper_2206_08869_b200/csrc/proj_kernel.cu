@@ -277,15 +277,20 @@ __global__ void __launch_bounds__(kDownThreads) down_tile_kernel(const __grid_co
 }
 
 // ---- the projection ----------------------------------------------------------------------------------------------
-// Persistent: a CTA takes units of one row tile and `chunk` output tiles. Two ways to come by h:
+// Persistent: a CTA takes units of one row tile and `chunk` output tiles; each output tile is an item: a product over K
+// into one of two accumulators. Two ways to come by h:
 //   fused     the CTA computes it itself, as further items of its pipeline in front of the unit's output tiles: the
 //             sums of `down x^T` go through the same accumulators, and h through global memory to the warps that lay it out
 //   separate  down_tile_kernel has computed it before (units of one output tile)
-// Fused repeats the product for every chunk of output tiles, separate costs a launch and a wait for it.
+// Fused repeats the product for every chunk of output tiles, separate costs a launch and a wait for it. Fused units hold all
+// of their x tile in shared memory: it is read once for all items, which are bound by what an SM draws from L2 otherwise
+// (48 KB a stage, some 1000 clocks, for 512 clocks of MMAs).
 constexpr int kMaxTile = 256;
 
+constexpr int kMaxX = 16;
+
 struct MainShared {
-  uint64_t full[kMaxRing], empty[kMaxRing], afull[2], aempty[2], tfull[2], tempty[2], lready[2], lfree[2], hready;
+  uint64_t xfull[kMaxX], xempty[kMaxX], wfull[kMaxRing], wempty[kMaxRing], afull[2], aempty[2], tfull[2], tempty[2], lready[2], lfree[2], hready;
   uint32_t abort_flag, tmem;
   int message[2];                        // an adapter step: its adapters, 256: the tile's last
   int n_list[2];
@@ -297,7 +302,7 @@ struct MainShared {
 
 struct MainShape {
   int tile;                              // rows per tile: 128 or 256
-  int ring;                              // stages
+  int xring, wring;                      // stages of x and of weights in shared memory
   int tmem_cols;
   int chunk, chunks;                     // output tiles of a unit, units of a row tile
   int units;
@@ -357,12 +362,16 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   __shared__ MainShared sh;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int RT = shp.tile, ring = shp.ring;
-  const uint32_t stage_bytes = (uint32_t)(RT * kProjStage + kBytesW);
+  const int RT = shp.tile;
+  const uint32_t xbytes = (uint32_t)(RT * kProjStage);
   if (tid == 0) {
-    for (int i = 0; i < ring; ++i) {
-      ptx::mbar_init(ptx::smem_u32(&sh.full[i]), 2);            // x, weights
-      ptx::mbar_init(ptx::smem_u32(&sh.empty[i]), 1);
+    for (int i = 0; i < shp.xring; ++i) {
+      ptx::mbar_init(ptx::smem_u32(&sh.xfull[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&sh.xempty[i]), 1);
+    }
+    for (int i = 0; i < shp.wring; ++i) {
+      ptx::mbar_init(ptx::smem_u32(&sh.wfull[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&sh.wempty[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(ptx::smem_u32(&sh.afull[i]), kFill + 1);
@@ -380,39 +389,43 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
-  const uint32_t base = ptx::smem_u32(smem), abase = base + ring * stage_bytes, tmem = sh.tmem;
+  const uint32_t base = ptx::smem_u32(smem), wbase = base + shp.xring * xbytes, abase = wbase + shp.wring * kBytesW, tmem = sh.tmem;
   volatile uint32_t* abort_flag = &sh.abort_flag;
   auto wait = [&](uint64_t* bar, uint32_t parity) { return ptx::quick_wait(abort_flag, a.status, bar, parity, kSpinLimit); };
   const int per = kProjTileN / a.rp;                  // adapters of one product `down x^T`
   const bool adapters = a.n_seg != 0;
 
-  if (warp == 0 && ptx::elect_one()) {
-    Turn turn;                                          // of x; the weights of a stage follow, at most a ring behind
-    Turn wturn;
+  // x of a unit: fused, xring is once or twice the stages and unit ui has slots from xslot0(ui) on; else it is a plain ring
+  const int sets = kFused ? shp.xring / a.stages : 1;
+  auto xslot0 = [&](int ui) { return sets == 2 ? (ui & 1) * a.stages : 0; };
+  auto xphase = [&](int ui) { return (uint32_t)(sets == 2 ? ui >> 1 : ui) & 1u; };
+
+  if (warp == 3 && ptx::elect_one()) {
+    Turn turn;
     int ui = 0;
     bool ok = true;
-    auto ask_x = [&](int ks, int row0) {
-      ok = wait(&sh.empty[turn.slot], turn.phase ^ 1);
-      if (!ok) return;
-      const uint32_t bar = ptx::smem_u32(&sh.full[turn.slot]);
-      ptx::mbar_expect_tx(bar, RT * kProjStage);
-      ptx::tile_g2s(base + turn.slot * stage_bytes, &xmap, ks * kProjStage, row0, bar);
-      turn.next(ring);
-    };
+    for (int u = blockIdx.x; ok && u < shp.units; u += gridDim.x, ++ui)
+      for (int ks = 0; ks < a.stages; ++ks, turn.next(shp.xring)) {
+        const int s = kFused ? xslot0(ui) + ks : turn.slot;
+        if (!(ok = wait(&sh.xempty[s], (kFused ? xphase(ui) : turn.phase) ^ 1))) break;
+        const uint32_t bar = ptx::smem_u32(&sh.xfull[s]);
+        ptx::mbar_expect_tx(bar, xbytes);
+        ptx::tile_g2s(base + s * xbytes, &xmap, ks * kProjStage, u / shp.chunks * RT, bar);
+      }
+  } else if (warp == 0 && ptx::elect_one()) {
+    Turn turn;
+    int ui = 0;
+    bool ok = true;
     for (int u = blockIdx.x; ok && u < shp.units; u += gridDim.x, ++ui) {
-      const int row0 = u / shp.chunks * RT, t0 = u % shp.chunks * shp.chunk, t1 = min(t0 + shp.chunk, a.tiles_n);
+      const int t0 = u % shp.chunks * shp.chunk, t1 = min(t0 + shp.chunk, a.tiles_n);
       if (kFused && adapters) {
-        // x of the first product does not depend on the rows' adapters: it is asked for before they are known
-        const int ahead = min(ring, a.stages);
-        for (int ks = 0; ok && ks < ahead; ++ks) ask_x(ks, row0);
-        if (!ok || !(ok = wait(&sh.lready[ui & 1], (ui >> 1) & 1))) break;
+        if (!(ok = wait(&sh.lready[ui & 1], (ui >> 1) & 1))) break;
         const int n_list = sh.n_list[ui & 1];
         for (int g = 0; ok && g < n_list; g += per) {
           const int n = min(per, n_list - g), parts = per / n * n;     // fewer adapters: copies, see the epilogue
-          for (int ks = 0; ks < a.stages; ++ks, wturn.next(ring)) {
-            if (g > 0 || ks >= ahead) ask_x(ks, row0);
-            if (!ok) break;
-            const uint32_t bar = ptx::smem_u32(&sh.full[wturn.slot]), dst = base + wturn.slot * stage_bytes + RT * kProjStage;
+          for (int ks = 0; ks < a.stages; ++ks, turn.next(shp.wring)) {
+            if (!(ok = wait(&sh.wempty[turn.slot], turn.phase ^ 1))) break;
+            const uint32_t bar = ptx::smem_u32(&sh.wfull[turn.slot]), dst = wbase + turn.slot * kBytesW;
             ptx::mbar_expect_tx(bar, (uint32_t)(parts * a.rp * kProjStage));
             for (int i = 0; i < parts; ++i)
               ptx::bulk_g2s(dst + i * a.rp * kProjStage, a.down + ((size_t)sh.list[ui & 1][g + i % n] * a.stages + ks) * a.rp * kProjStage,
@@ -421,47 +434,48 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         }
       }
       for (int tn = t0; ok && tn < t1; ++tn)
-        for (int ks = 0; ks < a.stages; ++ks, wturn.next(ring)) {
-          // the stages asked for ahead are the first output tile's where no row has an adapter
-          if (!(kFused && adapters && tn == t0 && ks < min(ring, a.stages) && sh.n_list[ui & 1] == 0)) ask_x(ks, row0);
-          if (!ok) break;
-          const uint32_t bar = ptx::smem_u32(&sh.full[wturn.slot]);
+        for (int ks = 0; ks < a.stages; ++ks, turn.next(shp.wring)) {
+          if (!(ok = wait(&sh.wempty[turn.slot], turn.phase ^ 1))) break;
+          const uint32_t bar = ptx::smem_u32(&sh.wfull[turn.slot]);
           ptx::mbar_expect_tx(bar, kBytesW);
-          ptx::bulk_g2s(base + wturn.slot * stage_bytes + RT * kProjStage, a.w + ((size_t)tn * a.stages + ks) * kBytesW, kBytesW, bar);
+          ptx::bulk_g2s(wbase + turn.slot * kBytesW, a.w + ((size_t)tn * a.stages + ks) * kBytesW, kBytesW, bar);
         }
     }
   } else if (warp == 1 && ptx::elect_one()) {
     const uint32_t id = idesc((uint32_t)RT, a.x_unsigned), ida = idesc((uint32_t)RT, false);
     const uint32_t hhi = core_hi(128u);
-    Turn turn;
+    Turn xturn, wturn;
     int ai = 0, ti = 0, ui = 0;
     bool ok = true;
-    auto product = [&]() {                              // one accumulator: all stages of K
+    auto product = [&](bool first, bool last) {         // one accumulator: all stages of K; the unit's first and last item
       ok = wait(&sh.tempty[ti & 1], ((ti >> 1) & 1) ^ 1);
       if (!ok) return;
       ptx::tc_fence_after();
       const uint32_t d = tmem + (ti & 1) * RT;
-      for (int ks = 0; ks < a.stages; ++ks, turn.next(ring)) {
-        const int s = turn.slot;
-        if (!(ok = wait(&sh.full[s], turn.phase))) return;
+      for (int ks = 0; ks < a.stages; ++ks, xturn.next(shp.xring), wturn.next(shp.wring)) {
+        const int xs = kFused ? xslot0(ui) + ks : xturn.slot, ws = wturn.slot;
+        if (first && !(ok = wait(&sh.xfull[xs], kFused ? xphase(ui) : xturn.phase))) return;
+        if (!(ok = wait(&sh.wfull[ws], wturn.phase))) return;
         ptx::tc_fence_after();
-        const uint32_t st = base + s * stage_bytes;
-        stage_mmas(d, core_lo(st + RT * kProjStage), ptx::umma_desc_lo(st, 16u), id, min(4, (a.k - ks * kProjStage + 31) >> 5), ks == 0);
-        ptx::umma_commit(ptx::smem_u32(&sh.empty[s]));
+        stage_mmas(d, core_lo(wbase + ws * kBytesW), ptx::umma_desc_lo(base + xs * xbytes, 16u), id, min(4, (a.k - ks * kProjStage + 31) >> 5), ks == 0);
+        ptx::umma_commit(ptx::smem_u32(&sh.wempty[ws]));
+        if (last) ptx::umma_commit(ptx::smem_u32(&sh.xempty[xs]));
       }
     };
     for (int u = blockIdx.x; ok && u < shp.units; u += gridDim.x, ++ui) {
       const int t0 = u % shp.chunks * shp.chunk, t1 = min(t0 + shp.chunk, a.tiles_n);
+      bool first = true;                                // no item of the unit has waited for its x yet
       if (kFused && adapters) {
         if (!(ok = wait(&sh.lready[ui & 1], (ui >> 1) & 1))) break;
         const int n_list = sh.n_list[ui & 1];
+        first = n_list == 0;
         for (int g = 0; ok && g < n_list; g += per, ++ti) {
-          product();
+          product(g == 0, false);
           if (ok) ptx::umma_commit(ptx::smem_u32(&sh.tfull[ti & 1]));
         }
       }
       for (int tn = t0; ok && tn < t1; ++tn, ++ti) {
-        product();
+        product(first && tn == t0, tn + 1 == t1);
         const uint32_t d = tmem + (ti & 1) * RT;
         for (int last = !adapters; ok && !last; ++ai) {
           if (!(ok = wait(&sh.afull[ai & 1], (ai >> 1) & 1))) break;
@@ -680,9 +694,18 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
             }
           } else if (n < a.n) {
             YT* p = y;
+            if (sizeof(YT) == 1) {
 #pragma unroll
-            for (int e = 0; e < 32; ++e, p += a.ldy)
-              if (rows32 >> e & 1) *p = sizeof(YT) == 4 ? (YT)o[e] : (YT)min(max(o[e], YT(-1) < YT(0) ? -128 : 0), YT(-1) < YT(0) ? 127 : 255);
+              for (int e = 0; e < 32; ++e) o[e] = min(max(o[e], YT(-1) < YT(0) ? -128 : 0), YT(-1) < YT(0) ? 127 : 255);
+            }
+            if (rows32 == 0xFFFFFFFFu) {
+#pragma unroll
+              for (int e = 0; e < 32; ++e, p += a.ldy) *p = (YT)o[e];
+            } else {
+#pragma unroll
+              for (int e = 0; e < 32; ++e, p += a.ldy)
+                if (rows32 >> e & 1) *p = (YT)o[e];
+            }
           }
         }
         done(&sh.tempty[ti & 1]);
@@ -855,8 +878,31 @@ int split_tile(const ProjArgs& a) {
   return (long long)a.tiles_n * ((a.rows + t - 1) / t) <= a.sms ? t : 0;
 }
 
+// Shared memory of the persistent kernel with tiles of `tile` rows: false if it does not fit.
+bool main_rings(const ProjArgs& a, int tile, bool fused, MainShape* s) {
+  const int x = tile * kProjStage;
+  for (s->step_adapters = a.rp == 32 ? 2 : 1; s->step_adapters >= 1; --s->step_adapters) {
+    s->abytes = (kProjTileN + tile) * a.rp * s->step_adapters;
+    const int room = kMaxSmem - (a.n_seg ? 2 * s->abytes : 0);
+    if (fused) {
+      for (int sets = 2; sets >= 1; --sets) {
+        s->xring = sets * a.stages;
+        s->wring = std::min(kMaxRing, (room - s->xring * x) / kBytesW);
+        if (s->xring <= kMaxX && s->wring >= 3) return true;
+      }
+    } else {
+      s->xring = s->wring = std::min(kMaxRing, room / (x + kBytesW));
+      if (s->xring >= 2) return true;
+    }
+  }
+  return false;
+}
+
 // h within the projection's own kernel, or before it.
-bool fuse_down(const ProjArgs& a) { return a.stages <= 8; }
+bool fuse_down(const ProjArgs& a) {
+  MainShape s;
+  return main_rings(a, kMaxTile / 2, true, &s);
+}
 
 // Rows of a tile and output tiles of a unit of the persistent kernel: what costs the least in rounds of the SMs. A round is a
 // unit's items (its output tiles, and one more for h with adapters), and an item costs its rows and as much as 128
@@ -866,6 +912,8 @@ void main_tiles(const ProjArgs& a, int* tile, int* chunk) {
   long long least = LLONG_MAX;
   for (int t = kMaxTile; t >= kMaxTile / 2; t /= 2) {
     const long long row_tiles = (a.rows + t - 1) / t;
+    MainShape s;
+    if (!main_rings(a, t, fused, &s)) continue;
     for (int c = 1; c <= (fused ? a.tiles_n : 1); ++c) {
       const long long units = row_tiles * ((a.tiles_n + c - 1) / c);
       const long long cost = (units + a.sms - 1) / a.sms * (c + (fused && a.n_seg ? 1 : 0)) * (t + 128);
@@ -917,17 +965,16 @@ cudaError_t launch_main(const ProjArgs& a, const CUtensorMap& map, cudaStream_t 
   s.vector_y = a.y_bytes == 1 && a.ldy % 4 == 0 && y % 4 == 0;
   const int lo = a.y_type == IODF_I8 ? -128 : a.y_type == IODF_U8 ? 0 : INT_MIN, hi = a.y_type == IODF_I8 ? 127 : a.y_type == IODF_U8 ? 255 : INT_MAX;
   s.clip = a.lo > lo || a.hi < hi;
-  s.step_adapters = a.rp == 32 ? 2 : 1;
-  s.abytes = (kProjTileN + tile) * std::max(a.rp, 64);
-  const int ab = a.n_seg ? 2 * s.abytes : 0, row_tiles = (a.rows + tile - 1) / tile;
-  s.ring = std::min(kMaxRing, (kMaxSmem - ab) / stage);
   const bool fused = fuse_down(a);
+  main_rings(a, tile, fused, &s);
+  const int row_tiles = (a.rows + tile - 1) / tile;
   int unused;
   main_tiles(a, &unused, &s.chunk);
   s.chunks = (a.tiles_n + s.chunk - 1) / s.chunk;
   s.units = row_tiles * s.chunks;
   return launch_tiles(fused ? proj_tile_kernel<YT, kAnyShift, true> : proj_tile_kernel<YT, kAnyShift, false>, a, map, s,
-                      std::min(s.units, a.sms), 1, kMainThreads, (size_t)(s.ring * stage + ab + 1024), !fused, stream);
+                      std::min(s.units, a.sms), 1, kMainThreads,
+                      (size_t)(s.xring * tile * kProjStage + s.wring * kBytesW + (a.n_seg ? 2 * s.abytes : 0) + 1024), !fused, stream);
 }
 
 template <class YT, bool kAnyShift>
