@@ -360,7 +360,7 @@ int iodf_proj_forward(iodf_proj* p, const void* x, size_t ldx, int rows, const i
   OnDevice on(p->device);
   if (on.error() != cudaSuccess) return IODF_ECUDA;
   CUtensorMap map, map_down;
-  if (!x_map(*p, a, proj_row_tile(a), &map) || !x_map(*p, a, kProjDownRows, &map_down)) return IODF_ECUDA;
+  if (!x_map(*p, a, proj_x_rows(a), &map) || !x_map(*p, a, kProjDownRows, &map_down)) return IODF_ECUDA;
   return status_of(launch_proj(a, &map, &map_down, (cudaStream_t)cuda_stream));
 }
 

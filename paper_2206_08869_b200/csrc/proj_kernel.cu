@@ -33,9 +33,9 @@ constexpr int kDownThreads = 128 + 32 * kDownEpiWarps;   // warp 0 copies, 1 MMA
 constexpr int kDownStageBytes = kDownRows * kProjStage + kBytesW;
 constexpr int kScanRequests = 2048;      // up to here a tile reads every request, above it halves for each row
 
-// D = s32; A int8 (weights), B int8 or uint8, both K-major, M = 128, N = n
-__device__ __forceinline__ uint32_t idesc(uint32_t n, bool b_unsigned) {
-  return (2u << 4) | (1u << 7) | ((b_unsigned ? 0u : 1u) << 10) | ((n >> 3) << 17) | ((128u >> 4) << 24);
+// D = s32; A int8 (weights), B int8 or uint8, both K-major, M = m, N = n
+__device__ __forceinline__ uint32_t idesc(uint32_t n, bool b_unsigned, uint32_t m = 128u) {
+  return (2u << 4) | (1u << 7) | ((b_unsigned ? 0u : 1u) << 10) | ((n >> 3) << 17) | ((m >> 4) << 24);
 }
 // operand words: core matrices 128 bytes apart along K, groups of eight rows sbo apart
 __device__ __forceinline__ uint32_t core_lo(uint32_t saddr) { return ptx::umma_desc_lo(saddr, 128u); }
@@ -54,14 +54,21 @@ struct Turn {
   }
 };
 
+template <bool kPair>
+__device__ __forceinline__ void mma(uint32_t d, uint32_t alo, uint32_t ahi, uint32_t blo, uint32_t bhi, uint32_t id, uint32_t acc) {
+  if (kPair) ptx::umma_i8_hl_pair(d, alo, ahi, blo, bhi, id, acc);
+  else ptx::umma_i8_hl(d, alo, ahi, blo, bhi, id, acc);
+}
+
 // The MMAs of a stage: up to four steps of 32 channels, both operands K-major (x with the 128-byte swizzle).
+template <bool kPair = false>
 __device__ __forceinline__ void stage_mmas(uint32_t d, uint32_t alo, uint32_t blo, uint32_t id, int steps, bool first) {
-  ptx::umma_i8_hl(d, alo, core_hi(1024u), blo, kSwizzledHi, id, first ? 0u : 1u);
+  mma<kPair>(d, alo, core_hi(1024u), blo, kSwizzledHi, id, first ? 0u : 1u);
   if (steps == 4) {
 #pragma unroll
-    for (int k = 1; k < 4; ++k) ptx::umma_i8_hl(d, alo + k * 16, core_hi(1024u), blo + k * 2, kSwizzledHi, id, 1u);
+    for (int k = 1; k < 4; ++k) mma<kPair>(d, alo + k * 16, core_hi(1024u), blo + k * 2, kSwizzledHi, id, 1u);
   } else {
-    for (int k = 1; k < steps; ++k) ptx::umma_i8_hl(d, alo + k * 16, core_hi(1024u), blo + k * 2, kSwizzledHi, id, 1u);
+    for (int k = 1; k < steps; ++k) mma<kPair>(d, alo + k * 16, core_hi(1024u), blo + k * 2, kSwizzledHi, id, 1u);
   }
 }
 
@@ -277,23 +284,25 @@ __global__ void __launch_bounds__(kDownThreads) down_tile_kernel(const __grid_co
 }
 
 // ---- the projection ----------------------------------------------------------------------------------------------
-// Persistent: a CTA takes units of one row tile and `chunk` output tiles; each output tile is an item: a product over K
-// into one of two accumulators. Two ways to come by h:
-//   fused     the CTA computes it itself, as further items of its pipeline in front of the unit's output tiles: the
-//             sums of `down x^T` go through the same accumulators, and h through global memory to the warps that lay it out
-//   separate  down_tile_kernel has computed it before (units of one output tile)
-// Fused repeats the product for every chunk of output tiles, separate costs a launch and a wait for it. Fused units hold all
-// of their x tile in shared memory: it is read once for all items, which are bound by what an SM draws from L2 otherwise
-// (48 KB a stage, some 1000 clocks, for 512 clocks of MMAs).
+// Persistent: units of one row tile and some output tiles; each output tile is an item: a product over K into one of two
+// accumulators, the steps of its rows' adapters, the epilogue. Two forms, by whether an x tile fits in shared memory:
+//   fused  (K up to about 1000) a CTA per unit of `chunk` output tiles. It holds the unit's x tile, read once for all
+//          items, and computes h itself, as further items in front of the output tiles: the sums of `down x^T` go through the
+//          same accumulators, and h through global memory to the warps that lay it out. That repeats the product for
+//          every unit of a row tile and saves a launch and a wait for it.
+//   paired (larger K) two CTAs per unit of two output tiles, one each, and one MMA over both (M = 256). Each reads half of
+//          the x tile: a stage is 32 KB of copies and 32 KB of operand reads per SM for 512 clocks of MMAs, where single CTAs
+//          have 48 KB of each, more than the 128 bytes per clock of shared memory. down_tile_kernel computes h before.
 constexpr int kMaxTile = 256;
 
 constexpr int kMaxX = 16;
 
 struct MainShared {
-  uint64_t xfull[kMaxX], xempty[kMaxX], wfull[kMaxRing], wempty[kMaxRing], afull[2], aempty[2], tfull[2], tempty[2], lready[2], lfree[2], hready;
+  uint64_t xfull[kMaxX], xempty[kMaxX], wfull[kMaxRing], wempty[kMaxRing], wpeer[kMaxRing], apeer[2], afull[2], aempty[2], tfull[2], tempty[2], lready[2], lfree[2], hready;
   uint32_t abort_flag, tmem;
   int message[2];                        // an adapter step: its adapters, 256: the tile's last
   int n_list[2];
+  uint32_t firsts[kMaxTile / 32];        // rows whose adapter no row above has, a bit each
   alignas(16) int slot[2][kMaxTile];     // of a unit: adapter of each row
   int list[2][kMaxTile];                 //            every adapter once
   uint32_t live[2][kMaxTile / 32];       // of a unit: the rows that some request owns
@@ -304,7 +313,7 @@ struct MainShape {
   int tile;                              // rows per tile: 128 or 256
   int xring, wring;                      // stages of x and of weights in shared memory
   int tmem_cols;
-  int chunk, chunks;                     // output tiles of a unit, units of a row tile
+  int chunk, chunks;                     // output tiles of a unit (paired: of each CTA), units of a row tile
   int units;
   int abytes;                            // an adapter step's operands: `up`, h
   int step_adapters;                     // adapters of a step
@@ -362,8 +371,11 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   __shared__ MainShared sh;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int RT = shp.tile;
-  const uint32_t xbytes = (uint32_t)(RT * kProjStage);
+  constexpr bool kPair = !kFused;
+  const int RT = shp.tile, half = kPair ? RT / 2 : RT;      // rows of x (and of h) in this CTA's shared memory
+  const int part = kPair ? (int)ptx::cluster_rank() : 0;
+  const int unit0 = kPair ? blockIdx.x / 2 : blockIdx.x, unit_step = kPair ? gridDim.x / 2 : gridDim.x;
+  const uint32_t xbytes = (uint32_t)(half * kProjStage);
   if (tid == 0) {
     for (int i = 0; i < shp.xring; ++i) {
       ptx::mbar_init(ptx::smem_u32(&sh.xfull[i]), 1);
@@ -372,12 +384,14 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
     for (int i = 0; i < shp.wring; ++i) {
       ptx::mbar_init(ptx::smem_u32(&sh.wfull[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&sh.wempty[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&sh.wpeer[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(ptx::smem_u32(&sh.afull[i]), kFill + 1);
       ptx::mbar_init(ptx::smem_u32(&sh.aempty[i]), 1);
+      ptx::mbar_init(ptx::smem_u32(&sh.apeer[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&sh.tfull[i]), 1);
-      ptx::mbar_init(ptx::smem_u32(&sh.tempty[i]), kEpiWarps);
+      ptx::mbar_init(ptx::smem_u32(&sh.tempty[i]), kPair ? 2 * kEpiWarps : kEpiWarps);
       ptx::mbar_init(ptx::smem_u32(&sh.lready[i]), kFill);
       ptx::mbar_init(ptx::smem_u32(&sh.lfree[i]), kEpiWarps);
     }
@@ -385,7 +399,15 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
     ptx::mbar_init_fence();
     sh.abort_flag = 0;
   }
-  if (warp == 2) ptx::tmem_alloc(ptx::smem_u32(&sh.tmem), (uint32_t)shp.tmem_cols);
+  if (kPair) {                                          // both CTAs' barriers are there before either arrives on the other's
+    __syncwarp();
+    ptx::cluster_arrive();
+    ptx::cluster_wait();
+  }
+  if (warp == 2) {
+    if (kPair) ptx::tmem_alloc_pair(ptx::smem_u32(&sh.tmem), (uint32_t)shp.tmem_cols);
+    else ptx::tmem_alloc(ptx::smem_u32(&sh.tmem), (uint32_t)shp.tmem_cols);
+  }
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
@@ -395,19 +417,23 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
   const int per = kProjTileN / a.rp;                  // adapters of one product `down x^T`
   const bool adapters = a.n_seg != 0;
 
-  // x of a unit: fused, xring is once or twice the stages and unit ui has slots from xslot0(ui) on; else it is a plain ring
-  const int sets = kFused ? shp.xring / a.stages : 1;
+  // the output tiles of unit u: fused, first_tile to last_tile - 1 in turn; paired, one (the second CTA's may lie behind the last)
+  auto first_tile = [&](int u) { return kPair ? u % shp.chunks * 2 + part : u % shp.chunks * shp.chunk; };
+  auto last_tile = [&](int u) { return kPair ? first_tile(u) + 1 : min(first_tile(u) + shp.chunk, a.tiles_n); };
+  auto stored_tile = [&](int tn) { return kPair ? min(tn, a.tiles_n - 1) : tn; };      // whose weights stand in for one behind the last
+  // x of a fused unit: xring is once or twice the stages, unit ui has slots from xslot0(ui) on. Paired: a stage's x and
+  // weights are slots of one ring with one barrier.
+  const int sets = kPair ? 1 : shp.xring / a.stages;
   auto xslot0 = [&](int ui) { return sets == 2 ? (ui & 1) * a.stages : 0; };
   auto xphase = [&](int ui) { return (uint32_t)(sets == 2 ? ui >> 1 : ui) & 1u; };
 
-  if (warp == 3 && ptx::elect_one()) {
-    Turn turn;
+  if (!kPair && warp == 3 && ptx::elect_one()) {
     int ui = 0;
     bool ok = true;
-    for (int u = blockIdx.x; ok && u < shp.units; u += gridDim.x, ++ui)
-      for (int ks = 0; ks < a.stages; ++ks, turn.next(shp.xring)) {
-        const int s = kFused ? xslot0(ui) + ks : turn.slot;
-        if (!(ok = wait(&sh.xempty[s], (kFused ? xphase(ui) : turn.phase) ^ 1))) break;
+    for (int u = unit0; ok && u < shp.units; u += unit_step, ++ui)
+      for (int ks = 0; ks < a.stages; ++ks) {
+        const int s = xslot0(ui) + ks;
+        if (!(ok = wait(&sh.xempty[s], xphase(ui) ^ 1))) break;
         const uint32_t bar = ptx::smem_u32(&sh.xfull[s]);
         ptx::mbar_expect_tx(bar, xbytes);
         ptx::tile_g2s(base + s * xbytes, &xmap, ks * kProjStage, u / shp.chunks * RT, bar);
@@ -416,8 +442,8 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
     Turn turn;
     int ui = 0;
     bool ok = true;
-    for (int u = blockIdx.x; ok && u < shp.units; u += gridDim.x, ++ui) {
-      const int t0 = u % shp.chunks * shp.chunk, t1 = min(t0 + shp.chunk, a.tiles_n);
+    for (int u = unit0; ok && u < shp.units; u += unit_step, ++ui) {
+      const int t0 = first_tile(u), t1 = last_tile(u);
       if (kFused && adapters) {
         if (!(ok = wait(&sh.lready[ui & 1], (ui >> 1) & 1))) break;
         const int n_list = sh.n_list[ui & 1];
@@ -437,33 +463,61 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         for (int ks = 0; ks < a.stages; ++ks, turn.next(shp.wring)) {
           if (!(ok = wait(&sh.wempty[turn.slot], turn.phase ^ 1))) break;
           const uint32_t bar = ptx::smem_u32(&sh.wfull[turn.slot]);
-          ptx::mbar_expect_tx(bar, kBytesW);
-          ptx::bulk_g2s(wbase + turn.slot * kBytesW, a.w + ((size_t)tn * a.stages + ks) * kBytesW, kBytesW, bar);
+          ptx::mbar_expect_tx(bar, kPair ? kBytesW + xbytes : (uint32_t)kBytesW);
+          if (kPair) ptx::tile_g2s(base + turn.slot * xbytes, &xmap, ks * kProjStage, u / shp.chunks * RT + part * half, bar);
+          ptx::bulk_g2s(wbase + turn.slot * kBytesW, a.w + ((size_t)stored_tile(tn) * a.stages + ks) * kBytesW, kBytesW, bar);
         }
     }
-  } else if (warp == 1 && ptx::elect_one()) {
-    const uint32_t id = idesc((uint32_t)RT, a.x_unsigned), ida = idesc((uint32_t)RT, false);
+  } else if (warp == 1 && part == 1 && ptx::elect_one()) {
+    // the second CTA of a pair tells the first, which issues the MMAs, what has arrived in its shared memory
+    Turn turn;
+    int ai = 0;
+    bool ok = true;
+    for (int u = unit0; ok && u < shp.units; u += unit_step) {
+      for (int ks = 0; ks < a.stages; ++ks, turn.next(shp.wring)) {
+        if (!(ok = wait(&sh.wfull[turn.slot], turn.phase))) break;
+        ptx::mbar_arrive_cluster(ptx::cluster_addr(ptx::smem_u32(&sh.wpeer[turn.slot]), 0u));
+      }
+      for (int last = !adapters; ok && !last; ++ai) {
+        if (!(ok = wait(&sh.afull[ai & 1], (ai >> 1) & 1))) break;
+        last = sh.message[ai & 1] & 256;
+        ptx::mbar_arrive_cluster(ptx::cluster_addr(ptx::smem_u32(&sh.apeer[ai & 1]), 0u));
+      }
+    }
+  } else if (warp == 1 && part == 0 && ptx::elect_one()) {
+    const uint32_t m_rows = kPair ? 256u : 128u;
+    const uint32_t id = idesc((uint32_t)RT, a.x_unsigned, m_rows), ida = idesc((uint32_t)RT, false, m_rows);
     const uint32_t hhi = core_hi(128u);
-    Turn xturn, wturn;
+    Turn wturn;
     int ai = 0, ti = 0, ui = 0;
     bool ok = true;
+    auto commit = [&](uint64_t* bar) {
+      if (kPair) ptx::umma_commit_pair(ptx::smem_u32(bar));
+      else ptx::umma_commit(ptx::smem_u32(bar));
+    };
+    auto wait_peer = [&](uint64_t* bar, uint32_t parity) {      // what the other CTA released into the barrier, acquired at cluster scope
+      if (!wait(bar, parity)) return false;
+      if (kPair) ptx::mbar_acquire_cluster(ptx::smem_u32(bar), parity);
+      return true;
+    };
     auto product = [&](bool first, bool last) {         // one accumulator: all stages of K; the unit's first and last item
-      ok = wait(&sh.tempty[ti & 1], ((ti >> 1) & 1) ^ 1);
+      ok = wait_peer(&sh.tempty[ti & 1], ((ti >> 1) & 1) ^ 1);
       if (!ok) return;
       ptx::tc_fence_after();
       const uint32_t d = tmem + (ti & 1) * RT;
-      for (int ks = 0; ks < a.stages; ++ks, xturn.next(shp.xring), wturn.next(shp.wring)) {
-        const int xs = kFused ? xslot0(ui) + ks : xturn.slot, ws = wturn.slot;
-        if (first && !(ok = wait(&sh.xfull[xs], kFused ? xphase(ui) : xturn.phase))) return;
+      for (int ks = 0; ks < a.stages; ++ks, wturn.next(shp.wring)) {
+        const int ws = wturn.slot, xs = kPair ? ws : xslot0(ui) + ks;
+        if (!kPair && first && !(ok = wait(&sh.xfull[xs], xphase(ui)))) return;
         if (!(ok = wait(&sh.wfull[ws], wturn.phase))) return;
+        if (kPair && !(ok = wait_peer(&sh.wpeer[ws], wturn.phase))) return;
         ptx::tc_fence_after();
-        stage_mmas(d, core_lo(wbase + ws * kBytesW), ptx::umma_desc_lo(base + xs * xbytes, 16u), id, min(4, (a.k - ks * kProjStage + 31) >> 5), ks == 0);
-        ptx::umma_commit(ptx::smem_u32(&sh.wempty[ws]));
-        if (last) ptx::umma_commit(ptx::smem_u32(&sh.xempty[xs]));
+        stage_mmas<kPair>(d, core_lo(wbase + ws * kBytesW), ptx::umma_desc_lo(base + xs * xbytes, 16u), id, min(4, (a.k - ks * kProjStage + 31) >> 5), ks == 0);
+        commit(&sh.wempty[ws]);
+        if (!kPair && last) commit(&sh.xempty[xs]);
       }
     };
-    for (int u = blockIdx.x; ok && u < shp.units; u += gridDim.x, ++ui) {
-      const int t0 = u % shp.chunks * shp.chunk, t1 = min(t0 + shp.chunk, a.tiles_n);
+    for (int u = unit0; ok && u < shp.units; u += unit_step, ++ui) {
+      const int t0 = first_tile(u), t1 = last_tile(u);
       bool first = true;                                // no item of the unit has waited for its x yet
       if (kFused && adapters) {
         if (!(ok = wait(&sh.lready[ui & 1], (ui >> 1) & 1))) break;
@@ -471,7 +525,7 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         first = n_list == 0;
         for (int g = 0; ok && g < n_list; g += per, ++ti) {
           product(g == 0, false);
-          if (ok) ptx::umma_commit(ptx::smem_u32(&sh.tfull[ti & 1]));
+          if (ok) commit(&sh.tfull[ti & 1]);
         }
       }
       for (int tn = t0; ok && tn < t1; ++tn, ++ti) {
@@ -479,18 +533,19 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         const uint32_t d = tmem + (ti & 1) * RT;
         for (int last = !adapters; ok && !last; ++ai) {
           if (!(ok = wait(&sh.afull[ai & 1], (ai >> 1) & 1))) break;
+          if (kPair && !(ok = wait_peer(&sh.apeer[ai & 1], (ai >> 1) & 1))) break;
           ptx::tc_fence_after();
           const int msg = sh.message[ai & 1], slices = msg & 15;
           last = msg & 256;
           const uint32_t up = abase + (ai & 1) * shp.abytes, h = up + (uint32_t)(shp.step_adapters * kProjTileN * a.rp);
           for (int i = 0; i < slices; ++i) {
             const uint32_t alo = core_lo(up + (uint32_t)(i * kProjTileN * a.rp));
-            const uint32_t blo = ptx::umma_desc_lo(h + (uint32_t)(i * RT * a.rp), (uint32_t)RT * 16u);
-            for (int k = 0; k < a.rp / 32; ++k) ptx::umma_i8_hl(d, alo + k * 16, core_hi(8u * a.rp), blo + k * 2 * RT, hhi, ida, 1u);
+            const uint32_t blo = ptx::umma_desc_lo(h + (uint32_t)(i * half * a.rp), (uint32_t)half * 16u);
+            for (int k = 0; k < a.rp / 32; ++k) mma<kPair>(d, alo + k * 16, core_hi(8u * a.rp), blo + k * 2 * half, hhi, ida, 1u);
           }
-          ptx::umma_commit(ptx::smem_u32(&sh.aempty[ai & 1]));
+          commit(&sh.aempty[ai & 1]);
         }
-        if (ok) ptx::umma_commit(ptx::smem_u32(&sh.tfull[ti & 1]));
+        if (ok) commit(&sh.tfull[ti & 1]);
       }
     }
   } else if (warp >= 4 && warp < 8 && adapters) {
@@ -503,7 +558,6 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
       const int ub = ui & 1, row0 = u / shp.chunks * RT;
       if (!fill_all(wait(&sh.lfree[ub], ((ui >> 1) & 1) ^ 1))) return false;
       const bool scan = kFused && a.n_seg <= kScanRequests;
-      if (f == 0) sh.n_list[ub] = 0;
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int r = f + i * kFill, row = row0 + r;
@@ -535,21 +589,35 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         if (lane == 0 && r < RT) sh.live[ub][r >> 5] = live;
         bool first = s >= 0 && (r == 0 || sh.slot[ub][r - 1] != s);
         for (int e = 0; first && e < r; ++e) first = sh.slot[ub][e] != s;
-        if (first) sh.list[ub][atomicAdd(&sh.n_list[ub], 1)] = s;
+        const uint32_t firsts = __ballot_sync(0xFFFFFFFFu, first);
+        if (lane == 0 && r < RT) sh.firsts[r >> 5] = firsts;
+      }
+      fill_all(true);
+      // the list in the order of the rows: both CTAs of a pair walk it alike
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = f + i * kFill;
+        int at = 0;
+        for (int w = 0; w < (r >> 5) && w < RT / 32; ++w) at += __popc(sh.firsts[w]);
+        if (r < RT) {
+          const uint32_t word = sh.firsts[r >> 5];
+          if (word >> lane & 1) sh.list[ub][at + __popc(word & ((1u << lane) - 1))] = sh.slot[ub][r];
+          if (r == RT - 1) sh.n_list[ub] = at + __popc(word);
+        }
       }
       fill_all(true);
       ptx::mbar_arrive(ptx::smem_u32(&sh.lready[ub]));
       return true;
     };
     int ai = 0, ui = 0, hi = 0;
-    bool ok = (int)blockIdx.x >= shp.units || rows_of(blockIdx.x, 0);
-    for (int u = blockIdx.x; ok && u < shp.units; u += gridDim.x, ++ui) {
-      const int row0 = u / shp.chunks * RT, t0 = u % shp.chunks * shp.chunk, t1 = min(t0 + shp.chunk, a.tiles_n), ub = ui & 1;
+    bool ok = unit0 >= shp.units || rows_of(unit0, 0);
+    for (int u = unit0; ok && u < shp.units; u += unit_step, ++ui) {
+      const int row0 = u / shp.chunks * RT, t0 = first_tile(u), t1 = last_tile(u), ub = ui & 1;
       const int n_list = sh.n_list[ub];
       int slot[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) slot[i] = f + i * kFill < RT ? sh.slot[ub][f + i * kFill] : -2;
-      if (u + (int)gridDim.x < shp.units && !(ok = rows_of(u + gridDim.x, ui + 1))) break;   // a unit ahead
+      for (int i = 0; i < 2; ++i) slot[i] = f + i * kFill < half ? sh.slot[ub][part * half + f + i * kFill] : -2;
+      if (u + unit_step < shp.units && !(ok = rows_of(u + unit_step, ui + 1))) break;   // a unit ahead
       if (kFused && n_list && !(ok = fill_all(wait(&sh.hready, hi++ & 1)))) break;
       for (int tn = t0; ok && tn < t1; ++tn) {
         int at = 0;
@@ -565,7 +633,7 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
               const uint32_t bytes = (uint32_t)(kProjTileN * a.rp);
               ptx::mbar_expect_tx(bar, slices * bytes);
               for (int i = 0; i < slices; ++i)
-                ptx::bulk_g2s(up + i * bytes, a.up + ((size_t)sh.list[ub][at + i] * a.tiles_n + tn) * bytes, bytes, bar);
+                ptx::bulk_g2s(up + i * bytes, a.up + ((size_t)sh.list[ub][at + i] * a.tiles_n + stored_tile(tn)) * bytes, bytes, bar);
             } else {
               ptx::mbar_arrive(bar);
             }
@@ -578,12 +646,12 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
               for (int e = 0; e < 4; ++e) {
                 const bool mine = slot[e >> 1] == s;
                 t[e >> 1][e & 1] = make_int4(0, 0, 0, 0);
-                if (mine) t[e >> 1][e & 1] = __ldcg(reinterpret_cast<const int4*>(a.h + (size_t)(row0 + f + (e >> 1) * kFill) * a.rp) + c + (e & 1));
+                if (mine) t[e >> 1][e & 1] = __ldcg(reinterpret_cast<const int4*>(a.h + (size_t)(row0 + part * half + f + (e >> 1) * kFill) * a.rp) + c + (e & 1));
               }
 #pragma unroll
               for (int e = 0; e < 4; ++e)
-                if (f + (e >> 1) * kFill < RT)
-                  *reinterpret_cast<int4*>(h + ((i * (a.rp / 16) + c + (e & 1)) * RT + f + (e >> 1) * kFill) * 16) = t[e >> 1][e & 1];
+                if (f + (e >> 1) * kFill < half)
+                  *reinterpret_cast<int4*>(h + ((i * (a.rp / 16) + c + (e & 1)) * half + f + (e >> 1) * kFill) * 16) = t[e >> 1][e & 1];
             }
           }
           ptx::fence_async_smem();
@@ -608,11 +676,14 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
     auto done = [&](uint64_t* bar) {
       ptx::tc_fence_before();
       __syncwarp();
-      if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(bar));
+      if (lane == 0) {
+        if (kPair) ptx::mbar_arrive_cluster(ptx::cluster_addr(ptx::smem_u32(bar), 0u));
+        else ptx::mbar_arrive(ptx::smem_u32(bar));
+      }
     };
-    int4 rq_next = a.rq[(int)blockIdx.x % shp.chunks * shp.chunk * kProjTileN + q * 32 + lane];
-    for (int u = blockIdx.x; ok && u < shp.units; u += gridDim.x, ++ui) {
-      const int row0 = u / shp.chunks * RT, t0 = u % shp.chunks * shp.chunk, t1 = min(t0 + shp.chunk, a.tiles_n), ub = ui & 1;
+    int4 rq_next = a.rq[stored_tile(first_tile(unit0)) * kProjTileN + q * 32 + lane];
+    for (int u = unit0; ok && u < shp.units; u += unit_step, ++ui) {
+      const int row0 = u / shp.chunks * RT, t0 = first_tile(u), t1 = last_tile(u), ub = ui & 1;
       if (adapters && !(ok = __all_sync(0xFFFFFFFFu, wait(&sh.lready[ub], (ui >> 1) & 1)))) break;
       if (kFused && adapters) {
         // The product's lanes are rank channels: those of one adapter would be work for a quarter of the warps (tensor
@@ -642,9 +713,9 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         const int n0 = tn * kProjTileN + q * 32, n = n0 + lane;
         const int4 rq = rq_next;
         {                                               // the next tile's constants
-          const int un = u + gridDim.x;
-          const int next = tn + 1 < t1 ? tn + 1 : un < shp.units ? un % shp.chunks * shp.chunk : tn;
-          rq_next = a.rq[next * kProjTileN + q * 32 + lane];
+          const int un = u + unit_step;
+          const int next = tn + 1 < t1 ? tn + 1 : un < shp.units ? first_tile(un) : tn;
+          rq_next = a.rq[stored_tile(next) * kProjTileN + q * 32 + lane];
         }
         const long long add = (long long)(((unsigned long long)(uint32_t)rq.w << 32) | (uint32_t)rq.z);
         const int shift = max(rq.y - 1, 0);
@@ -716,7 +787,14 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
   __syncwarp();
   ptx::tc_fence_before();
   __syncthreads();
-  if (warp == 2) ptx::tmem_dealloc(tmem, (uint32_t)shp.tmem_cols);
+  if (kPair) {                                          // nothing of the pair reads or arrives in the other CTA any more
+    ptx::cluster_arrive();
+    ptx::cluster_wait();
+  }
+  if (warp == 2) {
+    if (kPair) ptx::tmem_dealloc_pair(tmem, (uint32_t)shp.tmem_cols);
+    else ptx::tmem_dealloc(tmem, (uint32_t)shp.tmem_cols);
+  }
 }
 
 // ---- the projection of few rows ------------------------------------------------------------------------------------
@@ -880,9 +958,9 @@ int split_tile(const ProjArgs& a) {
 
 // Shared memory of the persistent kernel with tiles of `tile` rows: false if it does not fit.
 bool main_rings(const ProjArgs& a, int tile, bool fused, MainShape* s) {
-  const int x = tile * kProjStage;
+  const int half = fused ? tile : tile / 2, x = half * kProjStage;
   for (s->step_adapters = a.rp == 32 ? 2 : 1; s->step_adapters >= 1; --s->step_adapters) {
-    s->abytes = (kProjTileN + tile) * a.rp * s->step_adapters;
+    s->abytes = (kProjTileN + half) * a.rp * s->step_adapters;
     const int room = kMaxSmem - (a.n_seg ? 2 * s->abytes : 0);
     if (fused) {
       for (int sets = 2; sets >= 1; --sets) {
@@ -910,13 +988,18 @@ bool fuse_down(const ProjArgs& a) {
 void main_tiles(const ProjArgs& a, int* tile, int* chunk) {
   const bool fused = fuse_down(a);
   long long least = LLONG_MAX;
+  if (!fused) {                                         // a pair's MMA has 256 rows at its best
+    *tile = kMaxTile;
+    *chunk = 1;
+    return;
+  }
   for (int t = kMaxTile; t >= kMaxTile / 2; t /= 2) {
     const long long row_tiles = (a.rows + t - 1) / t;
     MainShape s;
     if (!main_rings(a, t, fused, &s)) continue;
-    for (int c = 1; c <= (fused ? a.tiles_n : 1); ++c) {
+    for (int c = 1; c <= a.tiles_n; ++c) {
       const long long units = row_tiles * ((a.tiles_n + c - 1) / c);
-      const long long cost = (units + a.sms - 1) / a.sms * (c + (fused && a.n_seg ? 1 : 0)) * (t + 128);
+      const long long cost = (units + a.sms - 1) / a.sms * (c + (a.n_seg ? 1 : 0)) * (t + 128);
       if (cost < least) {
         least = cost;
         *tile = t;
@@ -924,6 +1007,12 @@ void main_tiles(const ProjArgs& a, int* tile, int* chunk) {
       }
     }
   }
+}
+
+int row_tile(const ProjArgs& a) {
+  int tile = split_tile(a), chunk;
+  if (!tile) main_tiles(a, &tile, &chunk);
+  return tile;
 }
 
 template <class Shape>
@@ -947,7 +1036,7 @@ cudaError_t launch_tiles(void (*kernel)(CUtensorMap, ProjArgs, Shape), const Pro
 
 template <class YT, bool kAnyShift>
 cudaError_t launch_main(const ProjArgs& a, const CUtensorMap& map, cudaStream_t stream) {
-  const int tile = proj_row_tile(a), tiles = a.tiles_n * ((a.rows + tile - 1) / tile), stage = tile * kProjStage + kBytesW;
+  const int tile = row_tile(a), tiles = a.tiles_n * ((a.rows + tile - 1) / tile), stage = tile * kProjStage + kBytesW;
   const uintptr_t y = reinterpret_cast<uintptr_t>(a.y);
   if (split_tile(a)) {
     SplitShape s;
@@ -970,11 +1059,12 @@ cudaError_t launch_main(const ProjArgs& a, const CUtensorMap& map, cudaStream_t 
   const int row_tiles = (a.rows + tile - 1) / tile;
   int unused;
   main_tiles(a, &unused, &s.chunk);
-  s.chunks = (a.tiles_n + s.chunk - 1) / s.chunk;
+  const int ctas = fused ? 1 : 2;                       // of a unit
+  s.chunks = (a.tiles_n + ctas * s.chunk - 1) / (ctas * s.chunk);
   s.units = row_tiles * s.chunks;
   return launch_tiles(fused ? proj_tile_kernel<YT, kAnyShift, true> : proj_tile_kernel<YT, kAnyShift, false>, a, map, s,
-                      std::min(s.units, a.sms), 1, kMainThreads,
-                      (size_t)(s.xring * tile * kProjStage + s.wring * kBytesW + (a.n_seg ? 2 * s.abytes : 0) + 1024), !fused, stream);
+                      std::min(s.units, a.sms / ctas) * ctas, ctas, kMainThreads,
+                      (size_t)(s.xring * tile / ctas * kProjStage + s.wring * kBytesW + (a.n_seg ? 2 * s.abytes : 0) + 1024), !fused, stream);
 }
 
 template <class YT, bool kAnyShift>
@@ -998,11 +1088,7 @@ cudaError_t configure_proj_kernels() {
   return e;
 }
 
-int proj_row_tile(const ProjArgs& a) {
-  int tile = split_tile(a), chunk;
-  if (!tile) main_tiles(a, &tile, &chunk);
-  return tile;
-}
+int proj_x_rows(const ProjArgs& a) { return split_tile(a) || fuse_down(a) ? row_tile(a) : row_tile(a) / 2; }
 
 cudaError_t launch_proj(const ProjArgs& a, const void* x_map, const void* x_map_down, cudaStream_t stream) {
   if (a.n_seg && (split_tile(a) || !fuse_down(a))) {

@@ -46,9 +46,9 @@ inline size_t core_offset(size_t row, size_t k, size_t width) {
 // Once per device, before the first launch.
 cudaError_t configure_proj_kernels();
 
-// x_map, x_map_down: CUtensorMaps of x [rows][k] with boxes of 128 bytes x proj_row_tile(a) or kProjDownRows rows and
+// x_map, x_map_down: CUtensorMaps of x [rows][k] with boxes of 128 bytes x proj_x_rows(a) or kProjDownRows rows and
 // the 128-byte swizzle.
-int proj_row_tile(const ProjArgs& a);
+int proj_x_rows(const ProjArgs& a);
 cudaError_t launch_proj(const ProjArgs& a, const void* x_map, const void* x_map_down, cudaStream_t stream);
 
 }  // namespace iodf

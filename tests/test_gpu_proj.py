@@ -144,6 +144,28 @@ def test_larger_sizes(G, rows, K, N, R):
     run(G, rng, rows, K, N, [R] * 3, [0] + cut + [rows], [0, 1, 2, -1, 1, 0])
 
 
+@pytest.mark.parametrize("rows,K,N,R", [(3000, 1300, 300, 0), (3000, 1300, 900, 33), (2500, 2050, 260, 128), (4099, 1025, 128, 40),
+                                        (2111, 700, 384, 100), (9000, 1100, 130, 16)])
+def test_many_rows_of_many_channels(G, rows, K, N, R):
+    """Sizes whose x tile does not stay in shared memory; odd numbers of output tiles, rows that end inside a tile."""
+    rng = np.random.default_rng(rows + K)
+    cut = sorted(rng.integers(5, rows - 7, 11).tolist())
+    cut[4] = cut[3]
+    which = [0, 1, 2, -1, 1, 0, 4, 3, 2, 2, 3, 4]
+    for x_dtype, y_dtype in ((torch.int8, torch.int8), (torch.uint8, torch.int32)):
+        if R:
+            run(G, rng, rows, K, N, [R, 1, R // 2 + 1, 0, R], [5] + cut + [rows - 7], which, x_dtype, y_dtype)
+        else:
+            run(G, rng, rows, K, N, [], None, None, x_dtype, y_dtype)
+
+
+def test_many_requests_of_many_channels(G):
+    rng = np.random.default_rng(61)
+    rows, n = 1100, 70
+    starts = list(range(0, rows + 1, 4))
+    run(G, rng, rows, 1200, 300, [64] * n, starts, [(i * 11) % n - 1 for i in range(len(starts) - 1)])
+
+
 def test_adapters_are_replaced_and_emptied(G):
     rng = np.random.default_rng(4)
     h, layer, ads = run(G, rng, 50, 80, 72, [8, 16], [0, 20, 50], [0, 1], max_rows=64)
