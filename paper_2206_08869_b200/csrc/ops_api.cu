@@ -22,6 +22,7 @@ typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, v
 struct iodf_proj {
   int device = 0;
   EncodeTiled encode = nullptr;
+  CUtensorMap w_map;
   uint32_t max_rows = 0, max_adapters = 0, max_rank = 0;
   int amax = 128;                            // largest |x|
   ProjArgs args{};
@@ -77,12 +78,12 @@ void pack_row(uint8_t* dst, size_t rows, size_t row, const int8_t* src, size_t K
     std::memcpy(dst + k / kProjStage * rows * kProjStage + core_offset(row, k % kProjStage, kProjStage), src + k, std::min<size_t>(16, K - k));
 }
 
-// x [rows][k] with a box of one stage x box_rows rows
-bool x_map(const iodf_proj& p, const ProjArgs& a, int box_rows, CUtensorMap* out) {
-  const cuuint64_t dims[2] = {(cuuint64_t)a.k, (cuuint64_t)a.rows}, strides[1] = {(cuuint64_t)a.ldx};
-  const cuuint32_t box[2] = {(cuuint32_t)kProjStage, (cuuint32_t)box_rows}, steps[2] = {1, 1};
-  return p.encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint8_t*>(a.x), dims, strides, box, steps,
-                  CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+// uint8 [rows][cols], row stride `ld`, boxes of one stage x box_rows rows
+bool tile_map(const iodf_proj& p, const void* base, uint64_t cols, uint64_t rows, uint64_t ld, uint32_t box_rows, bool swizzle, CUtensorMap* out) {
+  const cuuint64_t dims[2] = {cols, rows}, strides[1] = {ld};
+  const cuuint32_t box[2] = {(cuuint32_t)kProjStage, box_rows}, steps[2] = {1, 1};
+  return p.encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -186,6 +187,7 @@ int create_proj(const iodf_proj_desc& d, const int8_t* weights, size_t wn, const
   a.h = reinterpret_cast<int8_t*>(m + o_h);
   a.row_slot = reinterpret_cast<int*>(m + o_slot);
   a.status = reinterpret_cast<uint32_t*>(m + o_status);
+  if (!tile_map(p, a.w, S, tiles * stages * kProjTileN, S, kProjTileN, false, &p.w_map)) return IODF_ECUDA;
   return IODF_OK;
 }
 
@@ -360,8 +362,10 @@ int iodf_proj_forward(iodf_proj* p, const void* x, size_t ldx, int rows, const i
   OnDevice on(p->device);
   if (on.error() != cudaSuccess) return IODF_ECUDA;
   CUtensorMap map, map_down;
-  if (!x_map(*p, a, proj_x_rows(a), &map) || !x_map(*p, a, kProjDownRows, &map_down)) return IODF_ECUDA;
-  return status_of(launch_proj(a, &map, &map_down, (cudaStream_t)cuda_stream));
+  if (!tile_map(*p, x, (uint64_t)a.k, (uint64_t)rows, ldx, (uint32_t)proj_x_rows(a), true, &map) ||
+      !tile_map(*p, x, (uint64_t)a.k, (uint64_t)rows, ldx, kProjDownRows, true, &map_down))
+    return IODF_ECUDA;
+  return status_of(launch_proj(a, &map, &map_down, &p->w_map, (cudaStream_t)cuda_stream));
 }
 
 int iodf_proj_check(iodf_proj* p, void* cuda_stream, uint32_t* bad_requests) {

@@ -298,7 +298,7 @@ constexpr int kMaxTile = 256;
 constexpr int kMaxX = 16;
 
 struct MainShared {
-  uint64_t xfull[kMaxX], xempty[kMaxX], wfull[kMaxRing], wempty[kMaxRing], wpeer[kMaxRing], apeer[2], afull[2], aempty[2], tfull[2], tempty[2], lready[2], lfree[2], hready;
+  uint64_t xfull[kMaxX], xempty[kMaxX], wfull[kMaxRing], wempty[kMaxRing], apeer[2], afull[2], aempty[2], tfull[2], tempty[2], lready[2], lfree[2], hready;
   uint32_t abort_flag, tmem;
   int message[2];                        // an adapter step: its adapters, 256: the tile's last
   int n_list[2];
@@ -366,7 +366,7 @@ __device__ __forceinline__ bool fill_all(bool fine) {
 }
 
 template <class YT, bool kAnyShift, bool kFused>
-__global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid_constant__ CUtensorMap xmap, const ProjArgs a, const MainShape shp) {
+__global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid_constant__ CUtensorMap xmap, const __grid_constant__ CUtensorMap wmap, const ProjArgs a, const MainShape shp) {
   extern __shared__ uint8_t raw[];
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   __shared__ MainShared sh;
@@ -384,7 +384,6 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
     for (int i = 0; i < shp.wring; ++i) {
       ptx::mbar_init(ptx::smem_u32(&sh.wfull[i]), 1);
       ptx::mbar_init(ptx::smem_u32(&sh.wempty[i]), 1);
-      ptx::mbar_init(ptx::smem_u32(&sh.wpeer[i]), 1);
     }
     for (int i = 0; i < 2; ++i) {
       ptx::mbar_init(ptx::smem_u32(&sh.afull[i]), kFill + 1);
@@ -422,7 +421,7 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
   auto last_tile = [&](int u) { return kPair ? first_tile(u) + 1 : min(first_tile(u) + shp.chunk, a.tiles_n); };
   auto stored_tile = [&](int tn) { return kPair ? min(tn, a.tiles_n - 1) : tn; };      // whose weights stand in for one behind the last
   // x of a fused unit: xring is once or twice the stages, unit ui has slots from xslot0(ui) on. Paired: a stage's x and
-  // weights are slots of one ring with one barrier.
+  // weights are slots of one ring with one barrier, the first CTA's.
   const int sets = kPair ? 1 : shp.xring / a.stages;
   auto xslot0 = [&](int ui) { return sets == 2 ? (ui & 1) * a.stages : 0; };
   auto xphase = [&](int ui) { return (uint32_t)(sets == 2 ? ui >> 1 : ui) & 1u; };
@@ -463,27 +462,27 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         for (int ks = 0; ks < a.stages; ++ks, turn.next(shp.wring)) {
           if (!(ok = wait(&sh.wempty[turn.slot], turn.phase ^ 1))) break;
           const uint32_t bar = ptx::smem_u32(&sh.wfull[turn.slot]);
-          ptx::mbar_expect_tx(bar, kPair ? kBytesW + xbytes : (uint32_t)kBytesW);
-          if (kPair) ptx::tile_g2s(base + turn.slot * xbytes, &xmap, ks * kProjStage, u / shp.chunks * RT + part * half, bar);
-          ptx::bulk_g2s(wbase + turn.slot * kBytesW, a.w + ((size_t)stored_tile(tn) * a.stages + ks) * kBytesW, kBytesW, bar);
+          if (kPair) {                                  // both CTAs' copies count on the first one's barrier
+            if (part == 0) ptx::mbar_expect_tx(bar, 2u * (kBytesW + xbytes));
+            const uint32_t to = ptx::cluster_addr(bar, 0u);
+            ptx::tile_g2s_pair(base + turn.slot * xbytes, &xmap, ks * kProjStage, u / shp.chunks * RT + part * half, to);
+            ptx::tile_g2s_pair(wbase + turn.slot * kBytesW, &wmap, 0, (stored_tile(tn) * a.stages + ks) * kProjTileN, to);
+          } else {
+            ptx::mbar_expect_tx(bar, kBytesW);
+            ptx::bulk_g2s(wbase + turn.slot * kBytesW, a.w + ((size_t)tn * a.stages + ks) * kBytesW, kBytesW, bar);
+          }
         }
     }
   } else if (warp == 1 && part == 1 && ptx::elect_one()) {
-    // the second CTA of a pair tells the first, which issues the MMAs, what has arrived in its shared memory
-    Turn turn;
+    // the second CTA of a pair tells the first, which issues the MMAs, that its half of an adapter step is laid out
     int ai = 0;
     bool ok = true;
-    for (int u = unit0; ok && u < shp.units; u += unit_step) {
-      for (int ks = 0; ks < a.stages; ++ks, turn.next(shp.wring)) {
-        if (!(ok = wait(&sh.wfull[turn.slot], turn.phase))) break;
-        ptx::mbar_arrive_cluster(ptx::cluster_addr(ptx::smem_u32(&sh.wpeer[turn.slot]), 0u));
-      }
-      for (int last = !adapters; ok && !last; ++ai) {
+    for (int u = unit0; adapters && ok && u < shp.units; u += unit_step)
+      for (int last = 0; ok && !last; ++ai) {
         if (!(ok = wait(&sh.afull[ai & 1], (ai >> 1) & 1))) break;
         last = sh.message[ai & 1] & 256;
         ptx::mbar_arrive_cluster(ptx::cluster_addr(ptx::smem_u32(&sh.apeer[ai & 1]), 0u));
       }
-    }
   } else if (warp == 1 && part == 0 && ptx::elect_one()) {
     const uint32_t m_rows = kPair ? 256u : 128u;
     const uint32_t id = idesc((uint32_t)RT, a.x_unsigned, m_rows), ida = idesc((uint32_t)RT, false, m_rows);
@@ -509,7 +508,6 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         const int ws = wturn.slot, xs = kPair ? ws : xslot0(ui) + ks;
         if (!kPair && first && !(ok = wait(&sh.xfull[xs], xphase(ui)))) return;
         if (!(ok = wait(&sh.wfull[ws], wturn.phase))) return;
-        if (kPair && !(ok = wait_peer(&sh.wpeer[ws], wturn.phase))) return;
         ptx::tc_fence_after();
         stage_mmas<kPair>(d, core_lo(wbase + ws * kBytesW), ptx::umma_desc_lo(base + xs * xbytes, 16u), id, min(4, (a.k - ks * kProjStage + 31) >> 5), ks == 0);
         commit(&sh.wempty[ws]);
@@ -1015,9 +1013,9 @@ int row_tile(const ProjArgs& a) {
   return tile;
 }
 
-template <class Shape>
-cudaError_t launch_tiles(void (*kernel)(CUtensorMap, ProjArgs, Shape), const ProjArgs& a, const CUtensorMap& map, const Shape& s, int grid,
-                         int cluster, int threads, size_t smem, bool follows_down, cudaStream_t stream) {
+template <class... Params, class... Given>
+cudaError_t launch_tiles(void (*kernel)(Params...), int grid, int cluster, int threads, size_t smem, bool follows_down, cudaStream_t stream,
+                         const Given&... given) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)grid);
   cfg.blockDim = dim3((unsigned)threads);
@@ -1030,12 +1028,12 @@ cudaError_t launch_tiles(void (*kernel)(CUtensorMap, ProjArgs, Shape), const Pro
   attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr[1].val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = attr;
-  cfg.numAttrs = a.n_seg && follows_down ? 2 : 1;
-  return cudaLaunchKernelEx(&cfg, kernel, map, a, s);
+  cfg.numAttrs = follows_down ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kernel, given...);
 }
 
 template <class YT, bool kAnyShift>
-cudaError_t launch_main(const ProjArgs& a, const CUtensorMap& map, cudaStream_t stream) {
+cudaError_t launch_main(const ProjArgs& a, const CUtensorMap& map, const CUtensorMap& w_map, cudaStream_t stream) {
   const int tile = row_tile(a), tiles = a.tiles_n * ((a.rows + tile - 1) / tile), stage = tile * kProjStage + kBytesW;
   const uintptr_t y = reinterpret_cast<uintptr_t>(a.y);
   if (split_tile(a)) {
@@ -1046,7 +1044,8 @@ cudaError_t launch_main(const ProjArgs& a, const CUtensorMap& map, cudaStream_t 
     const int sums = tile * kProjTileN * 4, most = (a.stages + s.parts - 1) / s.parts;
     s.ring = std::min(std::min(kSplitRing, most), (kMaxSmem - sums) / stage);
     s.vector_y = a.ldy % 4 == 0 && y % (4 * a.y_bytes) == 0;
-    return launch_tiles(proj_split_kernel<YT, kAnyShift>, a, map, s, tiles * s.parts, s.parts, kSplitThreads, (size_t)(s.ring * stage + sums + 1024), true, stream);
+    return launch_tiles(proj_split_kernel<YT, kAnyShift>, tiles * s.parts, s.parts, kSplitThreads, (size_t)(s.ring * stage + sums + 1024),
+                        a.n_seg != 0, stream, map, a, s);
   }
   MainShape s;
   s.tile = tile;
@@ -1062,9 +1061,10 @@ cudaError_t launch_main(const ProjArgs& a, const CUtensorMap& map, cudaStream_t 
   const int ctas = fused ? 1 : 2;                       // of a unit
   s.chunks = (a.tiles_n + ctas * s.chunk - 1) / (ctas * s.chunk);
   s.units = row_tiles * s.chunks;
-  return launch_tiles(fused ? proj_tile_kernel<YT, kAnyShift, true> : proj_tile_kernel<YT, kAnyShift, false>, a, map, s,
+  return launch_tiles(fused ? proj_tile_kernel<YT, kAnyShift, true> : proj_tile_kernel<YT, kAnyShift, false>,
                       std::min(s.units, a.sms / ctas) * ctas, ctas, kMainThreads,
-                      (size_t)(s.xring * tile / ctas * kProjStage + s.wring * kBytesW + (a.n_seg ? 2 * s.abytes : 0) + 1024), !fused, stream);
+                      (size_t)(s.xring * tile / ctas * kProjStage + s.wring * kBytesW + (a.n_seg ? 2 * s.abytes : 0) + 1024),
+                      a.n_seg != 0 && !fused, stream, map, w_map, a, s);
 }
 
 template <class YT, bool kAnyShift>
@@ -1090,7 +1090,7 @@ cudaError_t configure_proj_kernels() {
 
 int proj_x_rows(const ProjArgs& a) { return split_tile(a) || fuse_down(a) ? row_tile(a) : row_tile(a) / 2; }
 
-cudaError_t launch_proj(const ProjArgs& a, const void* x_map, const void* x_map_down, cudaStream_t stream) {
+cudaError_t launch_proj(const ProjArgs& a, const void* x_map, const void* x_map_down, const void* w_map, cudaStream_t stream) {
   if (a.n_seg && (split_tile(a) || !fuse_down(a))) {
     if ((long long)a.rows * a.rp <= kDownRowsMost) {
       const dim3 grid((unsigned)a.rows, (unsigned)(a.rp / 8));
@@ -1103,10 +1103,10 @@ cudaError_t launch_proj(const ProjArgs& a, const void* x_map, const void* x_map_
     const cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
   }
-  const CUtensorMap& map = *static_cast<const CUtensorMap*>(x_map);
-  if (a.y_type == IODF_I8) return a.any_shift ? launch_main<int8_t, true>(a, map, stream) : launch_main<int8_t, false>(a, map, stream);
-  if (a.y_type == IODF_U8) return a.any_shift ? launch_main<uint8_t, true>(a, map, stream) : launch_main<uint8_t, false>(a, map, stream);
-  return a.any_shift ? launch_main<int, true>(a, map, stream) : launch_main<int, false>(a, map, stream);
+  const CUtensorMap &map = *static_cast<const CUtensorMap*>(x_map), &wm = *static_cast<const CUtensorMap*>(w_map);
+  if (a.y_type == IODF_I8) return a.any_shift ? launch_main<int8_t, true>(a, map, wm, stream) : launch_main<int8_t, false>(a, map, wm, stream);
+  if (a.y_type == IODF_U8) return a.any_shift ? launch_main<uint8_t, true>(a, map, wm, stream) : launch_main<uint8_t, false>(a, map, wm, stream);
+  return a.any_shift ? launch_main<int, true>(a, map, wm, stream) : launch_main<int, false>(a, map, wm, stream);
 }
 
 }  // namespace iodf

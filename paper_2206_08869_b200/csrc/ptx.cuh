@@ -343,6 +343,13 @@ __device__ __forceinline__ void umma_i8_hl_pair(uint32_t d_tmem, uint32_t a_lo, 
       "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+// The tile copy of tile_g2s whose bytes are counted on a barrier of either CTA of the pair (address from cluster_addr).
+__device__ __forceinline__ void tile_g2s_pair(uint32_t dst, const void* map, int32_t col, int32_t row, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(col), "r"(row), "r"(bar)
+      : "memory");
+}
 // Arrive on the barrier at this address in both CTAs once every tcgen05.mma issued so far by this thread has completed.
 __device__ __forceinline__ void umma_commit_pair(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
