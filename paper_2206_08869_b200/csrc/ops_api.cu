@@ -83,7 +83,7 @@ bool tile_map(const iodf_proj& p, const void* base, uint64_t cols, uint64_t rows
   const cuuint64_t dims[2] = {cols, rows}, strides[1] = {ld};
   const cuuint32_t box[2] = {(cuuint32_t)kProjStage, box_rows}, steps[2] = {1, 1};
   return p.encode(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, steps, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                  swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                  swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 

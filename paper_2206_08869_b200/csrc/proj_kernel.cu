@@ -31,7 +31,8 @@ constexpr int kDownRing = 6;             // stages at most
 constexpr int kDownEpiWarps = 8;
 constexpr int kDownThreads = 128 + 32 * kDownEpiWarps;   // warp 0 copies, 1 MMAs, 2 tensor memory, 4-11 epilogue
 constexpr int kDownStageBytes = kDownRows * kProjStage + kBytesW;
-constexpr int kScanRequests = 2048;      // up to here a tile reads every request, above it halves for each row
+constexpr int kScanRequests = 2048;      // up to here a tile (or row) reads every request, above it halves for each row
+constexpr int kSlotBits = 20;            // row_slot: an adapter's slot and above it its rank, -1 none, -2 in no request
 
 // D = s32; A int8 (weights), B int8 or uint8, both K-major, M = m, N = n
 __device__ __forceinline__ uint32_t idesc(uint32_t n, bool b_unsigned, uint32_t m = 128u) {
@@ -108,6 +109,8 @@ __device__ __forceinline__ int slot_of_row(const ProjArgs& a, int row) {
   return s >= 0 && s < a.max_adapters ? s : -1;
 }
 
+__device__ __forceinline__ int slot_only(int slot_rank) { return slot_rank < 0 ? slot_rank : slot_rank & ((1 << kSlotBits) - 1); }
+
 __device__ __forceinline__ void look_over_request(const ProjArgs& a, int q) {
   const int s0 = a.seg_start[q], s1 = a.seg_start[q + 1], ad = a.seg_adapter[q];
   if (s0 < 0 || s1 < s0 || s1 > a.rows || ad < -1 || ad >= a.max_adapters) atomicAdd(a.status + 1, 1u);
@@ -140,13 +143,26 @@ __device__ __forceinline__ void store_rank(int8_t* h, int rp, const uint32_t (&v
 // ---- h for few rows: a block per row and eight rank channels, a quarter of K per warp ----------------------
 template <bool kUnsigned>
 __global__ void __launch_bounds__(128) down_rows_kernel(const ProjArgs a) {
-  __shared__ int part[4][8];
+  __shared__ int part[4][8], found;
   ptx::grid_launch_dependents();
   const int row = blockIdx.x, g = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int slot;
+  if (a.n_seg <= kScanRequests) {                       // all requests at once: one trip to memory instead of one per halving
+    if (threadIdx.x == 0) found = -2;
+    __syncthreads();
+    for (int q = threadIdx.x; q < a.n_seg; q += blockDim.x) {
+      const int s0 = a.seg_start[q], s1 = a.seg_start[q + 1], ad = a.seg_adapter[q];
+      if (s0 <= row && row < s1) found = ad >= 0 && ad < a.max_adapters ? ad : -1;
+    }
+    __syncthreads();
+    slot = found;
+  } else {
+    slot = slot_of_row(a, row);
+  }
   if (row == 0 && g == 0) look_over_requests(a);
-  const int slot = slot_of_row(a, row);
-  if (g == 0 && threadIdx.x == 0) a.row_slot[row] = slot;
-  if (slot < 0 || g * 8 >= a.rank[slot]) return;
+  const int rank = slot < 0 ? 0 : a.rank[slot];
+  if (g == 0 && threadIdx.x == 0) a.row_slot[row] = slot < 0 ? slot : slot | rank << kSlotBits;
+  if (g * 8 >= rank) return;
   // 32 lanes: four chunks of 16 channels x eight rank channels, 512 contiguous bytes of `down`
   const int chunk = lane >> 3, j = lane & 7;
   const uint8_t* d = a.down + ((size_t)slot * a.stages * a.rp + g * 8) * kProjStage + j * 16;
@@ -559,7 +575,7 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int r = f + i * kFill, row = row0 + r;
-        if (r < RT) sh.slot[ub][r] = scan || row >= a.rows ? -2 : kFused ? slot_of_row(a, row) : a.row_slot[row];
+        if (r < RT) sh.slot[ub][r] = scan || row >= a.rows ? -2 : kFused ? slot_of_row(a, row) : slot_only(a.row_slot[row]);
       }
       fill_all(true);
       if (scan) {                                       // a warp reads 32 requests and writes the rows of those in the tile
@@ -906,16 +922,16 @@ __global__ void __launch_bounds__(kSplitThreads, 1) proj_split_kernel(const __gr
   for (int r = warp; r < own; r += kSplitThreads / 32) {
     const int row = row0 + part * own + r;
     if (row >= a.rows) break;
-    const int slot = a.n_seg ? a.row_slot[row] : -1;
-    if (slot == -2) continue;
+    const int slot_rank = a.n_seg ? a.row_slot[row] : -1;
+    if (slot_rank == -2) continue;
     int4 v = make_int4(0, 0, 0, 0);
     for (int p = 0; p < shp.parts; ++p) {
       const int4 u = *reinterpret_cast<const int4*>(sums + (p * own + r) * kProjTileN + lane * 4);
       v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
     }
     int acc[4] = {v.x, v.y, v.z, v.w};
-    if (slot >= 0) {
-      const int chunks = (a.rank[slot] + 15) >> 4;
+    if (slot_rank >= 0) {
+      const int slot = slot_rank & ((1 << kSlotBits) - 1), chunks = ((slot_rank >> kSlotBits) + 15) >> 4;
       const int4* h = reinterpret_cast<const int4*>(a.h + (size_t)row * a.rp);
       const uint8_t* up = a.up + ((size_t)slot * a.tiles_n + tn) * kProjTileN * a.rp + (lane >> 1) * a.rp * 8 + (lane & 1) * 64;
       for (int c = 0; c < chunks; ++c) {
@@ -980,9 +996,10 @@ bool fuse_down(const ProjArgs& a) {
   return main_rings(a, kMaxTile / 2, true, &s);
 }
 
-// Rows of a tile and output tiles of a unit of the persistent kernel: what costs the least in rounds of the SMs. A round is a
-// unit's items (its output tiles, and one more for h with adapters), and an item costs its rows and as much as 128
-// rows more (measured on 32768 x 256 -> 256 and 65536 x 512 -> 512: 4 to 6 us with 256 rows, latencies for half of it).
+// Rows of a tile and output tiles of a unit of the persistent kernel: what costs the least. The cost is the units per SM
+// (one at least) times a unit's items (its output tiles, and one more for h with adapters) times an item's cost, its rows
+// and as much as 128 rows more. Measured, us for (rows, chunk) = (128, 1) (128, 2) (128, 4) (256, 1) (256, 2) (256, 4):
+// 65536 x 512 -> 512: 76 53 46 49 40 35; 32768 x 256 -> 256: 25 18 18 18 14 14; 20011 x 173 -> 109 (one output tile): 18.6 and 21.6.
 void main_tiles(const ProjArgs& a, int* tile, int* chunk) {
   const bool fused = fuse_down(a);
   long long least = LLONG_MAX;
@@ -997,7 +1014,7 @@ void main_tiles(const ProjArgs& a, int* tile, int* chunk) {
     if (!main_rings(a, t, fused, &s)) continue;
     for (int c = 1; c <= a.tiles_n; ++c) {
       const long long units = row_tiles * ((a.tiles_n + c - 1) / c);
-      const long long cost = (units + a.sms - 1) / a.sms * (c + (a.n_seg ? 1 : 0)) * (t + 128);
+      const long long cost = std::max<long long>(units, a.sms) * (c + (a.n_seg ? 1 : 0)) * (t + 128);
       if (cost < least) {
         least = cost;
         *tile = t;

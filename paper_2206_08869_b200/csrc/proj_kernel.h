@@ -33,7 +33,7 @@ struct ProjArgs {
   const uint8_t* up;                   // [max_adapters][tiles_n][128 x rp as above]
   const int* rank;                     // [max_adapters]
   int8_t* h;                           // workspace [max_rows][rp]
-  int* row_slot;                       // workspace [max_rows]: adapter slot, -1 none, -2 in no request
+  int* row_slot;                       // workspace [max_rows]: adapter slot (and rank, see kSlotBits), -1 none, -2 in no request
   uint32_t* status;                    // [0] a bounded wait gave up, [1] bad requests
   int sms;
 };
