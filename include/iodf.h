@@ -474,7 +474,7 @@ int iodf_launches_per_call(const iodf_model* m, int inverse);
  * may be captured; the handle's workspace serves one call at a time (also for replayed graphs). Requests whose
  * bounds decrease or leave 0..rows, and slots outside -1..max_adapters-1, are counted on the device and
  * reported by iodf_proj_check (IODF_EDATA). Such a slot counts as -1; with bad bounds any row may be left
- * unwritten or computed without its adapter, and nothing outside the buffers is touched.
+ * unwritten or take the adapter of another request or none, and nothing outside the buffers is touched.
  */
 typedef struct {
   uint32_t abi_version;                /* IODF_ABI_VERSION                                           */
@@ -519,8 +519,8 @@ int iodf_proj_check(iodf_proj* p, void* cuda_stream, uint32_t* bad_requests);
  * iodf_norm_forward: element (row, c) of a residual stream lies at image_stride * (row / pixels) +
  * channel_stride * c + pixel_stride * (row % pixels) elements; either channel_stride is 1 (rows: pixels = rows),
  * or pixel_stride is 1 (planes, the layout of z and prior; channels <= 256 then). b, gate and n are DEV rows with
- * strides ldb, ldg, ldn in elements; ldg = 0: one gate per channel; gate NULL: none. r_out may be r with the same
- * view (in place), else the two must not overlap; it is NULL exactly if there is no block, n exactly if there is
+ * strides ldb, ldg, ldn in elements; ldg = 0: one gate per channel; gate NULL: none. out_view gives every element a
+ * place of its own (EINVAL otherwise); r_out may be r with the same view (in place), else the two must not overlap; it is NULL exactly if there is no block, n exactly if there is
  * no pre_norm. Pointers are aligned to their elements. Any rows >= 0. Enqueues one kernel, allocates nothing, keeps
  * no workspace: calls on one handle may overlap.
  */

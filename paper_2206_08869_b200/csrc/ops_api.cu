@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cstdlib>
 #include <cstring>
+#include <exception>
 #include <new>
 #include <vector>
 
@@ -72,6 +73,13 @@ bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) &
 
 size_t up_to(size_t n, size_t m) { return (n + m - 1) / m * m; }
 
+// Sum of |w| of one row (at most 32768 * 128).
+int magnitude(const int8_t* w, size_t n) {
+  int sum = 0;
+  for (size_t i = 0; i < n; ++i) sum += std::abs((int)w[i]);
+  return sum;
+}
+
 // A row of K channels of an operand of `rows` rows, cut into stages.
 void pack_row(uint8_t* dst, size_t rows, size_t row, const int8_t* src, size_t K) {
   for (size_t k = 0; k < K; k += 16)
@@ -117,9 +125,7 @@ int create_proj(const iodf_proj_desc& d, const int8_t* weights, size_t wn, const
   p.amax = d.x_type == IODF_U8 ? 255 : 128;
   p.room.resize(N);
   for (size_t n = 0; n < N; ++n) {
-    int64_t sum = 0;
-    for (size_t k = 0; k < K; ++k) sum += std::abs((int)w[n * K + k]);
-    p.room[n] = 0x7FFFFFFFll - (sum * p.amax + std::llabs((long long)bias[n]));
+    p.room[n] = 0x7FFFFFFFll - ((int64_t)magnitude(w + n * K, K) * p.amax + std::llabs((long long)bias[n]));
     if (p.room[n] < 0) return IODF_EOVERFLOW;
   }
 
@@ -197,14 +203,10 @@ int set_adapter(iodf_proj& p, uint32_t slot, uint32_t rank, const int8_t* down, 
   const size_t dbytes = R * p.args.stages * S, ubytes = (size_t)p.args.tiles_n * kProjTileN * R;
   for (uint32_t j = 0; j < rank; ++j) {
     if (rq[j] < (1 << 30) || rq[rank + j] < 0 || rq[rank + j] > 31) return IODF_EINVAL;
-    int64_t sum = 0;
-    for (size_t k = 0; k < K; ++k) sum += std::abs((int)down[j * K + k]);
-    if (sum * p.amax > 0x7FFFFFFFll) return IODF_EOVERFLOW;
+    if ((int64_t)magnitude(down + j * K, K) * p.amax > 0x7FFFFFFFll) return IODF_EOVERFLOW;
   }
   for (size_t n = 0; n < N; ++n) {
-    int64_t sum = 0;
-    for (uint32_t j = 0; j < rank; ++j) sum += std::abs((int)up[n * rank + j]);
-    if (sum * 128 > p.room[n]) return IODF_EOVERFLOW;
+    if ((int64_t)magnitude(up + n * rank, rank) * 128 > p.room[n]) return IODF_EOVERFLOW;
   }
   std::vector<uint8_t> dp(dbytes, 0), upp(ubytes, 0);
   std::vector<int2> q(R, make_int2(1 << 30, 0));
@@ -293,6 +295,21 @@ bool good_view(const iodf_view& v, uint32_t channels) {
   return v.channel_stride == 1 || (v.pixel_stride == 1 && channels <= kMaxPlanes);
 }
 
+// True if no two of rows x channels elements share a place, as far as the strides show it: in ascending order each is at
+// least the extent of what it steps over.
+bool apart(const iodf_view& v, uint64_t rows, uint64_t channels) {
+  struct Dim { uint64_t n, stride; } d[3] = {{channels, v.channel_stride}, {std::min<uint64_t>(v.pixels, rows), v.pixel_stride},
+                                             {(rows + v.pixels - 1) / v.pixels, v.image_stride}};
+  std::sort(d, d + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
+  uint64_t extent = 1;
+  for (const Dim& e : d) {
+    if (e.n == 1) continue;
+    if (e.stride < extent) return false;
+    extent += e.stride * (e.n - 1);
+  }
+  return true;
+}
+
 ViewArgs view_args(const iodf_view& v) {
   return {(long long)v.pixels, (long long)v.image_stride, (long long)v.channel_stride, (long long)v.pixel_stride};
 }
@@ -311,7 +328,7 @@ int iodf_proj_create(const iodf_proj_desc* desc, const int8_t* weights, size_t w
   int rc;
   try {
     rc = create_proj(*desc, weights, weights_count, requant, requant_count, device, *p);
-  } catch (const std::bad_alloc&) {
+  } catch (const std::exception&) {              // out of host memory, or a size beyond what a vector may have
     rc = IODF_ENOMEM;
   }
   if (rc != IODF_OK) {
@@ -337,7 +354,7 @@ int iodf_proj_set_adapter(iodf_proj* p, uint32_t slot, uint32_t rank, const int8
   if (rank && (!down || !down_requant || !up)) return IODF_EINVAL;
   try {
     return set_adapter(*p, slot, rank, down, down_requant, up, (cudaStream_t)cuda_stream);
-  } catch (const std::bad_alloc&) {
+  } catch (const std::exception&) {
     return IODF_ENOMEM;
   }
 }
@@ -392,7 +409,7 @@ int iodf_norm_create(const iodf_norm_desc* desc, int device, iodf_norm** out) {
   int rc;
   try {
     rc = create_norm(*desc, device, *nm);
-  } catch (const std::bad_alloc&) {
+  } catch (const std::exception&) {              // out of host memory, or a size beyond what a vector may have
     rc = IODF_ENOMEM;
   }
   if (rc != IODF_OK) {
@@ -426,6 +443,7 @@ int iodf_norm_forward(iodf_norm* nm, int rows, const void* r, const iodf_view* r
   if (!a.has_block && gate) return IODF_EINVAL;
   if (a.has_block) {
     if (!out_view || !good_view(*out_view, C) || !aligned(r_out, a.res_i16 ? 2 : 4)) return IODF_EINVAL;
+    if (!apart(*out_view, (uint64_t)rows, C)) return IODF_EINVAL;
     if (r_out == r && std::memcmp(r_view, out_view, sizeof(iodf_view))) return IODF_EINVAL;
     if (ldb < C || ldb >= big || !aligned(b, a.block_i8 ? 1 : 4)) return IODF_EINVAL;
     if (gate && ldg && (ldg < C || ldg >= big)) return IODF_EINVAL;

@@ -257,3 +257,57 @@ def test_refusals(G):
     assert e.value.status == -1
     o, n = G.iodf_norm_forward(h, r[:0], b[:0])
     assert o.shape == (0, 12) and n.shape == (0, 12)
+
+
+@pytest.mark.parametrize("C", [3, 40, 300, 2500])
+def test_rows_of_images_with_gaps(G, C):
+    """Channels side by side, images that do not follow each other: a view that only the C interface can name."""
+    import ctypes
+    from paper_2206_08869_b200 import binding as B
+    rng = np.random.default_rng(C)
+    images, px, pad = 3, 7, 5
+    rows = images * px
+    d = make_desc(rng, C, torch.int32, torch.int8, "rms", "centred")
+    r, b = values(rng, rows, C, torch.int32, 500), values(rng, rows, C, torch.int8, 25)
+    h = G.iodf_norm_create(d)
+    step = C + 3
+    buf = torch.full((images, px * step + pad), 17, dtype=torch.int32, device="cuda")
+    view = buf[:, :px * step].unflatten(1, (px, step))[:, :, :C]
+    view.copy_(torch.from_numpy(r).view(images, px, C))
+    out, n = torch.full_like(buf, 17), torch.empty((rows, C), dtype=torch.int8, device="cuda")
+    bt = torch.from_numpy(b).cuda()
+    v = B.View(px, px * step + pad, 1, step)
+    stream = torch.cuda.current_stream().cuda_stream
+    f = lambda ov: G.load_library().iodf_norm_forward(h.handle, rows, buf.data_ptr(), v, bt.data_ptr(), C, None, 0, out.data_ptr(), ov,
+                                                      n.data_ptr(), C, stream)
+    assert f(v) == 0
+    wo, wn = P.norm_step(d, r, b)
+    got = out[:, :px * step].unflatten(1, (px, step))
+    np.testing.assert_array_equal(got[:, :, :C].reshape(rows, C).cpu().numpy().astype(np.int64), wo)
+    np.testing.assert_array_equal(n.cpu().numpy().astype(np.int64), wn)
+    assert (got[:, :, C:] == 17).all() and (out[:, px * step:] == 17).all()
+    # places that rows or images share are refused
+    assert f(B.View(px, px * step + pad, 1, C - 1)) == -1
+    assert f(B.View(px, step, 1, step)) == -1
+    assert f(B.View(px, 0, 1, step)) == -1
+
+
+def test_a_plane_layout_with_channels_outermost(G):
+    rng = np.random.default_rng(2)
+    images, C, px = 4, 10, 33
+    d = make_desc(rng, C, torch.int32, torch.int8, "rms", None)
+    r, b = values(rng, images * px, C, torch.int32, 500), values(rng, images * px, C, torch.int8, 25)
+    t = torch.from_numpy(r).cuda().view(images, px, C).permute(2, 0, 1).contiguous().permute(1, 0, 2)     # [images, C, px], C outermost
+    out = torch.empty_like(t.permute(1, 0, 2).contiguous()).permute(1, 0, 2)
+    o, _ = G.iodf_norm_forward(G.iodf_norm_create(d), t, torch.from_numpy(b).cuda(), r_out=out)
+    np.testing.assert_array_equal(o.permute(0, 2, 1).reshape(-1, C).cpu().numpy().astype(np.int64), P.norm_step(d, r, b)[0])
+    with pytest.raises(G.IodfError):
+        G.iodf_norm_forward(G.iodf_norm_create(d), t, torch.from_numpy(b).cuda(), r_out=out[:1].expand(images, C, px))
+
+
+@pytest.mark.parametrize("rows,C", [(9000, 256), (700, 4096), (5000, 128), (3000, 512), (2000, 1024), (1200, 2048), (400, 8192), (6000, 64),
+                                    (9000, 160), (1500, 136), (5000, 97), (4000, 225)])
+def test_many_rows_of_every_form(G, rows, C):
+    rng = np.random.default_rng(rows)
+    check(G, rng, rows, C, torch.int16, torch.int32, "rms", "rms", "row")
+    check(G, rng, rows // 3, C, torch.int32, torch.int8, "centred", "rms", "channel", n_dtype=torch.uint8)

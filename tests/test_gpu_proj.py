@@ -307,3 +307,97 @@ def test_two_handles_at_once(G):
     torch.cuda.synchronize()
     for h, layer, ad, xh, x, st, wh, y, _ in lanes:
         np.testing.assert_array_equal(y.cpu().numpy(), P.projection(layer, xh, [ad], [0, len(xh)], [0]))
+
+
+@pytest.mark.parametrize("rows,K,N", [(5000, 160, 200), (20000, 40, 50), (3000, 1300, 400)])
+def test_many_rows_captured_and_replayed(G, rows, K, N):
+    rng = np.random.default_rng(rows)
+    layer = make_layer(rng, K, N, torch.int8)
+    ads = [make_adapter(rng, K, N, 30) for _ in range(3)]
+    h = G.iodf_proj_create(layer, rows, 3, 30, y_dtype=torch.int8)
+    for i, ad in enumerate(ads):
+        G.iodf_proj_set_adapter(h, i, ad)
+    xh, x = make_x(rng, rows, K, torch.int8)
+    st = torch.tensor([0, rows // 2, rows], dtype=torch.int32, device="cuda")
+    wh = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    y = torch.zeros((rows, N), dtype=torch.int8, device="cuda")
+    G.iodf_proj_forward(h, x, st, wh, y=y)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        G.iodf_proj_forward(h, x, st, wh, y=y)
+        G.iodf_proj_forward(h, x, st, wh, y=y)
+    for cut, w in ((rows, [2, 0]), (0, [0, 2]), (rows // 3, [-1, 1])):
+        xh2, x2 = make_x(rng, rows, K, torch.int8)
+        x.copy_(x2)
+        st.copy_(torch.tensor([0, cut, rows], dtype=torch.int32))
+        wh.copy_(torch.tensor(w, dtype=torch.int32))
+        g.replay()
+        g.replay()
+        np.testing.assert_array_equal(y.cpu().numpy(), P.projection(layer, xh2, ads, [0, cut, rows], w))
+    G.iodf_proj_check(h)
+
+
+@pytest.mark.parametrize("rows,K,N,R", [(3001, 70, 60, 20), (5003, 33, 140, 16), (2600, 1400, 140, 64)])
+def test_more_requests_than_are_read_at_once(G, rows, K, N, R):
+    rng = np.random.default_rng(rows)
+    which = (np.arange(rows) * 13 % 9 - 1).tolist()
+    run(G, rng, rows, K, N, [R] * 8, list(range(rows + 1)), which)
+    empty = sorted(rng.integers(0, rows + 1, 2500).tolist())
+    run(G, rng, rows, K, N, [R] * 8, [0] + empty + [rows], [i % 9 - 1 for i in range(2501)])
+
+
+def test_requests_as_short_as_the_deepest_levels_images(G):
+    """Sixteen rows each: sixteen adapters among the rows of a tile, in every one of its output tiles."""
+    rng = np.random.default_rng(44)
+    n = 500
+    run(G, rng, 16 * n, 64, 300, [8] * 40, list(range(0, 16 * n + 1, 16)), (rng.integers(0, 40, n)).tolist(), torch.uint8, torch.uint8)
+
+
+@pytest.mark.parametrize("rows,K,N", [(700, 96, 72), (9000, 96, 72), (2500, 1100, 260)])
+def test_calls_of_one_handle_in_a_row_with_other_rows(G, rows, K, N):
+    """The workspace of one call is the next one's: nothing of it may be taken for the next one's."""
+    rng = np.random.default_rng(rows)
+    layer = make_layer(rng, K, N, torch.int8)
+    ads = [make_adapter(rng, K, N, 17) for _ in range(4)]
+    h = G.iodf_proj_create(layer, rows, 4, 17, y_dtype=torch.int8)
+    for i, ad in enumerate(ads):
+        G.iodf_proj_set_adapter(h, i, ad)
+    todo = []
+    for i in range(6):
+        m = max(1, rows // (i + 1) - i)
+        xh, x = make_x(rng, m, K, torch.int8)
+        st = [0, m // 3, m // 3, m - i // 2]
+        w = [(i + j) % 5 - 1 for j in range(3)]
+        todo.append((xh, x, st, w, torch.tensor(st, dtype=torch.int32, device="cuda"), torch.tensor(w, dtype=torch.int32, device="cuda")))
+    torch.cuda.synchronize()
+    ys = [G.iodf_proj_forward(h, x, st_d, w_d) for _, x, _, _, st_d, w_d in todo]
+    G.iodf_proj_check(h)
+    for (xh, _, st, w, _, _), y in zip(todo, ys):
+        np.testing.assert_array_equal(y.cpu().numpy(), P.projection(layer, xh, ads, st, w, np.zeros((len(xh), N))))
+
+
+def test_narrow_clips(G):
+    rng = np.random.default_rng(3)
+    for rows, K, N in ((9, 64, 40), (700, 200, 150), (3000, 1200, 150)):
+        for y_dtype, clamp, relu in ((torch.int8, (-7, 5), False), (torch.uint8, (3, 200), True), (torch.int32, (-1000, 900), False),
+                                     (torch.int32, (-5, -2), True)):
+            layer = dict(make_layer(rng, K, N, y_dtype), clamp=clamp, relu=relu, s=np.full(N, 4, np.int32))
+            h = G.iodf_proj_create(layer, rows, y_dtype=y_dtype)
+            xh, x = make_x(rng, rows, K, torch.int8)
+            np.testing.assert_array_equal(G.iodf_proj_forward(h, x).cpu().numpy(), P.projection(layer, xh))
+
+
+@pytest.mark.parametrize("ldy_pad,skip", [(0, 0), (1, 0), (4, 4), (3, 1), (16, 2)])
+@pytest.mark.parametrize("rows,K,N", [(20, 64, 132), (900, 64, 132), (3000, 1100, 260)])
+def test_outputs_at_any_alignment(G, rows, K, N, ldy_pad, skip):
+    rng = np.random.default_rng(rows + ldy_pad)
+    for y_dtype in (torch.int8, torch.int32):
+        layer = make_layer(rng, K, N, y_dtype)
+        h = G.iodf_proj_create(layer, rows, y_dtype=y_dtype)
+        xh, x = make_x(rng, rows, K, torch.int8)
+        buf = torch.full((skip + rows * (N + ldy_pad) + 5,), 9, dtype=y_dtype, device="cuda")
+        y = buf[skip:skip + rows * (N + ldy_pad)].view(rows, N + ldy_pad)
+        G.iodf_proj_forward(h, x, y=y[:, :N])
+        np.testing.assert_array_equal(y[:, :N].cpu().numpy(), P.projection(layer, xh))
+        assert (y[:, N:] == 9).all() and (buf[:skip] == 9).all() and (buf[-5:] == 9).all()
