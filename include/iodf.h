@@ -555,6 +555,38 @@ int iodf_norm_forward(iodf_norm* nm, int rows, const void* r, const iodf_view* r
                       const uint8_t* gate, size_t ldg, void* r_out, const iodf_view* out_view, void* n, size_t ldn,
                       void* cuda_stream);
 
+/*
+ * Refinement of a level's prior parameters by a residual block of those layers, with adapters of each image's customer:
+ *   mu' = mu + scale * gate * norm(down(up(norm(mu))))         over the C/2 means of every pixel of the level
+ * as iodf_norm_forward (first: no block, its n feeds `up`), iodf_proj_forward twice and iodf_norm_forward (last: no n,
+ * its block is `down`'s output, its residual stream the means themselves, in place). The flow stays as it is and
+ * invertible; both sides of the codec refine alike, so what one codes the other decodes, and a codec with a
+ * refinement only understands streams of one with the same layers, adapters and image_adapter.
+ *
+ * iodf_codec_set_refinement gives level `level` of the codec a refinement, or none (parts NULL). From then on
+ * iodf_compress_host and iodf_decompress_host apply it after the level's prior parameters are known and
+ * before its block is coded. The handles, `gate` and `image_adapter` stay the caller's and must outlive it. All on the
+ * codec's device; first and last for C/2 channels and IODF_I32, first's n_type = up's x_type, up's y_type (8 bits) =
+ * down's x_type, down's c_out = C/2 and y_type = last's block_type, max_rows of both at least the model's max_batch
+ * times the level's pixels; IODF_EINVAL otherwise, or for a level without a prior head. Not while a call on the codec is in flight.
+ *
+ * iodf_refine_prior applies a level's refinement to a prior buffer (as iodf_forward or IODF_LEVEL_PRIOR wrote it), in place, for
+ * callers that take the steps themselves: before iodf_rans_encode, and between IODF_LEVEL_PRIOR and
+ * iodf_rans_decode_block. A level without one is left as it is. Allocates nothing. One call per
+ * codec at a time.
+ */
+typedef struct {
+  iodf_norm* first;
+  iodf_proj* up;
+  iodf_proj* down;
+  iodf_norm* last;
+  const uint8_t* gate;                 /* DEV, C/2 values, or NULL                                   */
+  const int32_t* image_adapter;        /* DEV, max_batch values: each image's adapter slot in both projections, -1 none; or NULL */
+} iodf_refinement;
+
+int iodf_codec_set_refinement(iodf_codec* c, int level, const iodf_refinement* parts);
+int iodf_refine_prior(iodf_codec* c, int level, int32_t* prior, int B, void* cuda_stream);
+
 const char* iodf_strerror(int status);
 int iodf_last_cuda_error(const iodf_model* m); /* the cudaError_t behind the last IODF_ECUDA          */
 

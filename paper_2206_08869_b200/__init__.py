@@ -13,7 +13,7 @@ from .binding import (IodfError, Model, iodf_create, iodf_destroy, iodf_forward,
                       iodf_launches_per_call, iodf_selftest_timeout, iodf_int8_mma_peak, iodf_level_kernel_name,
                       iodf_level_images_per_cta,
                       Projection, iodf_proj_create, iodf_proj_set_adapter, iodf_proj_forward, iodf_proj_check,
-                      Norm, iodf_norm_create, iodf_norm_forward,
+                      Norm, iodf_norm_create, iodf_norm_forward, iodf_codec_set_refinement, iodf_refine_prior,
                       load_library,
                       DECLARED_SYMBOLS)
 
@@ -28,6 +28,6 @@ __all__ = ["IodfError", "Model", "iodf_create", "iodf_destroy", "iodf_forward", 
            "iodf_launches_per_call", "iodf_selftest_timeout", "iodf_int8_mma_peak", "iodf_level_kernel_name",
            "iodf_level_images_per_cta",
            "Projection", "iodf_proj_create", "iodf_proj_set_adapter", "iodf_proj_forward", "iodf_proj_check",
-           "Norm", "iodf_norm_create", "iodf_norm_forward",
+           "Norm", "iodf_norm_create", "iodf_norm_forward", "iodf_codec_set_refinement", "iodf_refine_prior",
            "load_library",
            "DECLARED_SYMBOLS"]

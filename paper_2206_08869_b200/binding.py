@@ -23,6 +23,7 @@ DECLARED_SYMBOLS = ["iodf_create", "iodf_destroy", "iodf_get_layout", "iodf_forw
                     "iodf_level_images_per_cta",
                     "iodf_proj_create", "iodf_proj_destroy", "iodf_proj_set_adapter", "iodf_proj_forward",
                     "iodf_proj_check", "iodf_norm_create", "iodf_norm_destroy", "iodf_norm_forward",
+                    "iodf_codec_set_refinement", "iodf_refine_prior",
                     "iodf_strerror", "iodf_last_cuda_error"]
 
 
@@ -93,6 +94,11 @@ class NormDesc(C.Structure):
 class View(C.Structure):
     _fields_ = [("pixels", C.c_uint64), ("image_stride", C.c_uint64), ("channel_stride", C.c_uint64),
                 ("pixel_stride", C.c_uint64)]
+
+
+class RefinementDesc(C.Structure):
+    _fields_ = [("first", C.c_void_p), ("up", C.c_void_p), ("down", C.c_void_p), ("last", C.c_void_p),
+                ("gate", C.c_void_p), ("image_adapter", C.c_void_p)]
 
 
 class IodfError(RuntimeError):
@@ -194,6 +200,10 @@ def load_library(path=None):
     L.iodf_norm_forward.restype = C.c_int
     L.iodf_norm_forward.argtypes = [vp, C.c_int, vp, C.POINTER(View), vp, C.c_size_t, vp, C.c_size_t, vp,
                                     C.POINTER(View), vp, C.c_size_t, vp]
+    L.iodf_codec_set_refinement.restype = C.c_int
+    L.iodf_codec_set_refinement.argtypes = [vp, C.c_int, C.POINTER(RefinementDesc)]
+    L.iodf_refine_prior.restype = C.c_int
+    L.iodf_refine_prior.argtypes = [vp, C.c_int, vp, C.c_int, vp]
     L.iodf_strerror.restype = C.c_char_p
     L.iodf_strerror.argtypes = [C.c_int]
     L.iodf_last_cuda_error.restype = C.c_int
@@ -807,3 +817,35 @@ def iodf_norm_forward(norm, r, b=None, gate=None, r_out=None, n=None, stream=Non
     if rc != 0:
         raise IodfError(rc, "iodf_norm_forward")
     return r_out, n
+
+
+def iodf_codec_set_refinement(codec, level, first=None, up=None, down=None, last=None, gate=None, image_adapter=None):
+    """Give a level of the codec a refinement of its prior's means (see include/iodf.h), or take it away (no handles):
+    first, last: norms; up, down: projections; gate uint8 [c] and image_adapter int32 [max_batch] on the device."""
+    desc = None
+    if first is not None:
+        for h in (first, up, down, last):
+            if h is None:
+                raise ValueError("a refinement has two norms and two projections")
+        import torch
+        c = first.channels
+        if gate is not None and (_on(gate, first, torch.uint8, "gate").numel() != c or not gate.is_contiguous()):
+            raise ValueError("gate must hold %d contiguous values" % c)
+        if image_adapter is not None and (_on(image_adapter, first, torch.int32, "image_adapter").numel() < codec.model.max_batch
+                                          or not image_adapter.is_contiguous()):
+            raise ValueError("image_adapter must hold %d contiguous values" % codec.model.max_batch)
+        desc = RefinementDesc(first.handle, up.handle, down.handle, last.handle, _addr(gate), _addr(image_adapter))
+    rc = load_library().iodf_codec_set_refinement(codec.handle, int(level), C.byref(desc) if desc is not None else None)
+    if rc != 0:
+        raise IodfError(rc, "iodf_codec_set_refinement")
+    if not hasattr(codec, "refinements"):
+        codec.refinements = {}
+    codec.refinements[int(level)] = (first, up, down, last, gate, image_adapter)     # kept alive
+
+
+def iodf_refine_prior(codec, level, prior, stream=None):
+    """Apply a level's refinement to prior int32 [B, 2, d_fact] in place."""
+    rc = load_library().iodf_refine_prior(codec.handle, int(level), prior.data_ptr(), prior.shape[0],
+                                          _layer_stream(stream, prior.get_device()))
+    if rc != 0:
+        raise IodfError(rc, "iodf_refine_prior")

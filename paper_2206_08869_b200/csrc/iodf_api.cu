@@ -16,6 +16,7 @@
 #include "iodf_dev.h"
 #include "flow_level.h"
 #include "rans_kernel.h"
+#include "refine.h"
 #include "res_flow.h"
 #include "res_level.h"
 #include "level_kernel.h"
@@ -79,6 +80,9 @@ struct iodf_codec {
   size_t packed_capacity = 0;
   iodf::RansArgs args{};
   iodf_codec_layout layout{};
+  iodf::Refinement refine[IODF_MAX_LEVELS];                                  // of the levels that have one
+  uint64_t level_channels[IODF_MAX_LEVELS] = {}, level_pixels[IODF_MAX_LEVELS] = {};   // of the factored-out blocks with prior parameters
+  long long level_prior_off[IODF_MAX_LEVELS] = {};
 };
 
 namespace {
@@ -2067,6 +2071,11 @@ int iodf_codec_create(const iodf_model* m, const iodf_codec_desc* desc, iodf_cod
       return IODF_EINVAL;
     }
     add_block(P.z_off, (uint64_t)P.cb * P.px, P.has_prior ? (long long)P.prior_off : -1);
+    if (P.has_prior) {
+      c->level_channels[li] = (uint64_t)P.cb;
+      c->level_pixels[li] = (uint64_t)P.px;
+      c->level_prior_off[li] = (long long)P.prior_off;
+    }
     c->layout.block_level[nb - 1] = (int32_t)li;
   }
   add_block(m->layout.z_final_off, m->layout.d - m->layout.z_final_off, -1);
@@ -2117,7 +2126,30 @@ void iodf_codec_destroy(iodf_codec* c) {
   if (c->d_words) cudaFree(c->d_words);
   if (c->d_counts) cudaFree(c->d_counts);
   if (c->d_packed) cudaFree(c->d_packed);
+  for (auto& r : c->refine) refinement_free(&r);
   delete c;
+}
+
+int iodf_codec_set_refinement(iodf_codec* c, int level, const iodf_refinement* parts) {
+  if (!c || level < 0 || level >= IODF_MAX_LEVELS || !c->level_channels[level]) return IODF_EINVAL;
+  Refinement made;
+  if (parts) {
+    const int rc = refinement_create(*parts, c->device, c->level_channels[level], c->level_pixels[level], c->max_batch, &made);
+    if (rc) return rc;
+  }
+  int prev = -1;
+  CUC(c, cudaGetDevice(&prev));
+  CUC(c, cudaSetDevice(c->device));
+  refinement_free(&c->refine[level]);
+  cudaSetDevice(prev);
+  c->refine[level] = made;
+  return IODF_OK;
+}
+
+int iodf_refine_prior(iodf_codec* c, int level, int32_t* prior, int B, void* cuda_stream) {
+  if (!c || level < 0 || level >= IODF_MAX_LEVELS || !c->level_channels[level]) return IODF_EINVAL;
+  if (!prior || !aligned16(prior) || B < 1 || (uint32_t)B > c->max_batch) return IODF_EINVAL;
+  return refinement_run(c->refine[level], prior + c->level_prior_off[level], 2 * (uint64_t)c->args.d_fact, B, cuda_stream);
 }
 
 int iodf_codec_get_layout(const iodf_codec* c, iodf_codec_layout* out) {
@@ -2212,6 +2244,8 @@ int iodf_compress_host(iodf_model* m, iodf_codec* c, const uint8_t* x_u8_host, i
   CU(m, cudaMemcpyAsync(m->d_x, x_u8_host, (size_t)B * d, cudaMemcpyHostToDevice, st));
   rc = run_forward(m, m->d_x, B, m->d_z, prior, st);
   if (rc) return rc;
+  for (int li = 0; li < IODF_MAX_LEVELS; ++li)
+    if (c->refine[li].mem && (rc = iodf_refine_prior(c, li, prior, B, cuda_stream))) return rc;
   RansArgs a = c->args;
   a.batch = B;
   CUC(c, launch_rans_encode(a, m->d_z, prior, c->d_words, c->d_counts, st));
@@ -2254,6 +2288,7 @@ int iodf_decompress_host(iodf_model* m, iodf_codec* c, const uint8_t* in_host, s
       if (m->levels[li].plan.has_prior) {
         rc = launch_inverse_level(m, li, 1, m->d_z, B, nullptr, prior, nullptr, st, PatchGrid());
         if (rc) return rc;
+        if (c->refine[li].mem && (rc = iodf_refine_prior(c, li, prior, B, cuda_stream))) return rc;
       }
       CUC(c, launch_rans_decode(a, q, c->d_words, c->d_counts, prior, m->d_z, st));
     }

@@ -23,6 +23,7 @@ struct NormArgs {
   int post, pre;                      // 0, IODF_NORM_RMS, IODF_NORM_CENTRED
   int shift, n_shift;
   int res_lo, res_hi, n_lo, n_hi;
+  int n_type;                         // IODF_I8 or IODF_U8
   int n_full;                         // the clip of n is its type's range
   unsigned long long eps;
   const int32_t *mult, *n_mult, *n_bias;   // device, [channels]

@@ -13,6 +13,7 @@
 #include "../../include/iodf.h"
 #include "norm_kernel.h"
 #include "proj_kernel.h"
+#include "refine.h"
 
 using namespace iodf;
 
@@ -281,6 +282,7 @@ int create_norm(const iodf_norm_desc& d, int device, iodf_norm& nm) {
   a.res_hi = d.res_hi;
   a.n_lo = d.n_lo;
   a.n_hi = d.n_hi;
+  a.n_type = (int)d.n_type;
   a.n_full = d.n_type == IODF_I8 ? d.n_lo == -128 && d.n_hi == 127 : d.n_lo == 0 && d.n_hi == 255;
   a.eps = d.eps;
   a.mult = nm.d_consts;
@@ -466,3 +468,73 @@ int iodf_norm_forward(iodf_norm* nm, int rows, const void* r, const iodf_view* r
 }
 
 }  // extern "C"
+
+namespace iodf {
+
+int refinement_create(const iodf_refinement& p, int device, uint64_t channels, uint64_t pixels, uint32_t max_batch, Refinement* out) {
+  if (!p.first || !p.up || !p.down || !p.last) return IODF_EINVAL;
+  const NormArgs &f = p.first->args, &l = p.last->args;
+  const ProjArgs &u = p.up->args, &d = p.down->args;
+  if (p.first->device != device || p.last->device != device || p.up->device != device || p.down->device != device) return IODF_EINVAL;
+  if ((uint64_t)f.channels != channels || (uint64_t)l.channels != channels || (uint64_t)u.k != channels || (uint64_t)d.n != channels || d.k != u.n)
+    return IODF_EINVAL;
+  if (f.res_i16 || l.res_i16 || f.has_block || !f.pre || !l.has_block || l.pre) return IODF_EINVAL;
+  if ((f.n_type == IODF_U8) != (u.x_unsigned != 0) || u.y_type == IODF_I32 || (u.y_type == IODF_U8) != (d.x_unsigned != 0)) return IODF_EINVAL;
+  if (d.y_type != (l.block_i8 ? IODF_I8 : IODF_I32)) return IODF_EINVAL;
+  const uint64_t rows = pixels * max_batch;
+  if (rows < 1 || rows > p.up->max_rows || rows > p.down->max_rows || channels > kMaxPlanes) return IODF_EINVAL;
+  Refinement r;
+  r.parts = p;
+  r.channels = channels;
+  r.pixels = pixels;
+  r.ldn = up_to(channels, 16);
+  r.ldu = up_to((size_t)u.n, 16);
+  r.ldb = up_to(channels, 16);
+  std::vector<int32_t> start;
+  try {
+    start.resize((size_t)max_batch + 1);
+  } catch (const std::exception&) {
+    return IODF_ENOMEM;
+  }
+  for (size_t i = 0; i < start.size(); ++i) start[i] = (int32_t)(i * pixels);
+  const size_t on = 0, ou = on + up_to(rows * r.ldn, 256), ob = ou + up_to(rows * r.ldu, 256), os = ob + up_to(rows * r.ldb * (size_t)d.y_bytes, 256);
+  OnDevice dev(device);
+  if (dev.error() != cudaSuccess) return IODF_ECUDA;
+  cudaError_t e = cudaMalloc(&r.mem, os + 4 * start.size());
+  if (e != cudaSuccess) return status_of(e);
+  uint8_t* m = static_cast<uint8_t*>(r.mem);
+  r.n = m + on;
+  r.u = m + ou;
+  r.b = m + ob;
+  r.start = reinterpret_cast<int32_t*>(m + os);
+  e = cudaMemcpy(r.start, start.data(), 4 * start.size(), cudaMemcpyHostToDevice);
+  if (e != cudaSuccess) {
+    cudaFree(r.mem);
+    return status_of(e);
+  }
+  *out = r;
+  return IODF_OK;
+}
+
+void refinement_free(Refinement* r) {
+  if (r->mem) cudaFree(r->mem);
+  *r = Refinement();
+}
+
+int refinement_run(const Refinement& r, int32_t* mu, uint64_t image_stride, int batch, void* stream) {
+  if (!r.mem) return IODF_OK;
+  const iodf_refinement& p = r.parts;
+  const int rows = (int)(r.pixels * (uint64_t)batch);
+  const iodf_view v{r.pixels, image_stride, r.pixels, 1};
+  auto project = [&](iodf_proj* proj, const void* x, size_t ldx, void* y, size_t ldy) {
+    const bool adapters = p.image_adapter && proj->max_adapters;
+    return iodf_proj_forward(proj, x, ldx, rows, adapters ? r.start : nullptr, adapters ? p.image_adapter : nullptr, adapters ? batch : 0, y, ldy, stream);
+  };
+  int rc = iodf_norm_forward(p.first, rows, mu, &v, nullptr, 0, nullptr, 0, nullptr, nullptr, r.n, r.ldn, stream);
+  if (rc == IODF_OK) rc = project(p.up, r.n, r.ldn, r.u, r.ldu);
+  if (rc == IODF_OK) rc = project(p.down, r.u, r.ldu, r.b, r.ldb);
+  if (rc == IODF_OK) rc = iodf_norm_forward(p.last, rows, mu, &v, r.b, r.ldb, p.gate, 0, mu, &v, nullptr, 0, stream);
+  return rc;
+}
+
+}  // namespace iodf
