@@ -115,8 +115,9 @@ __device__ __forceinline__ void look_over_request(const ProjArgs& a, int q) {
   const int s0 = a.seg_start[q], s1 = a.seg_start[q + 1], ad = a.seg_adapter[q];
   if (s0 < 0 || s1 < s0 || s1 > a.rows || ad < -1 || ad >= a.max_adapters) atomicAdd(a.status + 1, 1u);
 }
+// by one warp
 __device__ __forceinline__ void look_over_requests(const ProjArgs& a) {
-  for (int q = threadIdx.x; q < a.n_seg; q += blockDim.x) look_over_request(a, q);
+  for (int q = threadIdx.x & 31; q < a.n_seg; q += 32) look_over_request(a, q);
 }
 
 __device__ __forceinline__ int8_t rank_value(int acc, int2 q) {
@@ -140,6 +141,17 @@ __device__ __forceinline__ void store_rank(int8_t* h, int rp, const uint32_t (&v
   }
 }
 
+// Is row r the first of its tile with adapter slots[r]? `starts` has a bit for each row whose slot differs from the row's above:
+// only those are looked at (a walk over all rows above took 4000 clocks where a request starts low in a tile).
+__device__ __forceinline__ bool first_of_slot(const int* slots, const uint32_t* starts, int r) {
+  const int s = slots[r];
+  if (s < 0 || !(starts[r >> 5] >> (r & 31) & 1)) return false;
+  for (int w = 0; w <= r >> 5; ++w)
+    for (uint32_t b = w < r >> 5 ? starts[w] : starts[w] & ((1u << (r & 31)) - 1); b; b &= b - 1)
+      if (slots[w * 32 + __ffs((int)b) - 1] == s) return false;
+  return true;
+}
+
 // ---- h for few rows: a block per row and eight rank channels, a quarter of K per warp ----------------------
 template <bool kUnsigned>
 __global__ void __launch_bounds__(128) down_rows_kernel(const ProjArgs a) {
@@ -159,7 +171,7 @@ __global__ void __launch_bounds__(128) down_rows_kernel(const ProjArgs a) {
   } else {
     slot = slot_of_row(a, row);
   }
-  if (row == 0 && g == 0) look_over_requests(a);
+  if (row == 0 && g == gridDim.y - 1 && warp == 3) look_over_requests(a);      // a block whose rank channels are mostly padding
   const int rank = slot < 0 ? 0 : a.rank[slot];
   if (g == 0 && threadIdx.x == 0) a.row_slot[row] = slot < 0 ? slot : slot | rank << kSlotBits;
   if (g * 8 >= rank) return;
@@ -188,6 +200,7 @@ struct DownShared {
   uint64_t full[kDownRing], empty[kDownRing], dfull, dempty;
   uint32_t abort_flag, tmem;
   int n_slots;
+  uint32_t starts[kDownRows / 32];
   alignas(16) int slot[kDownRows];
   int list[kDownRows];
 };
@@ -227,14 +240,14 @@ __global__ void __launch_bounds__(kDownThreads) down_tile_kernel(const __grid_co
     }
     __syncthreads();
   }
-  if (blockIdx.x == 0) look_over_requests(a);
-  if (tid < kDownRows) {                              // the adapters of the tile, each once, in any order
+  if (tid < kDownRows) {
     const int s = sh.slot[tid];
     if (row0 + tid < a.rows) a.row_slot[row0 + tid] = s;
-    bool first = s >= 0 && (tid == 0 || sh.slot[tid - 1] != s);
-    for (int i = 0; first && i < tid; ++i) first = sh.slot[i] != s;
-    if (first) sh.list[atomicAdd(&sh.n_slots, 1)] = s;
+    const uint32_t starts = __ballot_sync(0xFFFFFFFFu, tid == 0 || sh.slot[tid - 1] != s);
+    if (lane == 0) sh.starts[warp] = starts;
   }
+  __syncthreads();                                    // the adapters of the tile, each once, in any order
+  if (tid < kDownRows && first_of_slot(sh.slot, sh.starts, tid)) sh.list[atomicAdd(&sh.n_slots, 1)] = sh.slot[tid];
   __syncthreads();
   const int n_slots = sh.n_slots, groups = (n_slots + per - 1) / per;
   const uint32_t base = ptx::smem_u32(smem), tmem = sh.tmem;
@@ -271,6 +284,8 @@ __global__ void __launch_bounds__(kDownThreads) down_tile_kernel(const __grid_co
       }
       ptx::umma_commit(ptx::smem_u32(&sh.dfull));
     }
+  } else if (warp == 3 && blockIdx.x == 0) {
+    look_over_requests(a);
   } else if (warp >= 4) {
     const int q = warp & 3, half = (warp - 4) >> 2, m = q * 32 + lane, j = m % a.rp;
     for (int g = 0; g < groups; ++g) {
@@ -318,7 +333,7 @@ struct MainShared {
   uint32_t abort_flag, tmem;
   int message[2];                        // an adapter step: its adapters, 256: the tile's last
   int n_list[2];
-  uint32_t firsts[kMaxTile / 32];        // rows whose adapter no row above has, a bit each
+  uint32_t starts[kMaxTile / 32], firsts[kMaxTile / 32];      // rows with another adapter than the row above, than any row above: a bit each
   alignas(16) int slot[2][kMaxTile];     // of a unit: adapter of each row
   int list[2][kMaxTile];                 //            every adapter once
   uint32_t live[2][kMaxTile / 32];       // of a unit: the rows that some request owns
@@ -562,12 +577,12 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         if (ok) commit(&sh.tfull[ti & 1]);
       }
     }
+  } else if (kFused && adapters && warp == 2 && blockIdx.x == 0) {
+    look_over_requests(a);
   } else if (warp >= 4 && warp < 8 && adapters) {
     // The adapters of each unit's rows, then for each of its output tiles the operands of their steps.
     const int f = tid - 128;
     if (!kFused) ptx::grid_dependency_wait();
-    else if (blockIdx.x == 0)
-      for (int q = f; q < a.n_seg; q += kFill) look_over_request(a, q);
     auto rows_of = [&](int u, int ui) {                 // slot, live, list and n_list of unit u
       const int ub = ui & 1, row0 = u / shp.chunks * RT;
       if (!fill_all(wait(&sh.lfree[ub], ((ui >> 1) & 1) ^ 1))) return false;
@@ -601,9 +616,14 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         const int r = f + i * kFill, s = r < RT ? sh.slot[ub][r] : -2;
         const uint32_t live = __ballot_sync(0xFFFFFFFFu, s != -2);
         if (lane == 0 && r < RT) sh.live[ub][r >> 5] = live;
-        bool first = s >= 0 && (r == 0 || sh.slot[ub][r - 1] != s);
-        for (int e = 0; first && e < r; ++e) first = sh.slot[ub][e] != s;
-        const uint32_t firsts = __ballot_sync(0xFFFFFFFFu, first);
+        const uint32_t starts = __ballot_sync(0xFFFFFFFFu, r == 0 || (r < RT && sh.slot[ub][r - 1] != s));
+        if (lane == 0 && r < RT) sh.starts[r >> 5] = starts;
+      }
+      fill_all(true);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const int r = f + i * kFill;
+        const uint32_t firsts = __ballot_sync(0xFFFFFFFFu, r < RT && first_of_slot(sh.slot[ub], sh.starts, r));
         if (lane == 0 && r < RT) sh.firsts[r >> 5] = firsts;
       }
       fill_all(true);
