@@ -382,7 +382,7 @@ int iodf_proj_forward(iodf_proj* p, const void* x, size_t ldx, int rows, const i
   if (on.error() != cudaSuccess) return IODF_ECUDA;
   CUtensorMap map, map_down;
   if (!tile_map(*p, x, (uint64_t)a.k, (uint64_t)rows, ldx, (uint32_t)proj_x_rows(a), true, &map) ||
-      !tile_map(*p, x, (uint64_t)a.k, (uint64_t)rows, ldx, kProjDownRows, true, &map_down))
+      (proj_down_tiles(a) && !tile_map(*p, x, (uint64_t)a.k, (uint64_t)rows, ldx, kProjDownRows, true, &map_down)))
     return IODF_ECUDA;
   return status_of(launch_proj(a, &map, &map_down, &p->w_map, (cudaStream_t)cuda_stream));
 }

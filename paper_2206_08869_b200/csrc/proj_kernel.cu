@@ -1125,11 +1125,15 @@ cudaError_t configure_proj_kernels() {
   return e;
 }
 
+bool proj_down_tiles(const ProjArgs& a) {
+  return a.n_seg && !split_tile(a) && !fuse_down(a) && (long long)a.rows * a.rp > kDownRowsMost;
+}
+
 int proj_x_rows(const ProjArgs& a) { return split_tile(a) || fuse_down(a) ? row_tile(a) : row_tile(a) / 2; }
 
 cudaError_t launch_proj(const ProjArgs& a, const void* x_map, const void* x_map_down, const void* w_map, cudaStream_t stream) {
   if (a.n_seg && (split_tile(a) || !fuse_down(a))) {
-    if ((long long)a.rows * a.rp <= kDownRowsMost) {
+    if (!proj_down_tiles(a)) {
       const dim3 grid((unsigned)a.rows, (unsigned)(a.rp / 8));
       if (a.x_unsigned) down_rows_kernel<true><<<grid, 128, 0, stream>>>(a);
       else down_rows_kernel<false><<<grid, 128, 0, stream>>>(a);

@@ -49,6 +49,7 @@ cudaError_t configure_proj_kernels();
 // x_map, x_map_down: CUtensorMaps of x [rows][k] with boxes of 128 bytes x proj_x_rows(a) or kProjDownRows rows and
 // the 128-byte swizzle. w_map: of the weights as rows of 128 bytes, box 128 x 128, no swizzle.
 int proj_x_rows(const ProjArgs& a);
+bool proj_down_tiles(const ProjArgs& a);      // x_map_down is used
 cudaError_t launch_proj(const ProjArgs& a, const void* x_map, const void* x_map_down, const void* w_map, cudaStream_t stream);
 
 }  // namespace iodf
