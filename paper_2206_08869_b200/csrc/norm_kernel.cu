@@ -1,10 +1,16 @@
 // Norms before and after a block with its gate and residual scale (include/iodf.h: iodf_norm_forward).
 //
 // One pass: T threads hold a row of C channels in registers, E values each, from the loads to the stores; only the
-// sums of a norm (sum, sum of squares) cross threads. What bounds it is memory, so every operand is loaded before
-// the first value is used and the arithmetic is kept below the loads' time: per element and norm a square, and
-// two 32 x 32 -> 64 multiply-adds whose rounding constant is the addend and of whose result only the high word is
-// shifted. Three ways to lay a row over its threads:
+// sums of a norm (sum, sum of squares) cross threads. Every operand is loaded before the first value is used.
+// What bounds it: memory where the arithmetic stays below it. An element costs a 64-bit square (some 5 clocks per warp and
+// SM quarter), per norm two 32 x 32 -> 64 multiply-adds (5 each) and a shift of the pair (2), clips and packs; a row costs some
+// 250 instructions per thread beside its elements. 16384 x 4096 int16 with int32 blocks and gates: 134 us (5.0 TB/s; floor 104;
+// without the two norms 87), 32768 x 256 int32 with int8 blocks: 20.9 us (4.0 TB/s; floor 13), 20011 x 173 unaligned,
+// centred: 19.2 us (2.5 TB/s; floor 7.5; a row's own work), one row of 4096: 4 us (a launch).
+// Measured and not taken: 32 elements per thread (fewer instructions, a fifth of the warps: 228 us on the first of
+// these), rows copied ahead into shared memory (235 us: twice through the same pipe), a row's two roots worked out by one thread
+// for all (188 us: two more barriers), four elements per access (222 us: twice the accesses).
+// Three ways to lay a row over its threads:
 //   kVector  eight neighbouring channels per thread, 8 or 16-byte accesses (everything aligned to them)
 //   kScalar  neighbouring threads take neighbouring channels, one element per access (any alignment)
 //   kPlanes  the residual stream as planes: as kScalar with T = 1 or 8, so that neighbouring threads take
@@ -36,8 +42,9 @@ struct RowScale {
 // sigma = floor(sqrt(m)) and rho = floor((2^61 - 1) / sigma) for m = D 2^t in [2^60, 2^62). Both come from one
 // reciprocal root y of m: the hardware's estimate (more than 20 bits) and one step of third order, whose error (5/16 e^3 and
 // roundings, together below 2^-50) puts m y and 2^61 y (1 + e') within 2^-18 of the root and the quotient; e' = (root - sigma) y
-// < 2^-30 and its square, below 2^-60, moves rho by less than 2^-28. Rounded to integers by adding 1.5 * 2^52, each is
-// off by one at most, and put right by its exact remainder.
+// < 2^-30 and its square, below 2^-60, moves rho by less than 2^-28. Rounded to integers by adding 1.5 * 2^52,
+// sigma is the floor or one more; rho belongs to that integer and is up to three less for the one below it. Exact remainders put
+// both right.
 __device__ __forceinline__ RowScale row_scale(unsigned long long D) {
   constexpr double kMagic = 6755399441055744.0;         // 1.5 * 2^52: the low word of the sum is the nearest integer
   const int t = (__clzll((long long)D) - 2) & ~1;
@@ -52,7 +59,7 @@ __device__ __forceinline__ RowScale row_scale(unsigned long long D) {
   long long rem = (long long)(m - (unsigned long long)s * s);          // 0 .. 2 s if s is the floor
   const double e = (root - (rs - kMagic)) * y;
   unsigned int q = (unsigned int)__double2loint(fma(fma(y, e, y), 2305843009213693952.0, kMagic));
-  // s too large by one: rem < 0; too small: rem > 2 s. The quotient by the nearest integer is one by the floor, or the next.
+  // s too large by one: rem < 0; too small: rem > 2 s
   const int ds = rem < 0 ? -1 : rem > 2ll * s ? 1 : 0;
   s += ds;
   rem = (long long)(((1ull << 61) - 1) - (unsigned long long)q * s);   // 0 .. s - 1 if q is the floor
@@ -108,7 +115,7 @@ __device__ __forceinline__ void norm_row(int (&v)[E], int C, int kind, unsigned 
 #pragma unroll
   for (int e = 0; e < E; ++e) q += (long long)v[e] * v[e];
   const RowScale s = row_scale((unsigned long long)row_sum<T, false>(q, red + 16) + eps);
-  if (s.sh < 32) {                                      // sqrt(D) below 2^24: a funnel shift of the two words
+  if (s.sh < 32) {                                      // sqrt(D) below 2^23: a funnel shift of the two words
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const long long p = (long long)v[e] * s.rho + s.round;
@@ -177,10 +184,10 @@ template <int T>
 struct Block { static constexpr int threads = T <= 32 ? 128 : T, rows = threads / T; };
 
 // Blocks per SM that the registers have to leave room for: what measured best (32 to 40 warps; 16384 x 4096 int16 with
-// int32 blocks and gates 152 us without the bound, 134 with it).
+// int32 blocks and gates 152 us without the bound, 134 with it; 20011 x 173 int32 unaligned 19.8 and 19.2).
 template <int T, int E, int MODE>
 __host__ __device__ constexpr int min_blocks() {
-  return MODE != kVector ? 1 : T == 512 ? 2 : T == 256 ? 5 : T == 128 ? 9 : T == 64 ? 16 : E <= 8 ? 10 : 8;
+  return MODE == kScalar ? (T == 32 && E <= 8 ? 10 : 1) : MODE != kVector ? 1 : T == 512 ? 2 : T == 256 ? 5 : T == 128 ? 9 : T == 64 ? 16 : E <= 8 ? 10 : 8;
 }
 
 template <class RT, class BT, int T, int E, int MODE, bool kFull>
