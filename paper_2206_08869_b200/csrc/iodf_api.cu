@@ -2146,6 +2146,15 @@ int iodf_codec_set_refinement(iodf_codec* c, int level, const iodf_refinement* p
   return IODF_OK;
 }
 
+namespace {
+// The refinements write where the prior buffer of the codec's own model has its levels.
+bool refinements_fit(const iodf_codec* c, const iodf_model* m) {
+  for (const auto& r : c->refine)
+    if (r.mem && c->args.d_fact != (long long)m->layout.d_fact) return false;
+  return true;
+}
+}  // namespace
+
 int iodf_refine_prior(iodf_codec* c, int level, int32_t* prior, int B, void* cuda_stream) {
   if (!c || level < 0 || level >= IODF_MAX_LEVELS || !c->level_channels[level]) return IODF_EINVAL;
   if (!prior || !aligned16(prior) || B < 1 || (uint32_t)B > c->max_batch) return IODF_EINVAL;
@@ -2235,6 +2244,7 @@ int iodf_compress_host(iodf_model* m, iodf_codec* c, const uint8_t* x_u8_host, i
   if (!m || !c || !x_u8_host || !out_host || !out_bytes || B < 1 || (uint32_t)B > m->max_batch ||
       (uint32_t)B > c->max_batch || c->args.d != (long long)m->layout.d || c->args.cap > 65535)
     return IODF_EINVAL;
+  if (!refinements_fit(c, m)) return IODF_EINVAL;
   if (iodf_rans_packed_capacity(c, B) >= (1ull << 32) || c->args.n_streams > 8192) return IODF_EUNSUPPORTED;
   int rc = codec_staging(c);
   if (rc) return rc;
@@ -2266,6 +2276,7 @@ int iodf_decompress_host(iodf_model* m, iodf_codec* c, const uint8_t* in_host, s
   if (!m || !c || !in_host || !x_u8_host || B < 1 || (uint32_t)B > m->max_batch || (uint32_t)B > c->max_batch ||
       c->args.d != (long long)m->layout.d || c->args.cap > 65535)
     return IODF_EINVAL;
+  if (!refinements_fit(c, m)) return IODF_EINVAL;
   int rc = codec_staging(c);
   if (rc) return rc;
   if (in_bytes < 4 * ((size_t)B + 1) || in_bytes > c->packed_capacity) return IODF_EINVAL;

@@ -180,3 +180,18 @@ def test_refusals(G):
         G.iodf_refine_prior(codec, 0, prior)             # more images than the codec holds
     with pytest.raises(G.IodfError):
         G.iodf_refine_prior(codec, 2, prior[:2])
+
+
+def test_a_model_whose_prior_buffer_has_another_size_is_refused(G):
+    m, codec, blocks, x = _setup(G, 0xC0E1, batch=2)
+    other = G.iodf_create(S.make_model(5, 3, 32, 32, [False, True, False], 2, 24), 2)
+    assert other.d == m.d and other.d_fact != m.d_fact
+    _set(G, codec, {0: blocks[0]}, None)
+    xh = torch.from_numpy(x).pin_memory()
+    with pytest.raises(G.IodfError) as e:
+        G.iodf_compress_host(other, codec, xh)
+    assert e.value.status == -1
+    buf, n = G.iodf_compress_host(m, codec, xh)
+    with pytest.raises(G.IodfError) as e:
+        G.iodf_decompress_host(other, codec, buf, n, 2)
+    assert e.value.status == -1
