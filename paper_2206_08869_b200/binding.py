@@ -607,16 +607,19 @@ def _type_code(dtype, allowed):
 
 
 def _on(t, handle, dtype, what):
-    if t.get_device() != handle.device or t.dtype != dtype:        # -1: not on a GPU
+    if t.get_device() != handle.device or t.dtype is not dtype:    # -1: not on a GPU
         raise ValueError("%s must be a %s tensor on cuda:%d" % (what, dtype, handle.device))
     return t
 
 
-def _rows_of(t, rows, channels, what):
+def _rows_of(t, handle, dtype, rows, channels, what):
     """Row stride of a [rows, channels] tensor whose channels lie side by side."""
-    if t.shape != (rows, channels) or (channels > 1 and t.stride(1) != 1):
+    if t.get_device() != handle.device or t.dtype is not dtype:
+        _on(t, handle, dtype, what)
+    strides = t.stride()
+    if t.shape != (rows, channels) or (strides[1] != 1 and channels > 1):
         raise ValueError("%s must be [%d, %d] with channels side by side" % (what, rows, channels))
-    return t.stride(0) if rows > 1 else max(channels, t.stride(0))
+    return strides[0] if rows > 1 else max(channels, strides[0])
 
 
 def _layer_stream(stream, device):
@@ -690,24 +693,22 @@ def iodf_proj_forward(proj, x, seg_start=None, seg_adapter=None, y=None, stream=
     seg_adapter int32 [n] on the device: the rows and the slot of each request. Returns y [rows, c_out]; rows in no
     request keep what y held (zero where y is made here)."""
     rows = x.shape[0]
-    _on(x, proj, proj.x_dtype, "x")
-    ldx = _rows_of(x, rows, proj.c_in, "x")
+    ldx = _rows_of(x, proj, proj.x_dtype, rows, proj.c_in, "x")
     if rows == 1:
         ldx = (ldx + 15) // 16 * 16          # a single row has no stride of its own
-    n_seg = 0
+    n_seg, start, which = 0, None, None
     if seg_start is not None:
         n_seg = seg_adapter.numel()
-        for t, n, what in ((seg_start, n_seg + 1, "seg_start"), (seg_adapter, n_seg, "seg_adapter")):
-            _on(t, proj, proj.int32, what)
-            if t.numel() != n or not t.is_contiguous():
-                raise ValueError("%s must hold %d contiguous values" % (what, n))
+        _on(seg_start, proj, proj.int32, "seg_start")
+        _on(seg_adapter, proj, proj.int32, "seg_adapter")
+        if seg_start.numel() != n_seg + 1 or not seg_start.is_contiguous() or not seg_adapter.is_contiguous():
+            raise ValueError("seg_start must hold %d contiguous values, one more than seg_adapter" % (n_seg + 1))
+        start, which = seg_start.data_ptr(), seg_adapter.data_ptr()
     if y is None:
         import torch
         y = (torch.zeros if n_seg else torch.empty)((rows, proj.c_out), dtype=proj.y_dtype, device=x.device)
-    _on(y, proj, proj.y_dtype, "y")
-    ldy = _rows_of(y, rows, proj.c_out, "y")
-    rc = (_lib or load_library()).iodf_proj_forward(proj.handle, x.data_ptr(), ldx, rows, _addr(seg_start),
-                                                    _addr(seg_adapter), n_seg, y.data_ptr(), ldy,
+    ldy = _rows_of(y, proj, proj.y_dtype, rows, proj.c_out, "y")
+    rc = (_lib or load_library()).iodf_proj_forward(proj.handle, x.data_ptr(), ldx, rows, start, which, n_seg, y.data_ptr(), ldy,
                                                     _layer_stream(stream, proj.device))
     if rc != 0:
         raise IodfError(rc, "iodf_proj_forward")
@@ -728,7 +729,7 @@ class Norm:
         self.handle, self.device, self.channels = handle, device, channels
         self.res_dtype, self.block_dtype, self.n_dtype = res_dtype, block_dtype, n_dtype
         import torch
-        self.uint8 = torch.uint8
+        self.uint8, self.views = torch.uint8, {}
 
     def __del__(self):
         h, self.handle = getattr(self, "handle", None), None
@@ -768,14 +769,22 @@ def iodf_norm_create(desc, device=0):
     return Norm(out, int(device), c, desc["res_dtype"], block, n_dtype)
 
 
-def _view(t, channels, what):
+def _view(t, norm, what):
     """rows and strides of a residual stream: [rows, c] or planes [images, c, pixels]."""
-    shape = t.shape
-    if len(shape) == 2 and shape[1] == channels and (channels == 1 or t.stride(1) == 1):
-        return shape[0], View(max(1, shape[0]), 0, 1, t.stride(0))
-    if len(shape) == 3 and shape[1] == channels and (shape[2] == 1 or t.stride(2) == 1):
-        return shape[0] * shape[2], View(max(1, shape[2]), t.stride(0), t.stride(1), 1)
-    raise ValueError("%s must be [rows, %d] or [images, %d, pixels] with the last axis contiguous" % (what, channels, channels))
+    shape, strides, channels = t.shape, t.stride(), norm.channels
+    known = norm.views.get((shape, strides))          # by shape: the descriptor costs as much to make as the rest of the call's checks
+    if known is not None:
+        return known
+    if len(shape) == 2 and shape[1] == channels and (channels == 1 or strides[1] == 1):
+        made = shape[0], View(max(1, shape[0]), 0, 1, strides[0])
+    elif len(shape) == 3 and shape[1] == channels and (shape[2] == 1 or strides[2] == 1):
+        made = shape[0] * shape[2], View(max(1, shape[2]), strides[0], strides[1], 1)
+    else:
+        raise ValueError("%s must be [rows, %d] or [images, %d, pixels] with the last axis contiguous" % (what, channels, channels))
+    if len(norm.views) >= 64:
+        norm.views.clear()
+    norm.views[(shape, strides)] = made
+    return made
 
 
 def iodf_norm_forward(norm, r, b=None, gate=None, r_out=None, n=None, stream=None):
@@ -784,13 +793,13 @@ def iodf_norm_forward(norm, r, b=None, gate=None, r_out=None, n=None, stream=Non
     r_out may be r."""
     c = norm.channels
     _on(r, norm, norm.res_dtype, "r")
-    rows, rv = _view(r, c, "r")
+    rows, rv = _view(r, norm, "r")
     if (b is not None) != (norm.block_dtype is not None):
         raise ValueError("b is given exactly if the handle has a block")
     ldb = ldg = ldn = 0
     ov = None
     if b is not None:
-        ldb = _rows_of(_on(b, norm, norm.block_dtype, "b"), rows, c, "b")
+        ldb = _rows_of(b, norm, norm.block_dtype, rows, c, "b")
         if r_out is r:
             ov = rv
         else:
@@ -799,19 +808,18 @@ def iodf_norm_forward(norm, r, b=None, gate=None, r_out=None, n=None, stream=Non
                 r_out = torch.empty(r.shape, dtype=r.dtype, device=r.device)
             if _on(r_out, norm, norm.res_dtype, "r_out").shape != r.shape:
                 raise ValueError("r_out must have the shape of r")
-            _, ov = _view(r_out, c, "r_out")
+            ov = _view(r_out, norm, "r_out")[1]
     if gate is not None:
-        _on(gate, norm, norm.uint8, "gate")
         if gate.dim() == 1:
-            if gate.shape[0] != c or (c > 1 and gate.stride(0) != 1):
+            if _on(gate, norm, norm.uint8, "gate").shape[0] != c or (c > 1 and gate.stride(0) != 1):
                 raise ValueError("gate must be [%d] or [%d, %d]" % (c, rows, c))
         else:
-            ldg = _rows_of(gate, rows, c, "gate")
+            ldg = _rows_of(gate, norm, norm.uint8, rows, c, "gate")
     if norm.n_dtype is not None:
         if n is None:
             import torch
             n = torch.empty((rows, c), dtype=norm.n_dtype, device=r.device)
-        ldn = _rows_of(_on(n, norm, norm.n_dtype, "n"), rows, c, "n")
+        ldn = _rows_of(n, norm, norm.n_dtype, rows, c, "n")
     rc = (_lib or load_library()).iodf_norm_forward(norm.handle, rows, r.data_ptr(), rv, _addr(b), ldb, _addr(gate), ldg,
                                                     _addr(r_out), ov, _addr(n), ldn, _layer_stream(stream, norm.device))
     if rc != 0:
