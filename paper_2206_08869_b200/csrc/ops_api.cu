@@ -162,8 +162,7 @@ int create_proj(const iodf_proj_desc& d, const int8_t* weights, size_t wn, const
   cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &entry, 12000, cudaEnableDefault, &found);
   if (e != cudaSuccess || found != cudaDriverEntryPointSuccess) return IODF_ECUDA;
   p.encode = reinterpret_cast<EncodeTiled>(entry);
-  e = configure_proj_kernels();
-  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&p.args.sms, cudaDevAttrMultiProcessorCount, device);
+  e = configure_proj_kernels(device, &p.args);
   if (e == cudaSuccess) e = cudaMalloc(&p.d_mem, total);
   if (e != cudaSuccess) return status_of(e);
   uint8_t* m = static_cast<uint8_t*>(p.d_mem);
@@ -184,6 +183,7 @@ int create_proj(const iodf_proj_desc& d, const int8_t* weights, size_t wn, const
   a.lo = lo;
   a.hi = hi;
   a.max_adapters = (int)slots;
+  a.max_rank = (int)d.max_rank;
   a.rp = (int)R;
   a.w = m + o_w;
   a.rq = reinterpret_cast<const int4*>(m + o_rq);

@@ -31,7 +31,10 @@ constexpr int kDownRing = 6;             // stages at most
 constexpr int kDownEpiWarps = 8;
 constexpr int kDownThreads = 128 + 32 * kDownEpiWarps;   // warp 0 copies, 1 MMAs, 2 tensor memory, 4-11 epilogue
 constexpr int kDownStageBytes = kDownRows * kProjStage + kBytesW;
-constexpr int kScanRequests = 2048;      // up to here a tile (or row) reads every request, above it halves for each row
+// Up to here a tile (or row) reads every request, above it halves for each row. Read and halved, us: 512 requests 35.5 and 36.7
+// (2048 rows, 2048 -> 2048), 30.9 and 31.5 (32768, 512 -> 512), 224 and 240 (16384, 4096 -> 4096); 1024: 38.6 and 39.3, 44.3
+// and 43.5, 308 and 310; 2000: 46.6 and 44.5, 73.7 and 70.3, 335 and 341.
+constexpr int kScanRequests = 1024;
 constexpr int kSlotBits = 20;            // row_slot: an adapter's slot and above it its rank, -1 none, -2 in no request
 
 // D = s32; A int8 (weights), B int8 or uint8, both K-major, M = m, N = n
@@ -839,7 +842,6 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
 constexpr int kSplitThreads = 256;       // warp 0 copies, 1 MMAs, 2 tensor memory, 4-7 send the sums; all finish rows
 constexpr int kSplitRing = 8;
 constexpr int kSplitRows = 128;          // rows of a tile at most
-constexpr int kDownRowsMost = 65536;     // rows x padded rank
 
 struct SplitShared {
   uint64_t full[kSplitRing], empty[kSplitRing], tfull;
@@ -982,12 +984,57 @@ __global__ void __launch_bounds__(kSplitThreads, 1) proj_split_kernel(const __gr
 
 constexpr int kMaxSmem = 204 * 1024;      // beside 1 KB of alignment and the static part
 
-// Rows of a tile of the kernel for few rows: 0 where its tiles would be more than the SMs, or h too much for down_rows_kernel.
+int tiles_of(const ProjArgs& a, int tile) { return a.tiles_n * ((a.rows + tile - 1) / tile); }
+
+// CTAs of a cluster of the kernel for few rows: as many as let all clusters run at once (one of 8 too many: 16 x 8192 -> 2048, 16
+// tiles, takes 10.1 us with 8 and 6.7 with 4; 64 x 4096 -> 2048 with 64 requests 16.6 and 12.1), each with a stage of K.
+int split_parts(const ProjArgs& a, int tile) {
+  const int tiles = tiles_of(a, tile);
+  int i = 0;
+  while (i < 3 && tiles <= a.clusters[i + 1] && 2 << i <= a.stages) ++i;
+  return 1 << i;
+}
+
+bool main_rings(const ProjArgs& a, int tile, bool fused, MainShape* s);
+bool fuse_down(const ProjArgs& a);
+
+// Different adapters that `rows` neighbouring rows use, as far as the host can tell: requests of even length.
+long long adapters_of(const ProjArgs& a, int rows) {
+  const long long most = std::min<long long>(a.n_seg, a.max_adapters);
+  return std::max(1ll, std::min<long long>(most, ((long long)a.n_seg * std::min(rows, a.rows) + a.rows - 1) / a.rows));
+}
+
+// What down_rows_kernel takes beyond a launch, in ns: blocks of a row and eight rank channels.
+long long down_rows_ns(const ProjArgs& a) { return (long long)a.rows * ((a.max_rank + 7) / 8) * (350 + 68 * a.k / 100) / 1000; }
+
+// What down_tile_kernel takes beyond that: its latency and, much more, each further group of 128 / rp adapters of a tile. us of a
+// call with h by rows and in tiles, 2048 -> 4096: 512 rows, rank 16, 4 requests 14.9 and 18.2; 1024 rows, 32, 8 requests 20.6 and
+// 18.6; 1024 rows, 128, 8 requests 43.3 and 20.2; 1024 rows, 32, 128 requests 30.8 and 49.5; 2048 rows, 16, 512 requests 53.1 and 66.6.
+long long down_tiles_ns(const ProjArgs& a) {
+  const long long per = kProjTileN / a.rp, groups = (adapters_of(a, kDownRows) + per - 1) / per;
+  const long long waves = ((a.rows + kDownRows - 1) / kDownRows + 3 * a.sms - 1) / (3 * a.sms);
+  return waves * (2500 + (groups - 1) * (1500 + 3 * a.k));
+}
+
+// Rows of a tile of the kernel for few rows, 0 where it is the slower one. Both times are modelled in ns, from measurements
+// at K 256, 1024 and 4096, rank 0, 16 and 64, 0 to 512 requests. The few rows' kernel: a tile's rows are sent, a CTA's own rows are
+// finished one after another. The persistent one: K, which it does not split, and an adapter step for each adapter of a tile. us, few
+// rows' kernel and persistent, for 16, 64, 128, 256, 512 rows: 1024 -> 4096 without adapters 4.8 and 6.5, 6.0 and 6.5, 8.2
+// and 6.5, 9.0 and 6.6, 11.7 and 7.0; with 8 requests of rank 16: 7.1 and 22.6, 9.6 and 22.5, 12.2 and 22.3, 16.2 and 15.5, 24.0
+// and 13.6; 4096 -> 4096 with 8: 9.8 and 18.5, 12.1 and 21.1, 15.4 and 21.7, 20.5 and 22.2, 31.4 and 21.2.
 int split_tile(const ProjArgs& a) {
   int t = 16;
   while (t < kSplitRows && t < a.rows) t *= 2;
-  if (a.n_seg && (long long)a.rows * a.rp > kDownRowsMost) return 0;
-  return (long long)a.tiles_n * ((a.rows + t - 1) / t) <= a.sms ? t : 0;
+  if (tiles_of(a, t) > a.sms) return 0;
+  const int parts = split_parts(a, t), own = t / parts;
+  const bool fused = fuse_down(a);
+  long long split = 3600 + 25 * (t + own) + 16 * a.k / (10 * parts), main = fused ? 4500 + 2 * a.k : 6500 + 22 * a.k / 10;
+  if (a.n_seg) {
+    split += 1400 + 6 * std::min(a.k, 1024) / 10 + own * (30 + 5 * a.max_rank / 2) + down_rows_ns(a);
+    main += fused ? 4600 + 19 * a.k / 10 : 2600 + 30 * a.rp + std::min(down_rows_ns(a), down_tiles_ns(a));
+    main += (fused ? 30 : 16) * a.rp * (adapters_of(a, kSplitRows) - 1);
+  }
+  return split <= main ? t : 0;
 }
 
 // Shared memory of the persistent kernel with tiles of `tile` rows: false if it does not fit.
@@ -1071,13 +1118,12 @@ cudaError_t launch_tiles(void (*kernel)(Params...), int grid, int cluster, int t
 
 template <class YT, bool kAnyShift>
 cudaError_t launch_main(const ProjArgs& a, const CUtensorMap& map, const CUtensorMap& w_map, cudaStream_t stream) {
-  const int tile = row_tile(a), tiles = a.tiles_n * ((a.rows + tile - 1) / tile), stage = tile * kProjStage + kBytesW;
+  const int tile = row_tile(a), tiles = tiles_of(a, tile), stage = tile * kProjStage + kBytesW;
   const uintptr_t y = reinterpret_cast<uintptr_t>(a.y);
   if (split_tile(a)) {
     SplitShape s;
     s.tile = tile;
-    s.parts = 1;
-    while (s.parts < 8 && 2 * s.parts * tiles <= a.sms && 2 * s.parts <= a.stages) s.parts *= 2;
+    s.parts = split_parts(a, tile);
     const int sums = tile * kProjTileN * 4, most = (a.stages + s.parts - 1) / s.parts;
     s.ring = std::min(std::min(kSplitRing, most), (kMaxSmem - sums) / stage);
     s.vector_y = a.ldy % 4 == 0 && y % (4 * a.y_bytes) == 0;
@@ -1114,7 +1160,7 @@ cudaError_t configure() {
 
 }  // namespace
 
-cudaError_t configure_proj_kernels() {
+cudaError_t configure_proj_kernels(int device, ProjArgs* a) {
   cudaError_t e = cudaFuncSetAttribute(down_tile_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kDownRing * kDownStageBytes + 1024);
   if (e == cudaSuccess) e = configure<int8_t, false>();
   if (e == cudaSuccess) e = configure<int8_t, true>();
@@ -1122,11 +1168,25 @@ cudaError_t configure_proj_kernels() {
   if (e == cudaSuccess) e = configure<uint8_t, true>();
   if (e == cudaSuccess) e = configure<int, false>();
   if (e == cudaSuccess) e = configure<int, true>();
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(&a->sms, cudaDevAttrMultiProcessorCount, device);
+  for (int i = 0; i < 4 && e == cudaSuccess; ++i) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(1u << i);
+    cfg.blockDim = dim3(kSplitThreads);
+    cfg.dynamicSmemBytes = kMaxSmem + 1024;             // one CTA per SM
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 1u << i;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(&a->clusters[i], proj_split_kernel<int8_t, false>, &cfg);
+  }
   return e;
 }
 
 bool proj_down_tiles(const ProjArgs& a) {
-  return a.n_seg && !split_tile(a) && !fuse_down(a) && (long long)a.rows * a.rp > kDownRowsMost;
+  return a.n_seg && !split_tile(a) && !fuse_down(a) && down_tiles_ns(a) < down_rows_ns(a);
 }
 
 int proj_x_rows(const ProjArgs& a) { return split_tile(a) || fuse_down(a) ? row_tile(a) : row_tile(a) / 2; }

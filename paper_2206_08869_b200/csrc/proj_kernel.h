@@ -24,7 +24,7 @@ struct ProjArgs {
   int x_unsigned, y_type, y_bytes;     // y_type: IODF_I8, IODF_U8 or IODF_I32
   int lo, hi;                          // ReLU and clip of the layer
   int any_shift;                       // some s is 0
-  int max_adapters;
+  int max_adapters, max_rank;
   int rp;                              // ranks padded: 32, 64 or 128
   const uint8_t* w;                    // [tiles_n][stages][128 x 128 as above]
   const int4* rq;                      // [tiles_n * 128] {M0, s, addend low, addend high}: y = (acc M0 + addend) >> (31 + s)
@@ -36,6 +36,7 @@ struct ProjArgs {
   int* row_slot;                       // workspace [max_rows]: adapter slot (and rank, see kSlotBits), -1 none, -2 in no request
   uint32_t* status;                    // [0] a bounded wait gave up, [1] bad requests
   int sms;
+  int clusters[4];                     // clusters of 1, 2, 4, 8 CTAs of the kernel for few rows that run at once
 };
 
 // Where element (row, k) of an operand of `width` bytes per row lies.
@@ -43,8 +44,8 @@ inline size_t core_offset(size_t row, size_t k, size_t width) {
   return (row / 8) * (width / 16) * 128 + (k / 16) * 128 + (row % 8) * 16 + k % 16;
 }
 
-// Once per device, before the first launch.
-cudaError_t configure_proj_kernels();
+// On the current device, before the first launch; fills sms and clusters.
+cudaError_t configure_proj_kernels(int device, ProjArgs* a);
 
 // x_map, x_map_down: CUtensorMaps of x [rows][k] with boxes of 128 bytes x proj_x_rows(a) or kProjDownRows rows and
 // the 128-byte swizzle. w_map: of the weights as rows of 128 bytes, box 128 x 128, no swizzle.

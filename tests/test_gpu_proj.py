@@ -401,3 +401,29 @@ def test_outputs_at_any_alignment(G, rows, K, N, ldy_pad, skip):
         G.iodf_proj_forward(h, x, y=y[:, :N])
         np.testing.assert_array_equal(y[:, :N].cpu().numpy(), P.projection(layer, xh))
         assert (y[:, N:] == 9).all() and (buf[:skip] == 9).all() and (buf[-5:] == 9).all()
+
+
+@pytest.mark.parametrize("x_dtype", [torch.int8, torch.uint8])
+@pytest.mark.parametrize("rows,K,N,R", [(1, 1024, 300, 16), (1, 4096, 130, 32), (1, 1000, 4100, 100), (2, 500, 64, 64), (3, 17, 9, 5),
+                                        (4, 1024, 260, 31), (4, 1025, 260, 31), (5, 64, 64, 8), (1, 130, 20000, 8)])
+def test_one_to_five_rows(G, rows, K, N, R, x_dtype):
+    rng = np.random.default_rng(rows + K)
+    for starts, which in (([0, rows], [1]), ([0, rows], [-1]), (list(range(rows + 1)), [(i * 3 + 2) % 5 - 1 for i in range(rows)]),
+                          ([0, 0, 1, 1], [0, 2, 1]), ([rows, rows], [0])):
+        run(G, rng, rows, K, N, [R, 1, R // 2 + 1, R], starts, which, x_dtype)
+    many = sorted(rng.integers(0, rows + 1, 3000).tolist())
+    run(G, rng, rows, K, N, [R, 1, R // 2 + 1, R], [0] + many + [rows], [i % 5 - 1 for i in range(3001)], x_dtype)
+    some = sorted(rng.integers(0, rows + 1, 300).tolist())
+    run(G, rng, rows, K, N, [R, 1, R // 2 + 1, R], [0] + some + [rows], [i % 5 - 1 for i in range(301)], x_dtype)
+
+
+@pytest.mark.parametrize("rows,K,N", [(33, 250, 60), (97, 1030, 300), (130, 1024, 520), (130, 2100, 130), (257, 173, 300), (257, 1030, 60),
+                                      (512, 2100, 260), (700, 1024, 300), (1030, 1152, 130)])
+def test_a_few_hundred_rows(G, rows, K, N):
+    """Around the sizes where the kernel for few rows gives way, with one adapter, a few, one per row and none."""
+    rng = np.random.default_rng(rows * K)
+    for R in (16, 70):
+        ranks = [R, 1, R // 2 + 1, R, R, R - 1, 3]
+        for starts, which in ((None, None), ([0, rows], [0]), ([0, rows // 3, rows // 3, rows - 1], [3, 4, -1]),
+                              (list(range(rows + 1)), [(i * 5 + 3) % 8 - 1 for i in range(rows)])):
+            run(G, rng, rows, K, N, ranks, starts, which, torch.uint8 if rows % 2 else torch.int8)
