@@ -16,7 +16,7 @@
 
 #include "../../include/iodf.h"
 #include "iodf_dev.h"
-#include "ptx.cuh"
+#include "ptx_cluster.cuh"
 
 namespace iodf {
 namespace {
