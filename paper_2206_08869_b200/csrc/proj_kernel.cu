@@ -156,6 +156,8 @@ __device__ __forceinline__ bool first_of_slot(const int* slots, const uint32_t* 
 }
 
 // ---- h for few rows: a block per row and eight rank channels, a quarter of K per warp ----------------------
+// A chain of dependent loads bounds it (request, rank, adapter and x). One row, 1024 -> 4096: 4.8 us without adapters, 5.8 with one of
+// rank 16. Beyond that a block adds about 0.35 ns and 0.68 ps for each channel of K (the fit that down_rows_ns uses).
 template <bool kUnsigned>
 __global__ void __launch_bounds__(128) down_rows_kernel(const ProjArgs a) {
   __shared__ int part[4][8], found;
@@ -198,7 +200,8 @@ __global__ void __launch_bounds__(128) down_rows_kernel(const ProjArgs a) {
 
 // ---- h for many rows: the same product as the main kernel's, M = the rank channels of 128 / rp adapters --------
 // Tiles of 128 rows; each reads x once per group of 128 / rp adapters that its rows use (mostly one group). A block's time is
-// mostly latency (requests, x, sums, h), so up to three blocks share an SM when there are more tiles than SMs.
+// mostly latency (requests, x, sums, h), so up to three blocks share an SM when there are more tiles than SMs. 16384 x 4096, rank 64:
+// some 15 us of the call's 185.
 struct DownShared {
   uint64_t full[kDownRing], empty[kDownRing], dfull, dempty;
   uint32_t abort_flag, tmem;
@@ -327,6 +330,9 @@ __global__ void __launch_bounds__(kDownThreads) down_tile_kernel(const __grid_co
 //   paired (larger K) two CTAs per unit of two output tiles, one each, and one MMA over both (M = 256). Each reads half of
 //          the x tile: a stage is 32 KB of copies and 32 KB of operand reads per SM for 512 clocks of MMAs, where single CTAs
 //          have 48 KB of each, more than the 128 bytes per clock of shared memory. down_tile_kernel computes h before.
+// 65536 x 512 -> 512, uint8, rank 32 (fused): 34.7 us, 1.1 POP/s, bound by the epilogue (15 clocks per 32 outputs and SM quarter, 5 of
+// them the 64-bit product); tensor pipe 27 % active. 16384 x 4096 -> 4096, rank 64 (paired): 171 of the call's 185 us, tensor pipe 85 %
+// active. 32768 x 256 -> 256: 14.3 us, the latency of one unit.
 constexpr int kMaxTile = 256;
 
 constexpr int kMaxX = 16;
@@ -838,7 +844,8 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
 // Where a tile per SM is not reached, the CTAs of a cluster share a tile: each multiplies a part of K, sends its int32
 // sums to the CTA that owns the row (shared memory of the cluster) and finishes RT / S rows itself. There are few
 // rows, mostly of different requests, so the adapters' products are dot products of 16 bytes here: an adapter
-// step of the main kernel costs a tile's time whatever the number of rows that use it.
+// step of the main kernel costs a tile's time whatever the number of rows that use it. Latency bounds it. One row, 1024 -> 4096, rank
+// 16: 6.0 us with h (0.7 TB/s of weights); 48 rows, 2048 -> 2048, an adapter each: 9.7 us.
 constexpr int kSplitThreads = 256;       // warp 0 copies, 1 MMAs, 2 tensor memory, 4-7 send the sums; all finish rows
 constexpr int kSplitRing = 8;
 constexpr int kSplitRows = 128;          // rows of a tile at most
