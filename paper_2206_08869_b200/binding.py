@@ -633,6 +633,18 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
+def _made(make, shape, dtype, device, stream):
+    """An output of a call on `stream` that the caller did not bring, in that stream's order: its memory is nobody's that the
+    current stream still works on, and a fill of it comes before the call's kernels."""
+    import torch
+    if stream is None:
+        return make(shape, dtype=dtype, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)) & ~1, device)   # 1: the legacy default stream, 0 to torch
+    with torch.cuda.stream(stream):
+        return make(shape, dtype=dtype, device=device)
+
+
 class Projection:
     """Handle of an iodf_proj; destroyed when garbage collected."""
 
@@ -691,7 +703,8 @@ def iodf_proj_set_adapter(proj, slot, adapter, stream=None):
 def iodf_proj_forward(proj, x, seg_start=None, seg_adapter=None, y=None, stream=None):
     """x: cuda [rows, c_in] of the handle's type, row stride a multiple of 16 bytes. seg_start int32 [n + 1] and
     seg_adapter int32 [n] on the device: the rows and the slot of each request. Returns y [rows, c_out]; rows in no
-    request keep what y held (zero where y is made here)."""
+    request keep what y held (zero where y is made here). On another stream than the current one, what the call reads has to be
+    ready on that stream; a y made here belongs to it."""
     rows = x.shape[0]
     ldx = _rows_of(x, proj, proj.x_dtype, rows, proj.c_in, "x")
     if rows == 1:
@@ -706,7 +719,7 @@ def iodf_proj_forward(proj, x, seg_start=None, seg_adapter=None, y=None, stream=
         start, which = seg_start.data_ptr(), seg_adapter.data_ptr()
     if y is None:
         import torch
-        y = (torch.zeros if n_seg else torch.empty)((rows, proj.c_out), dtype=proj.y_dtype, device=x.device)
+        y = _made(torch.zeros if n_seg else torch.empty, (rows, proj.c_out), proj.y_dtype, x.device, stream)
     ldy = _rows_of(y, proj, proj.y_dtype, rows, proj.c_out, "y")
     rc = (_lib or load_library()).iodf_proj_forward(proj.handle, x.data_ptr(), ldx, rows, start, which, n_seg, y.data_ptr(), ldy,
                                                     _layer_stream(stream, proj.device))
@@ -790,7 +803,7 @@ def _view(t, norm, what):
 def iodf_norm_forward(norm, r, b=None, gate=None, r_out=None, n=None, stream=None):
     """r: the residual stream, cuda [rows, c] or planes [images, c, pixels] (any outer strides); b [rows, c] the
     block's output; gate uint8 [rows, c] or [c]. Returns (r_out, n), None where the handle has no such part.
-    r_out may be r."""
+    r_out may be r. Outputs made here belong to the call's stream."""
     c = norm.channels
     _on(r, norm, norm.res_dtype, "r")
     rows, rv = _view(r, norm, "r")
@@ -805,7 +818,7 @@ def iodf_norm_forward(norm, r, b=None, gate=None, r_out=None, n=None, stream=Non
         else:
             if r_out is None:
                 import torch
-                r_out = torch.empty(r.shape, dtype=r.dtype, device=r.device)
+                r_out = _made(torch.empty, r.shape, r.dtype, r.device, stream)
             if _on(r_out, norm, norm.res_dtype, "r_out").shape != r.shape:
                 raise ValueError("r_out must have the shape of r")
             ov = _view(r_out, norm, "r_out")[1]
@@ -818,7 +831,7 @@ def iodf_norm_forward(norm, r, b=None, gate=None, r_out=None, n=None, stream=Non
     if norm.n_dtype is not None:
         if n is None:
             import torch
-            n = torch.empty((rows, c), dtype=norm.n_dtype, device=r.device)
+            n = _made(torch.empty, (rows, c), norm.n_dtype, r.device, stream)
         ldn = _rows_of(n, norm, norm.n_dtype, rows, c, "n")
     rc = (_lib or load_library()).iodf_norm_forward(norm.handle, rows, r.data_ptr(), rv, _addr(b), ldb, _addr(gate), ldg,
                                                     _addr(r_out), ov, _addr(n), ldn, _layer_stream(stream, norm.device))
