@@ -2100,6 +2100,7 @@ int iodf_codec_create(const iodf_model* m, const iodf_codec_desc* desc, iodf_cod
   if (e == cudaSuccess) e = cudaMalloc(&c->d_ranges, 4 * ranges.size());
   if (e == cudaSuccess) e = cudaMemcpy(c->d_ranges, ranges.data(), 4 * ranges.size(), cudaMemcpyHostToDevice);
   if (e == cudaSuccess) e = cudaHostAlloc(&c->h_payload, sizeof(uint32_t), cudaHostAllocDefault);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(0);        // the tables may still be on their way to the device
   cudaSetDevice(prev);
   if (e != cudaSuccess) {
     const int rc = e == cudaErrorMemoryAllocation ? IODF_ENOMEM : IODF_ECUDA;

@@ -170,7 +170,8 @@ int create_proj(const iodf_proj_desc& d, const int8_t* weights, size_t wn, const
   if (e == cudaSuccess) e = cudaMemcpy(m + o_rq, rq.data(), 16 * rq.size(), cudaMemcpyHostToDevice);
   if (e == cudaSuccess) e = cudaMemset(m + o_down, 0, o_h - o_down);     // an empty slot adds nothing: all zeros
   if (e == cudaSuccess) e = cudaMemset(m + o_status, 0, 8);
-  if (e == cudaSuccess) e = cudaStreamSynchronize(0);        // the first call may be on a stream that does not wait for it
+  // A copy from pageable memory is only known to have left it: the first call may be on a stream that does not wait for the rest.
+  if (e == cudaSuccess) e = cudaStreamSynchronize(0);
   if (e != cudaSuccess) return status_of(e);
   ProjArgs& a = p.args;
   a.k = (int)K;
@@ -268,6 +269,7 @@ int create_norm(const iodf_norm_desc& d, int device, iodf_norm& nm) {
   if (on.error() != cudaSuccess) return IODF_ECUDA;
   cudaError_t e = cudaMalloc(&nm.d_consts, 4 * tab.size());
   if (e == cudaSuccess) e = cudaMemcpy(nm.d_consts, tab.data(), 4 * tab.size(), cudaMemcpyHostToDevice);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(0);        // the copy may still be on its way, as in create_proj
   if (e != cudaSuccess) return status_of(e);
   NormArgs& a = nm.args;
   a.channels = (int)C;
@@ -508,6 +510,7 @@ int refinement_create(const iodf_refinement& p, int device, uint64_t channels, u
   r.b = m + ob;
   r.start = reinterpret_cast<int32_t*>(m + os);
   e = cudaMemcpy(r.start, start.data(), 4 * start.size(), cudaMemcpyHostToDevice);
+  if (e == cudaSuccess) e = cudaStreamSynchronize(0);        // as in create_proj
   if (e != cudaSuccess) {
     cudaFree(r.mem);
     return status_of(e);

@@ -78,3 +78,19 @@ def test_outputs_made_by_a_norm_on_a_side_stream(G):
     o, n = G.iodf_norm_forward(h, r, b, stream=side)
     torch.cuda.synchronize()
     assert torch.equal(o.cpu(), want[0]) and torch.equal(n.cpu(), want[1])
+
+
+def test_handles_used_at_once_on_a_stream_that_waits_for_nobody(G):
+    rng = np.random.default_rng(3)
+    rows, C = 3, 8192
+    r, b = rng.integers(-900, 900, (rows, C)).astype(np.int16), rng.integers(-60, 60, (rows, C)).astype(np.int8)
+    rt, bt = torch.from_numpy(r).cuda(), torch.from_numpy(b).cuda()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(6):
+        d = _norm_desc(rng, C)
+        o, n = G.iodf_norm_forward(G.iodf_norm_create(d), rt, bt, stream=side)
+        side.synchronize()
+        wo, wn = P.norm_step(d, r, b)
+        np.testing.assert_array_equal(o.cpu().numpy().astype(np.int64), wo)
+        np.testing.assert_array_equal(n.cpu().numpy().astype(np.int64), wn)
