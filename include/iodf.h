@@ -342,7 +342,8 @@ int iodf_decompress_host(iodf_model* m, iodf_codec* c, const uint8_t* in_host, s
                          uint8_t* x_u8_host, void* cuda_stream);
 
 /* Synchronise the stream; IODF_EDATA if any stream was flagged since the last check (their number
- * in *bad_streams, HOST, may be NULL). */
+ * in *bad_streams, HOST, may be NULL), or if a refinement (iodf_codec_set_refinement) met an adapter slot that its
+ * projections do not have; IODF_ETIMEOUT if a bounded wait in a refinement gave up. Clears all of it. */
 int iodf_codec_check(iodf_codec* c, void* cuda_stream, uint32_t* bad_streams);
 
 /*
@@ -411,6 +412,9 @@ size_t iodf_static_scratch_bytes_per_image(const iodf_model* m);
  * returns IODF_ETIMEOUT once, then IODF_OK, and the model works as before.
  */
 int iodf_selftest_timeout(iodf_model* m, uint32_t tries, void* cuda_stream);
+/* The same wait with the status word of a level's refinement, which iodf_codec_check and iodf_compress_host
+ * report. IODF_EINVAL for a level without one. */
+int iodf_codec_selftest_timeout(iodf_codec* c, int level, uint32_t tries, void* cuda_stream);
 
 /*
  * The tensor roofline's denominator, measured (the paper has no counterpart; Sec. 4.1's point is
@@ -569,6 +573,9 @@ int iodf_norm_forward(iodf_norm* nm, int rows, const void* r, const iodf_view* r
  * codec's device; first and last for C/2 channels and IODF_I32, first's n_type = up's x_type, up's y_type (8 bits) =
  * down's x_type, down's c_out = C/2 and y_type = last's block_type, max_rows of both at least the model's max_batch
  * times the level's pixels; IODF_EINVAL otherwise, or for a level without a prior head. Not while a call on the codec is in flight.
+ * What goes wrong in a refinement is the codec's to report, not iodf_proj_check's: iodf_codec_check says so, and
+ * iodf_compress_host returns IODF_ETIMEOUT and no bytes from when a bounded wait gave up until iodf_codec_check has been called
+ * (means that were not all written could not be decoded). A slot outside the projections' is reported and counts as -1.
  *
  * iodf_refine_prior applies a level's refinement to a prior buffer (as iodf_forward or IODF_LEVEL_PRIOR wrote it), in place, for
  * callers that take the steps themselves: before iodf_rans_encode, and between IODF_LEVEL_PRIOR and

@@ -23,7 +23,7 @@ DECLARED_SYMBOLS = ["iodf_create", "iodf_destroy", "iodf_get_layout", "iodf_forw
                     "iodf_level_images_per_cta",
                     "iodf_proj_create", "iodf_proj_destroy", "iodf_proj_set_adapter", "iodf_proj_forward",
                     "iodf_proj_check", "iodf_norm_create", "iodf_norm_destroy", "iodf_norm_forward",
-                    "iodf_codec_set_refinement", "iodf_refine_prior",
+                    "iodf_codec_set_refinement", "iodf_refine_prior", "iodf_codec_selftest_timeout",
                     "iodf_strerror", "iodf_last_cuda_error"]
 
 
@@ -204,6 +204,8 @@ def load_library(path=None):
     L.iodf_codec_set_refinement.argtypes = [vp, C.c_int, C.POINTER(RefinementDesc)]
     L.iodf_refine_prior.restype = C.c_int
     L.iodf_refine_prior.argtypes = [vp, C.c_int, vp, C.c_int, vp]
+    L.iodf_codec_selftest_timeout.restype = C.c_int
+    L.iodf_codec_selftest_timeout.argtypes = [vp, C.c_int, C.c_uint32, vp]
     L.iodf_strerror.restype = C.c_char_p
     L.iodf_strerror.argtypes = [C.c_int]
     L.iodf_last_cuda_error.restype = C.c_int
@@ -870,3 +872,10 @@ def iodf_refine_prior(codec, level, prior, stream=None):
                                           _layer_stream(stream, prior.get_device()))
     if rc != 0:
         raise IodfError(rc, "iodf_refine_prior")
+
+
+def iodf_codec_selftest_timeout(codec, level, tries=3, stream=None):
+    """Make a bounded wait of a level's refinement run out (see include/iodf.h); iodf_codec_check reports it."""
+    rc = load_library().iodf_codec_selftest_timeout(codec.handle, int(level), int(tries), _stream(stream))
+    if rc != 0:
+        raise IodfError(rc, "iodf_codec_selftest_timeout")

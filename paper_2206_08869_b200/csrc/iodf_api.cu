@@ -63,16 +63,18 @@ struct iodf_model {
   int32_t* d_prior = nullptr;
 };
 
+constexpr size_t kCodecWords = 1 + 2 * IODF_MAX_LEVELS;
+
 struct iodf_codec {
   int device = 0;
   int last_cuda = 0;
   uint32_t max_batch = 0;
   uint32_t elems_per_stream = 0;
   uint8_t* d_tables = nullptr;      // R then G
-  uint32_t* d_errors = nullptr;
+  uint32_t* d_errors = nullptr;     // kCodecWords: bad streams, then two words of each level's refinement
   uint32_t* d_sizes = nullptr;      // max_batch record sizes (packing scratch)
   uint32_t* d_ranges = nullptr;     // symbol ranges of the decoder's first look-up
-  uint32_t* h_payload = nullptr;    // pinned: payload size of the batch that is being compressed
+  uint32_t* h_payload = nullptr;    // pinned: payload size of the batch that is being compressed, then a copy of d_errors
   // staging of the host-buffer entry points, allocated by their first call
   uint16_t* d_words = nullptr;
   uint32_t* d_counts = nullptr;
@@ -2094,12 +2096,12 @@ int iodf_codec_create(const iodf_model* m, const iodf_codec_desc* desc, iodf_cod
   if (e == cudaSuccess) e = cudaMalloc(&c->d_tables, rbytes + gbytes);
   if (e == cudaSuccess) e = cudaMemcpy(c->d_tables, desc->inv_scale, rbytes, cudaMemcpyHostToDevice);
   if (e == cudaSuccess) e = cudaMemcpy(c->d_tables + rbytes, desc->sigmoid_table, gbytes, cudaMemcpyHostToDevice);
-  if (e == cudaSuccess) e = cudaMalloc(&c->d_errors, sizeof(uint32_t));
+  if (e == cudaSuccess) e = cudaMalloc(&c->d_errors, kCodecWords * sizeof(uint32_t));
   if (e == cudaSuccess) e = cudaMalloc(&c->d_sizes, sizeof(uint32_t) * (size_t)c->max_batch);
-  if (e == cudaSuccess) e = cudaMemset(c->d_errors, 0, sizeof(uint32_t));
+  if (e == cudaSuccess) e = cudaMemset(c->d_errors, 0, kCodecWords * sizeof(uint32_t));
   if (e == cudaSuccess) e = cudaMalloc(&c->d_ranges, 4 * ranges.size());
   if (e == cudaSuccess) e = cudaMemcpy(c->d_ranges, ranges.data(), 4 * ranges.size(), cudaMemcpyHostToDevice);
-  if (e == cudaSuccess) e = cudaHostAlloc(&c->h_payload, sizeof(uint32_t), cudaHostAllocDefault);
+  if (e == cudaSuccess) e = cudaHostAlloc(&c->h_payload, (1 + kCodecWords) * sizeof(uint32_t), cudaHostAllocDefault);
   if (e == cudaSuccess) e = cudaStreamSynchronize(0);        // the tables may still be on their way to the device
   cudaSetDevice(prev);
   if (e != cudaSuccess) {
@@ -2135,7 +2137,8 @@ int iodf_codec_set_refinement(iodf_codec* c, int level, const iodf_refinement* p
   if (!c || level < 0 || level >= IODF_MAX_LEVELS || !c->level_channels[level]) return IODF_EINVAL;
   Refinement made;
   if (parts) {
-    const int rc = refinement_create(*parts, c->device, c->level_channels[level], c->level_pixels[level], c->max_batch, &made);
+    const int rc = refinement_create(*parts, c->device, c->level_channels[level], c->level_pixels[level], c->max_batch,
+                                     c->d_errors + 1 + 2 * level, &made);
     if (rc) return rc;
   }
   int prev = -1;
@@ -2148,6 +2151,19 @@ int iodf_codec_set_refinement(iodf_codec* c, int level, const iodf_refinement* p
 }
 
 namespace {
+bool refines(const iodf_codec* c) {
+  for (const auto& r : c->refine)
+    if (r.mem) return true;
+  return false;
+}
+
+// words: a copy of d_errors
+bool refinement_gave_up(const uint32_t* words) {
+  for (size_t i = 1; i < kCodecWords; i += 2)
+    if (words[i]) return true;
+  return false;
+}
+
 // The refinements write where the prior buffer of the codec's own model has its levels.
 bool refinements_fit(const iodf_codec* c, const iodf_model* m) {
   for (const auto& r : c->refine)
@@ -2263,7 +2279,13 @@ int iodf_compress_host(iodf_model* m, iodf_codec* c, const uint8_t* x_u8_host, i
   CUC(c, launch_rans_pack(a, c->d_words, c->d_counts, c->d_sizes, c->d_packed, st));
   // the payload size is only known now: read it, then copy exactly header + payload
   CUC(c, cudaMemcpyAsync(c->h_payload, c->d_packed + 4 * (size_t)B, sizeof(uint32_t), cudaMemcpyDeviceToHost, st));
+  const bool refined = refines(c);
+  if (refined) CUC(c, cudaMemcpyAsync(c->h_payload + 1, c->d_errors, kCodecWords * sizeof(uint32_t), cudaMemcpyDeviceToHost, st));
   CUC(c, cudaStreamSynchronize(st));
+  if (refined && refinement_gave_up(c->h_payload + 1)) {      // means that were not all written: what is coded under them cannot be decoded
+    *out_bytes = 0;
+    return IODF_ETIMEOUT;
+  }
   const size_t total = 4 * ((size_t)B + 1) + *c->h_payload;
   *out_bytes = total;
   if (total > out_capacity) return IODF_ELIMIT;
@@ -2313,12 +2335,19 @@ int iodf_decompress_host(iodf_model* m, iodf_codec* c, const uint8_t* in_host, s
 
 int iodf_codec_check(iodf_codec* c, void* cuda_stream, uint32_t* bad_streams) {
   if (!c) return IODF_EINVAL;
-  uint32_t n = 0;
-  CUC(c, cudaMemcpyAsync(&n, c->d_errors, sizeof(n), cudaMemcpyDeviceToHost, (cudaStream_t)cuda_stream));
+  uint32_t words[kCodecWords] = {};
+  CUC(c, cudaMemcpyAsync(words, c->d_errors, sizeof(words), cudaMemcpyDeviceToHost, (cudaStream_t)cuda_stream));
   CUC(c, cudaStreamSynchronize((cudaStream_t)cuda_stream));
-  if (n) CUC(c, cudaMemsetAsync(c->d_errors, 0, sizeof(n), (cudaStream_t)cuda_stream));
-  if (bad_streams) *bad_streams = n;
-  return n ? IODF_EDATA : IODF_OK;
+  const bool any = std::any_of(words, words + kCodecWords, [](uint32_t w) { return w != 0; });
+  if (any) CUC(c, cudaMemsetAsync(c->d_errors, 0, sizeof(words), (cudaStream_t)cuda_stream));
+  if (bad_streams) *bad_streams = words[0];
+  return refinement_gave_up(words) ? IODF_ETIMEOUT : any ? IODF_EDATA : IODF_OK;
+}
+
+int iodf_codec_selftest_timeout(iodf_codec* c, int level, uint32_t tries, void* cuda_stream) {
+  if (!c || level < 0 || level >= IODF_MAX_LEVELS || !c->refine[level].mem || tries < 1 || tries > 100u) return IODF_EINVAL;
+  CUC(c, launch_timeout_probe(c->refine[level].status, tries, (cudaStream_t)cuda_stream));
+  return IODF_OK;
 }
 
 int iodf_forward_timed(iodf_model* m, const uint8_t* x_u8, int B, int32_t* z, int32_t* prior, void* cuda_stream,

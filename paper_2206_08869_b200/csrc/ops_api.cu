@@ -232,6 +232,32 @@ int set_adapter(iodf_proj& p, uint32_t slot, uint32_t rank, const int8_t* down, 
   return status_of(e != cudaSuccess ? e : e2);
 }
 
+// a: the handle's arguments, with a workspace and status words that may be another's
+int proj_forward(const iodf_proj& p, ProjArgs a, const void* x, size_t ldx, int rows, const int32_t* seg_start, const int32_t* seg_adapter,
+                 int n_seg, void* y, size_t ldy, cudaStream_t stream) {
+  if (rows < 0 || (uint32_t)rows > p.max_rows || n_seg < 0) return IODF_EINVAL;
+  if (rows == 0) return IODF_OK;
+  if (!x || !y || (n_seg && (!seg_start || !seg_adapter))) return IODF_EINVAL;
+  if (!aligned(x, 16) || ldx % 16 || ldx < (size_t)a.k || ldx >= (1ull << 40)) return IODF_EINVAL;
+  if (!aligned(y, (size_t)a.y_bytes) || ldy < (size_t)a.n || ldy >= (1ull << 40)) return IODF_EINVAL;
+  if (!aligned(seg_start, 4) || !aligned(seg_adapter, 4)) return IODF_EINVAL;
+  a.x = static_cast<const uint8_t*>(x);
+  a.ldx = (long long)ldx;
+  a.y = y;
+  a.ldy = (long long)ldy;
+  a.seg_start = seg_start;
+  a.seg_adapter = seg_adapter;
+  a.n_seg = n_seg;
+  a.rows = rows;
+  OnDevice on(p.device);
+  if (on.error() != cudaSuccess) return IODF_ECUDA;
+  CUtensorMap map, map_down;
+  if (!tile_map(p, x, (uint64_t)a.k, (uint64_t)rows, ldx, (uint32_t)proj_x_rows(a), true, &map) ||
+      (proj_down_tiles(a) && !tile_map(p, x, (uint64_t)a.k, (uint64_t)rows, ldx, kProjDownRows, true, &map_down)))
+    return IODF_ECUDA;
+  return status_of(launch_proj(a, &map, &map_down, &p.w_map, stream));
+}
+
 bool norm_kind(uint32_t k) { return k == IODF_NORM_RMS || k == IODF_NORM_CENTRED; }
 
 int create_norm(const iodf_norm_desc& d, int device, iodf_norm& nm) {
@@ -365,28 +391,7 @@ int iodf_proj_set_adapter(iodf_proj* p, uint32_t slot, uint32_t rank, const int8
 
 int iodf_proj_forward(iodf_proj* p, const void* x, size_t ldx, int rows, const int32_t* seg_start,
                       const int32_t* seg_adapter, int n_seg, void* y, size_t ldy, void* cuda_stream) {
-  if (!p || rows < 0 || (uint32_t)rows > p->max_rows || n_seg < 0) return IODF_EINVAL;
-  if (rows == 0) return IODF_OK;
-  if (!x || !y || (n_seg && (!seg_start || !seg_adapter))) return IODF_EINVAL;
-  if (!aligned(x, 16) || ldx % 16 || ldx < (size_t)p->args.k || ldx >= (1ull << 40)) return IODF_EINVAL;
-  if (!aligned(y, (size_t)p->args.y_bytes) || ldy < (size_t)p->args.n || ldy >= (1ull << 40)) return IODF_EINVAL;
-  if (!aligned(seg_start, 4) || !aligned(seg_adapter, 4)) return IODF_EINVAL;
-  ProjArgs a = p->args;
-  a.x = static_cast<const uint8_t*>(x);
-  a.ldx = (long long)ldx;
-  a.y = y;
-  a.ldy = (long long)ldy;
-  a.seg_start = seg_start;
-  a.seg_adapter = seg_adapter;
-  a.n_seg = n_seg;
-  a.rows = rows;
-  OnDevice on(p->device);
-  if (on.error() != cudaSuccess) return IODF_ECUDA;
-  CUtensorMap map, map_down;
-  if (!tile_map(*p, x, (uint64_t)a.k, (uint64_t)rows, ldx, (uint32_t)proj_x_rows(a), true, &map) ||
-      (proj_down_tiles(a) && !tile_map(*p, x, (uint64_t)a.k, (uint64_t)rows, ldx, kProjDownRows, true, &map_down)))
-    return IODF_ECUDA;
-  return status_of(launch_proj(a, &map, &map_down, &p->w_map, (cudaStream_t)cuda_stream));
+  return p ? proj_forward(*p, p->args, x, ldx, rows, seg_start, seg_adapter, n_seg, y, ldy, (cudaStream_t)cuda_stream) : IODF_EINVAL;
 }
 
 int iodf_proj_check(iodf_proj* p, void* cuda_stream, uint32_t* bad_requests) {
@@ -473,7 +478,8 @@ int iodf_norm_forward(iodf_norm* nm, int rows, const void* r, const iodf_view* r
 
 namespace iodf {
 
-int refinement_create(const iodf_refinement& p, int device, uint64_t channels, uint64_t pixels, uint32_t max_batch, Refinement* out) {
+int refinement_create(const iodf_refinement& p, int device, uint64_t channels, uint64_t pixels, uint32_t max_batch, uint32_t* status,
+                      Refinement* out) {
   if (!p.first || !p.up || !p.down || !p.last) return IODF_EINVAL;
   const NormArgs &f = p.first->args, &l = p.last->args;
   const ProjArgs &u = p.up->args, &d = p.down->args;
@@ -489,6 +495,7 @@ int refinement_create(const iodf_refinement& p, int device, uint64_t channels, u
   r.parts = p;
   r.channels = channels;
   r.pixels = pixels;
+  r.status = status;
   r.ldn = up_to(channels, 16);
   r.ldu = up_to((size_t)u.n, 16);
   r.ldb = up_to(channels, 16);
@@ -529,9 +536,12 @@ int refinement_run(const Refinement& r, int32_t* mu, uint64_t image_stride, int 
   const iodf_refinement& p = r.parts;
   const int rows = (int)(r.pixels * (uint64_t)batch);
   const iodf_view v{r.pixels, image_stride, r.pixels, 1};
-  auto project = [&](iodf_proj* proj, const void* x, size_t ldx, void* y, size_t ldy) {
+  auto project = [&](const iodf_proj* proj, const void* x, size_t ldx, void* y, size_t ldy) {
     const bool adapters = p.image_adapter && proj->max_adapters;
-    return iodf_proj_forward(proj, x, ldx, rows, adapters ? r.start : nullptr, adapters ? p.image_adapter : nullptr, adapters ? batch : 0, y, ldy, stream);
+    ProjArgs a = proj->args;
+    a.status = r.status;
+    return proj_forward(*proj, a, x, ldx, rows, adapters ? r.start : nullptr, adapters ? p.image_adapter : nullptr, adapters ? batch : 0, y, ldy,
+                        (cudaStream_t)stream);
   };
   int rc = iodf_norm_forward(p.first, rows, mu, &v, nullptr, 0, nullptr, 0, nullptr, nullptr, r.n, r.ldn, stream);
   if (rc == IODF_OK) rc = project(p.up, r.n, r.ldn, r.u, r.ldu);
