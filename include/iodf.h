@@ -569,7 +569,8 @@ int iodf_norm_forward(iodf_norm* nm, int rows, const void* r, const iodf_view* r
  *
  * iodf_codec_set_refinement gives level `level` of the codec a refinement, or none (parts NULL). From then on
  * iodf_compress_host and iodf_decompress_host apply it after the level's prior parameters are known and
- * before its block is coded. The handles, `gate` and `image_adapter` stay the caller's and must outlive it. All on the
+ * before its block is coded. The handles, `gate` and `image_adapter` stay the caller's and must outlive it; the projections are used
+ * with a workspace of the codec's, so codecs of batches in flight may share them (and their owner may call them meanwhile). All on the
  * codec's device; first and last for C/2 channels and IODF_I32, first's n_type = up's x_type, up's y_type (8 bits) =
  * down's x_type, down's c_out = C/2 and y_type = last's block_type, max_rows of both at least the model's max_batch
  * times the level's pixels; IODF_EINVAL otherwise, or for a level without a prior head. Not while a call on the codec is in flight.

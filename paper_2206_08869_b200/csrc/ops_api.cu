@@ -506,7 +506,9 @@ int refinement_create(const iodf_refinement& p, int device, uint64_t channels, u
     return IODF_ENOMEM;
   }
   for (size_t i = 0; i < start.size(); ++i) start[i] = (int32_t)(i * pixels);
-  const size_t on = 0, ou = on + up_to(rows * r.ldn, 256), ob = ou + up_to(rows * r.ldu, 256), os = ob + up_to(rows * r.ldb * (size_t)d.y_bytes, 256);
+  const size_t rank = std::max<size_t>(u.max_adapters ? u.rp : 0, d.max_adapters ? d.rp : 0);
+  const size_t on = 0, ou = on + up_to(rows * r.ldn, 256), ob = ou + up_to(rows * r.ldu, 256), oh = ob + up_to(rows * r.ldb * (size_t)d.y_bytes, 256),
+               oq = oh + up_to(rows * rank, 256), os = oq + up_to(4 * rows, 256);
   OnDevice dev(device);
   if (dev.error() != cudaSuccess) return IODF_ECUDA;
   cudaError_t e = cudaMalloc(&r.mem, os + 4 * start.size());
@@ -515,6 +517,8 @@ int refinement_create(const iodf_refinement& p, int device, uint64_t channels, u
   r.n = m + on;
   r.u = m + ou;
   r.b = m + ob;
+  r.h = reinterpret_cast<int8_t*>(m + oh);
+  r.row_slot = reinterpret_cast<int*>(m + oq);
   r.start = reinterpret_cast<int32_t*>(m + os);
   e = cudaMemcpy(r.start, start.data(), 4 * start.size(), cudaMemcpyHostToDevice);
   if (e == cudaSuccess) e = cudaStreamSynchronize(0);        // as in create_proj
@@ -539,6 +543,8 @@ int refinement_run(const Refinement& r, int32_t* mu, uint64_t image_stride, int 
   auto project = [&](const iodf_proj* proj, const void* x, size_t ldx, void* y, size_t ldy) {
     const bool adapters = p.image_adapter && proj->max_adapters;
     ProjArgs a = proj->args;
+    a.h = r.h;
+    a.row_slot = r.row_slot;
     a.status = r.status;
     return proj_forward(*proj, a, x, ldx, rows, adapters ? r.start : nullptr, adapters ? p.image_adapter : nullptr, adapters ? batch : 0, y, ldy,
                         (cudaStream_t)stream);

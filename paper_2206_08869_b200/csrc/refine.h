@@ -13,6 +13,8 @@ struct Refinement {
   void *mem = nullptr, *n = nullptr, *u = nullptr, *b = nullptr;
   size_t ldn = 0, ldu = 0, ldb = 0;
   int32_t* start = nullptr;               // first row of each image
+  int8_t* h = nullptr;                    // the projections' workspace: theirs serves the calls of their owner
+  int* row_slot = nullptr;
   uint32_t* status = nullptr;             // the codec's words for this level: [0] a bounded wait gave up, [1] bad adapter slots
 };
 

@@ -69,3 +69,40 @@ def test_an_adapter_slot_that_is_not_there_is_reported_by_the_codec(G):
     z, prior = G.iodf_forward(m, torch.from_numpy(x).cuda())
     G.iodf_refine_prior(codec, 1, prior)
     assert _status(G, G.iodf_codec_check, codec) == EDATA
+
+
+def test_codecs_in_flight_share_the_layers_of_their_refinements(G):
+    """Each with batches and customers of its own on a stream of its own, the owner of the projections beside them."""
+    import iodf_synth as S
+    n, B = 3, 64
+    m, codec, blocks, x = _setup(G, 0xD0E0, batch=B)
+    codecs = [codec] + [G.iodf_codec_create(m, S.logistic_codec()) for _ in range(n - 1)]
+    rng = np.random.default_rng(7)
+    b = blocks[1]
+    c, px, off = b.c, b.px, int(m.layout.prior_off[1])
+    lanes = []
+    for c_ in codecs:
+        who = rng.integers(-1, 3, B)
+        _set(G, c_, blocks, torch.from_numpy(who.astype(np.int32)).cuda())
+        z, prior = G.iodf_forward(m, torch.from_numpy(x).cuda())
+        want = prior.clone()
+        mu = prior[:, 0, off:off + c * px].reshape(B, c, px).cpu().numpy()
+        want[:, 0, off:off + c * px] = torch.from_numpy(b.plain(mu, who.tolist()).reshape(B, -1).astype(np.int32)).cuda()
+        lanes.append((c_, torch.cuda.Stream(), [prior.clone() for _ in range(12)], want))
+    own_x = torch.from_numpy(rng.integers(0, 256, (B * px, b.down.c_in + 15)).astype(np.uint8)).cuda()
+    own_x = own_x[:, :b.down.c_in // 16 * 16 + 16].contiguous()[:, :b.down.c_in]
+    starts, slots = torch.tensor([0, B * px // 2, B * px], dtype=torch.int32, device="cuda"), torch.tensor([1, 2], dtype=torch.int32, device="cuda")
+    own_want = G.iodf_proj_forward(b.down, own_x, starts, slots)
+    own = [torch.zeros_like(own_want) for _ in range(12)]
+    mine = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for i in range(12):
+        for c_, stream, priors, _ in lanes:
+            G.iodf_refine_prior(c_, 1, priors[i], stream=stream)
+        G.iodf_proj_forward(b.down, own_x, starts, slots, y=own[i], stream=mine)
+    torch.cuda.synchronize()
+    for c_, _, priors, want in lanes:
+        G.iodf_codec_check(c_)
+        for p in priors:
+            assert torch.equal(p, want)
+    assert all(torch.equal(y, own_want) for y in own)
