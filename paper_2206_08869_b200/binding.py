@@ -278,8 +278,8 @@ class _Marshalled:
 class Model:
     """Handle of an iodf_model; destroyed when garbage collected."""
 
-    def __init__(self, handle, layout, in_shape, max_batch):
-        self.handle, self.layout, self.in_shape, self.max_batch = handle, layout, in_shape, max_batch
+    def __init__(self, handle, layout, in_shape, max_batch, device=0):
+        self.handle, self.layout, self.in_shape, self.max_batch, self.device = handle, layout, in_shape, max_batch, device
         self.d, self.d_fact = int(layout.d), int(layout.d_fact)
 
     def __del__(self):
@@ -300,7 +300,7 @@ def iodf_create(model, max_batch, device=0, marshalled=None, plan=IODF_PLAN_LATE
         raise IodfError(rc, "iodf_create")
     lay = Layout()
     L.iodf_get_layout(out, C.byref(lay))
-    return Model(out, lay, (model["in_c"], model["in_h"], model["in_w"]), int(max_batch))
+    return Model(out, lay, (model["in_c"], model["in_h"], model["in_w"]), int(max_batch), int(device))
 
 
 def iodf_destroy(model):
@@ -868,6 +868,10 @@ def iodf_codec_set_refinement(codec, level, first=None, up=None, down=None, last
 
 def iodf_refine_prior(codec, level, prior, stream=None):
     """Apply a level's refinement to prior int32 [B, 2, d_fact] in place."""
+    import torch
+    _on(prior, codec.model, torch.int32, "prior")
+    if prior.dim() != 3 or prior.shape[1:] != (2, codec.model.d_fact) or not prior.is_contiguous():
+        raise ValueError("prior must be a contiguous [B, 2, %d]" % codec.model.d_fact)
     rc = load_library().iodf_refine_prior(codec.handle, int(level), prior.data_ptr(), prior.shape[0],
                                           _layer_stream(stream, prior.get_device()))
     if rc != 0:
