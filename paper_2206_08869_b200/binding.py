@@ -712,6 +712,8 @@ def iodf_proj_forward(proj, x, seg_start=None, seg_adapter=None, y=None, stream=
     if rows == 1:
         ldx = (ldx + 15) // 16 * 16          # a single row has no stride of its own
     n_seg, start, which = 0, None, None
+    if (seg_start is None) != (seg_adapter is None):
+        raise ValueError("seg_start and seg_adapter are given together or not at all")
     if seg_start is not None:
         n_seg = seg_adapter.numel()
         _on(seg_start, proj, proj.int32, "seg_start")

@@ -65,3 +65,19 @@ def test_refine_prior_takes_the_codecs_prior_buffer_only():
                 good(strides=(800, 200, 1)), good(strides=(400, 1, 2)), good(strides=(0, 200, 1)), torch.zeros((4, 2, 200), dtype=torch.int32)):
         with pytest.raises(ValueError):
             G.iodf_refine_prior(codec, 0, bad)
+
+
+def _projection(c_in=64, c_out=48, max_rows=100):
+    return B.Projection(None, 0, c_in, c_out, max_rows, torch.int8, torch.int8)
+
+
+def test_the_rows_of_requests_need_their_adapters_and_the_adapters_their_rows():
+    p, x, y = _projection(), Tensor((9, 64), torch.int8), Tensor((9, 48), torch.int8)
+    start, which = Tensor((4,), torch.int32), Tensor((3,), torch.int32)
+    with pytest.raises(Called):
+        G.iodf_proj_forward(p, x, start, which, y=y)
+    with pytest.raises(Called):
+        G.iodf_proj_forward(p, x, y=y)
+    for k in (dict(seg_start=start), dict(seg_adapter=which)):
+        with pytest.raises(ValueError):
+            G.iodf_proj_forward(p, x, y=y, **k)
