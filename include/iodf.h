@@ -473,8 +473,9 @@ int iodf_launches_per_call(const iodf_model* m, int inverse);
  *
  * iodf_proj_forward: x DEV [rows] x c_in elements, row stride ldx >= c_in bytes, a multiple of 16, x
  * 16-byte aligned; y DEV [rows] x c_out elements of y_type, row stride ldy >= c_out elements, aligned to its
- * element. seg_start DEV int32 [n_seg + 1], seg_adapter DEV int32 [n_seg]; with n_seg = 0 (both may be NULL) every row is
- * computed without an adapter. Rows in no request are not written. 0 <= rows <= max_rows. Allocates nothing,
+ * element. seg_start DEV int32 [n_seg + 1], seg_adapter DEV int32 [n_seg]; n_seg = 0 (both may be NULL) is a call
+ * without requests, every row is computed without an adapter (a batch that has run out of requests is not to be
+ * handed over so). Rows in no request are not written. 0 <= rows <= max_rows. Allocates nothing,
  * may be captured; the handle's workspace serves one call at a time (also for replayed graphs). Requests whose
  * bounds decrease or leave 0..rows, and slots outside -1..max_adapters-1, are counted on the device and
  * reported by iodf_proj_check (IODF_EDATA). Such a slot counts as -1; with bad bounds any row may be left

@@ -705,7 +705,8 @@ def iodf_proj_set_adapter(proj, slot, adapter, stream=None):
 def iodf_proj_forward(proj, x, seg_start=None, seg_adapter=None, y=None, stream=None):
     """x: cuda [rows, c_in] of the handle's type, row stride a multiple of 16 bytes. seg_start int32 [n + 1] and
     seg_adapter int32 [n] on the device: the rows and the slot of each request. Returns y [rows, c_out]; rows in no
-    request keep what y held (zero where y is made here). On another stream than the current one, what the call reads has to be
+    request keep what y held (zero where y is made here), with n = 0 all of them. Without requests (both None) every row is
+    computed without an adapter. On another stream than the current one, what the call reads has to be
     ready on that stream; a y made here belongs to it."""
     rows = x.shape[0]
     ldx = _rows_of(x, proj, proj.x_dtype, rows, proj.c_in, "x")
@@ -723,8 +724,10 @@ def iodf_proj_forward(proj, x, seg_start=None, seg_adapter=None, y=None, stream=
         start, which = seg_start.data_ptr(), seg_adapter.data_ptr()
     if y is None:
         import torch
-        y = _made(torch.zeros if n_seg else torch.empty, (rows, proj.c_out), proj.y_dtype, x.device, stream)
+        y = _made(torch.empty if seg_start is None else torch.zeros, (rows, proj.c_out), proj.y_dtype, x.device, stream)
     ldy = _rows_of(y, proj, proj.y_dtype, rows, proj.c_out, "y")
+    if start is not None and not n_seg:
+        return y                             # no request owns a row; to the library n_seg = 0 is a call without requests
     rc = (_lib or load_library()).iodf_proj_forward(proj.handle, x.data_ptr(), ldx, rows, start, which, n_seg, y.data_ptr(), ldy,
                                                     _layer_stream(stream, proj.device))
     if rc != 0:

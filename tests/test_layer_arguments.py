@@ -81,3 +81,17 @@ def test_the_rows_of_requests_need_their_adapters_and_the_adapters_their_rows():
     for k in (dict(seg_start=start), dict(seg_adapter=which)):
         with pytest.raises(ValueError):
             G.iodf_proj_forward(p, x, y=y, **k)
+
+
+def test_no_requests_left_own_no_rows(monkeypatch):
+    p, x, y = _projection(), Tensor((9, 64), torch.int8), Tensor((9, 48), torch.int8)
+    none = Tensor((1,), torch.int32), Tensor((0,), torch.int32)
+    assert G.iodf_proj_forward(p, x, *none, y=y) is y
+    made = []
+    monkeypatch.setattr(B, "_made", lambda make, shape, dtype, device, stream: made.append(make) or Tensor(shape, dtype))
+    G.iodf_proj_forward(p, x, *none)
+    assert made == [torch.zeros]
+    with pytest.raises(ValueError):
+        G.iodf_proj_forward(p, x, *none, y=Tensor((8, 48), torch.int8))
+    with pytest.raises(ValueError):
+        G.iodf_proj_forward(p, x, Tensor((0,), torch.int32), none[1], y=y)
