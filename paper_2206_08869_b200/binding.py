@@ -598,6 +598,29 @@ def iodf_level_images_per_cta(model, level):
 # ---- single integer layers ---------------------------------------------------------------------------------
 IODF_I8, IODF_U8, IODF_I16, IODF_I32 = 1, 2, 3, 4
 IODF_NORM_RMS, IODF_NORM_CENTRED = 1, 2
+_MOST = 2 ** 31 - 1                    # rows and requests of a call
+
+
+def _fits(value, ctype, what):
+    """The value as the library's integer type takes it; ctypes would cut it off."""
+    value = int(value)
+    if ctype(value).value != value:
+        raise ValueError("%s = %d is out of range" % (what, value))
+    return value
+
+
+def _record(cls, *values):
+    """A descriptor of the library, every integer in its range."""
+    return cls(*[_fits(v, t, name) if t in (C.c_uint32, C.c_int32, C.c_uint64) else v for (name, t), v in zip(cls._fields_, values)])
+
+
+def _integers(a, dtype, what):
+    """The array's values in another integer type, contiguous; a value that the type does not have is refused."""
+    a = np.asarray(a)
+    out = np.ascontiguousarray(a, dtype=dtype)
+    if a.dtype != out.dtype and not np.array_equal(a, out):
+        raise ValueError("%s holds values that are not %s" % (what, out.dtype))
+    return out
 
 
 def _type_code(dtype, allowed):
@@ -671,15 +694,18 @@ def iodf_proj_create(layer, max_rows, max_adapters=0, max_rank=0, x_dtype=None, 
     x_dtype, y_dtype = x_dtype or torch.int8, y_dtype or torch.int32
     if layer.get("gate") is not None:
         raise ValueError("gated (masked-dense) layers must be compacted before deployment")
-    w = np.ascontiguousarray(layer["w"], dtype=np.int8).reshape(-1)
-    par = np.concatenate([np.asarray(layer[k], dtype=np.int32).reshape(-1) for k in ("bias", "m0", "s")])
+    w = _integers(layer["w"], np.int8, "w").reshape(-1)
+    par = [_integers(layer[k], np.int32, k).reshape(-1) for k in ("bias", "m0", "s")]
+    if any(a.size != layer["c_out"] for a in par) or w.size > layer["k"] ** 2 * layer["c_in"] * layer["c_out"]:
+        raise ValueError("w, bias, m0 and s do not match the layer's k, c_in and c_out")
+    par = np.concatenate(par)
     cl = layer["clamp"]
-    lay = LayerDesc(layer["k"], layer["c_in"], layer["c_out"], int(layer["relu"]), int(cl is not None),
-                    cl[0] if cl else 0, cl[1] if cl else 0, 0, 0)
-    desc = ProjDesc(IODF_ABI_VERSION, lay, _type_code(x_dtype, (IODF_I8, IODF_U8)),
-                    _type_code(y_dtype, (IODF_I8, IODF_U8, IODF_I32)), int(max_rows), int(max_adapters), int(max_rank))
+    lay = _record(LayerDesc, layer["k"], layer["c_in"], layer["c_out"], int(layer["relu"]), int(cl is not None),
+                  cl[0] if cl else 0, cl[1] if cl else 0, 0, 0)
+    desc = _record(ProjDesc, IODF_ABI_VERSION, lay, _type_code(x_dtype, (IODF_I8, IODF_U8)),
+                   _type_code(y_dtype, (IODF_I8, IODF_U8, IODF_I32)), max_rows, max_adapters, max_rank)
     out = C.c_void_p()
-    rc = L.iodf_proj_create(C.byref(desc), w.ctypes.data, w.size, par.ctypes.data, par.size, int(device), C.byref(out))
+    rc = L.iodf_proj_create(C.byref(desc), w.ctypes.data, w.size, par.ctypes.data, par.size, _fits(device, C.c_int, "device"), C.byref(out))
     if rc != 0:
         raise IodfError(rc, "iodf_proj_create")
     return Projection(out, int(device), int(layer["c_in"]), int(layer["c_out"]), int(max_rows), x_dtype, y_dtype)
@@ -690,13 +716,13 @@ def iodf_proj_set_adapter(proj, slot, adapter, stream=None):
     rank = int(adapter["rank"]) if adapter else 0
     down = rq = up = None
     if rank:
-        down = np.ascontiguousarray(adapter["down"], dtype=np.int8)
-        up = np.ascontiguousarray(adapter["up"], dtype=np.int8)
-        rq = np.concatenate([np.asarray(adapter[k], dtype=np.int32).reshape(-1) for k in ("m0", "s")])
-        if down.shape != (rank, proj.c_in) or up.shape != (proj.c_out, rank) or rq.size != 2 * rank:
+        down, up = _integers(adapter["down"], np.int8, "down"), _integers(adapter["up"], np.int8, "up")
+        rq = [_integers(adapter[k], np.int32, k).reshape(-1) for k in ("m0", "s")]
+        if down.shape != (rank, proj.c_in) or up.shape != (proj.c_out, rank) or any(a.size != rank for a in rq):
             raise ValueError("adapter arrays do not match its rank and the layer's channels")
+        rq = np.concatenate(rq)
     ptr = [None if a is None else a.ctypes.data for a in (down, rq, up)]
-    rc = load_library().iodf_proj_set_adapter(proj.handle, int(slot), rank, ptr[0], ptr[1], ptr[2],
+    rc = load_library().iodf_proj_set_adapter(proj.handle, _fits(slot, C.c_uint32, "slot"), _fits(rank, C.c_uint32, "rank"), ptr[0], ptr[1], ptr[2],
                                               _layer_stream(stream, proj.device))
     if rc != 0:
         raise IodfError(rc, "iodf_proj_set_adapter")
@@ -726,6 +752,8 @@ def iodf_proj_forward(proj, x, seg_start=None, seg_adapter=None, y=None, stream=
         import torch
         y = _made(torch.empty if seg_start is None else torch.zeros, (rows, proj.c_out), proj.y_dtype, x.device, stream)
     ldy = _rows_of(y, proj, proj.y_dtype, rows, proj.c_out, "y")
+    if rows > _MOST or n_seg > _MOST:
+        raise ValueError("%d rows of %d requests are out of range" % (rows, n_seg))
     if start is not None and not n_seg:
         return y                             # no request owns a row; to the library n_seg = 0 is a call without requests
     rc = (_lib or load_library()).iodf_proj_forward(proj.handle, x.data_ptr(), ldx, rows, start, which, n_seg, y.data_ptr(), ldy,
@@ -769,21 +797,21 @@ def iodf_norm_create(desc, device=0):
     tabs = {}
     for name, part, key in (("mult", post, "mult"), ("n_mult", pre, "mult"), ("n_bias", pre, "bias")):
         if part is not None:
-            tabs[name] = np.ascontiguousarray(part[key], dtype=np.int32).reshape(-1)
+            tabs[name] = _integers(part[key], np.int32, name).reshape(-1)
             if tabs[name].size != c:
                 raise ValueError("%s must hold one value per channel" % name)
     ptr = {k: tabs[k].ctypes.data if k in tabs else None for k in ("mult", "n_mult", "n_bias")}
     block, (lo, hi) = desc.get("block_dtype"), desc.get("res_range", (0, 0))
     n_dtype = pre["dtype"] if pre else None
-    d = NormDesc(IODF_ABI_VERSION, c, _type_code(desc["res_dtype"], (IODF_I16, IODF_I32)),
-                 _type_code(block, (IODF_I8, IODF_I32)) if block else 0,
-                 _NORMS[post["norm"]] if post else 0, _NORMS[pre["norm"]] if pre else 0,
-                 _type_code(n_dtype, (IODF_I8, IODF_U8)) if pre else 0,
-                 int(post["shift"]) if post else 0, int(pre["shift"]) if pre else 0, int(lo), int(hi),
-                 int(pre["clamp"][0]) if pre else 0, int(pre["clamp"][1]) if pre else 0, int(desc.get("eps", 0)),
-                 ptr["mult"], ptr["n_mult"], ptr["n_bias"])
+    d = _record(NormDesc, IODF_ABI_VERSION, c, _type_code(desc["res_dtype"], (IODF_I16, IODF_I32)),
+                _type_code(block, (IODF_I8, IODF_I32)) if block else 0,
+                _NORMS[post["norm"]] if post else 0, _NORMS[pre["norm"]] if pre else 0,
+                _type_code(n_dtype, (IODF_I8, IODF_U8)) if pre else 0,
+                post["shift"] if post else 0, pre["shift"] if pre else 0, lo, hi,
+                pre["clamp"][0] if pre else 0, pre["clamp"][1] if pre else 0, desc.get("eps", 0),
+                ptr["mult"], ptr["n_mult"], ptr["n_bias"])
     out = C.c_void_p()
-    rc = L.iodf_norm_create(C.byref(d), int(device), C.byref(out))
+    rc = L.iodf_norm_create(C.byref(d), _fits(device, C.c_int, "device"), C.byref(out))
     if rc != 0:
         raise IodfError(rc, "iodf_norm_create")
     return Norm(out, int(device), c, desc["res_dtype"], block, n_dtype)
@@ -840,6 +868,8 @@ def iodf_norm_forward(norm, r, b=None, gate=None, r_out=None, n=None, stream=Non
             import torch
             n = _made(torch.empty, (rows, c), norm.n_dtype, r.device, stream)
         ldn = _rows_of(n, norm, norm.n_dtype, rows, c, "n")
+    if rows > _MOST:
+        raise ValueError("%d rows are out of range" % rows)
     rc = (_lib or load_library()).iodf_norm_forward(norm.handle, rows, r.data_ptr(), rv, _addr(b), ldb, _addr(gate), ldg,
                                                     _addr(r_out), ov, _addr(n), ldn, _layer_stream(stream, norm.device))
     if rc != 0:
@@ -863,7 +893,7 @@ def iodf_codec_set_refinement(codec, level, first=None, up=None, down=None, last
                                           or not image_adapter.is_contiguous()):
             raise ValueError("image_adapter must hold %d contiguous values" % codec.model.max_batch)
         desc = RefinementDesc(first.handle, up.handle, down.handle, last.handle, _addr(gate), _addr(image_adapter))
-    rc = load_library().iodf_codec_set_refinement(codec.handle, int(level), C.byref(desc) if desc is not None else None)
+    rc = load_library().iodf_codec_set_refinement(codec.handle, _fits(level, C.c_int, "level"), C.byref(desc) if desc is not None else None)
     if rc != 0:
         raise IodfError(rc, "iodf_codec_set_refinement")
     if not hasattr(codec, "refinements"):
@@ -877,7 +907,7 @@ def iodf_refine_prior(codec, level, prior, stream=None):
     _on(prior, codec.model, torch.int32, "prior")
     if prior.dim() != 3 or prior.shape[1:] != (2, codec.model.d_fact) or not prior.is_contiguous():
         raise ValueError("prior must be a contiguous [B, 2, %d]" % codec.model.d_fact)
-    rc = load_library().iodf_refine_prior(codec.handle, int(level), prior.data_ptr(), prior.shape[0],
+    rc = load_library().iodf_refine_prior(codec.handle, _fits(level, C.c_int, "level"), prior.data_ptr(), _fits(prior.shape[0], C.c_int, "B"),
                                           _layer_stream(stream, prior.get_device()))
     if rc != 0:
         raise IodfError(rc, "iodf_refine_prior")
@@ -885,6 +915,6 @@ def iodf_refine_prior(codec, level, prior, stream=None):
 
 def iodf_codec_selftest_timeout(codec, level, tries=3, stream=None):
     """Make a bounded wait of a level's refinement run out (see include/iodf.h); iodf_codec_check reports it."""
-    rc = load_library().iodf_codec_selftest_timeout(codec.handle, int(level), int(tries), _stream(stream))
+    rc = load_library().iodf_codec_selftest_timeout(codec.handle, _fits(level, C.c_int, "level"), _fits(tries, C.c_uint32, "tries"), _stream(stream))
     if rc != 0:
         raise IodfError(rc, "iodf_codec_selftest_timeout")

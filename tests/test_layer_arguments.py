@@ -95,3 +95,66 @@ def test_no_requests_left_own_no_rows(monkeypatch):
         G.iodf_proj_forward(p, x, *none, y=Tensor((8, 48), torch.int8))
     with pytest.raises(ValueError):
         G.iodf_proj_forward(p, x, Tensor((0,), torch.int32), none[1], y=y)
+
+
+WRAP = 2 ** 32
+
+
+def _layer(K=8, N=4, **kw):
+    return {"k": 1, "c_in": K, "c_out": N, "w": np.ones((N, K), np.int8), "bias": np.zeros(N, np.int32), "m0": np.full(N, 1 << 30, np.int32),
+            "s": np.zeros(N, np.int32), "relu": False, "clamp": (-128, 127), **kw}
+
+
+def _desc(**kw):
+    one = np.full(4, 1 << 30, np.int32)
+    d = {"c": 4, "res_dtype": torch.int16, "block_dtype": torch.int8, "eps": 1, "res_range": (-32768, 32767),
+         "post": {"norm": "rms", "mult": one, "shift": 8},
+         "pre": {"norm": "rms", "mult": one, "shift": 8, "bias": np.zeros(4, np.int32), "clamp": (-128, 127), "dtype": torch.int8}}
+    return {k: dict(v, **kw[k]) if isinstance(kw.get(k), dict) else kw.get(k, v) for k, v in d.items()}
+
+
+def _wrapped(n, value=5 + WRAP):
+    a = np.ones(n, np.int64)
+    a[-1] = value
+    return a
+
+
+def test_numbers_that_the_librarys_types_do_not_hold():
+    codec, p = _codec(), _projection()
+    norm = B.Norm(None, 0, 12, torch.int16, None, torch.int8)
+    ad = {"rank": 2, "down": np.ones((2, 64), np.int8), "m0": np.full(2, 1 << 30), "s": np.zeros(2, int), "up": np.ones((48, 2), np.int8)}
+    fine = [lambda: G.iodf_proj_create(_layer(), 4), lambda: G.iodf_proj_create(_layer(w=np.ones((4, 8), np.int64), clamp=(-2 ** 31, 2 ** 31 - 1)), 4),
+            lambda: G.iodf_norm_create(_desc()), lambda: G.iodf_proj_set_adapter(p, 0, ad), lambda: G.iodf_proj_set_adapter(p, 0, None),
+            lambda: G.iodf_norm_create(_desc(eps=2 ** 64 - 1)),
+            lambda: G.iodf_norm_forward(norm, Tensor((2 ** 31 - 1, 12), torch.int16), n=Tensor((2 ** 31 - 1, 12), torch.int8)),
+            lambda: G.iodf_proj_forward(p, Tensor((2 ** 31 - 1, 64), torch.int8), y=Tensor((2 ** 31 - 1, 48), torch.int8))]
+    for f in fine:
+        with pytest.raises(Called):
+            f()
+    bad = [lambda: G.iodf_proj_create(_layer(), 4 + WRAP), lambda: G.iodf_proj_create(_layer(), -1), lambda: G.iodf_proj_create(_layer(), 4, WRAP, 1),
+           lambda: G.iodf_proj_create(_layer(), 4, 1, 1 + WRAP), lambda: G.iodf_proj_create(_layer(), 4, device=WRAP),
+           lambda: G.iodf_proj_create(_layer(clamp=(-128 - WRAP, 127)), 4), lambda: G.iodf_proj_create(_layer(clamp=(0, 127 + WRAP)), 4),
+           lambda: G.iodf_proj_create(_layer(w=np.full((4, 8), 129)), 4), lambda: G.iodf_proj_create(_layer(bias=_wrapped(4)), 4),
+           lambda: G.iodf_proj_create(_layer(m0=_wrapped(4, (1 << 30) + WRAP)), 4), lambda: G.iodf_proj_create(_layer(s=[0, 0, 0, 0.5]), 4),
+           lambda: G.iodf_proj_create(_layer(bias=np.zeros(5, np.int32)), 4), lambda: G.iodf_proj_create(_layer(w=np.ones((4, 9), np.int8)), 4),
+           lambda: G.iodf_proj_create(_layer(c_in=8 + WRAP), 4),
+           lambda: G.iodf_proj_set_adapter(p, WRAP, ad), lambda: G.iodf_proj_set_adapter(p, -1, ad),
+           lambda: G.iodf_proj_set_adapter(p, 0, dict(ad, up=np.full((48, 2), 200))), lambda: G.iodf_proj_set_adapter(p, 0, dict(ad, m0=_wrapped(2))),
+           lambda: G.iodf_proj_set_adapter(p, 0, dict(ad, m0=np.full(3, 1 << 30), s=np.zeros(1, int))),
+           lambda: G.iodf_norm_create(_desc(eps=1 + 2 ** 64)), lambda: G.iodf_norm_create(_desc(eps=-1)), lambda: G.iodf_norm_create(_desc(c=4 + WRAP)),
+           lambda: G.iodf_norm_create(_desc(res_range=(-WRAP, 5))), lambda: G.iodf_norm_create(_desc(post={"shift": 8 + WRAP})),
+           lambda: G.iodf_norm_create(_desc(pre={"clamp": (-128, 127 + WRAP)})), lambda: G.iodf_norm_create(_desc(post={"mult": _wrapped(4)})),
+           lambda: G.iodf_norm_create(_desc(pre={"bias": _wrapped(4)})), lambda: G.iodf_norm_create(_desc(), device=WRAP),
+           lambda: G.iodf_norm_forward(norm, Tensor((WRAP + 5, 12), torch.int16), n=Tensor((WRAP + 5, 12), torch.int8)),
+           lambda: G.iodf_proj_forward(p, Tensor((WRAP + 5, 64), torch.int8), y=Tensor((WRAP + 5, 48), torch.int8)),
+           lambda: G.iodf_proj_forward(p, Tensor((5, 64), torch.int8), Tensor((WRAP + 2,), torch.int32), Tensor((WRAP + 1,), torch.int32),
+                                       y=Tensor((5, 48), torch.int8)),
+           lambda: G.iodf_codec_set_refinement(codec, WRAP), lambda: G.iodf_codec_selftest_timeout(codec, 0, 3 + WRAP),
+           lambda: G.iodf_refine_prior(codec, WRAP, Tensor((4, 2, 200), torch.int32, 1)),
+           lambda: G.iodf_refine_prior(codec, 0, Tensor((WRAP + 4, 2, 200), torch.int32, 1))]
+    for i, f in enumerate(bad):
+        try:
+            with pytest.raises(ValueError):
+                f()
+        except Called:
+            pytest.fail("case %d was not refused" % i)
