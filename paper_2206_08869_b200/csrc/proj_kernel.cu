@@ -439,7 +439,6 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
     sh.abort_flag = 0;
   }
   if (kPair) {                                          // both CTAs' barriers are there before either arrives on the other's
-    __syncwarp();
     ptx::cluster_arrive();
     ptx::cluster_wait();
   }
@@ -805,21 +804,25 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
                 if (rows32 >> (first + i) & 1) *reinterpret_cast<uint32_t*>(p) = w[i];
                 if (rows32 >> (16 + first + i) & 1) *reinterpret_cast<uint32_t*>(p + 16 * a.ldy) = w[4 + i];
               }
+              __syncwarp();                             // these stores may have parted the lanes; the loads of the next step are the whole warp's
             }
-          } else if (n < a.n) {
-            YT* p = y;
-            if (sizeof(YT) == 1) {
+          } else {
+            if (n < a.n) {
+              YT* p = y;
+              if (sizeof(YT) == 1) {
 #pragma unroll
-              for (int e = 0; e < 32; ++e) o[e] = min(max(o[e], YT(-1) < YT(0) ? -128 : 0), YT(-1) < YT(0) ? 127 : 255);
+                for (int e = 0; e < 32; ++e) o[e] = min(max(o[e], YT(-1) < YT(0) ? -128 : 0), YT(-1) < YT(0) ? 127 : 255);
+              }
+              if (rows32 == 0xFFFFFFFFu) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e, p += a.ldy) *p = (YT)o[e];
+              } else {
+#pragma unroll
+                for (int e = 0; e < 32; ++e, p += a.ldy)
+                  if (rows32 >> e & 1) *p = (YT)o[e];
+              }
             }
-            if (rows32 == 0xFFFFFFFFu) {
-#pragma unroll
-              for (int e = 0; e < 32; ++e, p += a.ldy) *p = (YT)o[e];
-            } else {
-#pragma unroll
-              for (int e = 0; e < 32; ++e, p += a.ldy)
-                if (rows32 >> e & 1) *p = (YT)o[e];
-            }
+            __syncwarp();
           }
         }
         done(&sh.tempty[ti & 1]);
@@ -935,12 +938,10 @@ __global__ void __launch_bounds__(kSplitThreads, 1) proj_split_kernel(const __gr
       ptx::tc_fence_before();
     }
   }
-  __syncwarp();
   if (warp < 4) ptx::cluster_wait();
   ptx::tc_fence_before();
   __syncthreads();
   if (warp == 2) ptx::tmem_dealloc(tmem, tmem_cols);
-  __syncwarp();
   ptx::cluster_arrive();
   const int n = tn * kProjTileN + lane * 4;                   // from here on a thread owns four neighbouring channels
   int4 rq[4];

@@ -32,10 +32,13 @@ __device__ __forceinline__ uint32_t cluster_rank() {
   return r;
 }
 // Both by all threads of all CTAs of the cluster; shared memory written before the arrival is visible to the cluster after the wait.
+// `.aligned` wants the whole warp at the instruction: lanes that parted before meet here.
 __device__ __forceinline__ void cluster_arrive() {
+  __syncwarp();
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void cluster_wait() {
+  __syncwarp();
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // Address of the same shared-memory word in CTA `rank` of the cluster, and a store to it.

@@ -1,0 +1,30 @@
+"""What the kernels of the single layers rely on, read from their source: conditions of the instructions that no run can be made to miss."""
+import os
+import re
+
+CSRC = os.path.join(os.path.dirname(os.path.abspath(__file__)), "..", "paper_2206_08869_b200", "csrc")
+
+
+def _text(name):
+    with open(os.path.join(CSRC, name)) as f:
+        return re.sub(r"//[^\n]*", "", f.read())
+
+
+def test_a_warp_is_whole_where_an_instruction_wants_it_whole():
+    """.aligned: every lane of the warp executes the same instruction. After code whose lanes may part (one thread sets barriers up, lanes
+    store the rows that are theirs) only __syncwarp brings them together for certain."""
+    functions = re.findall(r"__device__ __forceinline__ \w+ (cluster_\w+)\([^)]*\) \{\n(.*?)\n\}", _text("ptx_cluster.cuh"), flags=re.S)
+    barriers = [(name, body) for name, body in functions if ".aligned" in body]
+    assert len(barriers) == 2
+    for name, body in barriers:
+        assert body.strip().startswith("__syncwarp();"), name
+    text = _text("proj_kernel.cu")
+    loop = re.search(r"for \(int c = 0; c < cols; c \+= 32.*?done\(&sh\.tempty", text, flags=re.S).group(0)
+    loop = loop[loop.index("transpose4(t1"):]                  # behind the loads and what every lane does
+    parts = [m.start() for m in re.finditer(r"if \(rows32 >> \(|if \(n < a\.n\)", loop)]
+    assert len(parts) == 3
+    for at in parts:
+        assert "__syncwarp();" in loop[at:], loop[at:]
+    assert "__syncwarp();" in loop[parts[0]:parts[-1]]
+    # no barrier of a cluster beside the two wrappers
+    assert "barrier.cluster" not in text
