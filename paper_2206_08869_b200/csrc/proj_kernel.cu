@@ -58,6 +58,14 @@ struct Turn {
   }
 };
 
+// Waits until the MMAs have given every slot of a ring back. Nobody else waits for the last of these arrivals, and one that came after
+// the CTA had left (or, of a pair, the other CTA's) would find another CTA's shared memory. turn: of the copy that would be next.
+__device__ __forceinline__ bool given_back(volatile uint32_t* abort_flag, uint32_t* status, uint64_t* empty, Turn turn, int size) {
+  for (int i = 0; i < size; ++i, turn.next(size))
+    if (!ptx::quick_wait(abort_flag, status, &empty[turn.slot], turn.phase ^ 1, kSpinLimit)) return false;
+  return true;
+}
+
 template <bool kPair>
 __device__ __forceinline__ void mma(uint32_t d, uint32_t alo, uint32_t ahi, uint32_t blo, uint32_t bhi, uint32_t id, uint32_t acc) {
   if (kPair) ptx::umma_i8_hl_pair(d, alo, ahi, blo, bhi, id, acc);
@@ -274,6 +282,7 @@ __global__ void __launch_bounds__(kDownThreads) down_tile_kernel(const __grid_co
                         a.down + ((size_t)sh.list[g * per + i] * a.stages + ks) * a.rp * kProjStage, (uint32_t)(a.rp * kProjStage), bar);
       }
     }
+    given_back(abort_flag, a.status, sh.empty, turn, ring);
   } else if (warp == 1 && ptx::elect_one()) {
     const uint32_t id = idesc(kDownRows, a.x_unsigned);
     Turn turn;
@@ -476,6 +485,8 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         ptx::mbar_expect_tx(bar, xbytes);
         ptx::tile_g2s(base + s * xbytes, &xmap, ks * kProjStage, u / shp.chunks * RT, bar);
       }
+    for (int i = 0; i < sets; ++i)                      // as given_back
+      for (int ks = 0; ok && ks < a.stages; ++ks) ok = wait(&sh.xempty[xslot0(ui + i) + ks], xphase(ui + i) ^ 1);
   } else if (warp == 0 && ptx::elect_one()) {
     Turn turn;
     int ui = 0;
@@ -512,6 +523,7 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
           }
         }
     }
+    if (ok) given_back(abort_flag, a.status, sh.wempty, turn, shp.wring);
   } else if (warp == 1 && part == 1 && ptx::elect_one()) {
     // the second CTA of a pair tells the first, which issues the MMAs, that its half of an adapter step is laid out
     int ai = 0;
@@ -702,6 +714,7 @@ __global__ void __launch_bounds__(kMainThreads, 1) proj_tile_kernel(const __grid
         } while (at < n_list);
       }
     }
+    for (int i = 0; ok && i < 2; ++i, ++ai) ok = wait(&sh.aempty[ai & 1], ((ai >> 1) & 1) ^ 1);     // as given_back
   } else if (warp >= 8) {
     // A thread owns an output channel and walks over the rows. The exact requantisation runs on the half-rate integer
     // pipes (17 to 20 outputs per clock and SM with 16 warps, see the requantisation microbenchmark), so what is added to
@@ -907,6 +920,7 @@ __global__ void __launch_bounds__(kSplitThreads, 1) proj_split_kernel(const __gr
       ptx::bulk_g2s(st + RT * kProjStage, w + (size_t)ks * kBytesW, kBytesW, bar);
       ptx::tile_g2s(st, &xmap, ks * kProjStage, row0, bar);
     }
+    given_back(abort_flag, a.status, sh.empty, turn, ring);
   } else if (warp == 1 && ptx::elect_one()) {
     const uint32_t id = idesc((uint32_t)RT, a.x_unsigned);
     Turn turn;

@@ -28,3 +28,25 @@ def test_a_warp_is_whole_where_an_instruction_wants_it_whole():
     assert "__syncwarp();" in loop[parts[0]:parts[-1]]
     # no barrier of a cluster beside the two wrappers
     assert "barrier.cluster" not in text
+
+
+def _kernels():
+    """(name, body) of the projection's kernels that hand work to the tensor cores."""
+    text = _text("proj_kernel.cu")
+    for m in re.finditer(r"__global__ void [^(]*\([^)]*\) (\w+)\(.*?\n}\n", text, flags=re.S):
+        if "umma" in m.group(0) or "mma(" in m.group(0):
+            yield m.group(1), m.group(0)
+
+
+def test_no_arrival_of_the_mmas_is_left_to_come_when_a_cta_leaves():
+    """Every barrier that a commit arrives at is waited for after its last use: the full accumulators by the epilogue, the slots that
+    are given back by whoever fills them."""
+    kernels = dict(_kernels())
+    assert len(kernels) == 3, list(kernels)
+    for name, body in kernels.items():
+        for ring in set(re.findall(r"commit\((?:ptx::smem_u32\()?&sh\.(\w*empty)\[", body)):
+            if ring == "xempty" or ring == "aempty":
+                loop = r"for \(int \w+ = 0; ok && \w+ < [\w.]+; [^)]*\) ok = wait\(&sh\.%s\[" % ring
+                assert re.search(loop, body), (name, ring)
+            else:
+                assert "given_back(abort_flag, a.status, sh.%s," % ring in body, (name, ring)
