@@ -9,11 +9,28 @@ __device__ __forceinline__ void mbar_arrive(uint32_t bar) {
   asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 
-// bounded_wait with the first try in line: its call costs some 145 ns, as much as a stage's copies take to issue.
+// bounded_wait for a thread that may have copies or MMAs under way. Where it gives up, the CTA gives up: each of its threads gets here, stops
+// and meets the others at the end of the kernel, where tensor memory is freed and the CTA leaves. What the thread has asked for has to end
+// before: it reads this GPU's memory and takes microseconds, so ten milliseconds, in at most a thousand naps.
+static __device__ __noinline__ bool settled_wait(volatile uint32_t* abort_flag, uint32_t* status, uint64_t* bar, uint32_t parity,
+                                                 uint32_t limit) {
+  const uint32_t b = smem_u32(bar);
+  for (uint32_t it = 0; it < limit && !*abort_flag; ++it)
+    if (mbar_try_wait(b, parity)) return true;
+  if (!*abort_flag) {
+    *abort_flag = 1;
+    atomicExch(status, 1u);
+  }
+  const long long start = clock64();
+  for (int i = 0; i < 1000 && clock64() - start < 20000000; ++i) __nanosleep(100000);
+  return false;
+}
+
+// The same with the first try in line: a call costs some 145 ns, as much as a stage's copies take to issue.
 __device__ __forceinline__ bool quick_wait(volatile uint32_t* abort_flag, uint32_t* status, uint64_t* bar, uint32_t parity,
                                            uint32_t limit) {
   if (mbar_try_wait(smem_u32(bar), parity)) return true;
-  return bounded_wait(abort_flag, status, bar, parity, limit);
+  return settled_wait(abort_flag, status, bar, parity, limit);
 }
 
 // ---- tile of a row-major matrix global -> shared through a tensor map (128-byte swizzle), completion counted on an

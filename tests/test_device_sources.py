@@ -50,3 +50,17 @@ def test_no_arrival_of_the_mmas_is_left_to_come_when_a_cta_leaves():
                 assert re.search(loop, body), (name, ring)
             else:
                 assert "given_back(abort_flag, a.status, sh.%s," % ring in body, (name, ring)
+
+
+def test_a_cta_that_gives_up_lets_its_copies_and_mmas_end():
+    """Every wait of the projection's kernels, when it gives up, lets what its thread has asked for end before the thread stops: the CTA does
+    not free its tensor memory or leave before all of them have stopped."""
+    header, text = _text("ptx_cluster.cuh"), _text("proj_kernel.cu")
+    body = {m.group(1): m.group(2) for m in re.finditer(r"bool (\w+_wait)\([^)]*\) \{\n(.*?)\n\}", header, flags=re.S)}
+    assert set(body) == {"settled_wait", "quick_wait"}
+    gave_up = body["settled_wait"].split("return true;")[1]
+    assert "__nanosleep" in gave_up and re.search(r"i < \d+ &&", gave_up)              # and that ends, too
+    assert "return settled_wait(" in body["quick_wait"] and "bounded_wait" not in body["quick_wait"]
+    assert not re.search(r"bounded_wait|try_wait|test_wait", text)
+    for name, kernel in _kernels():
+        assert "__syncthreads();" in kernel[:kernel.index("tmem_dealloc")][-600:], name
