@@ -838,7 +838,7 @@ def _view(t, norm, what):
 def iodf_norm_forward(norm, r, b=None, gate=None, r_out=None, n=None, stream=None):
     """r: the residual stream, cuda [rows, c] or planes [images, c, pixels] (any outer strides); b [rows, c] the
     block's output; gate uint8 [rows, c] or [c]. Returns (r_out, n), None where the handle has no such part.
-    r_out may be r. Outputs made here belong to the call's stream."""
+    r_out may be r; else no output may overlap another operand. Outputs made here belong to the call's stream."""
     c = norm.channels
     _on(r, norm, norm.res_dtype, "r")
     rows, rv = _view(r, norm, "r")

@@ -232,6 +232,16 @@ int set_adapter(iodf_proj& p, uint32_t slot, uint32_t rank, const int8_t* down, 
   return status_of(e != cudaSuccess ? e : e2);
 }
 
+// Rows of `bytes` bytes at a stride, two of them: do they share memory? Of rows that lie within each other at one stride (columns of a
+// wider matrix) it is known; at two strides they count as sharing it.
+bool rows_overlap(const void* p, size_t pbytes, size_t pstride, const void* q, size_t qbytes, size_t qstride, size_t rows) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  if (a + (rows - 1) * pstride + pbytes <= b || b + (rows - 1) * qstride + qbytes <= a) return false;
+  if (pstride != qstride || rows == 1) return true;
+  const size_t at = b >= a ? (b - a) % pstride : (pstride - (a - b) % pstride) % pstride;      // of q's rows in p's
+  return at < pbytes || at + qbytes > pstride;
+}
+
 // a: the handle's arguments, with a workspace and status words that may be another's
 int proj_forward(const iodf_proj& p, ProjArgs a, const void* x, size_t ldx, int rows, const int32_t* seg_start, const int32_t* seg_adapter,
                  int n_seg, void* y, size_t ldy, cudaStream_t stream) {
@@ -241,6 +251,8 @@ int proj_forward(const iodf_proj& p, ProjArgs a, const void* x, size_t ldx, int 
   if (!aligned(x, 16) || ldx % 16 || ldx < (size_t)a.k || ldx >= (1ull << 40)) return IODF_EINVAL;
   if (!aligned(y, (size_t)a.y_bytes) || ldy < (size_t)a.n || ldy >= (1ull << 40)) return IODF_EINVAL;
   if (!aligned(seg_start, 4) || !aligned(seg_adapter, 4)) return IODF_EINVAL;
+  // tiles are written while others are still read
+  if (rows_overlap(x, (size_t)a.k, ldx, y, (size_t)a.n * a.y_bytes, ldy * a.y_bytes, (size_t)rows)) return IODF_EINVAL;
   a.x = static_cast<const uint8_t*>(x);
   a.ldx = (long long)ldx;
   a.y = y;
