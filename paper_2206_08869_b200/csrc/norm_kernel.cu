@@ -72,8 +72,8 @@ __device__ __forceinline__ RowScale row_scale(unsigned long long D) {
   return r;
 }
 
-// Sum over the T threads of a row of values 0 <= v < 2^54 / T (squares) or |v| < 2^47 / T (sums): in a whole warp two
-// 32-bit reductions, of 27 low bits (16 for signed values) and of the rest.
+// Sum over the T threads of a row. In a whole warp two 32-bit reductions, of 27 low bits (16 for signed values) and of the rest,
+// which hold values of a thread 0 <= v < 2^54 (squares; 16 centred values are at most 2^52) and |v| < 2^42 (sums; at most 2^27).
 template <int T, bool kSigned>
 __device__ __forceinline__ long long row_sum(long long v, long long* red) {
   if constexpr (T == 1) return v;
