@@ -324,15 +324,38 @@ def _ptr(t):
     return C.c_void_p(0 if t is None else t.data_ptr())
 
 
+def _on_stream(stream, device):
+    """The torch stream of a call's `stream` argument as the current one; None leaves the current one."""
+    import contextlib
+    import torch
+    if stream is None:
+        return contextlib.nullcontext()
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)) & ~1, device)   # 1: the legacy default stream, 0 to torch
+    return torch.cuda.stream(stream)
+
+
+def _made(make, shape, dtype, device, stream):
+    """An output of a call on `stream` that the caller did not bring, in that stream's order: its memory is nobody's that the
+    current stream still works on, and a fill of it comes before the call's kernels. Nor is it the next call's before the
+    current stream has done with it."""
+    with _on_stream(stream, device):
+        t = make(shape, dtype=dtype, device=device)
+    if stream is not None:
+        import torch
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 def iodf_forward(model, x_u8, z=None, prior=None, stream=None, want_prior=True):
     """x_u8: cuda uint8 [B,C,H,W]. Returns (z int32 [B,d], prior int32 [B,2,d_fact] | None)."""
     import torch
     B = x_u8.shape[0]
     assert x_u8.is_cuda and x_u8.dtype == torch.uint8 and x_u8.is_contiguous()
     if z is None:
-        z = torch.empty((B, model.d), dtype=torch.int32, device=x_u8.device)
+        z = _made(torch.empty, (B, model.d), torch.int32, x_u8.device, stream)
     if prior is None and want_prior and model.d_fact:
-        prior = torch.empty((B, 2, model.d_fact), dtype=torch.int32, device=x_u8.device)
+        prior = _made(torch.empty, (B, 2, model.d_fact), torch.int32, x_u8.device, stream)
     rc = load_library().iodf_forward(model.handle, _ptr(x_u8), B, _ptr(z), _ptr(prior), _stream(stream))
     if rc != 0:
         raise IodfError(rc, "iodf_forward")
@@ -345,7 +368,7 @@ def iodf_inverse(model, z, x_u8=None, prior=None, out_of_range=None, stream=None
     B = z.shape[0]
     assert z.is_cuda and z.dtype == torch.int32 and z.is_contiguous()
     if x_u8 is None:
-        x_u8 = torch.empty((B,) + tuple(model.in_shape), dtype=torch.uint8, device=z.device)
+        x_u8 = _made(torch.empty, (B,) + tuple(model.in_shape), torch.uint8, z.device, stream)
     rc = load_library().iodf_inverse(model.handle, _ptr(z), B, _ptr(x_u8), _ptr(prior), _ptr(out_of_range),
                                      _stream(stream))
     if rc != 0:
@@ -372,9 +395,9 @@ def iodf_forward_patches(model, image_u8, z=None, prior=None, stream=None):
     _, H, W = image_u8.shape
     B = (H // model.in_shape[1]) * (W // model.in_shape[2])
     if z is None:
-        z = torch.empty((B, model.d), dtype=torch.int32, device=image_u8.device)
+        z = _made(torch.empty, (B, model.d), torch.int32, image_u8.device, stream)
     if prior is None and model.d_fact:
-        prior = torch.empty((B, 2, model.d_fact), dtype=torch.int32, device=image_u8.device)
+        prior = _made(torch.empty, (B, 2, model.d_fact), torch.int32, image_u8.device, stream)
     rc = load_library().iodf_forward_patches(model.handle, _ptr(image_u8), H, W, _ptr(z), _ptr(prior), _stream(stream))
     if rc != 0:
         raise IodfError(rc, "iodf_forward_patches")
@@ -385,7 +408,7 @@ def iodf_inverse_patches(model, z, H, W, image_u8=None, prior=None, out_of_range
     """z: cuda int32 [B,d] of the patch batch. Returns the image uint8 [C,H,W]."""
     import torch
     if image_u8 is None:
-        image_u8 = torch.empty((model.in_shape[0], H, W), dtype=torch.uint8, device=z.device)
+        image_u8 = _made(torch.empty, (model.in_shape[0], H, W), torch.uint8, z.device, stream)
     rc = load_library().iodf_inverse_patches(model.handle, _ptr(z), H, W, _ptr(image_u8), _ptr(prior),
                                              _ptr(out_of_range), _stream(stream))
     if rc != 0:
@@ -428,9 +451,9 @@ def iodf_rans_encode(codec, z, prior, words=None, counts=None, stream=None):
     import torch
     B = z.shape[0]
     if words is None:
-        words = torch.empty((B, codec.n_streams, codec.words_per_stream), dtype=torch.int16, device=z.device)
+        words = _made(torch.empty, (B, codec.n_streams, codec.words_per_stream), torch.int16, z.device, stream)
     if counts is None:
-        counts = torch.empty((B, codec.n_streams), dtype=torch.int32, device=z.device)
+        counts = _made(torch.empty, (B, codec.n_streams), torch.int32, z.device, stream)
     rc = load_library().iodf_rans_encode(codec.handle, _ptr(z), _ptr(prior), B, _ptr(words), _ptr(counts), _stream(stream))
     if rc != 0:
         raise IodfError(rc, "iodf_rans_encode")
@@ -454,20 +477,21 @@ def iodf_rans_pack(codec, words, counts, packed=None, stream=None):
     import torch
     B = counts.shape[0]
     if packed is None:
-        packed = torch.empty(iodf_rans_packed_capacity(codec, B), dtype=torch.uint8, device=counts.device)
+        packed = _made(torch.empty, iodf_rans_packed_capacity(codec, B), torch.uint8, counts.device, stream)
     rc = load_library().iodf_rans_pack(codec.handle, _ptr(words), _ptr(counts), B, _ptr(packed), _stream(stream))
     if rc != 0:
         raise IodfError(rc, "iodf_rans_pack")
-    payload = int(packed[4 * B:4 * B + 4].cpu().numpy().view(np.uint32)[0])
+    with _on_stream(stream, packed.device):
+        payload = int(packed[4 * B:4 * B + 4].cpu().numpy().view(np.uint32)[0])
     return packed, 4 * (B + 1) + payload
 
 
 def iodf_rans_unpack(codec, packed, nbytes, B, words=None, counts=None, stream=None):
     import torch
     if words is None:
-        words = torch.zeros((B, codec.n_streams, codec.words_per_stream), dtype=torch.int16, device=packed.device)
+        words = _made(torch.zeros, (B, codec.n_streams, codec.words_per_stream), torch.int16, packed.device, stream)
     if counts is None:
-        counts = torch.zeros((B, codec.n_streams), dtype=torch.int32, device=packed.device)
+        counts = _made(torch.zeros, (B, codec.n_streams), torch.int32, packed.device, stream)
     rc = load_library().iodf_rans_unpack(codec.handle, _ptr(packed), int(nbytes), int(B), _ptr(words), _ptr(counts),
                                          _stream(stream))
     if rc != 0:
@@ -656,18 +680,6 @@ def _layer_stream(stream, device):
 
 def _addr(t):
     return None if t is None else t.data_ptr()
-
-
-def _made(make, shape, dtype, device, stream):
-    """An output of a call on `stream` that the caller did not bring, in that stream's order: its memory is nobody's that the
-    current stream still works on, and a fill of it comes before the call's kernels."""
-    import torch
-    if stream is None:
-        return make(shape, dtype=dtype, device=device)
-    if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(int(getattr(stream, "cuda_stream", stream)) & ~1, device)   # 1: the legacy default stream, 0 to torch
-    with torch.cuda.stream(stream):
-        return make(shape, dtype=dtype, device=device)
 
 
 class Projection:
