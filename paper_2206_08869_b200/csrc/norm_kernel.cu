@@ -7,9 +7,9 @@
 // 250 instructions per thread beside its elements. 16384 x 4096 int16 with int32 blocks and gates: 134 us (5.0 TB/s; floor 104;
 // without the two norms 87), 32768 x 256 int32 with int8 blocks: 20.9 us (4.0 TB/s; floor 13), 20011 x 173 unaligned,
 // centred: 19.2 us (2.5 TB/s; floor 7.5; a row's own work), one row of 4096: 4 us (a launch).
-// Measured and not taken: 32 elements per thread (fewer instructions, a fifth of the warps: 228 us on the first of
-// these), rows copied ahead into shared memory (235 us: twice through the same pipe), a row's two roots worked out by one thread
-// for all (188 us: two more barriers), four elements per access (222 us: twice the accesses).
+// Measured and not taken, on the first of these while it took 182 us (its loads still stood behind guards, so these say nothing of the
+// present form): 32 elements per thread 228 us (a fifth of the warps), rows copied ahead into shared memory 235 (twice through the same
+// pipe), a row's two roots worked out by one thread for all 188 (two more barriers), four elements per access 222.
 // Three ways to lay a row over its threads:
 //   kVector  eight neighbouring channels per thread, 8 or 16-byte accesses (everything aligned to them)
 //   kScalar  neighbouring threads take neighbouring channels, one element per access (any alignment)
@@ -183,8 +183,12 @@ __device__ __forceinline__ void store8_sat(uint8_t* p, const int (&v)[8], bool i
 template <int T>
 struct Block { static constexpr int threads = T <= 32 ? 128 : T, rows = threads / T; };
 
-// Blocks per SM that the registers have to leave room for: what measured best (32 to 40 warps; 16384 x 4096 int16 with
-// int32 blocks and gates 152 us without the bound, 134 with it; 20011 x 173 int32 unaligned 19.8 and 19.2).
+// Blocks per SM that the registers have to leave room for: what measured best (32 to 40 warps). It costs up to 64 bytes of spills in the
+// forms with int32 residuals (T = 256; 32 for T = 128, 8 to 56 for unaligned rows of 161 to 256 channels), up to 44 with int16. us without
+// and with the bound: 16384 x 4096 int16, int32 blocks, gates 153 and 134; int32 residuals, gates: 8192 x 8192, int8 blocks 238 and 174;
+// 16384 x 4096, int8 160 and 158, int32 171 and 177 (the one that loses by its spills); 32768 x 2048, int8 145 and 140, int32 156
+// and 152; 65536 x 1024, int8 141 and 135; 131072 x 256, int8 74 and 70; unaligned, 100003 rows, int32: 173 channels 73 and 72, 199 78
+// and 80, 225 86 and 86, 249 87 and 87.
 template <int T, int E, int MODE>
 __host__ __device__ constexpr int min_blocks() {
   return MODE == kScalar ? (T == 32 && E <= 8 ? 10 : 1) : MODE != kVector ? 1 : T == 512 ? 2 : T == 256 ? 5 : T == 128 ? 9 : T == 64 ? 16 : E <= 8 ? 10 : 8;

@@ -339,9 +339,12 @@ __global__ void __launch_bounds__(kDownThreads) down_tile_kernel(const __grid_co
 //   paired (larger K) two CTAs per unit of two output tiles, one each, and one MMA over both (M = 256). Each reads half of
 //          the x tile: a stage is 32 KB of copies and 32 KB of operand reads per SM for 512 clocks of MMAs, where single CTAs
 //          have 48 KB of each, more than the 128 bytes per clock of shared memory. down_tile_kernel computes h before.
-// 65536 x 512 -> 512, uint8, rank 32 (fused): 34.7 us, 1.1 POP/s, bound by the epilogue (15 clocks per 32 outputs and SM quarter, 5 of
-// them the 64-bit product); tensor pipe 27 % active. 16384 x 4096 -> 4096, rank 64 (paired): 171 of the call's 185 us, tensor pipe 85 %
-// active. 32768 x 256 -> 256: 14.3 us, the latency of one unit.
+// 65536 x 512 -> 512, uint8, rank 32 (fused): 34.7 us, 1.1 POP/s, tensor pipe 27 % active. Of the 72 000 clocks of a CTA with two units
+// (108 of 148 have two, 40 one; clock stamps) the epilogue of its eight output tiles takes 34 000 (some 1760 per 32 rows: 300 load, 720
+// requantisation, 280 transposition, 460 stores). The rest is the chain in front of a unit's first output tile (20 000 before the
+// first unit: start, requests, copies of `down`, the product, h and its way through L2; 8 000 before the second, as there is room for one
+// x tile only) and 8 000 of waits between tiles. 32768 x 256 -> 256: 14.3 us, one unit: 17 000 of 27 000 clocks before its first
+// output tile. 16384 x 4096 -> 4096, rank 64 (paired): 171 of the call's 185 us, tensor pipe 85 % active.
 constexpr int kMaxTile = 256;
 
 constexpr int kMaxX = 16;
