@@ -106,3 +106,29 @@ def test_codecs_in_flight_share_the_layers_of_their_refinements(G):
         for p in priors:
             assert torch.equal(p, want)
     assert all(torch.equal(y, own_want) for y in own)
+
+
+def test_a_refinement_captured_and_replayed(G):
+    """What the graph reads, the means and the images' customers, changes between replays."""
+    m, codec, blocks, x = _setup(G, 0xD0E1, batch=6)
+    who = torch.tensor([0, 1, 2, -1, 1, 0], dtype=torch.int32, device="cuda")
+    _set(G, codec, blocks, who)
+    z, prior = G.iodf_forward(m, torch.from_numpy(x).cuda())
+    buf = prior.clone()
+    G.iodf_refine_prior(codec, 0, buf)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        for level in blocks:
+            G.iodf_refine_prior(codec, level, buf)
+    for i, slots in enumerate(([2, 2, 0, 1, -1, 1], [-1] * 6, [0, 1, 2, 0, 1, 2])):
+        who.copy_(torch.tensor(slots, dtype=torch.int32))
+        buf.copy_(prior.roll(i, 0))
+        want = buf.cpu().numpy()
+        for level, b in blocks.items():
+            off = int(m.layout.prior_off[level])
+            part = want[:, 0, off:off + b.c * b.px]
+            part[:] = b.plain(part.reshape(6, b.c, b.px), slots).reshape(6, -1)
+        graph.replay()
+        np.testing.assert_array_equal(buf.cpu().numpy(), want)
+        G.iodf_codec_check(codec)
+    del graph
