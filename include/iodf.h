@@ -473,13 +473,14 @@ int iodf_launches_per_call(const iodf_model* m, int inverse);
  *
  * iodf_proj_forward: x DEV [rows] x c_in elements, row stride ldx >= c_in bytes, a multiple of 16, x
  * 16-byte aligned; y DEV [rows] x c_out elements of y_type, row stride ldy >= c_out elements, aligned to its
- * element; y must not overlap x (EINVAL; both may be columns of a wider matrix). seg_start DEV int32 [n_seg + 1], seg_adapter DEV int32 [n_seg]; n_seg = 0 (both may be NULL) is a call
- * without requests, every row is computed without an adapter (a batch that has run out of requests is not to be
- * handed over so). Rows in no request are not written. 0 <= rows <= max_rows. Allocates nothing,
- * may be captured; the handle's workspace serves one call at a time (also for replayed graphs). Requests whose
- * bounds decrease or leave 0..rows, and slots outside -1..max_adapters-1, are counted on the device and
- * reported by iodf_proj_check (IODF_EDATA). Such a slot counts as -1; with bad bounds any row may be left
- * unwritten or take the adapter of another request or none, and nothing outside the buffers is touched.
+ * element; y must not overlap x (EINVAL; both may be columns of a wider matrix). seg_start DEV int32 [n_seg + 1],
+ * seg_adapter DEV int32 [n_seg]; n_seg = 0 (both may be NULL) is a call without requests, every row is computed
+ * without an adapter (a batch that has run out of requests is not to be handed over so). Rows in no request are
+ * not written. 0 <= rows <= max_rows. Allocates nothing, may be captured; the handle's workspace serves one call
+ * at a time (also for replayed graphs). Requests whose bounds decrease or leave 0..rows, and slots outside
+ * -1..max_adapters-1, are counted on the device and reported by iodf_proj_check (IODF_EDATA). Such a slot counts
+ * as -1; with bad bounds any row may be left unwritten or take the adapter of another request or none, and nothing
+ * outside the buffers is touched.
  */
 typedef struct {
   uint32_t abi_version;                /* IODF_ABI_VERSION                                           */
@@ -525,9 +526,10 @@ int iodf_proj_check(iodf_proj* p, void* cuda_stream, uint32_t* bad_requests);
  * channel_stride * c + pixel_stride * (row % pixels) elements; either channel_stride is 1 (rows: pixels = rows),
  * or pixel_stride is 1 (planes, the layout of z and prior; channels <= 256 then). b, gate and n are DEV rows with
  * strides ldb, ldg, ldn in elements; ldg = 0: one gate per channel; gate NULL: none. out_view gives every element a
- * place of its own (EINVAL otherwise); r_out may be r with the same view (in place), else the two must not overlap; it is NULL exactly if there is no block, n exactly if there is
- * no pre_norm. Neither may overlap any other operand. Pointers are aligned to their elements. Any rows >= 0. Enqueues one kernel, allocates nothing, keeps
- * no workspace: calls on one handle may overlap.
+ * place of its own (EINVAL otherwise); r_out may be r with the same view (in place), else the two must not overlap;
+ * it is NULL exactly if there is no block, n exactly if there is no pre_norm. Neither may overlap any other operand.
+ * Pointers are aligned to their elements. Any rows >= 0. Enqueues one kernel, allocates nothing, keeps no workspace:
+ * calls on one handle may overlap.
  */
 #define IODF_NORM_RMS 1u
 #define IODF_NORM_CENTRED 2u

@@ -186,7 +186,7 @@ struct Block { static constexpr int threads = T <= 32 ? 128 : T, rows = threads 
 // Blocks per SM that the registers have to leave room for: what measured best (32 to 40 warps). It costs up to 64 bytes of spills in the
 // forms with int32 residuals (T = 256; 32 for T = 128, 8 to 56 for unaligned rows of 161 to 256 channels), up to 44 with int16. us without
 // and with the bound: 16384 x 4096 int16, int32 blocks, gates 153 and 134; int32 residuals, gates: 8192 x 8192, int8 blocks 238 and 174;
-// 16384 x 4096, int8 160 and 158, int32 171 and 177 (the one that loses by its spills); 32768 x 2048, int8 145 and 140, int32 156
+// 16384 x 4096, int8 160 and 158, int32 171 and 177 (spills); 32768 x 2048, int8 145 and 140, int32 156
 // and 152; 65536 x 1024, int8 141 and 135; 131072 x 256, int8 74 and 70; unaligned, 100003 rows, int32: 173 channels 73 and 72, 199 78
 // and 80, 225 86 and 86, 249 87 and 87.
 template <int T, int E, int MODE>
