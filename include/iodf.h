@@ -563,6 +563,100 @@ int iodf_norm_forward(iodf_norm* nm, int rows, const void* r, const iodf_view* r
                       void* cuda_stream);
 
 /*
+ * Attention of the rows of a request to the tokens before them, over a cache of blocks in 8 bits: what lets a network between the
+ * flow and the coder look at pixels, patches or tokens that are coded already. Any cut of a request's tokens into calls gives the same
+ * cache and the same outputs bit for bit: an encoder can pass over all tokens at once where its decoder takes one at a time.
+ *
+ * The cache is the caller's: `blocks` blocks of 128 tokens, each with its keys and values of every cache head and an exponent for both,
+ *   k DEV int8 [blocks][kv_heads][128][head_dim], v DEV int8 [blocks][kv_heads][head_dim][128] (both 16-byte aligned),
+ *   k_exp, v_exp DEV uint8 [blocks][kv_heads]: an element stands for k 2^k_exp; exponents above 12 count as 12.
+ * Token t of request q lies in block table[q][t / 128] at t % 128; its slot is that block * 128 + t % 128.
+ *
+ * iodf_attn_plan: blocks for the new tokens of a call's requests. held[q] tokens are in the cache, add[q] >= 0 come with this call, -1: the
+ * request ends. ring (ring_size = blocks of the cache) holds the free blocks from place state[0] on, state[1] of them, modulo its size.
+ * Requests in order take ceil((held + add) / 128) - ceil(held / 128) blocks from its front into their row of `table` (row stride ldt, `width`
+ * entries), the blocks of those that end go behind its end, for the next call to take; held_out[q] = held + add (0 at an end), row_start[q]
+ * = sum of add before q; row r of request q gets position[r] = held[q] + r - row_start[q] and its slot[r]; rows behind the last request
+ * get slot -1, position 0; state_out is the next call's state. A request that needs blocks when fewer than all taken so far and its own are
+ * free, that would not fit into `width` entries or whose rows would not into `rows`, or with held outside 0..128 width or add below -1,
+ * keeps what it holds, its rows get slot -1, and it is counted (iodf_attn_check: IODF_EDATA). The inputs but for table and ring stay as
+ * they are, no two operands may overlap (EINVAL), and the call repeated on the same inputs gives the same. width <= 1024, n_req <= 16384.
+ *
+ * iodf_attn_append: the call's tokens into the cache, its queries in 8 bits. q, k, v: DEV rows of x_type with strides in elements (columns of
+ * one projection's output, say), heads * head_dim and kv_heads * head_dim of them; values are taken in 16 bits, clip(x, -2^15, 2^15 - 1).
+ * The first rotary_dim dimensions of each query and key are rotated by the row's position; with pairs (x[i], x[i + rotary_dim / 2])
+ * (IODF_ROTARY_HALF) or (x[2 i], x[2 i + 1]) (IODF_ROTARY_INTERLEAVED) and (c, s) = rotary[position][i] in units of 2^-14,
+ *   x' = floor((x c - y s + 2^13) / 2^14),  y' = floor((x s + y c + 2^13) / 2^14)
+ * 8 bits: x8 = clip(floor((x + floor(2^e / 2)) / 2^e), -127, 127). Of a query's head e is the smallest with max|x| <= 127 2^e, written to q_exp DEV
+ * uint8 [rows][heads] beside q8 DEV int8 [rows][heads][head_dim] (16-byte aligned). Of a block's keys (values) e is decided by its first token
+ * and stays: the smallest with max|x| (8 + headroom) <= 1016 2^e, headroom 0..8 in eighths; later tokens beyond it are clipped. A row of slot -1
+ * writes its query only. A block's first token is in an earlier call or in row r - slot % 128 of this one; a slot appears once. A
+ * position outside the table (taken as its nearest) and a slot outside the cache (as -1) are counted.
+ *
+ * iodf_attn_forward: row r of request q, row_start[q] <= r < row_start[q + 1], is at position held[q] - row_start[q + 1] + r, with held the tokens
+ * after the call's (iodf_attn_plan's held_out), and sees tokens t < held[q]; if causal only t <= position; with a window only
+ * t > position - window. Query head i reads cache head i / (heads / kv_heads). Per head, in integers:
+ *   W = min(2^31 - 1, floor(score_m0 2^(q_exp + k_exp) / 2^score_s)),  t_j = floor(q8 . k_j W / 2^23)   (scores in 2^-13 octaves)
+ *   T = max t_j, V = max v_exp of the blocks with a token that is seen
+ *   p_j = 2^(15 + n / 2^13) rounded to nearest even, n = t_j - T - 2^13 (V - v_exp)   (0 .. 32768; the power as below)
+ *   A = sum p_j v_j,  L = sum p_j 2^(V - v_exp),  y = clip(rq(o; out_m0, out_s)), o = A 2^(V + 8) / L
+ * The power: with g = n mod 2^13 and c = floor(g / 128), 2^(n / 2^13) is m 2^floor(n / 2^13) / 2^23 with m = max(2^23, [2^(23 + (2 c + 1) / 128)] - 2^16)
+ * + 2^10 (g mod 128). The quotient: L' = floor(L 2^a) with 2^31 <= L' < 2^32, rho = floor((2^63 - 1) / L'), o = floor((floor(A 2^(a - 8)) rho +
+ * 2^(46 - V)) / 2^(47 - V)). Sums of integers: neither order nor split changes them. A row that sees nothing has o = 0. y: DEV rows of heads *
+ * head_dim elements of y_type with row stride ldy in elements; y must not overlap an input. Rows in no request are not written; bounds outside
+ * 0..rows are taken as the nearest and counted, as are held outside 0..128 width and blocks outside the cache, which nobody sees. A request
+ * whose row_start decreases has no rows. width <= 1024 (131072 tokens); it also tells the call how long contexts may be, so that few rows with
+ * long ones are spread over the GPU: give the longest request's.
+ *
+ * All three enqueue one kernel, allocate nothing, keep no workspace and may be captured; calls on one handle may overlap. head_dim 32, 64
+ * or 128 (EUNSUPPORTED otherwise), heads <= 1024, at most 128 for a cache head, rotary_dim a multiple of 16, score_s 0..62. Errors of
+ * iodf_attn_create: EINVAL, EUNSUPPORTED, EVERSION, ENOMEM, ECUDA; of the calls EINVAL (null or misaligned pointer, overlap), EUNSUPPORTED, ECUDA.
+ */
+#define IODF_ROTARY_HALF 1u
+#define IODF_ROTARY_INTERLEAVED 2u
+
+typedef struct {
+  uint32_t abi_version;                /* IODF_ABI_VERSION                                           */
+  uint32_t heads, kv_heads, head_dim;
+  uint32_t x_type;                     /* IODF_I8 or IODF_I32                                        */
+  uint32_t rotary_dim;                 /* 0: no rotation                                             */
+  uint32_t rotary_layout;
+  uint32_t positions;                  /* rows of the table                                          */
+  const int16_t* rotary;               /* HOST [positions][rotary_dim / 2][2]: cos, sin, at most 2^14 */
+  uint32_t k_headroom, v_headroom;
+  int32_t score_m0, score_s;
+  uint32_t causal, window;             /* 0 / 1; tokens, 0: no window                                */
+  uint32_t y_type;                     /* IODF_I32, or IODF_I8 / IODF_U8 with a clip inside          */
+  uint32_t has_clamp;
+  int32_t clamp_lo, clamp_hi;
+  const int32_t* out_m0;               /* HOST, heads * head_dim                                     */
+  const int32_t* out_s;                /* HOST, heads * head_dim                                     */
+} iodf_attn_desc;
+
+typedef struct {
+  int8_t* k;                           /* DEV, as all of them                                        */
+  int8_t* v;
+  uint8_t* k_exp;
+  uint8_t* v_exp;
+  uint32_t blocks;
+} iodf_attn_cache;
+
+typedef struct iodf_attn iodf_attn;
+
+int iodf_attn_create(const iodf_attn_desc* desc, int device, iodf_attn** out);
+void iodf_attn_destroy(iodf_attn* a);
+int iodf_attn_plan(iodf_attn* a, int n_req, const int32_t* held, const int32_t* add, int32_t* table, size_t ldt, uint32_t width, int32_t* ring,
+                   uint32_t ring_size, const int32_t* state, int rows, int32_t* held_out, int32_t* row_start, int32_t* slot, int32_t* position,
+                   int32_t* state_out, void* cuda_stream);
+int iodf_attn_append(iodf_attn* a, int rows, const void* q, size_t ldq, const void* k, size_t ldk, const void* v, size_t ldv, const int32_t* slot,
+                     const int32_t* position, const iodf_attn_cache* cache, int8_t* q8, uint8_t* q_exp, void* cuda_stream);
+int iodf_attn_forward(iodf_attn* a, int rows, const int8_t* q8, const uint8_t* q_exp, const int32_t* row_start, const int32_t* held, int n_req,
+                      const int32_t* table, size_t ldt, uint32_t width, const iodf_attn_cache* cache, void* y, size_t ldy, void* cuda_stream);
+/* Synchronise the stream; IODF_EDATA if a call since the last check met requests, rows or blocks that it could not serve (their number in
+ * *bad, HOST, may be NULL), IODF_ETIMEOUT if a bounded wait gave up. Clears both. */
+int iodf_attn_check(iodf_attn* a, void* cuda_stream, uint32_t* bad);
+
+/*
  * Refinement of a level's prior parameters by a residual block of those layers, with adapters of each image's customer:
  *   mu' = mu + scale * gate * norm(down(up(norm(mu))))         over the C/2 means of every pixel of the level
  * as iodf_norm_forward (first: no block, its n feeds `up`), iodf_proj_forward twice and iodf_norm_forward (last: no n,

@@ -24,6 +24,8 @@ DECLARED_SYMBOLS = ["iodf_create", "iodf_destroy", "iodf_get_layout", "iodf_forw
                     "iodf_proj_create", "iodf_proj_destroy", "iodf_proj_set_adapter", "iodf_proj_forward",
                     "iodf_proj_check", "iodf_norm_create", "iodf_norm_destroy", "iodf_norm_forward",
                     "iodf_codec_set_refinement", "iodf_refine_prior", "iodf_codec_selftest_timeout",
+                    "iodf_attn_create", "iodf_attn_destroy", "iodf_attn_plan", "iodf_attn_append", "iodf_attn_forward",
+                    "iodf_attn_check",
                     "iodf_strerror", "iodf_last_cuda_error"]
 
 
@@ -89,6 +91,19 @@ class NormDesc(C.Structure):
                 ("n_type", C.c_uint32), ("shift", C.c_int32), ("n_shift", C.c_int32), ("res_lo", C.c_int32),
                 ("res_hi", C.c_int32), ("n_lo", C.c_int32), ("n_hi", C.c_int32), ("eps", C.c_uint64),
                 ("mult", C.c_void_p), ("n_mult", C.c_void_p), ("n_bias", C.c_void_p)]
+
+
+class AttnDesc(C.Structure):
+    _fields_ = [("abi_version", C.c_uint32), ("heads", C.c_uint32), ("kv_heads", C.c_uint32), ("head_dim", C.c_uint32),
+                ("x_type", C.c_uint32), ("rotary_dim", C.c_uint32), ("rotary_layout", C.c_uint32), ("positions", C.c_uint32),
+                ("rotary", C.c_void_p), ("k_headroom", C.c_uint32), ("v_headroom", C.c_uint32), ("score_m0", C.c_int32),
+                ("score_s", C.c_int32), ("causal", C.c_uint32), ("window", C.c_uint32), ("y_type", C.c_uint32),
+                ("has_clamp", C.c_uint32), ("clamp_lo", C.c_int32), ("clamp_hi", C.c_int32), ("out_m0", C.c_void_p),
+                ("out_s", C.c_void_p)]
+
+
+class AttnCacheDesc(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_exp", C.c_void_p), ("v_exp", C.c_void_p), ("blocks", C.c_uint32)]
 
 
 class View(C.Structure):
@@ -204,6 +219,18 @@ def load_library(path=None):
     L.iodf_codec_set_refinement.argtypes = [vp, C.c_int, C.POINTER(RefinementDesc)]
     L.iodf_refine_prior.restype = C.c_int
     L.iodf_refine_prior.argtypes = [vp, C.c_int, vp, C.c_int, vp]
+    L.iodf_attn_create.restype = C.c_int
+    L.iodf_attn_create.argtypes = [C.POINTER(AttnDesc), C.c_int, C.POINTER(vp)]
+    L.iodf_attn_destroy.restype = None
+    L.iodf_attn_destroy.argtypes = [vp]
+    L.iodf_attn_plan.restype = C.c_int
+    L.iodf_attn_plan.argtypes = [vp, C.c_int, vp, vp, vp, C.c_size_t, C.c_uint32, vp, C.c_uint32, vp, C.c_int, vp, vp, vp, vp, vp, vp]
+    L.iodf_attn_append.restype = C.c_int
+    L.iodf_attn_append.argtypes = [vp, C.c_int, vp, C.c_size_t, vp, C.c_size_t, vp, C.c_size_t, vp, vp, C.POINTER(AttnCacheDesc), vp, vp, vp]
+    L.iodf_attn_forward.restype = C.c_int
+    L.iodf_attn_forward.argtypes = [vp, C.c_int, vp, vp, vp, vp, C.c_int, vp, C.c_size_t, C.c_uint32, C.POINTER(AttnCacheDesc), vp, C.c_size_t, vp]
+    L.iodf_attn_check.restype = C.c_int
+    L.iodf_attn_check.argtypes = [vp, vp, C.POINTER(C.c_uint32)]
     L.iodf_codec_selftest_timeout.restype = C.c_int
     L.iodf_codec_selftest_timeout.argtypes = [vp, C.c_int, C.c_uint32, vp]
     L.iodf_strerror.restype = C.c_char_p
@@ -930,3 +957,164 @@ def iodf_codec_selftest_timeout(codec, level, tries=3, stream=None):
     rc = load_library().iodf_codec_selftest_timeout(codec.handle, _fits(level, C.c_int, "level"), _fits(tries, C.c_uint32, "tries"), _stream(stream))
     if rc != 0:
         raise IodfError(rc, "iodf_codec_selftest_timeout")
+
+
+# ---- attention over a cache of blocks ------------------------------------------------------------------------
+IODF_ROTARY_HALF, IODF_ROTARY_INTERLEAVED = 1, 2
+IODF_ATTN_BLOCK = 128                  # tokens of a block
+_LAYOUTS = {"half": IODF_ROTARY_HALF, "interleaved": IODF_ROTARY_INTERLEAVED}
+
+
+class Attention:
+    """Handle of an iodf_attn; destroyed when garbage collected."""
+
+    def __init__(self, handle, device, heads, kv_heads, head_dim, x_dtype, y_dtype):
+        self.handle, self.device, self.heads, self.kv_heads, self.head_dim = handle, device, heads, kv_heads, head_dim
+        self.x_dtype, self.y_dtype = x_dtype, y_dtype
+        import torch
+        self.int32, self.int8, self.uint8 = torch.int32, torch.int8, torch.uint8
+
+    def __del__(self):
+        h, self.handle = getattr(self, "handle", None), None
+        if h and _lib is not None:
+            _lib.iodf_attn_destroy(h)
+
+
+def iodf_attn_create(desc, device=0):
+    """desc: dict with heads, kv_heads, head_dim, x_dtype (int8 | int32), score (m0, s), out {m0, s int32 [heads * head_dim], clamp
+    (lo, hi) | None, dtype int8 | uint8 | int32} and, as far as used, rotary {dim, layout "half" | "interleaved", table int16 [positions,
+    dim / 2, 2]}, headroom (keys, values) in eighths, causal (default True) and window (tokens)."""
+    L = load_library()
+    rotary, out = desc.get("rotary"), desc["out"]
+    heads, kv, dim = (int(desc[k]) for k in ("heads", "kv_heads", "head_dim"))
+    table, rot, positions = None, 0, 0
+    if rotary is not None:
+        table, rot = _integers(rotary["table"], np.int16, "rotary table"), int(rotary["dim"])
+        if table.ndim != 3 or rot < 2 or table.shape[1:] != (rot // 2, 2):
+            raise ValueError("the rotary table must be [positions, %d, 2]" % (rot // 2))
+        positions = table.shape[0]
+    par = [_integers(out[k], np.int32, k).reshape(-1) for k in ("m0", "s")]
+    if any(a.size != heads * dim for a in par):
+        raise ValueError("m0 and s must hold one value for each of the %d outputs" % (heads * dim))
+    cl, (m0, s), (kh, vh) = out.get("clamp"), desc["score"], desc.get("headroom", (0, 0))
+    d = _record(AttnDesc, IODF_ABI_VERSION, heads, kv, dim, _type_code(desc["x_dtype"], (IODF_I8, IODF_I32)), rot,
+                _LAYOUTS[rotary["layout"]] if rot else 0, positions, None if table is None else table.ctypes.data, kh, vh, m0, s,
+                int(bool(desc.get("causal", True))), desc.get("window", 0), _type_code(out["dtype"], (IODF_I8, IODF_U8, IODF_I32)),
+                int(cl is not None), cl[0] if cl else 0, cl[1] if cl else 0, par[0].ctypes.data, par[1].ctypes.data)
+    handle = C.c_void_p()
+    rc = L.iodf_attn_create(C.byref(d), _fits(device, C.c_int, "device"), C.byref(handle))
+    if rc != 0:
+        raise IodfError(rc, "iodf_attn_create")
+    return Attention(handle, int(device), heads, kv, dim, desc["x_dtype"], out["dtype"])
+
+
+def iodf_attn_cache(attn, blocks):
+    """The tensors of a cache of `blocks` blocks: dict k, v, k_exp, v_exp."""
+    import torch
+    d, kv, dim = "cuda:%d" % attn.device, attn.kv_heads, attn.head_dim
+    return {"k": torch.zeros((blocks, kv, IODF_ATTN_BLOCK, dim), dtype=torch.int8, device=d),
+            "v": torch.zeros((blocks, kv, dim, IODF_ATTN_BLOCK), dtype=torch.int8, device=d),
+            "k_exp": torch.zeros((blocks, kv), dtype=torch.uint8, device=d), "v_exp": torch.zeros((blocks, kv), dtype=torch.uint8, device=d)}
+
+
+def _flat(t, attn, dtype, shape, what):
+    """A contiguous tensor's address."""
+    if t.get_device() != attn.device or t.dtype is not dtype:
+        _on(t, attn, dtype, what)
+    if t.shape != shape or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous %s" % (what, list(shape)))
+    return t.data_ptr()
+
+
+def _table_of(t, attn, n):
+    """Address, row stride and width of a block table [n, width] whose entries lie side by side."""
+    if t.get_device() != attn.device or t.dtype is not attn.int32:
+        _on(t, attn, attn.int32, "table")
+    if t.dim() != 2 or t.shape[0] != n or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("table must be [%d, blocks] with a request's entries side by side" % n)
+    return t.data_ptr(), t.stride(0) if n > 1 else max(t.shape[1], t.stride(0)), t.shape[1]
+
+
+def _cache_of(cache, attn):
+    k, kv, dim = cache["k"], attn.kv_heads, attn.head_dim
+    blocks = k.shape[0]
+    return AttnCacheDesc(_flat(k, attn, attn.int8, (blocks, kv, IODF_ATTN_BLOCK, dim), "cache k"),
+                         _flat(cache["v"], attn, attn.int8, (blocks, kv, dim, IODF_ATTN_BLOCK), "cache v"),
+                         _flat(cache["k_exp"], attn, attn.uint8, (blocks, kv), "cache k_exp"),
+                         _flat(cache["v_exp"], attn, attn.uint8, (blocks, kv), "cache v_exp"), _fits(blocks, C.c_uint32, "blocks"))
+
+
+def iodf_attn_plan(attn, held, add, table, ring, state, rows, held_out=None, row_start=None, slot=None, position=None, state_out=None, stream=None):
+    """Blocks for `add` new tokens of each request (see include/iodf.h). held, add int32 [n]; table int32 [n, width] and ring int32
+    [blocks] are changed in place; state int32 [2]; rows: room for new tokens. Returns (held_out [n], row_start [n + 1], slot [rows],
+    position [rows], state_out [2]); outputs made here belong to the call's stream."""
+    n, rows = held.shape[0], int(rows)
+    if rows < 0 or rows > _MOST or n > _MOST:
+        raise ValueError("%d rows of %d requests are out of range" % (rows, n))
+    i32 = attn.int32
+    if held_out is None or row_start is None or slot is None or position is None or state_out is None:
+        import torch
+        made = lambda t, shape: t if t is not None else _made(torch.empty, shape, i32, held.device, stream)      # noqa: E731
+        held_out, row_start, slot = made(held_out, (n,)), made(row_start, (n + 1,)), made(slot, (rows,))
+        position, state_out = made(position, (rows,)), made(state_out, (2,))
+    at, ldt, width = _table_of(table, attn, n)
+    rc = (_lib or load_library()).iodf_attn_plan(
+        attn.handle, n, _flat(held, attn, i32, (n,), "held"), _flat(add, attn, i32, (n,), "add"), at, ldt, width,
+        _flat(ring, attn, i32, (ring.numel(),), "ring"), ring.numel(), _flat(state, attn, i32, (2,), "state"), rows,
+        _flat(held_out, attn, i32, (n,), "held_out"), _flat(row_start, attn, i32, (n + 1,), "row_start"), _flat(slot, attn, i32, (rows,), "slot"),
+        _flat(position, attn, i32, (rows,), "position"), _flat(state_out, attn, i32, (2,), "state_out"), _layer_stream(stream, attn.device))
+    if rc != 0:
+        raise IodfError(rc, "iodf_attn_plan")
+    return held_out, row_start, slot, position, state_out
+
+
+def iodf_attn_append(attn, q, k, v, slot, position, cache, q8=None, q_exp=None, stream=None):
+    """q [rows, heads * head_dim], k and v [rows, kv_heads * head_dim] of the handle's x_dtype (any row strides: columns of one matrix),
+    slot and position int32 [rows]. Writes the rotated keys and the values into the cache (dict as from iodf_attn_cache), in 8 bits.
+    Returns the queries (q8 int8 [rows, heads, head_dim], q_exp uint8 [rows, heads])."""
+    rows, heads, nk = q.shape[0], attn.heads, attn.kv_heads * attn.head_dim
+    if rows > _MOST:
+        raise ValueError("%d rows are out of range" % rows)
+    ldq = _rows_of(q, attn, attn.x_dtype, rows, heads * attn.head_dim, "q")
+    ldk, ldv = _rows_of(k, attn, attn.x_dtype, rows, nk, "k"), _rows_of(v, attn, attn.x_dtype, rows, nk, "v")
+    if q8 is None or q_exp is None:
+        import torch
+        if q8 is None:
+            q8 = _made(torch.empty, (rows, heads, attn.head_dim), torch.int8, q.device, stream)
+        if q_exp is None:
+            q_exp = _made(torch.empty, (rows, heads), torch.uint8, q.device, stream)
+    rc = (_lib or load_library()).iodf_attn_append(
+        attn.handle, rows, q.data_ptr(), ldq, k.data_ptr(), ldk, v.data_ptr(), ldv, _flat(slot, attn, attn.int32, (rows,), "slot"),
+        _flat(position, attn, attn.int32, (rows,), "position"), _cache_of(cache, attn), _flat(q8, attn, attn.int8, (rows, heads, attn.head_dim), "q8"),
+        _flat(q_exp, attn, attn.uint8, (rows, heads), "q_exp"), _layer_stream(stream, attn.device))
+    if rc != 0:
+        raise IodfError(rc, "iodf_attn_append")
+    return q8, q_exp
+
+
+def iodf_attn_forward(attn, q8, q_exp, row_start, held, table, cache, y=None, stream=None):
+    """Attention of the rows of each request (row_start int32 [n + 1]) to the `held` tokens [n] that it has with them (the plan's held_out).
+    Returns y [rows, heads * head_dim] of the handle's output type; rows in no request keep what y held (zero where y is made here)."""
+    rows, n = q8.shape[0], held.shape[0]
+    if rows > _MOST or n > _MOST:
+        raise ValueError("%d rows of %d requests are out of range" % (rows, n))
+    width_y = attn.heads * attn.head_dim
+    if y is None:
+        import torch
+        y = _made(torch.zeros, (rows, width_y), attn.y_dtype, q8.device, stream)
+    ldy = _rows_of(y, attn, attn.y_dtype, rows, width_y, "y")
+    at, ldt, width = _table_of(table, attn, n)
+    rc = (_lib or load_library()).iodf_attn_forward(
+        attn.handle, rows, _flat(q8, attn, attn.int8, (rows, attn.heads, attn.head_dim), "q8"),
+        _flat(q_exp, attn, attn.uint8, (rows, attn.heads), "q_exp"), _flat(row_start, attn, attn.int32, (n + 1,), "row_start"),
+        _flat(held, attn, attn.int32, (n,), "held"), n, at, ldt, width, _cache_of(cache, attn), y.data_ptr(), ldy, _layer_stream(stream, attn.device))
+    if rc != 0:
+        raise IodfError(rc, "iodf_attn_forward")
+    return y
+
+
+def iodf_attn_check(attn, stream=None):
+    n = C.c_uint32(0)
+    rc = load_library().iodf_attn_check(attn.handle, _layer_stream(stream, attn.device), C.byref(n))
+    if rc != 0:
+        raise IodfError(rc, "iodf_attn_check (%d requests, rows or blocks)" % n.value)

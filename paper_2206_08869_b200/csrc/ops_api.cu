@@ -11,15 +11,12 @@
 #include <vector>
 
 #include "../../include/iodf.h"
+#include "api_common.h"
 #include "norm_kernel.h"
 #include "proj_kernel.h"
 #include "refine.h"
 
 using namespace iodf;
-
-typedef CUresult (*EncodeTiled)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 
 struct iodf_proj {
   int device = 0;
@@ -40,39 +37,10 @@ struct iodf_norm {
 
 namespace {
 
-int status_of(cudaError_t e) {
-  return e == cudaSuccess ? IODF_OK : e == cudaErrorMemoryAllocation ? IODF_ENOMEM : IODF_ECUDA;
-}
-
-// Makes the handle's device current for the duration of a call.
-class OnDevice {
- public:
-  explicit OnDevice(int device) {
-    err_ = cudaGetDevice(&prev_);
-    if (err_ == cudaSuccess && prev_ != device) {
-      err_ = cudaSetDevice(device);
-      restore_ = err_ == cudaSuccess;
-    }
-  }
-  ~OnDevice() { if (restore_) cudaSetDevice(prev_); }
-  OnDevice(const OnDevice&) = delete;
-  OnDevice& operator=(const OnDevice&) = delete;
-  cudaError_t error() const { return err_; }
-
- private:
-  int prev_ = -1;
-  bool restore_ = false;
-  cudaError_t err_;
-};
-
 bool capturing(cudaStream_t s) {
   cudaStreamCaptureStatus st = cudaStreamCaptureStatusNone;
   return cudaStreamIsCapturing(s, &st) != cudaSuccess || st != cudaStreamCaptureStatusNone;
 }
-
-bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
-size_t up_to(size_t n, size_t m) { return (n + m - 1) / m * m; }
 
 // Sum of |w| of one row (at most 32768 * 128).
 int magnitude(const int8_t* w, size_t n) {
@@ -157,12 +125,9 @@ int create_proj(const iodf_proj_desc& d, const int8_t* weights, size_t wn, const
   p.max_rank = d.max_rank;
   OnDevice on(device);
   if (on.error() != cudaSuccess) return IODF_ECUDA;
-  cudaDriverEntryPointQueryResult found;
-  void* entry = nullptr;
-  cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &entry, 12000, cudaEnableDefault, &found);
-  if (e != cudaSuccess || found != cudaDriverEntryPointSuccess) return IODF_ECUDA;
-  p.encode = reinterpret_cast<EncodeTiled>(entry);
-  e = configure_proj_kernels(device, &p.args);
+  p.encode = tensor_map_encoder();
+  if (!p.encode) return IODF_ECUDA;
+  cudaError_t e = configure_proj_kernels(device, &p.args);
   if (e == cudaSuccess) e = cudaMalloc(&p.d_mem, total);
   if (e != cudaSuccess) return status_of(e);
   uint8_t* m = static_cast<uint8_t*>(p.d_mem);
