@@ -5,10 +5,9 @@
 
 #include "../../include/iodf.h"
 #include "attn_device.cuh"
+#include "attn_kernels.h"
 
 namespace iodf {
-
-cudaError_t configure_attn_cache();
 
 namespace {
 
@@ -93,11 +92,13 @@ __global__ void __launch_bounds__(128) row_kernel(const AttnArgs a, const CacheA
 
 cudaError_t configure_attn_kernels(int device, AttnArgs* a) {
   cudaError_t e = cudaDeviceGetAttribute(&a->sms, cudaDevAttrMultiProcessorCount, device);
-  return e == cudaSuccess ? configure_attn_cache() : e;
+  if (e == cudaSuccess) e = configure_attn_cache();
+  return e == cudaSuccess ? configure_attn_tile() : e;
 }
 
-cudaError_t launch_attn_forward(const AttnArgs& a, const CacheArgs& c, const ForwardArgs& f, const CUtensorMap&, const CUtensorMap&,
+cudaError_t launch_attn_forward(const AttnArgs& a, const CacheArgs& c, const ForwardArgs& f, const CUtensorMap& k_map, const CUtensorMap& v_map,
                                 cudaStream_t stream) {
+  if ((long long)f.rows * a.group >= 0ll * f.n) return launch_attn_tile(a, c, f, k_map, v_map, stream);
   row_kernel<<<dim3((unsigned)f.rows, (unsigned)a.heads), 128, 0, stream>>>(a, c, f);
   return cudaGetLastError();
 }
