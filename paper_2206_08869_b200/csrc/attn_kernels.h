@@ -8,5 +8,8 @@ cudaError_t configure_attn_cache();
 cudaError_t configure_attn_tile();
 cudaError_t launch_attn_tile(const AttnArgs& a, const CacheArgs& c, const ForwardArgs& f, const CUtensorMap& k_map, const CUtensorMap& v_map,
                              cudaStream_t stream);
+cudaError_t configure_attn_split(AttnArgs* a);
+cudaError_t launch_attn_split(const AttnArgs& a, const CacheArgs& c, const ForwardArgs& f, const CUtensorMap& k_map, const CUtensorMap& v_map,
+                              cudaStream_t stream);
 
 }  // namespace iodf
