@@ -10,6 +10,7 @@ constexpr int kAttnBlock = 128;          // tokens of a block
 constexpr int kAttnMaxBlocks = 1024;     // of a request: sums of 131072 products of at most 128 * 127 fit 32 bits
 constexpr int kAttnMaxRequests = 16384;  // of a call of iodf_attn_plan: their prefix sums lie in shared memory
 constexpr int kAttnSplitRequests = 8192; // of a call that the kernel for few rows takes: so do its prefix sums
+constexpr int kAttnMaxTeam = 16;
 constexpr int kAttnMaxExp = 12;          // exponents above count as this
 constexpr int kRotaryHalf = 1, kRotaryInterleaved = 2;
 
@@ -26,7 +27,7 @@ struct AttnArgs {                        // what a handle holds
   const int2* out;                       // [heads * dim] {M0, s}
   uint32_t* status;                      // [0] a bounded wait gave up, [1] requests or rows that could not be served
   int sms;
-  int clusters[2];                       // clusters of 8 and 16 CTAs of the kernel for few rows that run at once
+  int clusters[kAttnMaxTeam + 1];        // of the kernel for few rows: clusters of 8 .. 16 CTAs that run at once
 };
 
 struct CacheArgs {

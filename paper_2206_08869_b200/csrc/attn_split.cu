@@ -3,12 +3,14 @@
 // A unit of work is up to 16 rows ((token, query head) pairs) of a request and the keys of one head of the cache. The keys are the
 // MMA's M and the rows its N, so that K and V go from the copy's shared memory straight into the tensor cores:
 //   S^T [128 keys][16] = K q^T,   O^T [dim][16] += V^T p^T
-// and a thread of the softmax owns a key. K is read first: t of every key stays in shared memory (16 bits below its warp's largest)
-// (and two bits of each) until the largest of all is known, then V. What bounds it is the reading of K and V, once each.
+// and a thread of the softmax owns a key. K is read first and its scores stay where they are, in tensor memory, until the largest of all
+// is known (26 blocks; t of further ones lies in shared memory, and where that is full K is read again), then V. What bounds it is the
+// reading of K and V, once each.
 //
-// Work is spread in teams: a request's blocks go to 1, 2, 4 ... CTAs of a cluster, by their number; teams that are smaller than a
+// Work is spread in teams: a request's blocks go to 1, 2, 4 or 8 CTAs of a cluster, by their number; teams that are smaller than a
 // cluster share it. CTAs of a team tell each other their largest t and, at the end, their sums, each CTA the owners of the dimensions,
 // through the cluster's shared memory. Clusters are persistent and take the large teams first; copies run ahead into the next unit.
+// Where units are fewer than clusters, a cluster is one team and as large as still lets all units run at once.
 #include <algorithm>
 
 #include "../../include/iodf.h"
@@ -20,48 +22,52 @@
 namespace iodf {
 namespace {
 
-constexpr int kCols = 16;                // rows of a unit: the N of the MMAs
-constexpr int kThreadsS = 384;           // warp 0 copies, 1 MMAs, 2 units, 3 queries, 4-7 and 8-11 softmax
-constexpr int kWarpsS = kThreadsS / 32;
-constexpr int kRingS = 5, kUnitsS = 3, kScores = 4;
+constexpr int kN = 16;                   // of the MMAs, the least; a unit has up to 4, 8 or 16 rows
+constexpr int kGroups = 4;               // of four softmax warps
+constexpr int kThreadsS = 128 + 128 * kGroups;           // warp 0 copies, 1 MMAs, 2 units, 3 queries, then softmax
+constexpr int kWarpsS = kThreadsS / 32, kSoft = 4 * kGroups;
+constexpr int kRingS = 5, kUnitsS = 3;
+constexpr int kScores = 30, kHeld = 26;  // S in tensor memory; of the first blocks they stay there, the last ones take turns
 constexpr int kTileBytes = 16384;        // of a slot: 128 rows of up to 128 bytes; V^T is read as 128 rows whatever the dimension
-constexpr int kWordBytes = kWeightSegments * 128;
-constexpr int kDistBytes = 65536;
-constexpr int kSumBytes = 128 * kCols * 8;
-constexpr int kPBytes = kCols * 128;     // weights of 128 keys
-constexpr int kQBytes = kCols * 128;
-constexpr int kSmemS = kWordBytes + kRingS * kTileBytes + kDistBytes + kSumBytes + 4 * kPBytes + 2 * kQBytes;
-constexpr int kMaxTeam = 16, kClasses = 5;                        // teams of 1, 2, 4, 8, 16
-constexpr int kLeastCluster = 8;
+constexpr int kDynamic = 200 * 1024;
+constexpr int kLeastCluster = 8, kMaxTeam = kAttnMaxTeam, kClasses = 5;             // teams of 1, 2, 4, 8; of a whole cluster
 constexpr int kMaxPart = kAttnMaxBlocks / kLeastCluster;          // blocks of one CTA
 constexpr int kMaxChunks = kAttnSplitRequests / 32;
+
+// Shared memory beside the ring. Operands of 16 rows of which only the first kCols count: the others may be anything.
+template <int kCols>
+struct Layout {
+  static constexpr int kOperand = kCols > 8 ? 2048 : 1024;
+  static constexpr int kP = kRingS * kTileBytes, kQ = kP + kGroups * 2 * kOperand, kSums = kQ + 2 * kOperand + 1024;
+  static constexpr int kKept = kSums + 128 * kCols * 8;
+  static constexpr int kKeptBlocks = (kDynamic - 1024 - kKept) / (kCols * 512);      // t of 128 keys, 32 bits
+};
 
 struct UnitS {
   int request, head, row0, len;
   int flat0, cols;                       // rows of the unit: [flat0, flat0 + cols)
   int held, b0, n;                       // this CTA's blocks: [b0, b0 + n)
-  int team, member;                      // CTAs, and which of them
+  int cls, team, member;                 // CTAs, and which of them
 };
 
 struct SharedS {
-  uint64_t full[kRingS], empty[kRingS], sfull[kScores], sempty[kScores], pfull[2], pempty[2], qfull[2], qempty[2];
+  uint64_t full[kRingS], empty[kRingS], sfull[kScores], sempty[kScores], pfull[kGroups], pempty[kGroups], qfull[2], qempty[2];
   uint64_t ofull, oempty, ufull[kUnitsS], uempty[kUnitsS], tops[kClasses], sums[kClasses];
   uint32_t abort_flag, tmem;
   int total[kClasses];                   // units of each class
   UnitS units[kUnitsS];
   int ids[kUnitsS][kMaxPart];            // blocks; -1: outside the cache, nobody sees it
   uint8_t ek[kUnitsS][kMaxPart], ev[kUnitsS][kMaxPart];
-  int top[8][kCols], vexp[8][kCols];     // of the softmax warps
-  long long sum[8][kCols];
-  int vtop[kCols];                       // V of each row, over the team
-  int base[kDistBytes / 64];             // [block][quarter][row]: the largest t of a warp's keys,
-  uint2 high[kDistBytes / 64];           // of each key bit 16 of its distance to that, and whether it is seen and that less than 2^17
-  int team_top[kMaxTeam][kCols], team_vexp[kMaxTeam][kCols];
-  long long team_sum[kMaxTeam][kCols];
+  int top[kSoft][kN], vexp[kSoft][kN];   // of the softmax warps
+  long long sum[kSoft][kN];
+  int vtop[kN];                          // V of each row, over the team
+  int team_top[kMaxTeam][kN], team_vexp[kMaxTeam][kN];
+  long long team_sum[kMaxTeam][kN];
 };
 
 struct SplitArgs {
   int cluster, per_cta;                  // CTAs of a cluster; blocks that one CTA takes before the team grows
+  int one_team;                          // a cluster is a team
   int chunks;                            // of 32 requests
 };
 
@@ -79,29 +85,33 @@ struct RingS {
 // What a request asks for: its rows, its units of each cache head, the class of its teams.
 struct Ask {
   int start, len, held, tiles, cls;
-  __device__ __forceinline__ Ask(const AttnArgs& a, const ForwardArgs& f, const SplitArgs& s, int q) : start(0), len(0), held(0), tiles(0), cls(0) {
+  __device__ __forceinline__ Ask(const AttnArgs& a, const ForwardArgs& f, const SplitArgs& s, int cols, int q)
+      : start(0), len(0), held(0), tiles(0), cls(0) {
     if (q >= f.n) return;
     const int s0 = f.row_start[q], s1 = f.row_start[q + 1];
     held = min(max(f.held[q], 0), f.width * kAttnBlock);
     start = min(max(s0, 0), f.rows);
     len = max(min(max(s1, 0), f.rows) - start, 0);
-    tiles = (len * a.group + kCols - 1) / kCols;
+    tiles = (len * a.group + cols - 1) / cols;
     const int first = visible(a, held - len, held).first / kAttnBlock, blocks = (held + kAttnBlock - 1) / kAttnBlock - first;
-    while (s.cluster >> (cls + 1) && blocks > s.per_cta << cls) ++cls;
+    if (s.one_team) cls = kClasses - 1;
+    else while (s.cluster >> (cls + 1) && blocks > s.per_cta << cls) ++cls;
   }
 };
 
-template <int D>
+template <int D, int kCols>
 __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
                                                              const AttnArgs a, const CacheArgs c, const ForwardArgs f, const SplitArgs s) {
+  typedef Layout<kCols> At;
   extern __shared__ uint8_t raw[];
-  uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 8191) & ~(uintptr_t)8191);
+  uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
   __shared__ SharedS sh;
+  __shared__ int table[kWeightSegments * 32];           // a copy for each lane: no bank is asked twice
   __shared__ int before[kClasses][kMaxChunks + 1];      // units of each class before a chunk of 32 requests
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t words = ptx::smem_u32(smem), ring = words + kWordBytes, dist = ring + kRingS * kTileBytes, osum = dist + kDistBytes,
-                 pbuf = osum + kSumBytes, qbuf = pbuf + 4 * kPBytes;
-  const int* const osums = reinterpret_cast<const int*>(smem + (osum - words));
+  const uint32_t ring = ptx::smem_u32(smem), pbuf = ring + At::kP, qbuf = ring + At::kQ, osum = ring + At::kSums;
+  const int* const osums = reinterpret_cast<const int*>(smem + At::kSums);
+  int* const kept = reinterpret_cast<int*>(smem + At::kKept);
   volatile uint32_t* const abort_flag = &sh.abort_flag;
   const int rank = (int)ptx::cluster_rank();
   if (tid == 0) {
@@ -112,26 +122,26 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
     init(sh.empty, kRingS, 1);
     init(sh.sfull, kScores, 1);
     init(sh.sempty, kScores, 4);
-    init(sh.pfull, 2, 4);
-    init(sh.pempty, 2, 1);
+    init(sh.pfull, kGroups, 4);
+    init(sh.pempty, kGroups, 1);
     init(sh.qfull, 2, 1);
     init(sh.qempty, 2, 1);
     init(&sh.ofull, 1, 1);
-    init(&sh.oempty, 1, 8);
+    init(&sh.oempty, 1, kSoft);
     init(sh.ufull, kUnitsS, 1);
-    init(sh.uempty, kUnitsS, 11);
+    init(sh.uempty, kUnitsS, 3 + kSoft);
     for (int i = 0; i < kClasses; ++i) {
-      init(&sh.tops[i], 1, 1 << i);
-      init(&sh.sums[i], 1, 1 << i);
+      init(&sh.tops[i], 1, i == kClasses - 1 ? s.cluster : 1 << i);
+      init(&sh.sums[i], 1, i == kClasses - 1 ? s.cluster : 1 << i);
     }
     ptx::mbar_init_fence();
     sh.abort_flag = 0;
   }
   ptx::cluster_arrive();                                // every CTA runs, its barriers are set up
-  if (warp == 2) ptx::tmem_alloc(ptx::smem_u32(&sh.tmem), 128);
-  for (int i = tid; i < kWeightSegments * 32; i += kThreadsS) reinterpret_cast<int*>(smem)[i] = weight_word(i / 32);
+  if (warp == 2) ptx::tmem_alloc(ptx::smem_u32(&sh.tmem), 512);
+  for (int i = tid; i < kWeightSegments * 32; i += kThreadsS) table[i] = weight_word(i / 32);
   for (int k = warp; k < s.chunks; k += kWarpsS) {
-    const Ask ask(a, f, s, k * 32 + lane);
+    const Ask ask(a, f, s, kCols, k * 32 + lane);
 #pragma unroll
     for (int i = 0; i < kClasses; ++i) {
       const int n = __reduce_add_sync(0xFFFFFFFFu, ask.cls == i ? ask.tiles * a.kv : 0);
@@ -160,7 +170,7 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
     }
   }
   __syncthreads();
-  const uint32_t tmem = sh.tmem, o_hi = tmem + kScores * kCols, o_lo = o_hi + kCols;
+  const uint32_t tmem = sh.tmem, o_hi = tmem + kScores * kN, o_lo = o_hi + kN;
   auto wait = [&](uint64_t* bar, uint32_t phase) { return ptx::quick_wait(abort_flag, a.status, bar, phase, kSpinLimit); };
   auto warp_wait = [&](uint64_t* bar, uint32_t phase) { return __all_sync(0xFFFFFFFFu, wait(bar, phase)) != 0; };
   auto take = [&](const RingS& r, UnitS* u) {
@@ -174,8 +184,10 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
     ptx::mbar_acquire_cluster(ptx::smem_u32(bar), phase);
     return true;
   };
-  // blocks whose t are kept; the rest's scores are computed twice
-  auto kept = [](const UnitS& u) { return min(u.n, kDistBytes / (256 * u.cols)); };
+  // blocks whose scores or t are kept; the rest's scores are computed twice
+  constexpr int kKeep = kHeld + At::kKeptBlocks;
+  // where the scores of the unit's block i are: all of a call's uses of a slot are counted in bits, one for each
+  auto slot_of = [](int i) { return i < kHeld ? i : kHeld + (i - kHeld) % (kScores - kHeld); };
 
   if (warp == 0) {
     if (ptx::elect_one()) {
@@ -192,10 +204,9 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
       };
       for (; ok && take(ur, &u); ur.next(kUnitsS)) {
         const int* ids = sh.ids[ur.slot];
-        const int keep = kept(u);
         for (int i = 0; i < u.n && ok; ++i) copy(&kmap, (max(ids[i], 0) * a.kv + u.head) * kAttnBlock, D);
         for (int i = 0; i < u.n && ok; ++i) {
-          if (i >= keep) copy(&kmap, (max(ids[i], 0) * a.kv + u.head) * kAttnBlock, D);
+          if (i >= kKeep) copy(&kmap, (max(ids[i], 0) * a.kv + u.head) * kAttnBlock, D);
           copy(&vmap, (max(ids[i], 0) * a.kv + u.head) * D, D);
         }
         ptx::mbar_arrive(ptx::smem_u32(&sh.uempty[ur.slot]));
@@ -205,44 +216,44 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
     __syncwarp();
   } else if (warp == 1) {
     if (ptx::elect_one()) {
-      constexpr uint32_t id_s = idesc_i8(128, kCols, false, false), id_hi = idesc_i8(128, kCols, false, true), id_lo = idesc_i8(128, kCols, false, false);
+      constexpr uint32_t id_s = idesc_i8(128, kN, false, false), id_hi = idesc_i8(128, kN, false, true), id_lo = idesc_i8(128, kN, false, false);
       constexpr uint32_t hi_d = rows_hi(D), hi_128 = rows_hi(128);
-      RingS r, ur, qr, sr, orr;
-      uint32_t pphases = 0;
+      RingS r, ur, qr, orr;
+      uint32_t pphases = 0, sphases = 0;
       UnitS u;
       bool ok = true;
-      auto scores = [&](uint32_t q) {
-        ok = ok && wait(&sh.full[r.slot], r.phase) && wait(&sh.sempty[sr.slot], sr.phase ^ 1);
+      auto scores = [&](uint32_t q, int slot) {
+        ok = ok && wait(&sh.full[r.slot], r.phase) && wait(&sh.sempty[slot], (sphases >> slot & 1) ^ 1);
         if (!ok) return;
         ptx::tc_fence_after();
         const uint32_t k = rows_lo(ring + r.slot * kTileBytes);
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) ptx::umma_i8_hl(tmem + sr.slot * kCols, k + 2 * i, hi_d, q + 2 * i, hi_d, id_s, i > 0);
+        for (int i = 0; i < D / 32; ++i) ptx::umma_i8_hl(tmem + slot * kN, k + 2 * i, hi_d, q + 2 * i, hi_d, id_s, i > 0);
         ptx::umma_commit(ptx::smem_u32(&sh.empty[r.slot]));
-        ptx::umma_commit(ptx::smem_u32(&sh.sfull[sr.slot]));
+        ptx::umma_commit(ptx::smem_u32(&sh.sfull[slot]));
         r.next(kRingS);
-        sr.next(kScores);
+        sphases ^= 1u << slot;
       };
       for (; ok && take(ur, &u); ur.next(kUnitsS)) {
-        const int keep = kept(u);
         ok = wait(&sh.qfull[qr.slot], qr.phase);
         ptx::tc_fence_after();
-        const uint32_t q = rows_lo(qbuf + qr.slot * kQBytes);
-        for (int i = 0; i < u.n && ok; ++i) scores(q);
+        const uint32_t q = rows_lo(qbuf + qr.slot * At::kOperand);
+        for (int i = 0; i < u.n && ok; ++i) scores(q, slot_of(i));
         for (int i = 0; i < u.n && ok; ++i) {
-          if (i >= keep) scores(q);
+          const int g = i % kGroups;
+          if (i >= kKeep) scores(q, slot_of(i));
           if (i == 0) ok = ok && wait(&sh.oempty, orr.phase ^ 1);
-          ok = ok && wait(&sh.pfull[i & 1], (pphases >> (i & 1)) & 1) && wait(&sh.full[r.slot], r.phase);
+          ok = ok && wait(&sh.pfull[g], pphases >> g & 1) && wait(&sh.full[r.slot], r.phase);
           if (!ok) break;
           ptx::tc_fence_after();
-          const uint32_t v = rows_lo(ring + r.slot * kTileBytes), p = rows_lo(pbuf + (i & 1) * 2 * kPBytes);
+          const uint32_t v = rows_lo(ring + r.slot * kTileBytes), p = rows_lo(pbuf + g * 2 * At::kOperand);
 #pragma unroll
           for (int k = 0; k < 4; ++k) ptx::umma_i8_hl(o_hi, v + 2 * k, hi_128, p + 2 * k, hi_128, id_hi, i > 0 || k > 0);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) ptx::umma_i8_hl(o_lo, v + 2 * k, hi_128, p + (kPBytes >> 4) + 2 * k, hi_128, id_lo, i > 0 || k > 0);
+          for (int k = 0; k < 4; ++k) ptx::umma_i8_hl(o_lo, v + 2 * k, hi_128, p + (At::kOperand >> 4) + 2 * k, hi_128, id_lo, i > 0 || k > 0);
           ptx::umma_commit(ptx::smem_u32(&sh.empty[r.slot]));
-          ptx::umma_commit(ptx::smem_u32(&sh.pempty[i & 1]));
-          pphases ^= 1u << (i & 1);
+          ptx::umma_commit(ptx::smem_u32(&sh.pempty[g]));
+          pphases ^= 1u << g;
           r.next(kRingS);
         }
         if (ok && u.n) {
@@ -253,19 +264,20 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
         qr.next(2);
         ptx::mbar_arrive(ptx::smem_u32(&sh.uempty[ur.slot]));
       }
-      for (int i = 0; ok && i < 2; ++i) ok = wait(&sh.pempty[i], ((pphases >> i) & 1) ^ 1);
+      for (int i = 0; ok && i < kGroups; ++i) ok = wait(&sh.pempty[i], (pphases >> i & 1) ^ 1);
     }
     __syncwarp();
   } else if (warp == 2) {
     // Units: items of the cluster, class by class from the largest teams on; in one item a cluster's CTAs work in teams of one size.
     RingS ur;
     bool ok = true;
-    const int clusters = (int)gridDim.x / s.cluster, top_class = 31 - __clz(s.cluster);
+    const int clusters = (int)gridDim.x / s.cluster;
     int item = (int)blockIdx.x / s.cluster;
-    for (int cls = top_class; cls >= 0 && ok; --cls) {
-      const int teams = s.cluster >> cls, items = (sh.total[cls] + teams - 1) / teams;
+    for (int cls = kClasses - 1; cls >= 0 && ok; --cls) {
+      const int team = cls == kClasses - 1 ? s.cluster : 1 << cls, teams = max(1, s.cluster / team);
+      const int items = (sh.total[cls] + teams - 1) / teams;
       for (; item < items && ok; item += clusters) {
-        const int unit = item * teams + (rank >> cls);
+        const int unit = item * teams + rank / team;
         if (unit >= sh.total[cls]) continue;
         int lo = 0, hi = s.chunks - 1;                  // the chunk that holds it
         while (lo < hi) {
@@ -273,7 +285,7 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
           if (before[cls][mid + 1] > unit) hi = mid;
           else lo = mid + 1;
         }
-        const Ask ask(a, f, s, lo * 32 + lane);
+        const Ask ask(a, f, s, kCols, lo * 32 + lane);
         const int mine = ask.cls == cls ? ask.tiles * a.kv : 0;
         int upto = mine;
 #pragma unroll
@@ -292,8 +304,9 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
         u.head = at % a.kv;
         u.flat0 = at / a.kv * kCols;
         u.cols = min(kCols, u.len * a.group - u.flat0);
-        u.team = 1 << cls;
-        u.member = rank & (u.team - 1);
+        u.cls = cls;
+        u.team = team;
+        u.member = rank % team;
         const Range low = visible(a, u.held - u.len + u.flat0 / a.group, u.held);
         const Range high = visible(a, u.held - u.len + (u.flat0 + u.cols - 1) / a.group, u.held);
         const int b0 = low.first / kAttnBlock, n = high.last <= low.first ? 0 : (high.last + kAttnBlock - 1) / kAttnBlock - b0;
@@ -336,7 +349,7 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
         const int r = i / (D / 16), piece = i % (D / 16), flat = u.flat0 + r;
         const long long row = u.row0 + flat / a.group;
         const int4 v = *reinterpret_cast<const int4*>(f.q8 + (row * a.heads + u.head * a.group + flat % a.group) * D + piece * 16);
-        ptx::sts128(qbuf + qr.slot * kQBytes + swizzled(r, piece, D), v.x, v.y, v.z, v.w);
+        ptx::sts128(qbuf + qr.slot * At::kOperand + swizzled(r, piece, D), v.x, v.y, v.z, v.w);
       }
       ptx::fence_async_smem();
       __syncwarp();
@@ -348,14 +361,14 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
     for (int i = 0; ok && i < 2; ++i, qr.next(2)) ok = wait(&sh.qempty[qr.slot], qr.phase ^ 1);
   } else {
     const int w = (warp - 4) >> 2, quarter = warp & 3, key = quarter * 32 + lane, me = warp - 4;
-    const uint32_t lanes = (uint32_t)(quarter * 32) << 16, my_words = words + lane * 4;
-    const uint32_t p_hi = pbuf + w * 2 * kPBytes, p_lo = p_hi + kPBytes;
-    RingS ur, sr, orr;
-    uint32_t pphase = 1, team_phases = 0;
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const uint32_t p_hi = pbuf + w * 2 * At::kOperand, p_lo = p_hi + At::kOperand;
+    RingS ur, orr;
+    uint32_t pphase = 1, team_phases = 0, sphases = 0;
     UnitS u;
     bool ok = true;
-    while (ptx::all_agree(1, 256, take(ur, &u))) {
-      const int keep = kept(u), nc = u.cols, cls = 31 - __clz(u.team);
+    while (ptx::all_agree(1, 32 * kSoft, take(ur, &u))) {
+      const int nc = u.cols;
       // lane c < cols has the constants of row c
       const int flat = u.flat0 + min(lane, nc - 1);
       const long long row = u.row0 + flat / a.group;
@@ -365,64 +378,67 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
       const int whole0 = (__reduce_max_sync(0xFFFFFFFFu, see.first) + kAttnBlock - 1) / kAttnBlock;
       const int whole1 = max(__reduce_min_sync(0xFFFFFFFFu, see.last), 0) / kAttnBlock;
       int T = INT32_MIN, V = 0;                         // of row `lane`
-      // t of the keys of block i in the S that is next, seen or not: lowest
+      // t of the keys of block i from S, lowest where it is not seen
       auto octaves = [&](int i, int (&t)[kCols]) {
-        uint32_t x[16];
-        ptx::tmem_ld16(tmem + lanes + sr.slot * kCols, x);
-        ptx::tmem_ld_wait16(x);
+        uint32_t x[kCols];
+        if constexpr (kCols == 4) ptx::tmem_ld4(tmem + lanes + slot_of(i) * kN, x);
+        else if constexpr (kCols == 8) ptx::tmem_ld8(tmem + lanes + slot_of(i) * kN, x);
+        else ptx::tmem_ld16(tmem + lanes + slot_of(i) * kN, x);
         const int b = u.b0 + i, k = b * kAttnBlock + key;
         const int W = score_multiplier(a.score_m0, eq + sh.ek[ur.slot][i], a.score_s);
         const bool bad = sh.ids[ur.slot][i] < 0, whole = b >= whole0 && b < whole1 && !bad;
+        if constexpr (kCols == 4) ptx::tmem_ld_wait4(x);
+        else if constexpr (kCols == 8) ptx::tmem_ld_wait8(x);
+        else ptx::tmem_ld_wait16(x);
 #pragma unroll
-        for (int e = 0; e < kCols; ++e) {
-          if (e < nc) {
-            t[e] = score_octaves((int)x[e], __shfl_sync(0xFFFFFFFFu, W, e));
-            if (!whole) {
-              const int first = __shfl_sync(0xFFFFFFFFu, see.first, e), last = __shfl_sync(0xFFFFFFFFu, see.last, e);
-              if (bad || k < first || k >= last) t[e] = INT32_MIN;
-            }
+        for (int e = 0; e < kCols; ++e) t[e] = score_octaves((int)x[e], __shfl_sync(0xFFFFFFFFu, W, e));
+        if (!whole) {
+#pragma unroll
+          for (int e = 0; e < kCols; ++e) {
+            const int first = __shfl_sync(0xFFFFFFFFu, see.first, e), last = __shfl_sync(0xFFFFFFFFu, see.last, e);
+            if (bad || k < first || k >= last) t[e] = INT32_MIN;
           }
         }
+        return whole;
+      };
+      auto release = [&](int i) {                       // S of block i may be written over
         ptx::tc_fence_before();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.sempty[sr.slot]));
+        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.sempty[slot_of(i)]));
       };
-      // S buffers go round over all blocks of all units; a group skips the other's
-      for (int i = 0; i < u.n; ++i, sr.next(kScores)) {
-        if ((i & 1) != w) continue;
-        ok = ok && warp_wait(&sh.sfull[sr.slot], sr.phase);
-        if (!ok) continue;
+      int tops[kCols];
+#pragma unroll
+      for (int e = 0; e < kCols; ++e) tops[e] = INT32_MIN;
+      for (int i = w; i < u.n && ok; i += kGroups) {
+        ok = warp_wait(&sh.sfull[slot_of(i)], sphases >> slot_of(i) & 1);
+        if (!ok) break;
         ptx::tc_fence_after();
-        int t[kCols], base = INT32_MIN;
-        uint2 high = make_uint2(0, 0);
-        octaves(i, t);
+        int t[kCols];
+        const bool whole = octaves(i, t);
+        if (i >= kHeld) {
+          release(i);
+          sphases ^= 1u << slot_of(i);
+        }
+        if (whole) V = max(V, (int)sh.ev[ur.slot][i]);
 #pragma unroll
         for (int e = 0; e < kCols; ++e) {
-          if (e < nc) {
-            const int top = __reduce_max_sync(0xFFFFFFFFu, t[e]);
-            if (lane == e) base = top;
-            if (i < keep) {                             // from 2^17 on weights are 0
-              const uint32_t d = (uint32_t)top - (uint32_t)t[e];
-              const uint32_t bit = __ballot_sync(0xFFFFFFFFu, (d >> 16) & 1), near = __ballot_sync(0xFFFFFFFFu, t[e] != INT32_MIN && d < 1u << 17);
-              if (lane == e) high = make_uint2(bit, near);
-              asm volatile("st.shared.u16 [%0], %1;" ::"r"(dist + ((i * nc + e) * kAttnBlock + key) * 2), "h"((uint16_t)d) : "memory");
-            }
-          }
+          tops[e] = max(tops[e], t[e]);
+          if (!whole && __any_sync(0xFFFFFFFFu, t[e] != INT32_MIN) && lane == e) V = max(V, (int)sh.ev[ur.slot][i]);
+          if (i >= kHeld && i < kKeep) kept[((i - kHeld) * kCols + e) * kAttnBlock + key] = t[e];
         }
-        if (i < keep && lane < nc) {
-          sh.base[(i * 4 + quarter) * nc + lane] = base;
-          sh.high[(i * 4 + quarter) * nc + lane] = high;
-        }
-        if (base != INT32_MIN) V = max(V, (int)sh.ev[ur.slot][i]);
-        T = max(T, base);
+      }
+#pragma unroll
+      for (int e = 0; e < kCols; ++e) {
+        const int top = __reduce_max_sync(0xFFFFFFFFu, tops[e]);
+        if (lane == e) T = top;
       }
       if (lane < kCols) {
         sh.top[me][lane] = T;
         sh.vexp[me][lane] = V;
       }
-      ptx::named_barrier(1, 256);
+      ptx::named_barrier(1, 32 * kSoft);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < kSoft; ++i) {
         T = max(T, sh.top[i][lane & (kCols - 1)]);
         V = max(V, sh.vexp[i][lane & (kCols - 1)]);
       }
@@ -438,80 +454,84 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
               ptx::st_cluster(vexp + 4 * e, (uint32_t)v);
             }
           }
-          if (lane < u.team) ptx::mbar_arrive_cluster(ptx::cluster_addr(ptx::smem_u32(&sh.tops[cls]), to));
+          if (lane < u.team) ptx::mbar_arrive_cluster(ptx::cluster_addr(ptx::smem_u32(&sh.tops[u.cls]), to));
           __syncwarp();
         }
-        ok = ok && team_wait(&sh.tops[cls], (team_phases >> cls) & 1);
+        ok = ok && team_wait(&sh.tops[u.cls], team_phases >> u.cls & 1);
         for (int m = 0; m < u.team; ++m) {
           T = max(T, sh.team_top[m][lane & (kCols - 1)]);
           V = max(V, sh.team_vexp[m][lane & (kCols - 1)]);
         }
       }
       if (me == 0 && lane < kCols) sh.vtop[lane] = V;
-      long long L = 0;                                  // of row `lane`
-      for (int i = 0; i < u.n; ++i) {
-        const bool again = i >= keep;
-        if ((i & 1) == w) {
-          ok = ok && warp_wait(&sh.pempty[w], pphase) && (!again || warp_wait(&sh.sfull[sr.slot], sr.phase));
-          pphase ^= 1;
-        }
-        if ((i & 1) == w && ok) {
-          ptx::tc_fence_after();
-          const int below = max(V - sh.ev[ur.slot][i], 0);
-          int off = -(T + 8192 * below), t[kCols];
-          uint2 high = make_uint2(0, 0);
-          if (again) {
-            octaves(i, t);
-          } else {
-            off += sh.base[(i * 4 + quarter) * nc + min(lane, nc - 1)];
-            high = sh.high[(i * 4 + quarter) * nc + min(lane, nc - 1)];
-          }
+      long long Ls[kCols];
 #pragma unroll
-          for (int e = 0; e < kCols; ++e) {
-            if (e < nc) {
-              const int from = __shfl_sync(0xFFFFFFFFu, off, e);
-              int n;
-              if (again) {
-                n = t[e] == INT32_MIN ? kWeightLow : t[e] + from;
-              } else {
-                uint16_t d;
-                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(d) : "r"(dist + ((i * nc + e) * kAttnBlock + key) * 2));
-                const uint32_t bit = __shfl_sync(0xFFFFFFFFu, high.x, e) >> lane & 1, near = __shfl_sync(0xFFFFFFFFu, high.y, e) >> lane & 1;
-                n = near ? from - (int)(d + (bit << 16)) : kWeightLow;
-              }
-              n = max(n, kWeightLow);
-              const uint32_t x = weight_bits(n, (int)ptx::lds32((uint32_t)(n & ((kWeightSegments - 1) << 7)) | my_words));
-              const uint32_t at = (uint32_t)(e * 128 + (((key >> 4) ^ (e & 7)) << 4) + (key & 15));
-              asm volatile("st.shared.u8 [%0], %1;" ::"r"(p_hi + at), "r"(x >> 8) : "memory");
-              asm volatile("st.shared.u8 [%0], %1;" ::"r"(p_lo + at), "r"(x ^ 0x80u) : "memory");
-              const int sum = __reduce_add_sync(0xFFFFFFFFu, (int)(x - kWeightBias));
-              if (lane == e) L += (long long)sum << below;
-            }
-          }
-          ptx::tc_fence_before();
-          ptx::fence_async_smem();
-          __syncwarp();
-          if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.pfull[w]));
+      for (int e = 0; e < kCols; ++e) Ls[e] = 0;
+      for (int i = w; i < u.n && ok; i += kGroups) {
+        ok = warp_wait(&sh.pempty[w], pphase) && (i < kKeep || warp_wait(&sh.sfull[slot_of(i)], sphases >> slot_of(i) & 1));
+        pphase ^= 1;
+        if (!ok) break;
+        ptx::tc_fence_after();
+        const int below = max(V - sh.ev[ur.slot][i], 0), off = -(T + 8192 * below);
+        int t[kCols];
+        if (i < kHeld || i >= kKeep) {
+          octaves(i, t);
+          release(i);
+          sphases ^= 1u << slot_of(i);
+        } else {
+#pragma unroll
+          for (int e = 0; e < kCols; ++e) t[e] = kept[((i - kHeld) * kCols + e) * kAttnBlock + key];
         }
-        if (again) sr.next(kScores);
+#pragma unroll
+        for (int e = 0; e < kCols; ++e) {
+          const int down = __shfl_sync(0xFFFFFFFFu, off, e), by = __shfl_sync(0xFFFFFFFFu, below, e);
+          const int n = t[e] == INT32_MIN ? kWeightLow : max(t[e] + down, kWeightLow);
+          const uint32_t x = weight_bits(n, *reinterpret_cast<const int*>(reinterpret_cast<const char*>(table) + ((n & ((kWeightSegments - 1) << 7)) | lane * 4)));
+          const uint32_t at = (uint32_t)(e * 128 + (((key >> 4) ^ (e & 7)) << 4) + (key & 15));
+          asm volatile("st.shared.u8 [%0], %1;" ::"r"(p_hi + at), "r"(x >> 8) : "memory");
+          asm volatile("st.shared.u8 [%0], %1;" ::"r"(p_lo + at), "r"(x ^ 0x80u) : "memory");
+          Ls[e] += (x - kWeightBias) << by;             // below 2^28
+        }
+        ptx::tc_fence_before();
+        ptx::fence_async_smem();
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.pfull[w]));
+      }
+      long long L = 0;                                  // of row `lane`
+#pragma unroll
+      for (int e = 0; e < kCols; ++e) {                 // below 2^35 in a thread: summed in two parts
+        const uint32_t low = __reduce_add_sync(0xFFFFFFFFu, (uint32_t)(Ls[e] & 0xFFFFF)), high = __reduce_add_sync(0xFFFFFFFFu, (uint32_t)(Ls[e] >> 20));
+        if (lane == e) L = ((long long)high << 20) + low;
       }
       if (lane < kCols) sh.sum[me][lane] = L;
-      ptx::named_barrier(1, 256);
+      ptx::named_barrier(1, 32 * kSoft);
       L = 0;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) L += sh.sum[i][lane & (kCols - 1)];
-      uint32_t hi[16], lo[16];
+      for (int i = 0; i < kSoft; ++i) L += sh.sum[i][lane & (kCols - 1)];
+      uint32_t hi[kCols], lo[kCols];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) hi[e] = lo[e] = 0;
+      for (int e = 0; e < kCols; ++e) hi[e] = lo[e] = 0;
       if (u.n) {
         ok = ok && warp_wait(&sh.ofull, orr.phase);
         orr.next(1);
         ptx::tc_fence_after();
         if (ok) {
-          ptx::tmem_ld16(o_hi + lanes, hi);
-          ptx::tmem_ld16(o_lo + lanes, lo);
-          ptx::tmem_ld_wait16(hi);
-          ptx::tmem_ld_wait16_nosync(lo);
+          if constexpr (kCols == 4) {
+            ptx::tmem_ld4(o_hi + lanes, hi);
+            ptx::tmem_ld4(o_lo + lanes, lo);
+            ptx::tmem_ld_wait4(hi);
+            ptx::tmem_ld_wait4_nosync(lo);
+          } else if constexpr (kCols == 8) {
+            ptx::tmem_ld8(o_hi + lanes, hi);
+            ptx::tmem_ld_wait8(hi);
+            ptx::tmem_ld8(o_lo + lanes, lo);
+            ptx::tmem_ld_wait8(lo);
+          } else {
+            ptx::tmem_ld16(o_hi + lanes, hi);
+            ptx::tmem_ld16(o_lo + lanes, lo);
+            ptx::tmem_ld_wait16(hi);
+            ptx::tmem_ld_wait16_nosync(lo);
+          }
         }
         ptx::tc_fence_before();
         __syncwarp();
@@ -533,7 +553,7 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
             rec.a = __shfl_sync(0xFFFFFFFFu, mine.a, e);
             rec.V = __shfl_sync(0xFFFFFFFFu, V, e);
             const bool any = __shfl_sync(0xFFFFFFFFu, (int)(L > 0), e) != 0;
-            if ((e & 1) == w && key < D && ok) {
+            if (e % kGroups == w && key < D && ok) {
               const long long A = ((long long)(int)hi[e] << 8) + (int)lo[e];
               const int at = (u.head * a.group + (u.flat0 + e) % a.group) * D + key;
               store(e, key, requantised(any ? quotient(A, rec) : 0, a.out[at], a.lo, a.hi));
@@ -541,12 +561,12 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
           }
         }
       } else {
-        const int own = D / u.team;                     // dimensions that a CTA finishes
+        const int own = (D + u.team - 1) / u.team;      // dimensions that a CTA finishes
         if (key < D) {
           const uint32_t to = ptx::cluster_addr(osum + (uint32_t)((u.member * own + key % own) * kCols * 8), (uint32_t)(rank - u.member + key / own));
 #pragma unroll
           for (int e = 0; e < kCols; ++e) {
-            if (e < nc && (e & 1) == w) {
+            if (e < nc && e % kGroups == w) {
               ptx::st_cluster(to + 8 * e, hi[e]);
               ptx::st_cluster(to + 8 * e + 4, lo[e]);
             }
@@ -563,13 +583,14 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
             }
           }
         }
-        ptx::named_barrier(1, 256);                     // all of this CTA's sums are on their way
-        if (me == 0 && lane < u.team) ptx::mbar_arrive_cluster(ptx::cluster_addr(ptx::smem_u32(&sh.sums[cls]), peer));
+        ptx::named_barrier(1, 32 * kSoft);              // all of this CTA's sums are on their way
+        if (me == 0 && lane < u.team) ptx::mbar_arrive_cluster(ptx::cluster_addr(ptx::smem_u32(&sh.sums[u.cls]), peer));
         __syncwarp();
-        ok = ok && team_wait(&sh.sums[cls], (team_phases >> cls) & 1);
-        team_phases ^= 1u << cls;
-        for (int i = tid - 128; ok && i < own * nc; i += 256) {
+        ok = ok && team_wait(&sh.sums[u.cls], team_phases >> u.cls & 1);
+        team_phases ^= 1u << u.cls;
+        for (int i = tid - 128; ok && i < own * nc; i += 32 * kSoft) {
           const int dl = i % own, e = i / own, dim = u.member * own + dl;
+          if (dim >= D) continue;
           long long A = 0, all = 0;
           for (int m = 0; m < u.team; ++m) {
             const int* o = osums + ((m * own + dl) * kCols + e) * 2;
@@ -588,22 +609,30 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
-  if (warp == 2) ptx::tmem_dealloc(tmem, 128);
+  if (warp == 2) ptx::tmem_dealloc(tmem, 512);
   ptx::cluster_arrive();                                // nobody leaves while another CTA may still write into its memory
   ptx::cluster_wait();
 }
 
+template <int D, int kCols>
+cudaError_t configure() {
+  static_assert(sizeof(SharedS) + 4 * (kWeightSegments * 32 + kClasses * (kMaxChunks + 1)) + kDynamic <= 227 * 1024, "shared memory");
+  cudaError_t e = cudaFuncSetAttribute(split_kernel<D, kCols>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynamic);
+  return e == cudaSuccess ? cudaFuncSetAttribute(split_kernel<D, kCols>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) : e;
+}
+
 template <int D>
-cudaError_t configure(AttnArgs* a) {
-  cudaError_t e = cudaFuncSetAttribute(split_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmemS + 8192);
-  return e == cudaSuccess ? cudaFuncSetAttribute(split_kernel<D>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) : e;
+cudaError_t configure() {
+  cudaError_t e = configure<D, 4>();
+  if (e == cudaSuccess) e = configure<D, 8>();
+  return e == cudaSuccess ? configure<D, 16>() : e;
 }
 
 cudaLaunchConfig_t config(int cluster, int clusters, cudaLaunchAttribute* attr, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(cluster * clusters));
   cfg.blockDim = dim3(kThreadsS);
-  cfg.dynamicSmemBytes = kSmemS + 8192;
+  cfg.dynamicSmemBytes = kDynamic;
   cfg.stream = stream;
   attr->id = cudaLaunchAttributeClusterDimension;
   attr->val.clusterDim.x = (unsigned)cluster;
@@ -613,34 +642,52 @@ cudaLaunchConfig_t config(int cluster, int clusters, cudaLaunchAttribute* attr, 
   return cfg;
 }
 
+template <int D, int kCols>
+cudaError_t launch(const AttnArgs& a, const CacheArgs& c, const ForwardArgs& f, const CUtensorMap& k_map, const CUtensorMap& v_map,
+                   cudaStream_t stream) {
+  const long long units = ((long long)f.rows * a.group / kCols + f.n) * a.kv;             // at most
+  SplitArgs s;
+  s.chunks = (f.n + 31) / 32;
+  s.cluster = kLeastCluster;
+  s.one_team = 0;
+  for (int n = std::min(kMaxTeam, f.width); n > kLeastCluster && !s.one_team; --n) {
+    if (a.clusters[n] < units) continue;
+    s.cluster = n;
+    s.one_team = 1;
+  }
+  const int most = std::max(1, a.clusters[s.cluster]);
+  s.per_cta = (int)std::max<long long>(1, std::min<long long>(16, 2 * units / (most * s.cluster)));
+  cudaLaunchAttribute attr;
+  const cudaLaunchConfig_t cfg = config(s.cluster, (int)std::min<long long>(most, units), &attr, stream);
+  return cudaLaunchKernelEx(&cfg, split_kernel<D, kCols>, k_map, v_map, a, c, f, s);
+}
+
+template <int D>
+cudaError_t launch(const AttnArgs& a, const CacheArgs& c, const ForwardArgs& f, const CUtensorMap& k_map, const CUtensorMap& v_map,
+                   cudaStream_t stream) {
+  const long long flat = ((long long)f.rows * a.group + f.n - 1) / f.n;                   // rows of a request, about
+  return flat <= 4 ? launch<D, 4>(a, c, f, k_map, v_map, stream)
+                   : flat <= 8 ? launch<D, 8>(a, c, f, k_map, v_map, stream) : launch<D, 16>(a, c, f, k_map, v_map, stream);
+}
+
 }  // namespace
 
 cudaError_t configure_attn_split(AttnArgs* a) {
-  cudaError_t e = configure<32>(a);
-  if (e == cudaSuccess) e = configure<64>(a);
-  if (e == cudaSuccess) e = configure<128>(a);
-  for (int i = 0; i < 2 && e == cudaSuccess; ++i) {
+  cudaError_t e = configure<32>();
+  if (e == cudaSuccess) e = configure<64>();
+  if (e == cudaSuccess) e = configure<128>();
+  for (int i = kLeastCluster; i <= kMaxTeam && e == cudaSuccess; ++i) {
     cudaLaunchAttribute attr;
-    const cudaLaunchConfig_t cfg = config(kLeastCluster << i, 1, &attr, nullptr);
-    e = cudaOccupancyMaxActiveClusters(&a->clusters[i], split_kernel<128>, &cfg);
+    const cudaLaunchConfig_t cfg = config(i, 1, &attr, nullptr);
+    e = cudaOccupancyMaxActiveClusters(&a->clusters[i], split_kernel<128, 4>, &cfg);
   }
   return e;
 }
 
 cudaError_t launch_attn_split(const AttnArgs& a, const CacheArgs& c, const ForwardArgs& f, const CUtensorMap& k_map, const CUtensorMap& v_map,
                               cudaStream_t stream) {
-  const long long units = ((long long)f.rows * a.group / kCols + f.n) * a.kv;             // at most
-  // a cluster of 16 CTAs for each unit where clusters of 8 would leave half of the SMs idle
-  const int big = a.clusters[1] > 0 && units <= a.clusters[1] && f.width > kLeastCluster;
-  SplitArgs s;
-  s.cluster = kLeastCluster << big;
-  s.chunks = (f.n + 31) / 32;
-  const int most = std::max(1, a.clusters[big]);
-  s.per_cta = (int)std::max<long long>(1, std::min<long long>(16, 2 * units / (most * s.cluster)));
-  cudaLaunchAttribute attr;
-  const cudaLaunchConfig_t cfg = config(s.cluster, (int)std::min<long long>(most, units), &attr, stream);
-  const auto kernel = a.dim == 128 ? split_kernel<128> : a.dim == 64 ? split_kernel<64> : split_kernel<32>;
-  return cudaLaunchKernelEx(&cfg, kernel, k_map, v_map, a, c, f, s);
+  return a.dim == 128 ? launch<128>(a, c, f, k_map, v_map, stream)
+                      : a.dim == 64 ? launch<64>(a, c, f, k_map, v_map, stream) : launch<32>(a, c, f, k_map, v_map, stream);
 }
 
 }  // namespace iodf
