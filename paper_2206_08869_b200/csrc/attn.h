@@ -24,7 +24,7 @@ struct AttnArgs {                        // what a handle holds
   int score_s;
   int causal, window;
   int y_type, y_bytes, lo, hi;
-  const int2* out;                       // [heads * dim] {M0, s}
+  const int4* out;                       // [heads * dim] {M0, s, low and high word of 2^(30 + s)}
   uint32_t* status;                      // [0] a bounded wait gave up, [1] requests or rows that could not be served
   int sms;
   int clusters[kAttnMaxTeam + 1];        // of the kernel for few rows: clusters of 8 .. 16 CTAs that run at once
@@ -61,6 +61,7 @@ struct ForwardArgs {
   long long ldt, ldy;
   int rows, n, width;
   void* y;
+  int vector;                            // four neighbouring outputs lie on a boundary of their size
 };
 
 cudaError_t configure_attn_kernels(int device, AttnArgs* a);      // on the current device, before the first launch

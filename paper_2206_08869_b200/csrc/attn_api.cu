@@ -52,10 +52,11 @@ int create_attn(const iodf_attn_desc& d, int device, iodf_attn& h) {
   if (d.y_type == IODF_U8 && (lo < 0 || hi > 255)) return IODF_EINVAL;
   const size_t N = (size_t)d.heads * d.head_dim, R = (size_t)d.positions * (d.rotary_dim / 2);
   if (!d.out_m0 || !d.out_s) return IODF_EINVAL;
-  std::vector<int2> out(N);
+  std::vector<int4> out(N);
   for (size_t n = 0; n < N; ++n) {
     if (d.out_m0[n] < (1 << 30) || d.out_s[n] < 0 || d.out_s[n] > 31) return IODF_EINVAL;
-    out[n] = make_int2(d.out_m0[n], d.out_s[n]);
+    const uint64_t add = 1ull << (30 + d.out_s[n]);
+    out[n] = make_int4(d.out_m0[n], d.out_s[n], (int)(uint32_t)add, (int)(uint32_t)(add >> 32));
   }
   h.device = device;
   OnDevice on(device);
@@ -63,12 +64,12 @@ int create_attn(const iodf_attn_desc& d, int device, iodf_attn& h) {
   h.encode = tensor_map_encoder();
   if (!h.encode) return IODF_ECUDA;
   cudaError_t e = configure_attn_kernels(device, &h.args);
-  const size_t o_out = up_to(4 * R, 256), o_status = o_out + up_to(8 * N, 256);
+  const size_t o_out = up_to(4 * R, 256), o_status = o_out + up_to(16 * N, 256);
   if (e == cudaSuccess) e = cudaMalloc(&h.d_mem, o_status + 8);
   if (e != cudaSuccess) return status_of(e);
   uint8_t* m = static_cast<uint8_t*>(h.d_mem);
   if (R) e = cudaMemcpy(m, d.rotary, 4 * R, cudaMemcpyHostToDevice);
-  if (e == cudaSuccess) e = cudaMemcpy(m + o_out, out.data(), 8 * N, cudaMemcpyHostToDevice);
+  if (e == cudaSuccess) e = cudaMemcpy(m + o_out, out.data(), 16 * N, cudaMemcpyHostToDevice);
   if (e == cudaSuccess) e = cudaMemset(m + o_status, 0, 8);
   // A copy from pageable memory is only known to have left it: the first call may be on a stream that does not wait for the rest.
   if (e == cudaSuccess) e = cudaStreamSynchronize(0);
@@ -93,7 +94,7 @@ int create_attn(const iodf_attn_desc& d, int device, iodf_attn& h) {
   a.y_bytes = d.y_type == IODF_I32 ? 4 : 1;
   a.lo = lo;
   a.hi = hi;
-  a.out = reinterpret_cast<const int2*>(m + o_out);
+  a.out = reinterpret_cast<const int4*>(m + o_out);
   a.status = reinterpret_cast<uint32_t*>(m + o_status);
   return IODF_OK;
 }
@@ -233,7 +234,8 @@ int iodf_attn_forward(iodf_attn* h, int rows, const int8_t* q8, const uint8_t* q
   const Span ins[] = {{q8, R * N}, {q_exp, R * a.heads}, {row_start, 4 * (n + 1)}, {held, 4 * n}, {table, 4 * extent(n, ldt, width, 1)},
                       {cache->k, cache_bytes(*h, *cache)}, {cache->v, cache_bytes(*h, *cache)}, {cache->k_exp, blocks}, {cache->v_exp, blocks}};
   if (overlap(outs, ins)) return IODF_EINVAL;
-  const ForwardArgs f{q8, q_exp, row_start, held, table, (long long)ldt, (long long)ldy, rows, n_req, (int)width, y};
+  const ForwardArgs f{q8, q_exp, row_start, held, table, (long long)ldt, (long long)ldy, rows, n_req, (int)width, y,
+                      ldy % 4 == 0 && aligned(y, 4 * (size_t)a.y_bytes)};
   OnDevice on(h->device);
   if (on.error() != cudaSuccess) return IODF_ECUDA;
   CUtensorMap k_map, v_map;

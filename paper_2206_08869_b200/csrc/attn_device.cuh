@@ -51,17 +51,18 @@ __device__ __forceinline__ Reciprocal reciprocal(long long L, int V) {
   r.rho = (uint32_t)(0x7FFFFFFFFFFFFFFFull / l);
   return r;
 }
-__device__ __forceinline__ int quotient(long long A, const Reciprocal& r) {
-  const int a = r.a - 8;
-  const int scaled = (int)(a >= 0 ? A << a : A >> -a);             // |A| <= 127 L: 31 bits
-  const int hi = (int)(((long long)scaled * (long long)(unsigned long long)r.rho) >> 32);
-  return (hi + ((1 << (15 - r.V)) >> 1)) >> (15 - r.V);
+// A = 256 hi + lo
+__device__ __forceinline__ int quotient(int hi, int lo, const Reciprocal& r) {
+  const long long A = (long long)hi * 65536 + (long long)lo * 256;                       // 2^8 A, so that the next shift is to the right
+  const int scaled = (int)__funnelshift_r((uint32_t)A, (uint32_t)(A >> 32), (uint32_t)(16 - r.a));     // floor(A 2^(a - 8)): |A| <= 127 L, 31 bits
+  const int top = __mulhi(scaled, (int)r.rho) + scaled;            // scaled rho / 2^32: rho has its highest bit, as an int it is 2^32 less
+  return (top + ((1 << (15 - r.V)) >> 1)) >> (15 - r.V);
 }
 
-// y = clip(floor((o M0 + 2^(30 + s)) / 2^(31 + s)))
-__device__ __forceinline__ int requantised(int o, int2 rq, int lo, int hi) {
-  const long long v = ((long long)o * rq.x + (1ll << (30 + rq.y))) >> (31 + rq.y);
-  return (int)min(max(v, (long long)lo), (long long)hi);
+// y = clip(floor((o M0 + 2^(30 + s)) / 2^(31 + s))); out: {M0, s, low and high word of the addend}; |o| < 2^27
+__device__ __forceinline__ int requantised(int o, int4 out, int lo, int hi) {
+  const long long v = (long long)o * out.x + (long long)((unsigned long long)(uint32_t)out.w << 32 | (uint32_t)out.z);
+  return min(max((int)__funnelshift_l((uint32_t)v, (uint32_t)(v >> 32), 1) >> out.y, lo), hi);
 }
 
 // Keys that a row sees: [first, last)

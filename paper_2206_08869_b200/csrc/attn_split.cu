@@ -171,7 +171,8 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
   }
   __syncthreads();
   const uint32_t tmem = sh.tmem, o_hi = tmem + kScores * kN, o_lo = o_hi + kN;
-  auto wait = [&](uint64_t* bar, uint32_t phase) { return ptx::quick_wait(abort_flag, a.status, bar, phase, kSpinLimit); };
+  auto wait = [&](uint64_t* bar, uint32_t phase) { return ptx::spin_wait(abort_flag, a.status, bar, phase); };
+  auto lazy = [&](uint64_t* bar, uint32_t phase) { return ptx::lazy_wait(abort_flag, a.status, bar, phase); };
   auto warp_wait = [&](uint64_t* bar, uint32_t phase) { return __all_sync(0xFFFFFFFFu, wait(bar, phase)) != 0; };
   auto take = [&](const RingS& r, UnitS* u) {
     if (!wait(&sh.ufull[r.slot], r.phase)) return false;
@@ -312,7 +313,7 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
         const int b0 = low.first / kAttnBlock, n = high.last <= low.first ? 0 : (high.last + kAttnBlock - 1) / kAttnBlock - b0;
         u.b0 = b0 + u.member * n / u.team;
         u.n = b0 + (u.member + 1) * n / u.team - u.b0;
-        ok = warp_wait(&sh.uempty[ur.slot], ur.phase ^ 1);
+        ok = __all_sync(0xFFFFFFFFu, lazy(&sh.uempty[ur.slot], ur.phase ^ 1));
         if (!ok) break;
         for (int i = lane; i < u.n; i += 32) {
           const int id = f.table[(long long)u.request * f.ldt + u.b0 + i];
@@ -333,7 +334,7 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
       }
       item -= items;                                    // of the next class
     }
-    ok = ok && warp_wait(&sh.uempty[ur.slot], ur.phase ^ 1);
+    ok = ok && __all_sync(0xFFFFFFFFu, lazy(&sh.uempty[ur.slot], ur.phase ^ 1));
     if (ok && lane == 0) {
       sh.units[ur.slot].request = -1;
       ptx::mbar_arrive(ptx::smem_u32(&sh.ufull[ur.slot]));
@@ -344,7 +345,7 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
     UnitS u;
     bool ok = true;
     for (; ok && __all_sync(0xFFFFFFFFu, take(ur, &u)); ur.next(kUnitsS), qr.next(2)) {
-      ok = warp_wait(&sh.qempty[qr.slot], qr.phase ^ 1);
+      ok = __all_sync(0xFFFFFFFFu, lazy(&sh.qempty[qr.slot], qr.phase ^ 1));
       for (int i = lane; ok && i < u.cols * (D / 16); i += 32) {
         const int r = i / (D / 16), piece = i % (D / 16), flat = u.flat0 + r;
         const long long row = u.row0 + flat / a.group;
@@ -554,9 +555,8 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
             rec.V = __shfl_sync(0xFFFFFFFFu, V, e);
             const bool any = __shfl_sync(0xFFFFFFFFu, (int)(L > 0), e) != 0;
             if (e % kGroups == w && key < D && ok) {
-              const long long A = ((long long)(int)hi[e] << 8) + (int)lo[e];
               const int at = (u.head * a.group + (u.flat0 + e) % a.group) * D + key;
-              store(e, key, requantised(any ? quotient(A, rec) : 0, a.out[at], a.lo, a.hi));
+              store(e, key, requantised(any ? quotient((int)hi[e], (int)lo[e], rec) : 0, a.out[at], a.lo, a.hi));
             }
           }
         }
@@ -591,14 +591,16 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
         for (int i = tid - 128; ok && i < own * nc; i += 32 * kSoft) {
           const int dl = i % own, e = i / own, dim = u.member * own + dl;
           if (dim >= D) continue;
-          long long A = 0, all = 0;
+          int hi_all = 0, lo_all = 0;                   // no more than a row's sums
+          long long all = 0;
           for (int m = 0; m < u.team; ++m) {
             const int* o = osums + ((m * own + dl) * kCols + e) * 2;
-            A += ((long long)o[0] << 8) + o[1];
+            hi_all += o[0];
+            lo_all += o[1];
             all += sh.team_sum[m][e];
           }
           const int at = (u.head * a.group + (u.flat0 + e) % a.group) * D + dim;
-          store(e, dim, requantised(all ? quotient(A, reciprocal(all, sh.vtop[e])) : 0, a.out[at], a.lo, a.hi));
+          store(e, dim, requantised(all ? quotient(hi_all, lo_all, reciprocal(all, sh.vtop[e])) : 0, a.out[at], a.lo, a.hi));
         }
       }
       __syncwarp();

@@ -18,12 +18,15 @@
 namespace iodf {
 namespace {
 
-constexpr int kRows = 128;
-constexpr int kThreads2 = 384;           // warp 0 copies, 1 MMAs, 2-3 queries, 4-7 and 8-11 softmax
-constexpr int kKRing = 3, kVRing = 2, kUnits = 4, kMeta = 8;
+constexpr int kRows = 128, kHalf = kAttnBlock / 2;
+constexpr int kSoft = 16;                // softmax warps: two groups that take blocks in turn, two halves of a block's keys, 32 rows each
+constexpr int kThreads2 = 128 + 32 * kSoft;                       // warp 0 copies, 1 MMAs, 2 units, 3 queries, then softmax
+constexpr int kRing = 5, kUnits = 3, kScores = 4;     // S: four in the first pass, two beside O in the second
 constexpr int kBlockBytes = 16384;       // of a ring's slot: 128 rows of up to 128 bytes
 constexpr int kTableBytes = kWeightSegments * 128;                 // a copy of the table for each lane: no bank is asked twice
-constexpr int kSmem = kTableBytes + (2 + kKRing + kVRing + 4) * kBlockBytes;
+constexpr int kSmem = kTableBytes + (2 + kRing + 4) * kBlockBytes;
+// Blocks at the first pass's start that the second group takes alone while the first one stores the unit before.
+constexpr int kLead = 8;
 
 struct Unit {
   int request, head, row0, len;          // rows of the request: [row0, row0 + len)
@@ -32,13 +35,14 @@ struct Unit {
 };
 
 struct Shared {
-  uint64_t kfull[kKRing], kempty[kKRing], vfull[kVRing], vempty[kVRing], qfull[2], qempty[2], sfull[2], sempty[2], pfull[2], pempty[2];
+  uint64_t full[kRing], empty[kRing], qfull[2], qempty[2], sfull[kScores], sempty[kScores], pfull[2], pempty[2];
   uint64_t ofull, oempty, ufull[kUnits], uempty[kUnits];
   uint32_t abort_flag, tmem;
   Unit units[kUnits];
-  int2 meta[kMeta];                      // exponents of a block's keys and values, -1: nobody sees it
-  int top[2][kRows], vexp[2][kRows];     // of the two groups
-  long long sum[2][kRows];
+  int ids[kUnits][kAttnMaxBlocks];       // blocks of the unit; -1: outside the cache, nobody sees it
+  uint8_t ek[kUnits][kAttnMaxBlocks], ev[kUnits][kAttnMaxBlocks];
+  int top[4][kRows], vexp[4][kRows];     // of the groups' halves
+  long long sum[4][kRows];
 };
 
 struct Ring {                            // slot and phase, counted
@@ -121,27 +125,24 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 8191) & ~(uintptr_t)8191);
   __shared__ Shared sh;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t table = ptx::smem_u32(smem), qbuf = table + kTableBytes, kbuf = qbuf + 2 * kBlockBytes, vbuf = kbuf + kKRing * kBlockBytes,
-                 pbuf = vbuf + kVRing * kBlockBytes;
+  const uint32_t table = ptx::smem_u32(smem), qbuf = table + kTableBytes, ring = qbuf + 2 * kBlockBytes, pbuf = ring + kRing * kBlockBytes;
   volatile uint32_t* const abort_flag = &sh.abort_flag;
   if (tid == 0) {
     auto init = [](uint64_t* bars, int n, int count) {
       for (int i = 0; i < n; ++i) ptx::mbar_init(ptx::smem_u32(bars + i), count);
     };
-    init(sh.kfull, kKRing, 1);
-    init(sh.kempty, kKRing, 1);
-    init(sh.vfull, kVRing, 1);
-    init(sh.vempty, kVRing, 1);
-    init(sh.qfull, 2, 2);
+    init(sh.full, kRing, 1);
+    init(sh.empty, kRing, 1);
+    init(sh.qfull, 2, 1);
     init(sh.qempty, 2, 1);
-    init(sh.sfull, 2, 2);
-    init(sh.sempty, 2, 4);
-    init(sh.pfull, 2, 4);
+    init(sh.sfull, kScores, 1);
+    init(sh.sempty, kScores, kSoft / 2);
+    init(sh.pfull, 2, kSoft / 2);
     init(sh.pempty, 2, 1);
     init(&sh.ofull, 1, 1);
-    init(&sh.oempty, 1, 8);
+    init(&sh.oempty, 1, kSoft / 2);
     init(sh.ufull, kUnits, 1);
-    init(sh.uempty, kUnits, 11);
+    init(sh.uempty, kUnits, 3 + kSoft);
     ptx::mbar_init_fence();
     sh.abort_flag = 0;
   }
@@ -151,120 +152,103 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = sh.tmem, o_hi = tmem + 256, o_lo = o_hi + D;
-  auto wait = [&](uint64_t* bar, uint32_t phase) { return ptx::quick_wait(abort_flag, a.status, bar, phase, kSpinLimit); };
+  auto wait = [&](uint64_t* bar, uint32_t phase) { return ptx::spin_wait(abort_flag, a.status, bar, phase); };
+  auto lazy = [&](uint64_t* bar, uint32_t phase) { return ptx::lazy_wait(abort_flag, a.status, bar, phase); };
   auto warp_wait = [&](uint64_t* bar, uint32_t phase) { return __all_sync(0xFFFFFFFFu, wait(bar, phase)) != 0; };   // all lanes go on, or none
+  // the group of a block in the first pass (in the second they alternate)
+  auto first_pass = [](int j) { return j < kLead ? 1 : j & 1; };
   // the unit of a consumer's turn; false when there are no more
   auto take = [&](const Ring& r, Unit* u) {
-    if (!wait(&sh.ufull[r.slot], r.phase)) return false;
+    if (!lazy(&sh.ufull[r.slot], r.phase)) return false;
     *u = sh.units[r.slot];
     return u->request >= 0;
   };
 
   if (warp == 0) {
-    // Copies, and everything that is read to find out what to copy: units, blocks and their exponents, 32 over the lanes.
-    Finder finder;
-    Ring kr, vr, ur;
-    int count = 0;                                      // blocks, for meta
-    bool ok = true;
-    for (int round = 0; ok; ++round, ur.next(kUnits)) {
-      const int unit = round * (int)gridDim.x + ((round & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
+    if (ptx::elect_one()) {
+      Ring r, ur;
       Unit u;
-      const bool more = finder.find(a, f, unit, lane, &u);
-      if (!more) u.request = -1;
-      ok = warp_wait(&sh.uempty[ur.slot], ur.phase ^ 1);
-      if (!ok) break;
-      if (lane == 0) {
-        sh.units[ur.slot] = u;
-        ptx::mbar_arrive(ptx::smem_u32(&sh.ufull[ur.slot]));
-        if (more && u.tile == 0 && u.head == 0 && f.held[u.request] != u.held) atomicAdd(a.status + 1, 1u);
-      }
-      if (!more) break;
-      for (int pass = 0; pass < 2 && ok; ++pass) {
-        int id = 0, ek = 0, ev = 0;
-        for (int b = u.b0; b < u.b1 && ok; ++b, ++count) {
-          const int in = (b - u.b0) & 31;
-          if (in == 0) {
-            id = b + lane < u.b1 ? f.table[(long long)u.request * f.ldt + b + lane] : 0;
-            const bool good = (unsigned)id < (unsigned)c.blocks;
-            if (!good && pass) atomicAdd(a.status + 1, 1u);
-            if (!good) id = 0;
-            const long long at = (long long)id * a.kv + u.head;
-            ek = min((int)c.k_exp[at], kAttnMaxExp);
-            ev = good ? min((int)c.v_exp[at], kAttnMaxExp) : -1;
-          }
-          const int at = __shfl_sync(0xFFFFFFFFu, id, in) * a.kv + u.head;
-          const int2 m = make_int2(__shfl_sync(0xFFFFFFFFu, ek, in), __shfl_sync(0xFFFFFFFFu, ev, in));
-          ok = warp_wait(&sh.kempty[kr.slot], kr.phase ^ 1);
-          if (ok && ptx::elect_one()) {
-            sh.meta[count % kMeta] = m;
-            const uint32_t bar = ptx::smem_u32(&sh.kfull[kr.slot]);
-            ptx::mbar_expect_tx(bar, kAttnBlock * D);
-            ptx::tile_g2s(kbuf + kr.slot * kBlockBytes, &kmap, 0, at * kAttnBlock, bar);
-          }
-          __syncwarp();
-          kr.next(kKRing);
-          if (pass && ok) {
-            ok = warp_wait(&sh.vempty[vr.slot], vr.phase ^ 1);
-            if (ok && ptx::elect_one()) {
-              const uint32_t bar = ptx::smem_u32(&sh.vfull[vr.slot]);
-              ptx::mbar_expect_tx(bar, kAttnBlock * D);
-              ptx::tile_g2s(vbuf + vr.slot * kBlockBytes, &vmap, 0, at * D, bar);
-            }
-            __syncwarp();
-            vr.next(kVRing);
-          }
+      bool ok = true;
+      auto copy = [&](const CUtensorMap* map, int row) {
+        ok = ok && wait(&sh.empty[r.slot], r.phase ^ 1);
+        if (!ok) return;
+        const uint32_t bar = ptx::smem_u32(&sh.full[r.slot]);
+        ptx::mbar_expect_tx(bar, kAttnBlock * D);
+        ptx::tile_g2s(ring + r.slot * kBlockBytes, map, 0, row, bar);
+        r.next(kRing);
+      };
+      for (; ok && take(ur, &u); ur.next(kUnits)) {    // in the order in which the MMAs read them
+        const int* ids = sh.ids[ur.slot];
+        const int n = u.b1 - u.b0;
+        auto at = [&](int j) { return max(ids[j], 0) * a.kv + u.head; };
+        for (int j = 0; j < n && ok; ++j) copy(&kmap, at(j) * kAttnBlock);
+        for (int j = -2; j < n && ok; ++j) {
+          if (j + 2 < n) copy(&kmap, at(j + 2) * kAttnBlock);
+          if (j >= 0) copy(&vmap, at(j) * D);
         }
+        ptx::mbar_arrive(ptx::smem_u32(&sh.uempty[ur.slot]));
       }
+      // whoever fills a ring waits until the MMAs have given all of it back: no copy or arrival outlives the CTA
+      for (int i = 0; ok && i < kRing; ++i, r.next(kRing)) ok = wait(&sh.empty[r.slot], r.phase ^ 1);
     }
-    // whoever fills a ring waits until the MMAs have given all of it back: no copy or arrival outlives the CTA
-    for (int i = 0; ok && i < kKRing; ++i, kr.next(kKRing)) ok = wait(&sh.kempty[kr.slot], kr.phase ^ 1);
-    for (int i = 0; ok && i < kVRing; ++i, vr.next(kVRing)) ok = wait(&sh.vempty[vr.slot], vr.phase ^ 1);
+    __syncwarp();
   } else if (warp == 1) {
     if (ptx::elect_one()) {
       constexpr uint32_t id_s = idesc_i8(kRows, kAttnBlock, false, false), id_hi = idesc_i8(kRows, D, true, false), id_lo = idesc_i8(kRows, D, false, false);
       constexpr uint32_t hi_d = rows_hi(D), hi_128 = rows_hi(128);
-      Ring kr, vr, ur, qr, sr, orr;                     // sr: S and its barriers, two in turn
-      uint32_t pphases = 0;                             // of the two groups' weights
+      Ring r, ur, qr, orr;
+      uint32_t pphases = 0, sphases = 0;                // of each group's weights and of each S, in bits
       Unit u;
       bool ok = true;
-      auto scores = [&](uint32_t q) {                   // S of the next block
-        ok = ok && wait(&sh.kfull[kr.slot], kr.phase) && wait(&sh.sempty[sr.slot], sr.phase ^ 1);
+      auto scores = [&](uint32_t q, int slot) {         // S of the next block
+        ok = ok && wait(&sh.full[r.slot], r.phase) && wait(&sh.sempty[slot], (sphases >> slot & 1) ^ 1);
         if (!ok) return;
         ptx::tc_fence_after();
-        const uint32_t k = rows_lo(kbuf + kr.slot * kBlockBytes);
+        const uint32_t k = rows_lo(ring + r.slot * kBlockBytes);
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) ptx::umma_i8_hl(tmem + sr.slot * 128, q + 2 * i, hi_d, k + 2 * i, hi_d, id_s, i > 0);
-        ptx::umma_commit(ptx::smem_u32(&sh.kempty[kr.slot]));
-        ptx::umma_commit(ptx::smem_u32(&sh.sfull[sr.slot]));
-        ptx::mbar_arrive(ptx::smem_u32(&sh.sfull[sr.slot]));      // what the copying warp wrote of the block is passed on
-        kr.next(kKRing);
-        sr.next(2);
+        for (int i = 0; i < D / 32; ++i) ptx::umma_i8_hl(tmem + slot * 128, q + 2 * i, hi_d, k + 2 * i, hi_d, id_s, i > 0);
+        ptx::umma_commit(ptx::smem_u32(&sh.empty[r.slot]));
+        ptx::umma_commit(ptx::smem_u32(&sh.sfull[slot]));
+        r.next(kRing);
+        sphases ^= 1u << slot;
       };
       for (; ok && take(ur, &u); ur.next(kUnits)) {
         const int n = u.b1 - u.b0;
+        bool o_free = false;                            // the unit before has been read out of O
+        auto free_o = [&] {
+          if (!o_free) ok = ok && wait(&sh.oempty, orr.phase ^ 1);
+          o_free = true;
+        };
         ok = wait(&sh.qfull[qr.slot], qr.phase);
         ptx::tc_fence_after();
         const uint32_t q = rows_lo(qbuf + qr.slot * kBlockBytes);
-        for (int j = 0; j < n && ok; ++j) scores(q);
-        int ps = sr.slot;                               // the weights of a block are where its S is
-        for (int j = 0; j < n + 2 && ok; ++j) {
-          if (j >= 2) {
-            if (j == 2) ok = wait(&sh.oempty, orr.phase ^ 1);
-            ok = ok && wait(&sh.pfull[ps], (pphases >> ps) & 1) && wait(&sh.vfull[vr.slot], vr.phase);
-            if (!ok) break;
-            ptx::tc_fence_after();
-            const uint32_t p = rows_lo(pbuf + ps * 2 * kBlockBytes), v = rows_lo(vbuf + vr.slot * kBlockBytes);
+        int turns[2] = {0, 0};                          // of the groups' two S in the first pass
+        for (int j = 0; j < n && ok; ++j) {
+          const int g = first_pass(j), slot = g + 2 * (turns[g]++ & 1);
+          if (slot >= 2) free_o();                      // these lie where O will be
+          scores(q, slot);
+        }
+        for (int j = 0; j < 2 && j < n; ++j) scores(q, j);
+        if (n) {
+          free_o();
+          for (int i = 2; i < 4; ++i) ok = ok && wait(&sh.sempty[i], (sphases >> i & 1) ^ 1);
+        }
+        for (int j = 0; j < n && ok; ++j) {
+          const int g = j & 1;
+          // The next scores go first: the group whose weights come now waits for nothing else.
+          if (j + 2 < n) scores(q, g);
+          ok = ok && wait(&sh.pfull[g], pphases >> g & 1) && wait(&sh.full[r.slot], r.phase);
+          if (!ok) break;
+          ptx::tc_fence_after();
+          const uint32_t p = rows_lo(pbuf + g * 2 * kBlockBytes), v = rows_lo(ring + r.slot * kBlockBytes);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) ptx::umma_i8_hl(o_hi, p + 2 * i, hi_128, v + 2 * i, hi_128, id_hi, j > 2 || i > 0);
+          for (int i = 0; i < 4; ++i) ptx::umma_i8_hl(o_hi, p + 2 * i, hi_128, v + 2 * i, hi_128, id_hi, j > 0 || i > 0);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) ptx::umma_i8_hl(o_lo, p + (kBlockBytes >> 4) + 2 * i, hi_128, v + 2 * i, hi_128, id_lo, j > 2 || i > 0);
-            ptx::umma_commit(ptx::smem_u32(&sh.vempty[vr.slot]));
-            ptx::umma_commit(ptx::smem_u32(&sh.pempty[ps]));
-            vr.next(kVRing);
-            pphases ^= 1u << ps;
-            ps ^= 1;
-          }
-          if (j < n) scores(q);
+          for (int i = 0; i < 4; ++i) ptx::umma_i8_hl(o_lo, p + (kBlockBytes >> 4) + 2 * i, hi_128, v + 2 * i, hi_128, id_lo, j > 0 || i > 0);
+          ptx::umma_commit(ptx::smem_u32(&sh.empty[r.slot]));
+          ptx::umma_commit(ptx::smem_u32(&sh.pempty[g]));
+          r.next(kRing);
+          pphases ^= 1u << g;
         }
         if (ok && n) {
           ptx::umma_commit(ptx::smem_u32(&sh.ofull));
@@ -279,22 +263,51 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
       for (int i = 0; ok && i < 2; ++i) ok = wait(&sh.pempty[i], ((pphases >> i) & 1) ^ 1);
     }
     __syncwarp();
-  } else if (warp < 4) {
+  } else if (warp == 2) {
+    // Units, and everything that is read to find out what to copy: blocks and their exponents, over the lanes.
+    Finder finder;
+    Ring ur;
+    bool ok = true, more = true;
+    for (int round = 0; ok && more; ++round, ur.next(kUnits)) {
+      const int unit = round * (int)gridDim.x + ((round & 1) ? (int)gridDim.x - 1 - (int)blockIdx.x : (int)blockIdx.x);
+      Unit u;
+      more = finder.find(a, f, unit, lane, &u);
+      if (!more) u.request = -1;
+      ok = __all_sync(0xFFFFFFFFu, lazy(&sh.uempty[ur.slot], ur.phase ^ 1));
+      if (!ok) break;
+      const int n = more ? u.b1 - u.b0 : 0;
+      const int32_t* row = f.table + (long long)u.request * f.ldt + u.b0;
+#pragma unroll 4
+      for (int i = lane; i < n; i += 32) {
+        const int id = row[i];
+        const bool good = (unsigned)id < (unsigned)c.blocks;
+        if (!good) atomicAdd(a.status + 1, 1u);
+        const long long at = (long long)(good ? id : 0) * a.kv + u.head;
+        sh.ids[ur.slot][i] = good ? id : -1;
+        sh.ek[ur.slot][i] = (uint8_t)min((int)c.k_exp[at], kAttnMaxExp);
+        sh.ev[ur.slot][i] = (uint8_t)min((int)c.v_exp[at], kAttnMaxExp);
+      }
+      if (lane == 0) {
+        sh.units[ur.slot] = u;
+        if (more && u.tile == 0 && u.head == 0 && f.held[u.request] != u.held) atomicAdd(a.status + 1, 1u);
+      }
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.ufull[ur.slot]));
+    }
+  } else if (warp == 3) {
     // Queries: rows of D bytes into the layout of the MMA's operand.
-    const int t = tid - 64;
     Ring qr, ur;
     Unit u;
     bool ok = true;
     for (; ok && __all_sync(0xFFFFFFFFu, take(ur, &u)); ur.next(kUnits), qr.next(2)) {
-      ok = warp_wait(&sh.qempty[qr.slot], qr.phase ^ 1);
+      ok = __all_sync(0xFFFFFFFFu, lazy(&sh.qempty[qr.slot], qr.phase ^ 1));
       const Tile tile(a, u);
-      for (int i = t; ok && i < kRows * (D / 16); i += 64) {
-        const int r = i / (D / 16), piece = i % (D / 16), flat = tile.flat0 + r;
-        if (flat < tile.flats) {
-          const long long row = u.row0 + flat / a.group;
-          const int4 v = *reinterpret_cast<const int4*>(f.q8 + (row * a.heads + u.head * a.group + flat % a.group) * D + piece * 16);
-          ptx::sts128(qbuf + qr.slot * kBlockBytes + swizzled(r, piece, D), v.x, v.y, v.z, v.w);
-        }
+#pragma unroll 8
+      for (int i = lane; ok && i < kRows * (D / 16); i += 32) {
+        const int r = i / (D / 16), piece = i % (D / 16), flat = min(tile.flat0 + r, tile.flats - 1);     // rows behind the last one: any
+        const long long row = u.row0 + flat / a.group;
+        const int4 v = *reinterpret_cast<const int4*>(f.q8 + (row * a.heads + u.head * a.group + flat % a.group) * D + piece * 16);
+        ptx::sts128(qbuf + qr.slot * kBlockBytes + swizzled(r, piece, D), v.x, v.y, v.z, v.w);
       }
       ptx::fence_async_smem();
       __syncwarp();
@@ -305,17 +318,23 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
     }
     for (int i = 0; ok && i < 2; ++i, qr.next(2)) ok = wait(&sh.qempty[qr.slot], qr.phase ^ 1);
   } else {
-    const int w = (warp - 4) >> 2, quarter = warp & 3, r = quarter * 32 + lane;          // group, lanes of tensor memory, row of the tile
-    const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_mem = tmem + lanes + w * 128, words = table + lane * 4;
+    const int w = (warp - 4) >> 3, half = (warp - 4) >> 2 & 1, part = (warp - 4) >> 2;   // group, half of a block's keys, both in one
+    const int quarter = warp & 3, r = quarter * 32 + lane;                               // lanes of tensor memory, row of the tile
+    const uint32_t lanes = (uint32_t)(quarter * 32) << 16, s_mem = tmem + lanes + half * kHalf, words = table + lane * 4;
     const uint32_t p_hi = pbuf + w * 2 * kBlockBytes, p_lo = p_hi + kBlockBytes;
     Ring ur, orr;
-    uint32_t sphase = 0, pphase = 1;
-    int count = 0;                                      // blocks of the units before
+    uint32_t sphases = 0, pphase = 1;
     Unit u;
     bool ok = true;
-    while (ptx::all_agree(1, 256, take(ur, &u))) {      // in step: there are barriers below, whatever the other waits return
+    for (;;) {
+      // The two groups meet twice in a unit: here behind the first pass, whatever their other waits return (both leave, or none), and
+      // behind the second. Then the first one stores the unit, and the other begins the next.
+      const bool more = __all_sync(0xFFFFFFFFu, take(ur, &u));
+      if (!more) u.b0 = u.b1 = u.len = u.tile = 0;
       const Tile tile(a, u);
-      const int flat = tile.flat0 + r, n = u.b1 - u.b0;
+      const int n = u.b1 - u.b0;
+      const int rem0 = tile.flat0 % a.group, token0 = tile.flat0 / a.group;
+      const int flat = tile.flat0 + r;
       const bool live = flat < tile.flats;
       const long long row = u.row0 + (live ? flat : tile.flat0) / a.group;
       const int head = u.head * a.group + flat % a.group;
@@ -325,71 +344,84 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
       const Range low = visible(a, tile.position(a, u, tile.flat0), u.held), high = visible(a, tile.position(a, u, tile.flats - 1), u.held);
       const int whole0 = (high.first + kAttnBlock - 1) / kAttnBlock, whole1 = max(low.last, 0) / kAttnBlock;
       int T = INT32_MIN, V = 0;
-      // S and weights alternate between the groups over all blocks of all units, so who begins depends on the blocks before
-      // (each pass has n of them)
-      for (int j = (w ^ count) & 1; j < n; j += 2) {
-        ok = ok && warp_wait(&sh.sfull[w], sphase);
-        sphase ^= 1;
+      int turn = 0;
+      for (int j = 0; j < n; ++j) {
+        if (first_pass(j) != w) continue;
+        const int b = u.b0 + j, slot = w + 2 * (turn++ & 1), W = score_multiplier(a.score_m0, eq + sh.ek[ur.slot][j], a.score_s);
+        const bool whole = b >= whole0 && b < whole1;
+        ok = ok && warp_wait(&sh.sfull[slot], sphases >> slot & 1);
+        sphases ^= 1u << slot;
         if (!ok) break;
         ptx::tc_fence_after();
-        const int b = u.b0 + j;
-        const int2 m = sh.meta[(count + j) % kMeta];
-        const bool whole = b >= whole0 && b < whole1;
         int top = INT32_MIN;
+        uint32_t s0[32], s1[32];
+        ptx::tmem_ld32(s_mem + slot * 128, s0);
+        ptx::tmem_ld32(s_mem + slot * 128 + 32, s1);
+        ptx::tmem_ld_wait32(s0);
+        ptx::tmem_ld_wait32(s1);
+        if (whole) {
+          int m[4] = {(int)s0[0], (int)s0[1], (int)s0[2], (int)s0[3]};
 #pragma unroll
-        for (int c0 = 0; c0 < kAttnBlock; c0 += 32) {
-          uint32_t s[32];
-          ptx::tmem_ld32(s_mem + c0, s);
-          ptx::tmem_ld_wait32(s);
-          if (whole) {
+          for (int i = 0; i < 32; ++i) m[i & 3] = max(m[i & 3], max((int)s0[i], (int)s1[i]));
+          top = max(max(m[0], m[1]), max(m[2], m[3]));
+        } else {
+          const int first = see.first - b * kAttnBlock - half * kHalf, last = see.last - b * kAttnBlock - half * kHalf;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) top = max(top, (int)s[i]);
-          } else {
-            const int first = see.first - b * kAttnBlock - c0, last = see.last - b * kAttnBlock - c0;
-#pragma unroll
-            for (int i = 0; i < 32; ++i) top = i >= first && i < last ? max(top, (int)s[i]) : top;
+          for (int i = 0; i < 32; ++i) {
+            top = i >= first && i < last ? max(top, (int)s0[i]) : top;
+            top = i + 32 >= first && i + 32 < last ? max(top, (int)s1[i]) : top;
           }
         }
         ptx::tc_fence_before();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.sempty[w]));
-        if (m.y >= 0 && top != INT32_MIN) {
-          T = max(T, score_octaves(top, score_multiplier(a.score_m0, eq + m.x, a.score_s)));
-          V = max(V, m.y);
+        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.sempty[slot]));
+        if (sh.ids[ur.slot][j] >= 0 && top != INT32_MIN) {
+          T = max(T, score_octaves(top, W));
+          V = max(V, (int)sh.ev[ur.slot][j]);
         }
       }
-      count += n;
-      sh.top[w][r] = T;
-      sh.vexp[w][r] = V;
-      ptx::named_barrier(1, 256);
-      T = max(T, sh.top[w ^ 1][r]);
-      V = max(V, sh.vexp[w ^ 1][r]);
+      sh.top[part][r] = T;
+      sh.vexp[part][r] = V;
+      if (!ptx::all_agree(1, 32 * kSoft, more)) break;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        T = max(T, sh.top[i][r]);
+        V = max(V, sh.vexp[i][r]);
+      }
       long long L = 0;
-      for (int j = (w ^ count) & 1; j < n; j += 2) {
-        ok = ok && warp_wait(&sh.sfull[w], sphase) && warp_wait(&sh.pempty[w], pphase);
-        sphase ^= 1;
-        pphase ^= 1;
+      for (int j = w; j < n; j += 2) {
+        const int b = u.b0 + j, W = score_multiplier(a.score_m0, eq + sh.ek[ur.slot][j], a.score_s);
+        const bool bad = sh.ids[ur.slot][j] < 0, whole = b >= whole0 && b < whole1 && !bad;
+        const int d = max(V - sh.ev[ur.slot][j], 0), C = -(T + 8192 * d);
+        const int first = bad ? INT32_MAX : see.first - b * kAttnBlock - half * kHalf, last = see.last - b * kAttnBlock - half * kHalf;
+        ok = ok && warp_wait(&sh.sfull[w], sphases >> w & 1);
+        sphases ^= 1u << w;
         if (!ok) break;
         ptx::tc_fence_after();
-        const int b = u.b0 + j;
-        const int2 m = sh.meta[(count + j) % kMeta];
-        const bool whole = b >= whole0 && b < whole1 && m.y >= 0;
-        const int W = score_multiplier(a.score_m0, eq + m.x, a.score_s), d = max(V - m.y, 0), C = -(T + 8192 * d);
-        const int first = m.y < 0 ? INT32_MAX : see.first - b * kAttnBlock, last = see.last - b * kAttnBlock;
         uint32_t sum = 0;
+        uint32_t ahead[16];
+        ptx::tmem_ld16(s_mem + w * 128, ahead);
 #pragma unroll
-        for (int c0 = 0; c0 < kAttnBlock; c0 += 32) {
-          uint32_t s[32];
-          ptx::tmem_ld32(s_mem + c0, s);
-          ptx::tmem_ld_wait32(s);
-          uint32_t hi[8], lo[8];
+        for (int c0 = 0; c0 < kHalf; c0 += 16) {
+          uint32_t s[16];
+          ptx::tmem_ld_wait16(ahead);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = ahead[i];
+          if (c0 + 16 < kHalf) {                        // the next ones come while these are worked on
+            ptx::tmem_ld16(s_mem + w * 128 + c0 + 16, ahead);
+          } else {                       // S may be written over
+            ptx::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.sempty[w]));
+          }
+          uint32_t hi[4], lo[4];
           auto weights = [&](auto masked) {
 #pragma unroll
-            for (int i = 0; i < 32; i += 4) {
+            for (int i = 0; i < 16; i += 4) {
               uint32_t x[4];
 #pragma unroll
               for (int e = 0; e < 4; ++e) {
-                int t = max(score_octaves((int)s[i + e], W) + C, kWeightLow);
+                int t = __viaddmax_s32(score_octaves((int)s[i + e], W), C, kWeightLow);
                 if (masked.value) t = c0 + i + e >= first && c0 + i + e < last ? t : kWeightLow;
                 x[e] = weight_bits(t, (int)ptx::lds32((uint32_t)(t & ((kWeightSegments - 1) << 7)) | words));
                 sum += x[e];
@@ -399,78 +431,93 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
           };
           if (whole) weights(std::false_type());
           else weights(std::true_type());
-          const int piece = c0 / 16;
+          if (c0 == 0) ok = warp_wait(&sh.pempty[w], pphase);           // the MMAs have read the weights before these
+          const int piece = (half * kHalf + c0) / 16;
           ptx::sts128(p_hi + swizzled(r, piece, 128), hi[0], hi[1], hi[2], hi[3]);
-          ptx::sts128(p_hi + swizzled(r, piece + 1, 128), hi[4], hi[5], hi[6], hi[7]);
           ptx::sts128(p_lo + swizzled(r, piece, 128), lo[0], lo[1], lo[2], lo[3]);
-          ptx::sts128(p_lo + swizzled(r, piece + 1, 128), lo[4], lo[5], lo[6], lo[7]);
         }
-        ptx::tc_fence_before();
+        pphase ^= 1;
         ptx::fence_async_smem();
         __syncwarp();
-        if (lane == 0) {
-          ptx::mbar_arrive(ptx::smem_u32(&sh.sempty[w]));
-          ptx::mbar_arrive(ptx::smem_u32(&sh.pfull[w]));
-        }
-        L += (long long)(sum - kAttnBlock * kWeightBias) << d;
+        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.pfull[w]));
+        L += (long long)(sum - kHalf * kWeightBias) << d;
       }
-      count += n;
-      sh.sum[w][r] = L;
-      ptx::named_barrier(1, 256);
-      L += sh.sum[w ^ 1][r];
+      sh.sum[part][r] = L;
+      ptx::named_barrier(1, 32 * kSoft);
+      if (w == 1) {
+        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.uempty[ur.slot]));
+        ur.next(kUnits);
+        continue;
+      }
+      L = sh.sum[0][r] + sh.sum[1][r] + sh.sum[2][r] + sh.sum[3][r];
+      const Reciprocal rec = reciprocal(max(L, 1ll), V);
+      constexpr int kLanes = D / 4, kAtOnce = 32 / kLanes, kRounds = kRows / (kSoft / 2 * kAtOnce);   // lanes of a row, rows of a warp
+      const int piece = lane % kLanes;
+      int t = (warp - 4) * kAtOnce + lane / kLanes, token = (rem0 + t) / a.group, hd = u.head * a.group + rem0 + t - token * a.group;
+      int4 rq[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) rq[e] = a.out[hd * D + piece * 4 + e];
       if (n) {
         ok = ok && warp_wait(&sh.ofull, orr.phase);
         orr.next(1);
         ptx::tc_fence_after();
       }
-      const Reciprocal rec = reciprocal(max(L, 1ll), V);
-      const long long y_at = row * f.ldy + head * D;
-#pragma unroll 1
-      for (int c0 = w * (D / 2); c0 < (w + 1) * (D / 2); c0 += 16) {
-        uint32_t h[16], l[16];
-        if (n) {
-          ptx::tmem_ld16(o_hi + lanes + c0, h);
-          ptx::tmem_ld16(o_lo + lanes + c0, l);
-          ptx::tmem_ld_wait16(h);
-          ptx::tmem_ld_wait16_nosync(l);
-        }
-        int y[16];
+      // Quotients go through the weights' shared memory (all MMAs have read it), so that a warp then has rows whose elements lie side by
+      // side: 16-byte piece c of row r at c ^ (r & 7).
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const long long A = ((long long)(int)h[i] << 8) + (int)l[i];
-          y[i] = requantised(L ? quotient(A, rec) : 0, a.out[head * D + c0 + i], a.lo, a.hi);
-        }
-        if (live && ok) {
-          if (a.y_bytes == 1) {
-            int8_t* p = (int8_t*)f.y + y_at + c0;
-            uint32_t v[4];
+      for (int c0 = half * (D / 2); c0 < (half + 1) * (D / 2); c0 += 8) {
+        uint32_t h[8], l[8];
+        ptx::tmem_ld8(o_hi + lanes + c0, h);
+        ptx::tmem_ld8(o_lo + lanes + c0, l);
+        ptx::tmem_ld_wait8(h);
+        ptx::tmem_ld_wait8(l);
+        int o[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              v[i] = (uint32_t)(y[4 * i] & 255) | (uint32_t)(y[4 * i + 1] & 255) << 8 | (uint32_t)(y[4 * i + 2] & 255) << 16 | (uint32_t)y[4 * i + 3] << 24;
-            if ((reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-              *reinterpret_cast<uint4*>(p) = make_uint4(v[0], v[1], v[2], v[3]);
-            } else {
+        for (int i = 0; i < 8; ++i) o[i] = L ? quotient((int)h[i], (int)l[i], rec) : 0;
 #pragma unroll
-              for (int i = 0; i < 16; ++i) p[i] = (int8_t)y[i];
-            }
-          } else {
-            int* p = (int*)f.y + y_at + c0;
-            if ((reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-#pragma unroll
-              for (int i = 0; i < 16; i += 4) *reinterpret_cast<int4*>(p + i) = make_int4(y[i], y[i + 1], y[i + 2], y[i + 3]);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) p[i] = y[i];
-            }
-          }
-        }
+        for (int i = 0; i < 8; i += 4)
+          ptx::sts128(pbuf + r * (4 * D) + ((((c0 + i) >> 2) ^ (r & 7)) << 4), (uint32_t)o[i], (uint32_t)o[i + 1], (uint32_t)o[i + 2], (uint32_t)o[i + 3]);
       }
       ptx::tc_fence_before();
       __syncwarp();
-      if (lane == 0) {
-        if (n) ptx::mbar_arrive(ptx::smem_u32(&sh.oempty));
-        ptx::mbar_arrive(ptx::smem_u32(&sh.uempty[ur.slot]));
+      if (lane == 0 && n) ptx::mbar_arrive(ptx::smem_u32(&sh.oempty));
+      ptx::named_barrier(2, 16 * kSoft);
+#pragma unroll 2
+      for (int i = 0; i < kRounds && ok; ++i) {
+        if (tile.flat0 + t >= tile.flats) break;
+        const int4 o = *reinterpret_cast<const int4*>(smem + (pbuf - table) + t * (4 * D) + ((piece ^ (t & 7)) << 4));
+        const int y[4] = {requantised(o.x, rq[0], a.lo, a.hi), requantised(o.y, rq[1], a.lo, a.hi), requantised(o.z, rq[2], a.lo, a.hi),
+                          requantised(o.w, rq[3], a.lo, a.hi)};
+        const long long to = (long long)(u.row0 + token0 + token) * f.ldy + hd * D + piece * 4;
+        if (a.y_bytes == 1) {
+          int8_t* p = (int8_t*)f.y + to;
+          if (f.vector) {
+            *reinterpret_cast<uint32_t*>(p) = __byte_perm(__byte_perm((uint32_t)y[0], (uint32_t)y[1], 0x0040),
+                                                          __byte_perm((uint32_t)y[2], (uint32_t)y[3], 0x0040), 0x5410);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[e] = (int8_t)y[e];
+          }
+        } else {
+          int* p = (int*)f.y + to;
+          if (f.vector) {
+            *reinterpret_cast<int4*>(p) = make_int4(y[0], y[1], y[2], y[3]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[e] = y[e];
+          }
+        }
+        t += kSoft / 2 * kAtOnce;
+        token = (rem0 + t) / a.group;
+        const int next = u.head * a.group + rem0 + t - token * a.group;
+        if (next != hd) {
+          hd = next;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) rq[e] = a.out[hd * D + piece * 4 + e];
+        }
       }
+      __syncwarp();
+      if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.uempty[ur.slot]));
       ur.next(kUnits);
     }
   }
