@@ -21,7 +21,8 @@ namespace {
 constexpr int kRows = 128, kHalf = kAttnBlock / 2;
 constexpr int kSoft = 16;                // softmax warps: two groups that take blocks in turn, two halves of a block's keys, 32 rows each
 constexpr int kThreads2 = 128 + 32 * kSoft;                       // warp 0 copies, 1 MMAs, 2 units, 3 queries, then softmax
-constexpr int kRing = 5, kUnits = 3, kScores = 4;     // S: four in the first pass, two beside O in the second
+constexpr int kRing = 5, kUnits = 3;     // stages, units
+constexpr int kScores = 6;               // barriers of S: see `place`
 constexpr int kBlockBytes = 16384;       // of a ring's slot: 128 rows of up to 128 bytes
 constexpr int kTableBytes = kWeightSegments * 128;                 // a copy of the table for each lane: no bank is asked twice
 constexpr int kSmem = kTableBytes + (2 + kRing + 4) * kBlockBytes;
@@ -40,10 +41,13 @@ struct Shared {
   uint32_t abort_flag, tmem;
   Unit units[kUnits];
   int ids[kUnits][kAttnMaxBlocks];       // blocks of the unit; -1: outside the cache, nobody sees it
-  uint8_t ek[kUnits][kAttnMaxBlocks], ev[kUnits][kAttnMaxBlocks];
+  uint16_t exps[kUnits][kAttnMaxBlocks]; // their exponents: of the keys, above eight bits of the values, kBad
+  int multipliers[2 * kAttnMaxExp + 1];  // W by the sum of the exponents
   int top[4][kRows], vexp[4][kRows];     // of the groups' halves
   long long sum[4][kRows];
 };
+
+constexpr int kBad = 1 << 15;
 
 struct Ring {                            // slot and phase, counted
   int slot = 0;
@@ -147,6 +151,7 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
     sh.abort_flag = 0;
   }
   for (int i = tid; i < kWeightSegments * 32; i += kThreads2) reinterpret_cast<int*>(smem)[i] = weight_word(i / 32);
+  if (tid <= 2 * kAttnMaxExp) sh.multipliers[tid] = score_multiplier(a.score_m0, tid, a.score_s);
   if (warp == 2) ptx::tmem_alloc(ptx::smem_u32(&sh.tmem), 512);
   ptx::tc_fence_before();
   __syncthreads();
@@ -155,8 +160,10 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
   auto wait = [&](uint64_t* bar, uint32_t phase) { return ptx::spin_wait(abort_flag, a.status, bar, phase); };
   auto lazy = [&](uint64_t* bar, uint32_t phase) { return ptx::lazy_wait(abort_flag, a.status, bar, phase); };
   auto warp_wait = [&](uint64_t* bar, uint32_t phase) { return __all_sync(0xFFFFFFFFu, wait(bar, phase)) != 0; };   // all lanes go on, or none
-  // the group of a block in the first pass (in the second they alternate)
-  auto first_pass = [](int j) { return j < kLead ? 1 : j & 1; };
+  // S of a block in the first pass: 0 to 3, each read by half of a group; of the lead 4 and 5, which lie where 0 and 1 do but have barriers of
+  // their own: their reader is another one than that of 0, and who waits for a phase must not be two phases late. In the second pass
+  // the groups alternate, in S 0 and 1. S 2 and 3 lie where O will be.
+  auto place = [](int j) { return j < kLead ? 4 + (j & 1) : j & 3; };
   // the unit of a consumer's turn; false when there are no more
   auto take = [&](const Ring& r, Unit* u) {
     if (!lazy(&sh.ufull[r.slot], r.phase)) return false;
@@ -206,7 +213,7 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
         ptx::tc_fence_after();
         const uint32_t k = rows_lo(ring + r.slot * kBlockBytes);
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) ptx::umma_i8_hl(tmem + slot * 128, q + 2 * i, hi_d, k + 2 * i, hi_d, id_s, i > 0);
+        for (int i = 0; i < D / 32; ++i) ptx::umma_i8_hl(tmem + (slot & 3) * 128, q + 2 * i, hi_d, k + 2 * i, hi_d, id_s, i > 0);
         ptx::umma_commit(ptx::smem_u32(&sh.empty[r.slot]));
         ptx::umma_commit(ptx::smem_u32(&sh.sfull[slot]));
         r.next(kRing);
@@ -222,16 +229,24 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
         ok = wait(&sh.qfull[qr.slot], qr.phase);
         ptx::tc_fence_after();
         const uint32_t q = rows_lo(qbuf + qr.slot * kBlockBytes);
-        int turns[2] = {0, 0};                          // of the groups' two S in the first pass
+        auto free_s = [&](int i) { ok = ok && wait(&sh.sempty[i], (sphases >> i & 1) ^ 1); };
+        free_s(0);
+        free_s(1);
         for (int j = 0; j < n && ok; ++j) {
-          const int g = first_pass(j), slot = g + 2 * (turns[g]++ & 1);
-          if (slot >= 2) free_o();                      // these lie where O will be
-          scores(q, slot);
+          if (j == kLead) {
+            free_s(4);
+            free_s(5);
+          }
+          if (j >= kLead && (j & 2)) free_o();
+          scores(q, place(j));
         }
+        free_s(4);
+        free_s(5);
         for (int j = 0; j < 2 && j < n; ++j) scores(q, j);
         if (n) {
           free_o();
-          for (int i = 2; i < 4; ++i) ok = ok && wait(&sh.sempty[i], (sphases >> i & 1) ^ 1);
+          free_s(2);
+          free_s(3);
         }
         for (int j = 0; j < n && ok; ++j) {
           const int g = j & 1;
@@ -284,8 +299,7 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
         if (!good) atomicAdd(a.status + 1, 1u);
         const long long at = (long long)(good ? id : 0) * a.kv + u.head;
         sh.ids[ur.slot][i] = good ? id : -1;
-        sh.ek[ur.slot][i] = (uint8_t)min((int)c.k_exp[at], kAttnMaxExp);
-        sh.ev[ur.slot][i] = (uint8_t)min((int)c.v_exp[at], kAttnMaxExp);
+        sh.exps[ur.slot][i] = (uint16_t)(min((int)c.k_exp[at], kAttnMaxExp) | min((int)c.v_exp[at], kAttnMaxExp) << 8 | (good ? 0 : kBad));
       }
       if (lane == 0) {
         sh.units[ur.slot] = u;
@@ -326,6 +340,13 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
     uint32_t sphases = 0, pphase = 1;
     Unit u;
     bool ok = true;
+    // S may be written over: an arrival for each of the warps that share it in the second pass
+    auto release = [&](int which, int arrivals) {
+      ptx::tc_fence_before();
+      __syncwarp();
+      if (lane < arrivals) ptx::mbar_arrive(ptx::smem_u32(&sh.sempty[which]));
+    };
+    const uint32_t by_group = 65536 / a.group + 1;      // x / group = x * this >> 16 for x < 256, group <= 128
     for (;;) {
       // The two groups meet twice in a unit: here behind the first pass, whatever their other waits return (both leave, or none), and
       // behind the second. Then the first one stores the unit, and the other begins the next.
@@ -344,40 +365,50 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
       const Range low = visible(a, tile.position(a, u, tile.flat0), u.held), high = visible(a, tile.position(a, u, tile.flats - 1), u.held);
       const int whole0 = (high.first + kAttnBlock - 1) / kAttnBlock, whole1 = max(low.last, 0) / kAttnBlock;
       int T = INT32_MIN, V = 0;
-      int turn = 0;
-      for (int j = 0; j < n; ++j) {
-        if (first_pass(j) != w) continue;
-        const int b = u.b0 + j, slot = w + 2 * (turn++ & 1), W = score_multiplier(a.score_m0, eq + sh.ek[ur.slot][j], a.score_s);
-        const bool whole = b >= whole0 && b < whole1;
+      const int lead = min(n, kLead), rest = max(n - kLead, 0);
+      bool leading = w == 1;
+      int slot = leading ? 4 + half : w + 2 * half, j1 = leading ? half : kLead + slot;
+      for (;; j1 += leading ? 2 : 4) {
+        if (leading && j1 >= lead) {
+          leading = false;
+          slot = w + 2 * half;
+          j1 = kLead + slot;
+        }
+        if (j1 >= n) break;
+        const int j = j1;
+        const int b = u.b0 + j, exps = sh.exps[ur.slot][j], W = sh.multipliers[eq + (exps & 255)];
         ok = ok && warp_wait(&sh.sfull[slot], sphases >> slot & 1);
         sphases ^= 1u << slot;
         if (!ok) break;
         ptx::tc_fence_after();
-        int top = INT32_MIN;
-        uint32_t s0[32], s1[32];
-        ptx::tmem_ld32(s_mem + slot * 128, s0);
-        ptx::tmem_ld32(s_mem + slot * 128 + 32, s1);
-        ptx::tmem_ld_wait32(s0);
-        ptx::tmem_ld_wait32(s1);
-        if (whole) {
-          int m[4] = {(int)s0[0], (int)s0[1], (int)s0[2], (int)s0[3]};
+        int m[4] = {INT32_MIN, INT32_MIN, INT32_MIN, INT32_MIN};
+        auto most = [&](auto masked) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) m[i & 3] = max(m[i & 3], max((int)s0[i], (int)s1[i]));
-          top = max(max(m[0], m[1]), max(m[2], m[3]));
-        } else {
-          const int first = see.first - b * kAttnBlock - half * kHalf, last = see.last - b * kAttnBlock - half * kHalf;
+          for (int c0 = 0; c0 < kAttnBlock; c0 += 64) {
+            uint32_t s0[32], s1[32];
+            ptx::tmem_ld32(tmem + lanes + (slot & 3) * 128 + c0, s0);
+            ptx::tmem_ld32(tmem + lanes + (slot & 3) * 128 + c0 + 32, s1);
+            ptx::tmem_ld_wait32(s0);
+            ptx::tmem_ld_wait32(s1);
+            if (c0) release(slot, 2);
+            const int first = see.first - b * kAttnBlock - c0, last = see.last - b * kAttnBlock - c0;
 #pragma unroll
-          for (int i = 0; i < 32; ++i) {
-            top = i >= first && i < last ? max(top, (int)s0[i]) : top;
-            top = i + 32 >= first && i + 32 < last ? max(top, (int)s1[i]) : top;
+            for (int i = 0; i < 32; ++i) {
+              if (masked.value) {
+                m[i & 3] = i >= first && i < last ? max(m[i & 3], (int)s0[i]) : m[i & 3];
+                m[i & 3] = i + 32 >= first && i + 32 < last ? max(m[i & 3], (int)s1[i]) : m[i & 3];
+              } else {
+                m[i & 3] = max(m[i & 3], max((int)s0[i], (int)s1[i]));
+              }
+            }
           }
-        }
-        ptx::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.sempty[slot]));
-        if (sh.ids[ur.slot][j] >= 0 && top != INT32_MIN) {
+        };
+        if (b >= whole0 && b < whole1) most(std::false_type());
+        else most(std::true_type());
+        const int top = max(max(m[0], m[1]), max(m[2], m[3]));
+        if (!(exps & kBad) && top != INT32_MIN) {
           T = max(T, score_octaves(top, W));
-          V = max(V, (int)sh.ev[ur.slot][j]);
+          V = max(V, exps >> 8 & 127);
         }
       }
       sh.top[part][r] = T;
@@ -388,11 +419,14 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
         T = max(T, sh.top[i][r]);
         V = max(V, sh.vexp[i][r]);
       }
+      // S 0 and 1 are read by all of a group from here on: what its other half has read counts, too
+      const int other = w + 2 * (half ^ 1);
+      sphases ^= (uint32_t)((rest - other + 3) >> 2 & (rest > other)) << other;
       long long L = 0;
       for (int j = w; j < n; j += 2) {
-        const int b = u.b0 + j, W = score_multiplier(a.score_m0, eq + sh.ek[ur.slot][j], a.score_s);
-        const bool bad = sh.ids[ur.slot][j] < 0, whole = b >= whole0 && b < whole1 && !bad;
-        const int d = max(V - sh.ev[ur.slot][j], 0), C = -(T + 8192 * d);
+        const int b = u.b0 + j, exps = sh.exps[ur.slot][j], W = sh.multipliers[eq + (exps & 255)];
+        const bool bad = exps & kBad, whole = b >= whole0 && b < whole1 && !bad;
+        const int d = max(V - (exps >> 8 & 127), 0), C = -(T + 8192 * d);
         const int first = bad ? INT32_MAX : see.first - b * kAttnBlock - half * kHalf, last = see.last - b * kAttnBlock - half * kHalf;
         ok = ok && warp_wait(&sh.sfull[w], sphases >> w & 1);
         sphases ^= 1u << w;
@@ -409,10 +443,8 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
           for (int i = 0; i < 16; ++i) s[i] = ahead[i];
           if (c0 + 16 < kHalf) {                        // the next ones come while these are worked on
             ptx::tmem_ld16(s_mem + w * 128 + c0 + 16, ahead);
-          } else {                       // S may be written over
-            ptx::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.sempty[w]));
+          } else {
+            release(w, 1);
           }
           uint32_t hi[4], lo[4];
           auto weights = [&](auto masked) {
@@ -453,7 +485,9 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
       const Reciprocal rec = reciprocal(max(L, 1ll), V);
       constexpr int kLanes = D / 4, kAtOnce = 32 / kLanes, kRounds = kRows / (kSoft / 2 * kAtOnce);   // lanes of a row, rows of a warp
       const int piece = lane % kLanes;
-      int t = (warp - 4) * kAtOnce + lane / kLanes, token = (rem0 + t) / a.group, hd = u.head * a.group + rem0 + t - token * a.group;
+      const int t0 = (warp - 4) * kAtOnce + lane / kLanes;
+      auto head_of = [&](int t) { return u.head * a.group + rem0 + t - (int)((uint32_t)(rem0 + t) * by_group >> 16) * a.group; };
+      int hd = head_of(t0);
       int4 rq[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) rq[e] = a.out[hd * D + piece * 4 + e];
@@ -482,38 +516,45 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
       __syncwarp();
       if (lane == 0 && n) ptx::mbar_arrive(ptx::smem_u32(&sh.oempty));
       ptx::named_barrier(2, 16 * kSoft);
-#pragma unroll 2
-      for (int i = 0; i < kRounds && ok; ++i) {
-        if (tile.flat0 + t >= tile.flats) break;
-        const int4 o = *reinterpret_cast<const int4*>(smem + (pbuf - table) + t * (4 * D) + ((piece ^ (t & 7)) << 4));
-        const int y[4] = {requantised(o.x, rq[0], a.lo, a.hi), requantised(o.y, rq[1], a.lo, a.hi), requantised(o.z, rq[2], a.lo, a.hi),
-                          requantised(o.w, rq[3], a.lo, a.hi)};
-        const long long to = (long long)(u.row0 + token0 + token) * f.ldy + hd * D + piece * 4;
-        if (a.y_bytes == 1) {
-          int8_t* p = (int8_t*)f.y + to;
-          if (f.vector) {
-            *reinterpret_cast<uint32_t*>(p) = __byte_perm(__byte_perm((uint32_t)y[0], (uint32_t)y[1], 0x0040),
-                                                          __byte_perm((uint32_t)y[2], (uint32_t)y[3], 0x0040), 0x5410);
-          } else {
+#pragma unroll 1
+      for (int i = 0; i < kRounds && ok; i += 4) {      // four rows on their way at a time
+        int4 o[4];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) p[e] = (int8_t)y[e];
-          }
-        } else {
-          int* p = (int*)f.y + to;
-          if (f.vector) {
-            *reinterpret_cast<int4*>(p) = make_int4(y[0], y[1], y[2], y[3]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) p[e] = y[e];
-          }
+        for (int e = 0; e < 4; ++e) {
+          const int t = t0 + (i + e) * (kSoft / 2 * kAtOnce);
+          o[e] = *reinterpret_cast<const int4*>(smem + (pbuf - table) + t * (4 * D) + ((piece ^ (t & 7)) << 4));
         }
-        t += kSoft / 2 * kAtOnce;
-        token = (rem0 + t) / a.group;
-        const int next = u.head * a.group + rem0 + t - token * a.group;
-        if (next != hd) {
-          hd = next;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) rq[e] = a.out[hd * D + piece * 4 + e];
+        for (int e = 0; e < 4; ++e) {
+          const int t = t0 + (i + e) * (kSoft / 2 * kAtOnce), at = head_of(t);
+          if (at != hd) {
+            hd = at;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) rq[k] = a.out[hd * D + piece * 4 + k];
+          }
+          const int y[4] = {requantised(o[e].x, rq[0], a.lo, a.hi), requantised(o[e].y, rq[1], a.lo, a.hi), requantised(o[e].z, rq[2], a.lo, a.hi),
+                            requantised(o[e].w, rq[3], a.lo, a.hi)};
+          if (tile.flat0 + t < tile.flats) {
+            const long long to = (long long)(u.row0 + token0 + (int)((uint32_t)(rem0 + t) * by_group >> 16)) * f.ldy + hd * D + piece * 4;
+            if (a.y_bytes == 1) {
+              int8_t* p = (int8_t*)f.y + to;
+              if (f.vector) {
+                *reinterpret_cast<uint32_t*>(p) = __byte_perm(__byte_perm((uint32_t)y[0], (uint32_t)y[1], 0x0040),
+                                                              __byte_perm((uint32_t)y[2], (uint32_t)y[3], 0x0040), 0x5410);
+              } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) p[k] = (int8_t)y[k];
+              }
+            } else {
+              int* p = (int*)f.y + to;
+              if (f.vector) {
+                *reinterpret_cast<int4*>(p) = make_int4(y[0], y[1], y[2], y[3]);
+              } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) p[k] = y[k];
+              }
+            }
+          }
         }
       }
       __syncwarp();

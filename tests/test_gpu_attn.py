@@ -186,6 +186,14 @@ def test_forward_lengths(held, add, dim):
     G.iodf_attn_check(_forward_both(C.description(torch, 4, 2, dim), held, add, dim + len(held), padding=2))
 
 
+@pytest.mark.parametrize("held,add,heads,kv,dim,window", [([1500, 1300], [1500, 200], 2, 1, 32, 0), ([2300], [700], 4, 2, 128, 0), ([1100] * 5, [150] * 5, 8, 8, 64, 0),
+                                                          ([3000], [260], 16, 2, 64, 1400), ([1025, 1024, 1152, 1153], [129, 128, 40, 300], 6, 2, 32, 0)])
+def test_forward_of_many_blocks(held, add, heads, kv, dim, window):
+    """Rows that see more than eight blocks, and more units than fit on the GPU at once."""
+    torch, G = _modules()
+    G.iodf_attn_check(_forward_both(C.description(torch, heads, kv, dim, window=window), held, add, len(held)))
+
+
 @pytest.mark.parametrize("heads,kv", [(1, 1), (3, 1), (8, 8), (8, 1), (10, 2), (17, 1), (40, 2), (64, 1), (129, 3)])
 @pytest.mark.parametrize("held,add", [([200], [1]), ([300, 77], [1, 1]), ([140, 3], [40, 3])])
 def test_forward_heads(heads, kv, held, add):
