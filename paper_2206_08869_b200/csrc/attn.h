@@ -24,6 +24,7 @@ struct AttnArgs {                        // what a handle holds
   int score_s;
   int causal, window;
   int y_type, y_bytes, lo, hi;
+  int y_full;                            // 8-bit signed outputs, clipped to their type's range
   const int4* out;                       // [heads * dim] {M0, s, low and high word of 2^(30 + s)}
   uint32_t* status;                      // [0] a bounded wait gave up, [1] requests or rows that could not be served
   int sms;

@@ -92,6 +92,7 @@ int create_attn(const iodf_attn_desc& d, int device, iodf_attn& h) {
   a.window = (int)d.window;
   a.y_type = (int)d.y_type;
   a.y_bytes = d.y_type == IODF_I32 ? 4 : 1;
+  a.y_full = d.y_type == IODF_I8 && lo == -128 && hi == 127;
   a.lo = lo;
   a.hi = hi;
   a.out = reinterpret_cast<const int4*>(m + o_out);

@@ -48,7 +48,12 @@ __device__ __forceinline__ Reciprocal reciprocal(long long L, int V) {
   r.V = V;
   r.a = __clzll(L) - 32;                       // 2^31 <= L 2^a < 2^32
   const unsigned long long l = r.a >= 0 ? (unsigned long long)L << r.a : (unsigned long long)L >> -r.a;
-  r.rho = (uint32_t)(0x7FFFFFFFFFFFFFFFull / l);
+  // The quotient of doubles is off by less than one (it has 32 bits); the remainder says which way.
+  constexpr unsigned long long kTop = 0x7FFFFFFFFFFFFFFFull;
+  unsigned long long q = (unsigned long long)(9223372036854775808.0 * __drcp_rn((double)l));
+  if (q * l > kTop) --q;
+  else if (kTop - q * l >= l) ++q;
+  r.rho = (uint32_t)q;
   return r;
 }
 // A = 256 hi + lo
@@ -59,11 +64,12 @@ __device__ __forceinline__ int quotient(int hi, int lo, const Reciprocal& r) {
   return (top + ((1 << (15 - r.V)) >> 1)) >> (15 - r.V);
 }
 
-// y = clip(floor((o M0 + 2^(30 + s)) / 2^(31 + s))); out: {M0, s, low and high word of the addend}; |o| < 2^27
-__device__ __forceinline__ int requantised(int o, int4 out, int lo, int hi) {
+// floor((o M0 + 2^(30 + s)) / 2^(31 + s)), and its clip; out: {M0, s, low and high word of the addend}; |o| < 2^27
+__device__ __forceinline__ int requantised(int o, int4 out) {
   const long long v = (long long)o * out.x + (long long)((unsigned long long)(uint32_t)out.w << 32 | (uint32_t)out.z);
-  return min(max((int)__funnelshift_l((uint32_t)v, (uint32_t)(v >> 32), 1) >> out.y, lo), hi);
+  return (int)__funnelshift_l((uint32_t)v, (uint32_t)(v >> 32), 1) >> out.y;
 }
+__device__ __forceinline__ int clipped(int y, int lo, int hi) { return min(max(y, lo), hi); }
 
 // Keys that a row sees: [first, last)
 struct Range {

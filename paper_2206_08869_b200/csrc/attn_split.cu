@@ -556,7 +556,7 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
             const bool any = __shfl_sync(0xFFFFFFFFu, (int)(L > 0), e) != 0;
             if (e % kGroups == w && key < D && ok) {
               const int at = (u.head * a.group + (u.flat0 + e) % a.group) * D + key;
-              store(e, key, requantised(any ? quotient((int)hi[e], (int)lo[e], rec) : 0, a.out[at], a.lo, a.hi));
+              store(e, key, clipped(requantised(any ? quotient((int)hi[e], (int)lo[e], rec) : 0, a.out[at]), a.lo, a.hi));
             }
           }
         }
@@ -600,7 +600,7 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
             all += sh.team_sum[m][e];
           }
           const int at = (u.head * a.group + (u.flat0 + e) % a.group) * D + dim;
-          store(e, dim, requantised(all ? quotient(hi_all, lo_all, reciprocal(all, sh.vtop[e])) : 0, a.out[at], a.lo, a.hi));
+          store(e, dim, clipped(requantised(all ? quotient(hi_all, lo_all, reciprocal(all, sh.vtop[e])) : 0, a.out[at]), a.lo, a.hi));
         }
       }
       __syncwarp();

@@ -122,6 +122,17 @@ __device__ __forceinline__ void split4(const uint32_t (&w)[4], uint32_t* hi, uin
   *hi = __byte_perm(a, b, 0x7632);
 }
 
+// Four outputs of a word, saturated to signed 8 bits.
+__device__ __forceinline__ uint32_t packed(int a, int b, int c, int d) {
+  uint32_t r;
+  asm("{\n\t.reg .b32 t;\n\t"
+      "cvt.pack.sat.s8.s32.b32 t, %4, %3, 0;\n\t"
+      "cvt.pack.sat.s8.s32.b32 %0, %2, %1, t;\n\t}"
+      : "=r"(r)
+      : "r"(a), "r"(b), "r"(c), "r"(d));
+  return r;
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
                                                             const AttnArgs a, const CacheArgs c, const ForwardArgs f) {
@@ -516,43 +527,48 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
       __syncwarp();
       if (lane == 0 && n) ptx::mbar_arrive(ptx::smem_u32(&sh.oempty));
       ptx::named_barrier(2, 16 * kSoft);
-#pragma unroll 1
-      for (int i = 0; i < kRounds && ok; i += 4) {      // four rows on their way at a time
-        int4 o[4];
+      constexpr int kStep = kSoft / 2 * kAtOnce;                       // rows of the eight warps together
+      const uint8_t* const piece_at = smem + (pbuf - table);
+      auto quotients = [&](int t) { return *reinterpret_cast<const int4*>(piece_at + t * (4 * D) + ((piece ^ (t & 7)) << 4)); };
+      if (f.vector && a.y_full && kStep % a.group == 0 && tile.flats - tile.flat0 == kRows && ok) {
+        // Rows of a warp have one head, tokens at one distance, and the outputs' clip is the type's: 8-bit outputs in words.
+        int8_t* p = (int8_t*)f.y + (long long)(u.row0 + token0 + (int)((uint32_t)(rem0 + t0) * by_group >> 16)) * f.ldy + hd * D + piece * 4;
+        const long long step = (long long)(kStep / a.group) * f.ldy;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int t = t0 + (i + e) * (kSoft / 2 * kAtOnce);
-          o[e] = *reinterpret_cast<const int4*>(smem + (pbuf - table) + t * (4 * D) + ((piece ^ (t & 7)) << 4));
+        for (int i = 0; i < kRounds; ++i, p += step) {
+          const int4 o = quotients(t0 + i * kStep);
+          *reinterpret_cast<uint32_t*>(p) = packed(requantised(o.x, rq[0]), requantised(o.y, rq[1]), requantised(o.z, rq[2]), requantised(o.w, rq[3]));
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int t = t0 + (i + e) * (kSoft / 2 * kAtOnce), at = head_of(t);
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < kRounds && ok; ++i) {
+          const int t = t0 + i * kStep, at = head_of(t);
           if (at != hd) {
             hd = at;
 #pragma unroll
             for (int k = 0; k < 4; ++k) rq[k] = a.out[hd * D + piece * 4 + k];
           }
-          const int y[4] = {requantised(o[e].x, rq[0], a.lo, a.hi), requantised(o[e].y, rq[1], a.lo, a.hi), requantised(o[e].z, rq[2], a.lo, a.hi),
-                            requantised(o[e].w, rq[3], a.lo, a.hi)};
-          if (tile.flat0 + t < tile.flats) {
-            const long long to = (long long)(u.row0 + token0 + (int)((uint32_t)(rem0 + t) * by_group >> 16)) * f.ldy + hd * D + piece * 4;
-            if (a.y_bytes == 1) {
-              int8_t* p = (int8_t*)f.y + to;
-              if (f.vector) {
-                *reinterpret_cast<uint32_t*>(p) = __byte_perm(__byte_perm((uint32_t)y[0], (uint32_t)y[1], 0x0040),
-                                                              __byte_perm((uint32_t)y[2], (uint32_t)y[3], 0x0040), 0x5410);
-              } else {
-#pragma unroll
-                for (int k = 0; k < 4; ++k) p[k] = (int8_t)y[k];
-              }
+          if (tile.flat0 + t >= tile.flats) break;
+          const int4 o = quotients(t);
+          const int y[4] = {clipped(requantised(o.x, rq[0]), a.lo, a.hi), clipped(requantised(o.y, rq[1]), a.lo, a.hi),
+                            clipped(requantised(o.z, rq[2]), a.lo, a.hi), clipped(requantised(o.w, rq[3]), a.lo, a.hi)};
+          const long long to = (long long)(u.row0 + token0 + (int)((uint32_t)(rem0 + t) * by_group >> 16)) * f.ldy + hd * D + piece * 4;
+          if (a.y_bytes == 1) {
+            int8_t* p = (int8_t*)f.y + to;
+            if (f.vector) {
+              *reinterpret_cast<uint32_t*>(p) = __byte_perm(__byte_perm((uint32_t)y[0], (uint32_t)y[1], 0x0040),
+                                                            __byte_perm((uint32_t)y[2], (uint32_t)y[3], 0x0040), 0x5410);
             } else {
-              int* p = (int*)f.y + to;
-              if (f.vector) {
-                *reinterpret_cast<int4*>(p) = make_int4(y[0], y[1], y[2], y[3]);
-              } else {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) p[k] = y[k];
-              }
+              for (int k = 0; k < 4; ++k) p[k] = (int8_t)y[k];
+            }
+          } else {
+            int* p = (int*)f.y + to;
+            if (f.vector) {
+              *reinterpret_cast<int4*>(p) = make_int4(y[0], y[1], y[2], y[3]);
+            } else {
+#pragma unroll
+              for (int k = 0; k < 4; ++k) p[k] = y[k];
             }
           }
         }
