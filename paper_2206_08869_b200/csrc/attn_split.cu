@@ -22,25 +22,31 @@
 namespace iodf {
 namespace {
 
-constexpr int kN = 16;                   // of the MMAs, the least; a unit has up to 4, 8 or 16 rows
-constexpr int kGroups = 4;               // of four softmax warps
-constexpr int kThreadsS = 128 + 128 * kGroups;           // warp 0 copies, 1 MMAs, 2 units, 3 queries, then softmax
-constexpr int kWarpsS = kThreadsS / 32, kSoft = 4 * kGroups;
-constexpr int kRingS = 5, kUnitsS = 3;
-constexpr int kScores = 30, kHeld = 26;  // S in tensor memory; of the first blocks they stay there, the last ones take turns
+constexpr int kN = 16;                   // of the scores' MMAs, the least; a unit has up to 4, 8 or 16 rows
+constexpr int kUnitsS = 3;
 constexpr int kTileBytes = 16384;        // of a slot: 128 rows of up to 128 bytes; V^T is read as 128 rows whatever the dimension
-constexpr int kDynamic = 200 * 1024;
 constexpr int kLeastCluster = 8, kMaxTeam = kAttnMaxTeam, kClasses = 5;             // teams of 1, 2, 4, 8; of a whole cluster
 constexpr int kMaxPart = kAttnMaxBlocks / kLeastCluster;          // blocks of one CTA
 constexpr int kMaxChunks = kAttnSplitRequests / 32;
 
-// Shared memory beside the ring. Operands of 16 rows of which only the first kCols count: the others may be anything.
-template <int kCols>
-struct Layout {
-  static constexpr int kOperand = kCols > 8 ? 2048 : 1024;
-  static constexpr int kP = kRingS * kTileBytes, kQ = kP + kGroups * 2 * kOperand, kSums = kQ + 2 * kOperand + 1024;
+// Two shapes: one CTA to an SM, with room for the scores of many blocks, or two, so that one unit's waits are another's work.
+//   weights: hi = (p + 128) >> 8 and the low byte of p + 128, which is 128 more than lo; both are unsigned, so one MMA has rows of hi, rows of
+//   lo and a row of ones, whose product (the sum of v) takes the 128 off again. 16 rows need two MMAs: hi, and lo signed.
+template <int kCols, int kGroups>
+struct Shape {
+  static constexpr int kThreads = 128 + 128 * kGroups, kWarps = kThreads / 32, kSoft = 4 * kGroups;     // warp 0 copies, 1 MMAs, 2 units, 3 queries, then softmax
+  static constexpr bool kBig = kGroups == 4;
+  static constexpr int kRing = kBig ? 5 : 3, kColumns = kBig ? 512 : 256;                               // stages; of tensor memory
+  static constexpr int kO = kCols == 4 ? 16 : 32;                                                      // of O: N of its MMAs, or twice 16
+  static constexpr int kScores = (kColumns - 32) / kN, kHeld = kScores - 4;      // S: of the first blocks they stay, the last four take turns
+  static constexpr int kDynamic = (kBig ? 200 : 86) * 1024;
+  static constexpr int kOperand = kCols > 4 ? 4096 : 2048;                                             // of weights: rows of 128 bytes
+  static constexpr int kQBytes = kCols > 8 ? 2048 : 1024;                                              // of queries; MMAs read 16 rows, the others may be anything
+  static constexpr int kP = kRing * kTileBytes, kQ = kP + 2 * kGroups * kOperand, kSums = kQ + 2 * kQBytes + 1024;
   static constexpr int kKept = kSums + 128 * kCols * 8;
-  static constexpr int kKeptBlocks = (kDynamic - 1024 - kKept) / (kCols * 512);      // t of 128 keys, 32 bits
+  static constexpr int kKeptBlocks = (kDynamic - 1024 - kKept) / (kCols * 512) > 0 ? (kDynamic - 1024 - kKept) / (kCols * 512) : 0;      // t of 128 keys, 32 bits
+  static constexpr int kKeep = kHeld + kKeptBlocks;
+  static_assert(kKept + 1024 <= kDynamic, "shared memory");
 };
 
 struct UnitS {
@@ -50,16 +56,17 @@ struct UnitS {
   int cls, team, member;                 // CTAs, and which of them
 };
 
+template <class Sh>
 struct SharedS {
-  uint64_t full[kRingS], empty[kRingS], sfull[kScores], sempty[kScores], pfull[kGroups], pempty[kGroups], qfull[2], qempty[2];
+  uint64_t full[Sh::kRing], empty[Sh::kRing], sfull[Sh::kScores], sempty[Sh::kScores], pfull[Sh::kWarps], pempty[Sh::kWarps], qfull[2], qempty[2];
   uint64_t ofull, oempty, ufull[kUnitsS], uempty[kUnitsS], tops[kClasses], sums[kClasses];
   uint32_t abort_flag, tmem;
   int total[kClasses];                   // units of each class
   UnitS units[kUnitsS];
   int ids[kUnitsS][kMaxPart];            // blocks; -1: outside the cache, nobody sees it
   uint8_t ek[kUnitsS][kMaxPart], ev[kUnitsS][kMaxPart];
-  int top[kSoft][kN], vexp[kSoft][kN];   // of the softmax warps
-  long long sum[kSoft][kN];
+  int top[Sh::kSoft][kN], vexp[Sh::kSoft][kN];           // of the softmax warps
+  long long sum[Sh::kSoft][kN];
   int vtop[kN];                          // V of each row, over the team
   int team_top[kMaxTeam][kN], team_vexp[kMaxTeam][kN];
   long long team_sum[kMaxTeam][kN];
@@ -99,13 +106,15 @@ struct Ask {
   }
 };
 
-template <int D, int kCols>
-__global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
+template <int D, int kCols, int kGroups>
+__global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) split_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
                                                              const AttnArgs a, const CacheArgs c, const ForwardArgs f, const SplitArgs s) {
-  typedef Layout<kCols> At;
+  typedef Shape<kCols, kGroups> At;
+  constexpr int kThreadsS = At::kThreads, kWarpsS = At::kWarps, kSoft = At::kSoft, kRingS = At::kRing, kScores = At::kScores, kHeld = At::kHeld,
+                kKeep = At::kKeep, kBuffers = 2 * kGroups;
   extern __shared__ uint8_t raw[];
   uint8_t* const smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~(uintptr_t)1023);
-  __shared__ SharedS sh;
+  __shared__ SharedS<At> sh;
   __shared__ int table[kWeightSegments * 32];           // a copy for each lane: no bank is asked twice
   __shared__ int before[kClasses][kMaxChunks + 1];      // units of each class before a chunk of 32 requests
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -122,8 +131,8 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
     init(sh.empty, kRingS, 1);
     init(sh.sfull, kScores, 1);
     init(sh.sempty, kScores, 4);
-    init(sh.pfull, kGroups, 4);
-    init(sh.pempty, kGroups, 1);
+    init(sh.pfull, kBuffers, 4);
+    init(sh.pempty, kBuffers, 1);
     init(sh.qfull, 2, 1);
     init(sh.qempty, 2, 1);
     init(&sh.ofull, 1, 1);
@@ -138,8 +147,12 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
     sh.abort_flag = 0;
   }
   ptx::cluster_arrive();                                // every CTA runs, its barriers are set up
-  if (warp == 2) ptx::tmem_alloc(ptx::smem_u32(&sh.tmem), 512);
+  if (warp == 2) ptx::tmem_alloc(ptx::smem_u32(&sh.tmem), At::kColumns);
   for (int i = tid; i < kWeightSegments * 32; i += kThreadsS) table[i] = weight_word(i / 32);
+  if (kCols < 16)                                       // the rows of ones
+    for (int i = tid; i < kBuffers * 32; i += kThreadsS)
+      reinterpret_cast<uint32_t*>(smem + At::kP + i / 32 * At::kOperand + 2 * kCols * 128)[i % 32] = 0x01010101u;
+  ptx::fence_async_smem();
   for (int k = warp; k < s.chunks; k += kWarpsS) {
     const Ask ask(a, f, s, kCols, k * 32 + lane);
 #pragma unroll
@@ -170,8 +183,8 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
     }
   }
   __syncthreads();
-  const uint32_t tmem = sh.tmem, o_hi = tmem + kScores * kN, o_lo = o_hi + kN;
-  auto wait = [&](uint64_t* bar, uint32_t phase) { return ptx::spin_wait(abort_flag, a.status, bar, phase); };
+  const uint32_t tmem = sh.tmem, o_mem = tmem + kScores * kN;
+  auto wait = [&](uint64_t* bar, uint32_t phase) { return ptx::quick_wait(abort_flag, a.status, bar, phase, kSpinLimit); };
   auto lazy = [&](uint64_t* bar, uint32_t phase) { return ptx::lazy_wait(abort_flag, a.status, bar, phase); };
   auto warp_wait = [&](uint64_t* bar, uint32_t phase) { return __all_sync(0xFFFFFFFFu, wait(bar, phase)) != 0; };
   auto take = [&](const RingS& r, UnitS* u) {
@@ -185,9 +198,9 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
     ptx::mbar_acquire_cluster(ptx::smem_u32(bar), phase);
     return true;
   };
-  // blocks whose scores or t are kept; the rest's scores are computed twice
-  constexpr int kKeep = kHeld + At::kKeptBlocks;
+  // of blocks from kKeep on the scores are computed twice
   // where the scores of the unit's block i are: all of a call's uses of a slot are counted in bits, one for each
+  auto buffer_of = [](int i) { return 2 * (i % kGroups) + (i / kGroups & 1); };     // of weights, two for each group
   auto slot_of = [](int i) { return i < kHeld ? i : kHeld + (i - kHeld) % (kScores - kHeld); };
 
   if (warp == 0) {
@@ -217,7 +230,8 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
     __syncwarp();
   } else if (warp == 1) {
     if (ptx::elect_one()) {
-      constexpr uint32_t id_s = idesc_i8(128, kN, false, false), id_hi = idesc_i8(128, kN, false, true), id_lo = idesc_i8(128, kN, false, false);
+      constexpr uint32_t id_s = idesc_i8(128, kN, false, false), id_lo = idesc_i8(128, 16, false, false);
+      constexpr uint32_t id_p = idesc_i8(128, kCols == 16 ? 16 : At::kO, false, true);
       constexpr uint32_t hi_d = rows_hi(D), hi_128 = rows_hi(128);
       RingS r, ur, qr, orr;
       uint32_t pphases = 0, sphases = 0;
@@ -238,20 +252,22 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
       for (; ok && take(ur, &u); ur.next(kUnitsS)) {
         ok = wait(&sh.qfull[qr.slot], qr.phase);
         ptx::tc_fence_after();
-        const uint32_t q = rows_lo(qbuf + qr.slot * At::kOperand);
+        const uint32_t q = rows_lo(qbuf + qr.slot * At::kQBytes);
         for (int i = 0; i < u.n && ok; ++i) scores(q, slot_of(i));
         for (int i = 0; i < u.n && ok; ++i) {
-          const int g = i % kGroups;
+          const int g = buffer_of(i);
           if (i >= kKeep) scores(q, slot_of(i));
           if (i == 0) ok = ok && wait(&sh.oempty, orr.phase ^ 1);
           ok = ok && wait(&sh.pfull[g], pphases >> g & 1) && wait(&sh.full[r.slot], r.phase);
           if (!ok) break;
           ptx::tc_fence_after();
-          const uint32_t v = rows_lo(ring + r.slot * kTileBytes), p = rows_lo(pbuf + g * 2 * At::kOperand);
+          const uint32_t v = rows_lo(ring + r.slot * kTileBytes), p = rows_lo(pbuf + g * At::kOperand);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) ptx::umma_i8_hl(o_hi, v + 2 * k, hi_128, p + 2 * k, hi_128, id_hi, i > 0 || k > 0);
+          for (int k = 0; k < 4; ++k) ptx::umma_i8_hl(o_mem, v + 2 * k, hi_128, p + 2 * k, hi_128, id_p, i > 0 || k > 0);
+          if (kCols == 16) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k) ptx::umma_i8_hl(o_lo, v + 2 * k, hi_128, p + (At::kOperand >> 4) + 2 * k, hi_128, id_lo, i > 0 || k > 0);
+            for (int k = 0; k < 4; ++k) ptx::umma_i8_hl(o_mem + 16, v + 2 * k, hi_128, p + (2048 >> 4) + 2 * k, hi_128, id_lo, i > 0 || k > 0);
+          }
           ptx::umma_commit(ptx::smem_u32(&sh.empty[r.slot]));
           ptx::umma_commit(ptx::smem_u32(&sh.pempty[g]));
           pphases ^= 1u << g;
@@ -265,7 +281,7 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
         qr.next(2);
         ptx::mbar_arrive(ptx::smem_u32(&sh.uempty[ur.slot]));
       }
-      for (int i = 0; ok && i < kGroups; ++i) ok = wait(&sh.pempty[i], (pphases >> i & 1) ^ 1);
+      for (int i = 0; ok && i < kBuffers; ++i) ok = wait(&sh.pempty[i], (pphases >> i & 1) ^ 1);
     }
     __syncwarp();
   } else if (warp == 2) {
@@ -350,7 +366,7 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
         const int r = i / (D / 16), piece = i % (D / 16), flat = u.flat0 + r;
         const long long row = u.row0 + flat / a.group;
         const int4 v = *reinterpret_cast<const int4*>(f.q8 + (row * a.heads + u.head * a.group + flat % a.group) * D + piece * 16);
-        ptx::sts128(qbuf + qr.slot * At::kOperand + swizzled(r, piece, D), v.x, v.y, v.z, v.w);
+        ptx::sts128(qbuf + qr.slot * At::kQBytes + swizzled(r, piece, D), v.x, v.y, v.z, v.w);
       }
       ptx::fence_async_smem();
       __syncwarp();
@@ -363,9 +379,8 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
   } else {
     const int w = (warp - 4) >> 2, quarter = warp & 3, key = quarter * 32 + lane, me = warp - 4;
     const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
-    const uint32_t p_hi = pbuf + w * 2 * At::kOperand, p_lo = p_hi + At::kOperand;
     RingS ur, orr;
-    uint32_t pphase = 1, team_phases = 0, sphases = 0;
+    uint32_t pphases = 0, team_phases = 0, sphases = 0;
     UnitS u;
     bool ok = true;
     while (ptx::all_agree(1, 32 * kSoft, take(ur, &u))) {
@@ -469,8 +484,10 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
 #pragma unroll
       for (int e = 0; e < kCols; ++e) Ls[e] = 0;
       for (int i = w; i < u.n && ok; i += kGroups) {
-        ok = warp_wait(&sh.pempty[w], pphase) && (i < kKeep || warp_wait(&sh.sfull[slot_of(i)], sphases >> slot_of(i) & 1));
-        pphase ^= 1;
+        const int buffer = buffer_of(i);
+        const uint32_t p_hi = pbuf + buffer * At::kOperand, p_lo = p_hi + kCols * 128;
+        ok = warp_wait(&sh.pempty[buffer], (pphases >> buffer & 1) ^ 1) && (i < kKeep || warp_wait(&sh.sfull[slot_of(i)], sphases >> slot_of(i) & 1));
+        pphases ^= 1u << buffer;
         if (!ok) break;
         ptx::tc_fence_after();
         const int below = max(V - sh.ev[ur.slot][i], 0), off = -(T + 8192 * below);
@@ -489,14 +506,15 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
           const int n = t[e] == INT32_MIN ? kWeightLow : max(t[e] + down, kWeightLow);
           const uint32_t x = weight_bits(n, *reinterpret_cast<const int*>(reinterpret_cast<const char*>(table) + ((n & ((kWeightSegments - 1) << 7)) | lane * 4)));
           const uint32_t at = (uint32_t)(e * 128 + (((key >> 4) ^ (e & 7)) << 4) + (key & 15));
+          const uint32_t at_lo = (uint32_t)(e * 128 + (((key >> 4) ^ ((e + kCols) & 7)) << 4) + (key & 15));
           asm volatile("st.shared.u8 [%0], %1;" ::"r"(p_hi + at), "r"(x >> 8) : "memory");
-          asm volatile("st.shared.u8 [%0], %1;" ::"r"(p_lo + at), "r"(x ^ 0x80u) : "memory");
+          asm volatile("st.shared.u8 [%0], %1;" ::"r"(p_lo + at_lo), "r"(kCols == 16 ? x ^ 0x80u : x) : "memory");
           Ls[e] += (x - kWeightBias) << by;             // below 2^28
         }
         ptx::tc_fence_before();
         ptx::fence_async_smem();
         __syncwarp();
-        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.pfull[w]));
+        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.pfull[buffer]));
       }
       long long L = 0;                                  // of row `lane`
 #pragma unroll
@@ -517,21 +535,25 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
         orr.next(1);
         ptx::tc_fence_after();
         if (ok) {
-          if constexpr (kCols == 4) {
-            ptx::tmem_ld4(o_hi + lanes, hi);
-            ptx::tmem_ld4(o_lo + lanes, lo);
-            ptx::tmem_ld_wait4(hi);
-            ptx::tmem_ld_wait4_nosync(lo);
-          } else if constexpr (kCols == 8) {
-            ptx::tmem_ld8(o_hi + lanes, hi);
-            ptx::tmem_ld_wait8(hi);
-            ptx::tmem_ld8(o_lo + lanes, lo);
-            ptx::tmem_ld_wait8(lo);
+          uint32_t x[16];
+          ptx::tmem_ld16(o_mem + lanes, x);
+          ptx::tmem_ld_wait16(x);
+          if constexpr (kCols == 16) {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) hi[e] = x[e];
+            ptx::tmem_ld16(o_mem + 16 + lanes, lo);
+            ptx::tmem_ld_wait16(lo);
           } else {
-            ptx::tmem_ld16(o_hi + lanes, hi);
-            ptx::tmem_ld16(o_lo + lanes, lo);
-            ptx::tmem_ld_wait16(hi);
-            ptx::tmem_ld_wait16_nosync(lo);
+            uint32_t more[4] = {x[8], 0, 0, 0};
+            if constexpr (kCols == 8) {
+              ptx::tmem_ld4(o_mem + 16 + lanes, more);
+              ptx::tmem_ld_wait4(more);
+            }
+#pragma unroll
+            for (int e = 0; e < kCols; ++e) {
+              hi[e] = x[e];
+              lo[e] = x[kCols + e] - 128u * more[0];
+            }
           }
         }
         ptx::tc_fence_before();
@@ -611,30 +633,37 @@ __global__ void __launch_bounds__(kThreadsS, 1) split_kernel(const __grid_consta
   ptx::tc_fence_before();
   __syncthreads();
   ptx::tc_fence_after();
-  if (warp == 2) ptx::tmem_dealloc(tmem, 512);
+  if (warp == 2) ptx::tmem_dealloc(tmem, At::kColumns);
   ptx::cluster_arrive();                                // nobody leaves while another CTA may still write into its memory
   ptx::cluster_wait();
 }
 
-template <int D, int kCols>
+template <int D, int kCols, int kGroups>
 cudaError_t configure() {
-  static_assert(sizeof(SharedS) + 4 * (kWeightSegments * 32 + kClasses * (kMaxChunks + 1)) + kDynamic <= 227 * 1024, "shared memory");
-  cudaError_t e = cudaFuncSetAttribute(split_kernel<D, kCols>, cudaFuncAttributeMaxDynamicSharedMemorySize, kDynamic);
-  return e == cudaSuccess ? cudaFuncSetAttribute(split_kernel<D, kCols>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) : e;
+  typedef Shape<kCols, kGroups> At;
+  static_assert(sizeof(SharedS<At>) + 4 * (kWeightSegments * 32 + kClasses * (kMaxChunks + 1)) + At::kDynamic + 1024 <= (kGroups == 4 ? 228 : 114) * 1024,
+                "shared memory");
+  cudaError_t e = cudaFuncSetAttribute(split_kernel<D, kCols, kGroups>, cudaFuncAttributeMaxDynamicSharedMemorySize, At::kDynamic);
+  return e == cudaSuccess ? cudaFuncSetAttribute(split_kernel<D, kCols, kGroups>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) : e;
 }
 
 template <int D>
 cudaError_t configure() {
-  cudaError_t e = configure<D, 4>();
-  if (e == cudaSuccess) e = configure<D, 8>();
-  return e == cudaSuccess ? configure<D, 16>() : e;
+  cudaError_t e = configure<D, 4, 4>();
+  if (e == cudaSuccess) e = configure<D, 8, 4>();
+  if (e == cudaSuccess) e = configure<D, 16, 4>();
+  if (e == cudaSuccess) e = configure<D, 4, 2>();
+  if (e == cudaSuccess) e = configure<D, 8, 2>();
+  return e == cudaSuccess ? configure<D, 16, 2>() : e;
 }
 
+template <int kGroups>
 cudaLaunchConfig_t config(int cluster, int clusters, cudaLaunchAttribute* attr, cudaStream_t stream) {
+  typedef Shape<4, kGroups> At;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)(cluster * clusters));
-  cfg.blockDim = dim3(kThreadsS);
-  cfg.dynamicSmemBytes = kDynamic;
+  cfg.blockDim = dim3(At::kThreads);
+  cfg.dynamicSmemBytes = At::kDynamic;
   cfg.stream = stream;
   attr->id = cudaLaunchAttributeClusterDimension;
   attr->val.clusterDim.x = (unsigned)cluster;
@@ -642,6 +671,17 @@ cudaLaunchConfig_t config(int cluster, int clusters, cudaLaunchAttribute* attr, 
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   return cfg;
+}
+
+template <int kGroups>
+cudaError_t clusters_of(int* clusters, int most) {
+  cudaError_t e = cudaSuccess;
+  for (int i = kLeastCluster; i <= most && e == cudaSuccess; ++i) {
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = config<kGroups>(i, 1, &attr, nullptr);
+    e = cudaOccupancyMaxActiveClusters(clusters + i, split_kernel<128, 4, kGroups>, &cfg);
+  }
+  return e;
 }
 
 template <int D, int kCols>
@@ -652,16 +692,22 @@ cudaError_t launch(const AttnArgs& a, const CacheArgs& c, const ForwardArgs& f, 
   s.chunks = (f.n + 31) / 32;
   s.cluster = kLeastCluster;
   s.one_team = 0;
-  for (int n = std::min(kMaxTeam, f.width); n > kLeastCluster && !s.one_team; --n) {
+  const bool pairs = units > a.sms;
+  for (int n = std::min(kMaxTeam, f.width); n > kLeastCluster && !s.one_team && !pairs; --n) {
     if (a.clusters[n] < units) continue;
     s.cluster = n;
     s.one_team = 1;
   }
-  const int most = std::max(1, a.clusters[s.cluster]);
+  const int most = std::max(1, pairs ? a.clusters_of_pairs : a.clusters[s.cluster]);
   s.per_cta = (int)std::max<long long>(1, std::min<long long>(16, 2 * units / (most * s.cluster)));
+  const int clusters = (int)std::min<long long>(most, units);
   cudaLaunchAttribute attr;
-  const cudaLaunchConfig_t cfg = config(s.cluster, (int)std::min<long long>(most, units), &attr, stream);
-  return cudaLaunchKernelEx(&cfg, split_kernel<D, kCols>, k_map, v_map, a, c, f, s);
+  if (pairs) {
+    const cudaLaunchConfig_t cfg = config<2>(s.cluster, clusters, &attr, stream);
+    return cudaLaunchKernelEx(&cfg, split_kernel<D, kCols, 2>, k_map, v_map, a, c, f, s);
+  }
+  const cudaLaunchConfig_t cfg = config<4>(s.cluster, clusters, &attr, stream);
+  return cudaLaunchKernelEx(&cfg, split_kernel<D, kCols, 4>, k_map, v_map, a, c, f, s);
 }
 
 template <int D>
@@ -678,11 +724,10 @@ cudaError_t configure_attn_split(AttnArgs* a) {
   cudaError_t e = configure<32>();
   if (e == cudaSuccess) e = configure<64>();
   if (e == cudaSuccess) e = configure<128>();
-  for (int i = kLeastCluster; i <= kMaxTeam && e == cudaSuccess; ++i) {
-    cudaLaunchAttribute attr;
-    const cudaLaunchConfig_t cfg = config(i, 1, &attr, nullptr);
-    e = cudaOccupancyMaxActiveClusters(&a->clusters[i], split_kernel<128, 4>, &cfg);
-  }
+  int pairs[kMaxTeam + 1] = {};
+  if (e == cudaSuccess) e = clusters_of<4>(a->clusters, kMaxTeam);
+  if (e == cudaSuccess) e = clusters_of<2>(pairs, kLeastCluster);
+  a->clusters_of_pairs = pairs[kLeastCluster];
   return e;
 }
 
