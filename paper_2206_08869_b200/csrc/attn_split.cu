@@ -24,6 +24,7 @@ namespace {
 
 constexpr int kN = 16;                   // of the scores' MMAs, the least; a unit has up to 4, 8 or 16 rows
 constexpr int kUnitsS = 3;
+constexpr int kAhead = 3;                // blocks that scores computed a second time are ahead of the values
 constexpr int kTileBytes = 16384;        // of a slot: 128 rows of up to 128 bytes; V^T is read as 128 rows whatever the dimension
 constexpr int kLeastCluster = 8, kMaxTeam = kAttnMaxTeam, kClasses = 5;             // teams of 1, 2, 4, 8; of a whole cluster
 constexpr int kMaxPart = kAttnMaxBlocks / kLeastCluster;          // blocks of one CTA
@@ -59,7 +60,7 @@ struct UnitS {
 template <class Sh>
 struct SharedS {
   uint64_t full[Sh::kRing], empty[Sh::kRing], sfull[Sh::kScores], sempty[Sh::kScores], pfull[Sh::kWarps], pempty[Sh::kWarps], qfull[2], qempty[2];
-  uint64_t ofull, oempty, ufull[kUnitsS], uempty[kUnitsS], tops[kClasses], sums[kClasses];
+  uint64_t ofull, oempty, ufull[kUnitsS], efull[kUnitsS], uempty[kUnitsS], tops[kClasses], sums[kClasses];
   uint32_t abort_flag, tmem;
   int total[kClasses];                   // units of each class
   UnitS units[kUnitsS];
@@ -138,6 +139,7 @@ __global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) spl
     init(&sh.ofull, 1, 1);
     init(&sh.oempty, 1, kSoft);
     init(sh.ufull, kUnitsS, 1);
+    init(sh.efull, kUnitsS, 1);
     init(sh.uempty, kUnitsS, 3 + kSoft);
     for (int i = 0; i < kClasses; ++i) {
       init(&sh.tops[i], 1, i == kClasses - 1 ? s.cluster : 1 << i);
@@ -153,8 +155,9 @@ __global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) spl
     for (int i = tid; i < kBuffers * 32; i += kThreadsS)
       reinterpret_cast<uint32_t*>(smem + At::kP + i / 32 * At::kOperand + 2 * kCols * 128)[i % 32] = 0x01010101u;
   ptx::fence_async_smem();
-  for (int k = warp; k < s.chunks; k += kWarpsS) {
-    const Ask ask(a, f, s, kCols, k * 32 + lane);
+  const Ask first(a, f, s, kCols, warp == 2 ? lane : f.n);          // warp 2 has the first requests at hand when it looks for units
+  for (int k = (warp + kWarpsS - 2) % kWarpsS; k < s.chunks; k += kWarpsS) {
+    const Ask ask = k ? Ask(a, f, s, kCols, k * 32 + lane) : first;
 #pragma unroll
     for (int i = 0; i < kClasses; ++i) {
       const int n = __reduce_add_sync(0xFFFFFFFFu, ask.cls == i ? ask.tiles * a.kv : 0);
@@ -219,9 +222,9 @@ __global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) spl
       for (; ok && take(ur, &u); ur.next(kUnitsS)) {
         const int* ids = sh.ids[ur.slot];
         for (int i = 0; i < u.n && ok; ++i) copy(&kmap, (max(ids[i], 0) * a.kv + u.head) * kAttnBlock, D);
-        for (int i = 0; i < u.n && ok; ++i) {
-          if (i >= kKeep) copy(&kmap, (max(ids[i], 0) * a.kv + u.head) * kAttnBlock, D);
-          copy(&vmap, (max(ids[i], 0) * a.kv + u.head) * D, D);
+        for (int i = -kAhead; i < u.n && ok; ++i) {
+          if (i + kAhead >= kKeep && i + kAhead < u.n) copy(&kmap, (max(ids[i + kAhead], 0) * a.kv + u.head) * kAttnBlock, D);
+          if (i >= 0) copy(&vmap, (max(ids[i], 0) * a.kv + u.head) * D, D);
         }
         ptx::mbar_arrive(ptx::smem_u32(&sh.uempty[ur.slot]));
       }
@@ -254,9 +257,10 @@ __global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) spl
         ptx::tc_fence_after();
         const uint32_t q = rows_lo(qbuf + qr.slot * At::kQBytes);
         for (int i = 0; i < u.n && ok; ++i) scores(q, slot_of(i));
-        for (int i = 0; i < u.n && ok; ++i) {
+        for (int i = -kAhead; i < u.n && ok; ++i) {
+          if (i + kAhead >= kKeep && i + kAhead < u.n) scores(q, slot_of(i + kAhead));
+          if (i < 0) continue;
           const int g = buffer_of(i);
-          if (i >= kKeep) scores(q, slot_of(i));
           if (i == 0) ok = ok && wait(&sh.oempty, orr.phase ^ 1);
           ok = ok && wait(&sh.pfull[g], pphases >> g & 1) && wait(&sh.full[r.slot], r.phase);
           if (!ok) break;
@@ -302,7 +306,7 @@ __global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) spl
           if (before[cls][mid + 1] > unit) hi = mid;
           else lo = mid + 1;
         }
-        const Ask ask(a, f, s, kCols, lo * 32 + lane);
+        const Ask ask = lo ? Ask(a, f, s, kCols, lo * 32 + lane) : first;
         const int mine = ask.cls == cls ? ask.tiles * a.kv : 0;
         int upto = mine;
 #pragma unroll
@@ -335,10 +339,7 @@ __global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) spl
           const int id = f.table[(long long)u.request * f.ldt + u.b0 + i];
           const bool good = (unsigned)id < (unsigned)c.blocks;
           if (!good) atomicAdd(a.status + 1, 1u);
-          const long long e = (long long)(good ? id : 0) * a.kv + u.head;
           sh.ids[ur.slot][i] = good ? id : -1;
-          sh.ek[ur.slot][i] = (uint8_t)min((int)c.k_exp[e], kAttnMaxExp);
-          sh.ev[ur.slot][i] = (uint8_t)min((int)c.v_exp[e], kAttnMaxExp);
         }
         if (lane == 0) {
           sh.units[ur.slot] = u;
@@ -346,6 +347,13 @@ __global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) spl
         }
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.ufull[ur.slot]));
+        for (int i = lane; i < u.n; i += 32) {          // needed later than the blocks themselves
+          const long long e = (long long)max(sh.ids[ur.slot][i], 0) * a.kv + u.head;
+          sh.ek[ur.slot][i] = (uint8_t)min((int)c.k_exp[e], kAttnMaxExp);
+          sh.ev[ur.slot][i] = (uint8_t)min((int)c.v_exp[e], kAttnMaxExp);
+        }
+        __syncwarp();
+        if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.efull[ur.slot]));
         ur.next(kUnitsS);
       }
       item -= items;                                    // of the next class
@@ -422,6 +430,7 @@ __global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) spl
         __syncwarp();
         if (lane == 0) ptx::mbar_arrive(ptx::smem_u32(&sh.sempty[slot_of(i)]));
       };
+      ok = ok && warp_wait(&sh.efull[ur.slot], ur.phase);
       int tops[kCols];
 #pragma unroll
       for (int e = 0; e < kCols; ++e) tops[e] = INT32_MIN;
@@ -608,6 +617,8 @@ __global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) spl
         ptx::named_barrier(1, 32 * kSoft);              // all of this CTA's sums are on their way
         if (me == 0 && lane < u.team) ptx::mbar_arrive_cluster(ptx::cluster_addr(ptx::smem_u32(&sh.sums[u.cls]), peer));
         __syncwarp();
+        const int mine = min(tid - 128, own * nc - 1), my_dim = min(u.member * own + mine % own, D - 1);
+        const int4 my_out = a.out[(u.head * a.group + (u.flat0 + mine / own) % a.group) * D + my_dim];      // of the first output, asked for early
         ok = ok && team_wait(&sh.sums[u.cls], team_phases >> u.cls & 1);
         team_phases ^= 1u << u.cls;
         for (int i = tid - 128; ok && i < own * nc; i += 32 * kSoft) {
@@ -622,7 +633,7 @@ __global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) spl
             all += sh.team_sum[m][e];
           }
           const int at = (u.head * a.group + (u.flat0 + e) % a.group) * D + dim;
-          store(e, dim, clipped(requantised(all ? quotient(hi_all, lo_all, reciprocal(all, sh.vtop[e])) : 0, a.out[at]), a.lo, a.hi));
+          store(e, dim, clipped(requantised(all ? quotient(hi_all, lo_all, reciprocal(all, sh.vtop[e])) : 0, i == tid - 128 ? my_out : a.out[at]), a.lo, a.hi));
         }
       }
       __syncwarp();
@@ -644,6 +655,7 @@ cudaError_t configure() {
   static_assert(sizeof(SharedS<At>) + 4 * (kWeightSegments * 32 + kClasses * (kMaxChunks + 1)) + At::kDynamic + 1024 <= (kGroups == 4 ? 228 : 114) * 1024,
                 "shared memory");
   cudaError_t e = cudaFuncSetAttribute(split_kernel<D, kCols, kGroups>, cudaFuncAttributeMaxDynamicSharedMemorySize, At::kDynamic);
+  if (e == cudaSuccess) e = cudaFuncSetAttribute(split_kernel<D, kCols, kGroups>, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
   return e == cudaSuccess ? cudaFuncSetAttribute(split_kernel<D, kCols, kGroups>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) : e;
 }
 
