@@ -28,8 +28,7 @@ struct AttnArgs {                        // what a handle holds
   const int4* out;                       // [heads * dim] {M0, s, low and high word of 2^(30 + s)}
   uint32_t* status;                      // [0] a bounded wait gave up, [1] requests or rows that could not be served
   int sms;
-  int clusters[kAttnMaxTeam + 1];        // of the kernel for few rows: clusters of 8 .. 16 CTAs that run at once,
-  int clusters_of_pairs;                 // of 8 with two CTAs to an SM
+  int clusters[kAttnMaxTeam + 1];        // of the kernel for few rows: clusters of 8 .. 16 CTAs that run at once
 };
 
 struct CacheArgs {

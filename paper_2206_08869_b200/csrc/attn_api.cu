@@ -211,7 +211,7 @@ int iodf_attn_append(iodf_attn* h, int rows, const void* q, size_t ldq, const vo
                        {q8, R * nq}, {q_exp, R * a.heads}};
   const Span ins[] = {{q, extent(R, ldq, nq, x)}, {k, extent(R, ldk, nk, x)}, {v, extent(R, ldv, nk, x)}, {slot, 4 * R}, {position, 4 * R}};
   if (overlap(outs, ins)) return IODF_EINVAL;
-  const size_t lane = a.dim / 32 * x;             // bytes of a lane's elements
+  const size_t lane = 4 * x;                      // bytes of a lane's elements
   const bool vector = aligned(q, lane) && aligned(k, lane) && aligned(v, lane) && ldq * x % lane == 0 && ldk * x % lane == 0 && ldv * x % lane == 0;
   const AppendArgs p{q, k, v, (long long)ldq, (long long)ldk, (long long)ldv, rows, slot, position, q8, q_exp, vector};
   OnDevice on(h->device);

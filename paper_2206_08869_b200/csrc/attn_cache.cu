@@ -132,10 +132,12 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs p) {
 }
 
 // ---- append ----------------------------------------------------------------------------------------------------
-// A warp takes rows of one head of the cache with the query heads that go with it; a lane holds dim / 32 neighbouring elements, its
-// rotation's partner is in another lane (half layout) or its own. Bound by the bytes of q, k and v: each is read once, but for the first
-// token of a block, whose size decides the block's exponent: a warp whose rows have it outside of them reads it again (from L2).
+// A warp takes 128 neighbouring elements of a row of q, k or v at a time (one head of 128, two of 64, four of 32), a lane four of them; the
+// rotation's partner is in another lane (half layout) or the lane's own. Bound by the bytes of q, k and v: each is read once, but for the
+// first token of a block, whose size decides the block's exponent: a warp whose rows have it outside of them reads it again (from L2).
+// What comes next is instructions, about 45 for 128 elements. Values of a tile of rows go through shared memory to be turned around.
 constexpr int kAppendWarps = 8;
+constexpr int kChunk = 128, kPitch = kChunk + 4;
 
 __device__ __forceinline__ uint32_t pack16(int hi, int lo) {       // both saturated to 16 bits
   uint32_t r;
@@ -145,126 +147,110 @@ __device__ __forceinline__ uint32_t pack16(int hi, int lo) {       // both satur
 __device__ __forceinline__ int low16(uint32_t v) { return (int)(short)(v & 0xFFFFu); }
 __device__ __forceinline__ int high16(uint32_t v) { return (int)v >> 16; }
 
-// A lane's elements of a row, in 16 bits.
-template <class X, int E, bool kVector>
-__device__ __forceinline__ void load(const X* p, int (&x)[E]) {
-  if (kVector && sizeof(X) * E >= 2) {
-    if (sizeof(X) == 4) {
-      if (E == 4) {
-        const int4 v = *reinterpret_cast<const int4*>(p);
-        x[0] = v.x; x[1 % E] = v.y; x[2 % E] = v.z; x[3 % E] = v.w;
-      } else if (E == 2) {
-        const int2 v = *reinterpret_cast<const int2*>(p);
-        x[0] = v.x; x[1 % E] = v.y;
-      } else {
-        x[0] = (int)p[0];
-      }
-    } else if (E == 4) {
-      const char4 v = *reinterpret_cast<const char4*>(p);
-      x[0] = v.x; x[1 % E] = v.y; x[2 % E] = v.z; x[3 % E] = v.w;
-    } else {
-      const char2 v = *reinterpret_cast<const char2*>(p);
-      x[0] = v.x; x[1 % E] = v.y;
-    }
+// A lane's four elements, in 16 bits: two words of two.
+struct Four {
+  uint32_t a, b;
+};
+
+template <class X, bool kVector>
+__device__ __forceinline__ Four load(const X* p, bool live) {
+  if (!live) return {0, 0};
+  int x[4];
+  if (kVector && sizeof(X) == 4) {
+    const int4 v = *reinterpret_cast<const int4*>(p);
+    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+  } else if (kVector) {
+    const char4 v = *reinterpret_cast<const char4*>(p);
+    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
   } else {
 #pragma unroll
-    for (int i = 0; i < E; ++i) x[i] = (int)p[i];
+    for (int i = 0; i < 4; ++i) x[i] = (int)p[i];
   }
-  if (sizeof(X) == 4) {
-#pragma unroll
-    for (int i = 0; i < E; ++i) x[i] = min(max(x[i], -32768), 32767);
-  }
+  return {pack16(x[1], x[0]), pack16(x[3], x[2])};
 }
 
 // Factors of a lane's elements and of their partners, in 2^-14 (1 and 0 where nothing is rotated), and where the partners are.
-template <int E>
 struct Rotation {
-  int c[E], s[E], from;
+  int c[4], s[4], from;
 };
 
-template <int E, int kLayout>
-__device__ __forceinline__ Rotation<E> rotation(const AttnArgs& a, int position, int lane) {
-  Rotation<E> r;
-  const int half = a.rot / 2, d0 = lane * E;
-  r.from = kLayout == kRotaryHalf ? (d0 < half ? lane + half / E : lane - half / E) : E == 1 ? lane ^ 1 : lane;
-  if (d0 >= a.rot) r.from = lane;
-  const short2* t = a.rotary + (long long)position * half;
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const int d = d0 + i;
-    r.c[i] = 16384;
-    r.s[i] = 0;
-    if (d < a.rot) {
-      const bool low = kLayout == kRotaryHalf ? d < half : (d & 1) == 0;
-      const short2 v = t[kLayout == kRotaryHalf ? (low ? d : d - half) : d >> 1];
-      r.c[i] = v.x;
-      r.s[i] = low ? -(int)v.y : (int)v.y;
+template <int D, int kLayout>
+__device__ __forceinline__ Rotation rotation(const AttnArgs& a, int position, int lane) {
+  Rotation r;
+  const int half = a.rot / 2, d0 = lane * 4 % D;
+  const bool turned = d0 < a.rot, low = d0 < half;
+  r.from = kLayout == kRotaryHalf && turned ? (low ? lane + half / 4 : lane - half / 4) : lane;
+  int4 cs = make_int4(16384, 16384, 16384, 16384);                  // cos in the low half of each, sin in the high one
+  if (turned) {
+    const short2* t = a.rotary + (long long)position * half;
+    if (kLayout == kRotaryHalf) {
+      cs = *reinterpret_cast<const int4*>(t + (low ? d0 : d0 - half));
+    } else {
+      const int2 v = *reinterpret_cast<const int2*>(t + d0 / 2);
+      cs = make_int4(v.x, v.x, v.y, v.y);
     }
+  }
+  const int v[4] = {cs.x, cs.y, cs.z, cs.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    r.c[i] = low16((uint32_t)v[i]);
+    r.s[i] = (kLayout == kRotaryHalf ? low : i % 2 == 0) ? -high16((uint32_t)v[i]) : high16((uint32_t)v[i]);
   }
   return r;
 }
 
-template <int E, int kLayout>
-__device__ __forceinline__ void rotate(int (&x)[E], const Rotation<E>& r) {
-  int o[E];
-  if (kLayout == kRotaryHalf || E == 1) {
-    if (E == 1) {
-      o[0] = __shfl_sync(0xFFFFFFFFu, x[0], r.from);
-    } else {
-#pragma unroll
-      for (int i = 0; i < E; i += 2) {
-        const uint32_t v = __shfl_sync(0xFFFFFFFFu, pack16(x[(i + 1) % E], x[i]), r.from);
-        o[i] = low16(v);
-        o[(i + 1) % E] = high16(v);
-      }
-    }
+template <int kLayout>
+__device__ __forceinline__ void rotate(const Four& v, const Rotation& r, bool any, int (&x)[4]) {
+  x[0] = low16(v.a); x[1] = high16(v.a); x[2] = low16(v.b); x[3] = high16(v.b);
+  if (!any) return;
+  int o[4];
+  if (kLayout == kRotaryHalf) {
+    const uint32_t a = __shfl_sync(0xFFFFFFFFu, v.a, r.from), b = __shfl_sync(0xFFFFFFFFu, v.b, r.from);
+    o[0] = low16(a); o[1] = high16(a); o[2] = low16(b); o[3] = high16(b);
   } else {
-#pragma unroll
-    for (int i = 0; i < E; ++i) o[i] = x[i ^ (E > 1 ? 1 : 0)];
+    o[0] = x[1]; o[1] = x[0]; o[2] = x[3]; o[3] = x[2];
   }
 #pragma unroll
-  for (int i = 0; i < E; ++i) x[i] = (x[i] * r.c[i] + o[i] * r.s[i] + 8192) >> 14;
+  for (int i = 0; i < 4; ++i) x[i] = (x[i] * r.c[i] + o[i] * r.s[i] + 8192) >> 14;
 }
 
-template <int E>
-__device__ __forceinline__ int largest(const int (&x)[E]) {        // |x| over the warp
-  int m = abs(x[0]);
-#pragma unroll
-  for (int i = 1; i < E; ++i) m = max(m, abs(x[i]));
-  return __reduce_max_sync(0xFFFFFFFFu, m);
+template <int D>
+__device__ __forceinline__ int largest(const int (&x)[4], int lane) {        // |x| over the lanes of a head
+  const int m = max(max(abs(x[0]), abs(x[1])), max(abs(x[2]), abs(x[3])));
+  return __reduce_max_sync(D == 128 ? 0xFFFFFFFFu : D == 64 ? 0xFFFFu << (lane & 16) : 0xFFu << (lane & 24), m);
 }
 
 // The smallest e with amax (8 + headroom) <= 1016 2^e.
 __device__ __forceinline__ int exponent(int amax, int headroom) {
-  const int over = (amax * (8 + headroom) + 1015) / 1016;
-  return over <= 1 ? 0 : 32 - __clz(over - 1);
+  const int z = amax * (8 + headroom), e = max(22 - __clz(z), 0);      // z < 2^(e + 10)
+  return e + (z > 1016 << e);
 }
 
-// The elements in 8 bits, -127 .. 127, in a word's low bytes.
-template <int E>
-__device__ __forceinline__ uint32_t pack8(const int (&x)[E], int e) {
+// The elements in 8 bits, -127 .. 127.
+__device__ __forceinline__ uint32_t pack8(const int (&x)[4], int e) {
   const int half = (1 << e) >> 1;
-  uint32_t r = 0;
+  int y[4];
 #pragma unroll
-  for (int i = 0; i < E; ++i) r |= (uint32_t)(min(max((x[i] + half) >> e, -127), 127) & 255) << (8 * i);
+  for (int i = 0; i < 4; ++i) y[i] = max((x[i] + half) >> e, -127);
+  uint32_t r;
+  asm("{\n\t.reg .b32 t;\n\t"
+      "cvt.pack.sat.s8.s32.b32 t, %4, %3, 0;\n\t"
+      "cvt.pack.sat.s8.s32.b32 %0, %2, %1, t;\n\t}"
+      : "=r"(r)
+      : "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]));
   return r;
 }
 
-template <int E>
-__device__ __forceinline__ void store8(int8_t* p, uint32_t v) {
-  if (E == 4) *reinterpret_cast<uint32_t*>(p) = v;
-  else if (E == 2) *reinterpret_cast<uint16_t*>(p) = (uint16_t)v;
-  else *p = (int8_t)v;
-}
-
-template <class X, int E, int kLayout, bool kVector>
+template <class X, int D, int kLayout, bool kVector>
 __global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AttnArgs a, const CacheArgs c, const AppendArgs p, const int per_warp) {
-  constexpr int D = 32 * E, kPitch = D + 4;
-  extern __shared__ uint8_t v8[];                  // [rows of the tile][kPitch]: values, to be turned around
+  extern __shared__ uint8_t v8[];                  // [rows of the tile][kPitch]
   __shared__ int slots[4 * kAppendWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tile = per_warp * kAppendWarps;
-  const int h = blockIdx.y, row0 = blockIdx.x * tile, d0 = lane * E;
-  const int slot_end = c.blocks * kAttnBlock;      // below 2^31: the binding of a cache sees to that
+  const int row0 = blockIdx.x * tile, parts = gridDim.y, part = blockIdx.y;
+  const int slot_end = c.blocks * kAttnBlock;      // below 2^31
+  const int nq = a.heads * D, nk = a.kv * D, q_chunks = (nq + kChunk - 1) / kChunk;
+  const int at = part * kChunk + lane * 4, h = at / D, d0 = at % D;          // the lane's keys and values
+  const bool live = at < nk, rotary = a.rot != 0;
   int first_row = -1, first_k = 0, first_v = 0;    // the last first token of a block that was looked at: exponents
   for (int i = 0; i < per_warp; ++i) {
     const int t = warp * per_warp + i, row = row0 + t;
@@ -272,95 +258,95 @@ __global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AttnArg
     if (row < p.rows) {
       slot = p.slot[row];
       int pos = p.position[row];
-      bool bad = (a.rot && (unsigned)pos >= (unsigned)a.positions) || slot < -1 || slot >= slot_end;
-      if (bad && lane == 0 && h == 0) atomicAdd(a.status + 1, 1u);
+      const Four k4 = load<X, kVector>((const X*)p.k + row * p.ldk + at, live), v4 = load<X, kVector>((const X*)p.v + row * p.ldv + at, live);
+      const bool bad = (rotary && (unsigned)pos >= (unsigned)a.positions) || slot < -1 || slot >= slot_end;
+      if (bad && lane == 0 && part == 0) atomicAdd(a.status + 1, 1u);
       if (slot < 0 || slot >= slot_end) slot = -1;
       pos = min(max(pos, 0), a.positions - 1);
-      const Rotation<E> rot = rotation<E, kLayout>(a, pos, lane);
-      const X* kr = (const X*)p.k + row * p.ldk + h * D + d0;
-      const X* vr = (const X*)p.v + row * p.ldv + h * D + d0;
-      int k[E], v[E];
-      load<X, E, kVector>(kr, k);
-      load<X, E, kVector>(vr, v);
-      for (int g = 0; g < a.group; ++g) {
-        const int head = h * a.group + g;
-        int q[E];
-        load<X, E, kVector>((const X*)p.q + row * p.ldq + head * D + d0, q);
-        rotate<E, kLayout>(q, rot);
-        const int e = exponent(largest<E>(q), 0);
-        store8<E>(p.q8 + ((long long)row * a.heads + head) * D + d0, pack8<E>(q, e));
-        if (lane == 0) p.q_exp[(long long)row * a.heads + head] = (uint8_t)e;
+      const Rotation rot = rotation<D, kLayout>(a, pos, lane);
+#pragma unroll 2
+      for (int j = part * q_chunks / parts; j < (part + 1) * q_chunks / parts; ++j) {
+        const int qa = j * kChunk + lane * 4;
+        int q[4];
+        rotate<kLayout>(load<X, kVector>((const X*)p.q + row * p.ldq + qa, qa < nq), rot, rotary, q);
+        const int e = exponent(largest<D>(q, lane), 0);
+        if (qa < nq) {
+          *reinterpret_cast<uint32_t*>(p.q8 + (long long)row * nq + qa) = pack8(q, e);
+          if (qa % D == 0) p.q_exp[(long long)row * a.heads + qa / D] = (uint8_t)e;
+        }
       }
       if (slot >= 0) {
-        rotate<E, kLayout>(k, rot);
         const int off = slot % kAttnBlock, from = row - off;
-        const long long at = (long long)(slot / kAttnBlock) * a.kv + h;
-        int ek, ev;
+        const long long head = (long long)(slot / kAttnBlock) * a.kv + h;
+        int k[4], v[4], ek = 0, ev = 0;
+        rotate<kLayout>(k4, rot, rotary, k);
+        rotate<kLayout>(v4, rot, false, v);
         if (off == 0) {
-          ek = exponent(largest<E>(k), a.k_headroom);
-          ev = exponent(largest<E>(v), a.v_headroom);
-          if (lane == 0) {
-            c.k_exp[at] = (uint8_t)ek;
-            c.v_exp[at] = (uint8_t)ev;
+          ek = exponent(largest<D>(k, lane), a.k_headroom);
+          ev = exponent(largest<D>(v, lane), a.v_headroom);
+          if (live && d0 == 0) {
+            c.k_exp[head] = (uint8_t)ek;
+            c.v_exp[head] = (uint8_t)ev;
           }
         } else if (from >= 0 && (from == first_row || p.slot[from] == slot - off)) {
           if (from != first_row) {
-            int f[E];
-            load<X, E, kVector>((const X*)p.v + from * p.ldv + h * D + d0, f);
-            first_v = exponent(largest<E>(f), a.v_headroom);
-            load<X, E, kVector>((const X*)p.k + from * p.ldk + h * D + d0, f);
-            rotate<E, kLayout>(f, rotation<E, kLayout>(a, min(max(p.position[from], 0), a.positions - 1), lane));
-            first_k = exponent(largest<E>(f), a.k_headroom);
+            int x[4];
+            rotate<kLayout>(load<X, kVector>((const X*)p.v + from * p.ldv + at, live), rot, false, x);
+            first_v = exponent(largest<D>(x, lane), a.v_headroom);
+            rotate<kLayout>(load<X, kVector>((const X*)p.k + from * p.ldk + at, live),
+                            rotation<D, kLayout>(a, min(max(p.position[from], 0), a.positions - 1), lane), rotary, x);
+            first_k = exponent(largest<D>(x, lane), a.k_headroom);
             first_row = from;
           }
           ek = first_k;
           ev = first_v;
-        } else {
-          ek = min((int)c.k_exp[at], kAttnMaxExp);
-          ev = min((int)c.v_exp[at], kAttnMaxExp);
+        } else if (live) {
+          ek = min((int)c.k_exp[head], kAttnMaxExp);
+          ev = min((int)c.v_exp[head], kAttnMaxExp);
         }
-        store8<E>(c.k + (at * kAttnBlock + off) * D + d0, pack8<E>(k, ek));
-        const uint32_t w = pack8<E>(v, ev);
-#pragma unroll
-        for (int j = 0; j < E; ++j) v8[t * kPitch + d0 + j] = (uint8_t)(w >> (8 * j));
+        if (live) {
+          *reinterpret_cast<uint32_t*>(c.k + (head * kAttnBlock + off) * D + d0) = pack8(k, ek);
+          *reinterpret_cast<uint32_t*>(v8 + t * kPitch + lane * 4) = pack8(v, ev);
+        }
       }
     }
     if (lane == 0) slots[t] = slot;
   }
   __syncthreads();
   // values of four neighbouring tokens of a dimension lie side by side
-  for (int i = threadIdx.x; i < tile / 4 * D; i += 32 * kAppendWarps) {
-    const int t = i % (tile / 4) * 4, d = i / (tile / 4);
+  for (int i = threadIdx.x; i < tile / 4 * kChunk; i += 32 * kAppendWarps) {
+    const int t = i % (tile / 4) * 4, el = i / (tile / 4), head = (part * kChunk + el) / D, d = el % D;
+    if (head >= a.kv) break;
     const int s = slots[t];
-    int8_t* out = c.v + ((long long)(s / kAttnBlock) * a.kv + h) * D * kAttnBlock + d * kAttnBlock + s % kAttnBlock;
+    auto place = [&](int slot) { return c.v + (((long long)(slot / kAttnBlock) * a.kv + head) * D + d) * kAttnBlock + slot % kAttnBlock; };
+    const uint8_t* x = v8 + t * kPitch + el;
     if (s >= 0 && s % 4 == 0 && slots[t + 1] == s + 1 && slots[t + 2] == s + 2 && slots[t + 3] == s + 3) {
-      *reinterpret_cast<uint32_t*>(out) = v8[t * kPitch + d] | v8[(t + 1) * kPitch + d] << 8 | v8[(t + 2) * kPitch + d] << 16 |
-                                          (uint32_t)v8[(t + 3) * kPitch + d] << 24;
+      *reinterpret_cast<uint32_t*>(place(s)) = x[0] | x[kPitch] << 8 | x[2 * kPitch] << 16 | (uint32_t)x[3 * kPitch] << 24;
     } else {
       for (int j = 0; j < 4; ++j) {
         const int sj = slots[t + j];
-        if (sj >= 0)
-          c.v[((long long)(sj / kAttnBlock) * a.kv + h) * D * kAttnBlock + d * kAttnBlock + sj % kAttnBlock] = (int8_t)v8[(t + j) * kPitch + d];
+        if (sj >= 0) *place(sj) = (int8_t)x[j * kPitch];
       }
     }
   }
 }
 
-template <class X, int E, int kLayout>
+template <class X, int D, int kLayout>
 cudaError_t launch_append(const AttnArgs& a, const CacheArgs& c, const AppendArgs& p, cudaStream_t stream) {
+  const int parts = (a.kv * D + kChunk - 1) / kChunk;
   // four rows to a warp where that still leaves two CTAs to an SM
-  const int per_warp = (long long)p.rows * a.kv >= 2ll * a.sms * 4 * kAppendWarps ? 4 : 1, tile = per_warp * kAppendWarps;
-  const dim3 grid((unsigned)((p.rows + tile - 1) / tile), (unsigned)a.kv);
-  const size_t smem = (size_t)tile * (32 * E + 4);
-  if (p.vector) append_kernel<X, E, kLayout, true><<<grid, 32 * kAppendWarps, smem, stream>>>(a, c, p, per_warp);
-  else append_kernel<X, E, kLayout, false><<<grid, 32 * kAppendWarps, smem, stream>>>(a, c, p, per_warp);
+  const int per_warp = (long long)p.rows * parts >= 2ll * a.sms * 4 * kAppendWarps ? 4 : 1, tile = per_warp * kAppendWarps;
+  const dim3 grid((unsigned)((p.rows + tile - 1) / tile), (unsigned)parts);
+  const size_t smem = (size_t)tile * kPitch;
+  if (p.vector) append_kernel<X, D, kLayout, true><<<grid, 32 * kAppendWarps, smem, stream>>>(a, c, p, per_warp);
+  else append_kernel<X, D, kLayout, false><<<grid, 32 * kAppendWarps, smem, stream>>>(a, c, p, per_warp);
   return cudaGetLastError();
 }
 
 template <class X, int kLayout>
 cudaError_t launch_append(const AttnArgs& a, const CacheArgs& c, const AppendArgs& p, cudaStream_t stream) {
-  return a.dim == 128 ? launch_append<X, 4, kLayout>(a, c, p, stream)
-                      : a.dim == 64 ? launch_append<X, 2, kLayout>(a, c, p, stream) : launch_append<X, 1, kLayout>(a, c, p, stream);
+  return a.dim == 128 ? launch_append<X, 128, kLayout>(a, c, p, stream)
+                      : a.dim == 64 ? launch_append<X, 64, kLayout>(a, c, p, stream) : launch_append<X, 32, kLayout>(a, c, p, stream);
 }
 
 }  // namespace

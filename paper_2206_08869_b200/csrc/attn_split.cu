@@ -685,21 +685,11 @@ cudaLaunchConfig_t config(int cluster, int clusters, cudaLaunchAttribute* attr, 
   return cfg;
 }
 
-template <int kGroups>
-cudaError_t clusters_of(int* clusters, int most) {
-  cudaError_t e = cudaSuccess;
-  for (int i = kLeastCluster; i <= most && e == cudaSuccess; ++i) {
-    cudaLaunchAttribute attr;
-    const cudaLaunchConfig_t cfg = config<kGroups>(i, 1, &attr, nullptr);
-    e = cudaOccupancyMaxActiveClusters(clusters + i, split_kernel<128, 4, kGroups>, &cfg);
-  }
-  return e;
-}
-
 template <int D, int kCols>
 cudaError_t launch(const AttnArgs& a, const CacheArgs& c, const ForwardArgs& f, const CUtensorMap& k_map, const CUtensorMap& v_map,
                    cudaStream_t stream) {
-  const long long units = ((long long)f.rows * a.group / kCols + f.n) * a.kv;             // at most
+  // at most: whole units and one that is not for each request, or the units of each token by itself
+  const long long units = std::min((long long)f.rows * a.group / kCols + f.n, (long long)f.rows * ((a.group + kCols - 1) / kCols)) * a.kv;
   SplitArgs s;
   s.chunks = (f.n + 31) / 32;
   s.cluster = kLeastCluster;
@@ -710,8 +700,11 @@ cudaError_t launch(const AttnArgs& a, const CacheArgs& c, const ForwardArgs& f, 
     s.cluster = n;
     s.one_team = 1;
   }
-  const int most = std::max(1, pairs ? a.clusters_of_pairs : a.clusters[s.cluster]);
-  s.per_cta = (int)std::max<long long>(1, std::min<long long>(16, 2 * units / (most * s.cluster)));
+  // (of CTAs of which two fit an SM the occupancy query, too, counts one: 64 requests take 43 us with as many clusters, 35 with twice as many)
+  const int most = std::max(1, a.clusters[s.cluster]) * (pairs ? 2 : 1);
+  // Blocks of a request that are still left to one CTA: 64 requests with up to 64 blocks take 47.7, 39.5, 35.1, 35.6 us with 2, 4, 8, 16
+  // (512 units on 240 CTAs: 8 by this rule).
+  s.per_cta = (int)std::max<long long>(1, std::min<long long>(16, 4 * units / (most * s.cluster)));
   const int clusters = (int)std::min<long long>(most, units);
   cudaLaunchAttribute attr;
   if (pairs) {
@@ -736,10 +729,11 @@ cudaError_t configure_attn_split(AttnArgs* a) {
   cudaError_t e = configure<32>();
   if (e == cudaSuccess) e = configure<64>();
   if (e == cudaSuccess) e = configure<128>();
-  int pairs[kMaxTeam + 1] = {};
-  if (e == cudaSuccess) e = clusters_of<4>(a->clusters, kMaxTeam);
-  if (e == cudaSuccess) e = clusters_of<2>(pairs, kLeastCluster);
-  a->clusters_of_pairs = pairs[kLeastCluster];
+  for (int i = kLeastCluster; i <= kMaxTeam && e == cudaSuccess; ++i) {
+    cudaLaunchAttribute attr;
+    const cudaLaunchConfig_t cfg = config<4>(i, 1, &attr, nullptr);
+    e = cudaOccupancyMaxActiveClusters(a->clusters + i, split_kernel<128, 4, 4>, &cfg);
+  }
   return e;
 }
 
