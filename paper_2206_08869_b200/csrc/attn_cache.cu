@@ -242,7 +242,7 @@ __device__ __forceinline__ uint32_t pack8(const int (&x)[4], int e) {
 }
 
 template <class X, int D, int kLayout, bool kVector>
-__global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AttnArgs a, const CacheArgs c, const AppendArgs p, const int per_warp) {
+__global__ void __launch_bounds__(32 * kAppendWarps, 8) append_kernel(const AttnArgs a, const CacheArgs c, const AppendArgs p, const int per_warp) {
   extern __shared__ uint8_t v8[];                  // [rows of the tile][kPitch]
   __shared__ int slots[4 * kAppendWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tile = per_warp * kAppendWarps;
@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AttnArg
       if (slot < 0 || slot >= slot_end) slot = -1;
       pos = min(max(pos, 0), a.positions - 1);
       const Rotation rot = rotation<D, kLayout>(a, pos, lane);
-#pragma unroll 2
+#pragma unroll 1
       for (int j = part * q_chunks / parts; j < (part + 1) * q_chunks / parts; ++j) {
         const int qa = j * kChunk + lane * 4;
         int q[4];
@@ -313,21 +313,27 @@ __global__ void __launch_bounds__(32 * kAppendWarps) append_kernel(const AttnArg
     if (lane == 0) slots[t] = slot;
   }
   __syncthreads();
-  // values of four neighbouring tokens of a dimension lie side by side
-  for (int i = threadIdx.x; i < tile / 4 * kChunk; i += 32 * kAppendWarps) {
-    const int t = i % (tile / 4) * 4, el = i / (tile / 4), head = (part * kChunk + el) / D, d = el % D;
-    if (head >= a.kv) break;
-    const int s = slots[t];
-    auto place = [&](int slot) { return c.v + (((long long)(slot / kAttnBlock) * a.kv + head) * D + d) * kAttnBlock + slot % kAttnBlock; };
-    const uint8_t* x = v8 + t * kPitch + el;
-    if (s >= 0 && s % 4 == 0 && slots[t + 1] == s + 1 && slots[t + 2] == s + 2 && slots[t + 3] == s + 3) {
-      *reinterpret_cast<uint32_t*>(place(s)) = x[0] | x[kPitch] << 8 | x[2 * kPitch] << 16 | (uint32_t)x[3 * kPitch] << 24;
-    } else {
-      for (int j = 0; j < 4; ++j) {
-        const int sj = slots[t + j];
-        if (sj >= 0) *place(sj) = (int8_t)x[j * kPitch];
+  // Values of neighbouring tokens of a dimension lie side by side: four to a word where their slots are.
+  const int s0 = slots[0], elements = min(kChunk, nk - part * kChunk);
+  const bool run = __syncthreads_and(s0 >= 0 && s0 % kAttnBlock + tile <= kAttnBlock && ((int)threadIdx.x >= tile || slots[threadIdx.x] == s0 + (int)threadIdx.x));
+  if (run) {                                       // all rows of the tile one after another in one block
+    int8_t* const base = c.v + ((long long)(s0 / kAttnBlock) * a.kv * D + part * kChunk) * kAttnBlock + s0 % kAttnBlock;
+    const int shift = s0 & 3, words = (shift + tile + 3) / 4;        // words of a dimension: the first and the last may be partly of others
+    for (int i = threadIdx.x; i < words * elements; i += 32 * kAppendWarps) {
+      const int el = i / words, t = (i - el * words) * 4 - shift;
+      const uint8_t* x = v8 + t * kPitch + el;
+      int8_t* const to = base + (long long)el * kAttnBlock + t;
+      if (t >= 0 && t + 4 <= tile) {
+        *reinterpret_cast<uint32_t*>(to) = x[0] | x[kPitch] << 8 | x[2 * kPitch] << 16 | (uint32_t)x[3 * kPitch] << 24;
+      } else {
+        for (int j = max(0, -t); j < min(4, tile - t); ++j) to[j] = (int8_t)x[j * kPitch];
       }
     }
+    return;
+  }
+  for (int i = threadIdx.x; i < tile * elements; i += 32 * kAppendWarps) {
+    const int t = i % tile, el = i / tile, s = slots[t];
+    if (s >= 0) c.v[((long long)(s / kAttnBlock) * a.kv * D + part * kChunk + el) * kAttnBlock + s % kAttnBlock] = (int8_t)v8[t * kPitch + el];
   }
 }
 
