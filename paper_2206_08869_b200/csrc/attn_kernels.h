@@ -9,6 +9,7 @@ cudaError_t configure_attn_tile();
 cudaError_t launch_attn_tile(const AttnArgs& a, const CacheArgs& c, const ForwardArgs& f, const CUtensorMap& k_map, const CUtensorMap& v_map,
                              cudaStream_t stream);
 cudaError_t configure_attn_split(AttnArgs* a);
+int attn_split_cols(const AttnArgs& a, const ForwardArgs& f);      // rows of a unit of the kernel for few rows
 cudaError_t launch_attn_split(const AttnArgs& a, const CacheArgs& c, const ForwardArgs& f, const CUtensorMap& k_map, const CUtensorMap& v_map,
                               cudaStream_t stream);
 

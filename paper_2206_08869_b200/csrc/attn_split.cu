@@ -702,9 +702,11 @@ cudaError_t launch(const AttnArgs& a, const CacheArgs& c, const ForwardArgs& f, 
   }
   // (of CTAs of which two fit an SM the occupancy query, too, counts one: 64 requests take 43 us with as many clusters, 35 with twice as many)
   const int most = std::max(1, a.clusters[s.cluster]) * (pairs ? 2 : 1);
-  // Blocks of a request that are still left to one CTA: 64 requests with up to 64 blocks take 47.7, 39.5, 35.1, 35.6 us with 2, 4, 8, 16
-  // (512 units on 240 CTAs: 8 by this rule).
-  s.per_cta = (int)std::max<long long>(1, std::min<long long>(16, 4 * units / (most * s.cluster)));
+  // Blocks of a request that are still left to one CTA: such that the longest contexts' teams fill the GPU, and 16 at most, since contexts may
+  // differ (64 requests with up to 64 blocks, 512 units: 47.7, 39.5, 35.1, 35.6 us with 2, 4, 8, 16).
+  int team = 1;
+  while (2 * team <= s.cluster && 2 * team * units <= (long long)most * s.cluster) team *= 2;
+  s.per_cta = std::min(16, (f.width + team - 1) / team);
   const int clusters = (int)std::min<long long>(most, units);
   cudaLaunchAttribute attr;
   if (pairs) {
@@ -718,12 +720,17 @@ cudaError_t launch(const AttnArgs& a, const CacheArgs& c, const ForwardArgs& f, 
 template <int D>
 cudaError_t launch(const AttnArgs& a, const CacheArgs& c, const ForwardArgs& f, const CUtensorMap& k_map, const CUtensorMap& v_map,
                    cudaStream_t stream) {
-  const long long flat = ((long long)f.rows * a.group + f.n - 1) / f.n;                   // rows of a request, about
-  return flat <= 4 ? launch<D, 4>(a, c, f, k_map, v_map, stream)
-                   : flat <= 8 ? launch<D, 8>(a, c, f, k_map, v_map, stream) : launch<D, 16>(a, c, f, k_map, v_map, stream);
+  const int cols = attn_split_cols(a, f);
+  return cols == 4 ? launch<D, 4>(a, c, f, k_map, v_map, stream)
+                   : cols == 8 ? launch<D, 8>(a, c, f, k_map, v_map, stream) : launch<D, 16>(a, c, f, k_map, v_map, stream);
 }
 
 }  // namespace
+
+int attn_split_cols(const AttnArgs& a, const ForwardArgs& f) {
+  const long long flat = ((long long)f.rows * a.group + f.n - 1) / f.n;                   // rows of a request, about
+  return flat <= 4 ? 4 : flat <= 8 ? 8 : 16;
+}
 
 cudaError_t configure_attn_split(AttnArgs* a) {
   cudaError_t e = configure<32>();
