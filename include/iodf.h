@@ -579,8 +579,9 @@ int iodf_norm_forward(iodf_norm* nm, int rows, const void* r, const iodf_view* r
  * = sum of add before q; row r of request q gets position[r] = held[q] + r - row_start[q] and its slot[r]; rows behind the last request
  * get slot -1, position 0; state_out is the next call's state. A request that needs blocks when fewer than all taken so far and its own are
  * free, that would not fit into `width` entries or whose rows would not into `rows`, or with held outside 0..128 width or add below -1,
- * keeps what it holds, its rows get slot -1, and it is counted (iodf_attn_check: IODF_EDATA). The inputs but for table and ring stay as
- * they are, no two operands may overlap (EINVAL), and the call repeated on the same inputs gives the same. width <= 1024, n_req <= 16384.
+ * keeps what it holds, its rows get slot -1, and it is counted (iodf_attn_check: IODF_EDATA), as are more free blocks than the ring has places
+ * and a row's block outside the cache (slot -1). The inputs but for table and ring stay as they are, no two operands may overlap (EINVAL),
+ * and the call repeated on the same inputs gives the same. width <= 1024, n_req <= 16384.
  *
  * iodf_attn_append: the call's tokens into the cache, its queries in 8 bits. q, k, v: DEV rows of x_type with strides in elements (columns of
  * one projection's output, say), heads * head_dim and kv_heads * head_dim of them; values are taken in 16 bits, clip(x, -2^15, 2^15 - 1).
@@ -603,10 +604,11 @@ int iodf_norm_forward(iodf_norm* nm, int rows, const void* r, const iodf_view* r
  * The power: with g = n mod 2^13 and c = floor(g / 128), 2^(n / 2^13) is m 2^floor(n / 2^13) / 2^23 with m = max(2^23, [2^(23 + (2 c + 1) / 128)] - 2^16)
  * + 2^10 (g mod 128). The quotient: L' = floor(L 2^a) with 2^31 <= L' < 2^32, rho = floor((2^63 - 1) / L'), o = floor((floor(A 2^(a - 8)) rho +
  * 2^(46 - V)) / 2^(47 - V)). Sums of integers: neither order nor split changes them. A row that sees nothing has o = 0. y: DEV rows of heads *
- * head_dim elements of y_type with row stride ldy in elements; y must not overlap an input. Rows in no request are not written; bounds outside
- * 0..rows are taken as the nearest and counted, as are held outside 0..128 width and blocks outside the cache, which nobody sees. A request
- * whose row_start decreases has no rows. width <= 1024 (131072 tokens); it also tells the call how long contexts may be, so that few rows with
- * long ones are spread over the GPU: give the longest request's.
+ * head_dim elements of y_type with row stride ldy in elements; y must not overlap an input. Rows in no request are not written, and no row is
+ * in two. Bounds outside 0..rows are taken as the nearest, a request whose row_start falls has no rows; held outside 0..128 width (taken as the
+ * nearest) of a request with rows and blocks outside the cache, which nobody sees, are counted. width <= 1024 (131072 tokens); it also tells the
+ * call how long contexts may be, so that few rows with long ones are spread over the GPU: give the longest request's. n_req <= 2^20,
+ * rows * heads <= 2^30.
  *
  * All three enqueue one kernel, allocate nothing, keep no workspace and may be captured; calls on one handle may overlap. head_dim 32, 64
  * or 128 (EUNSUPPORTED otherwise), heads <= 1024, at most 128 for a cache head, rotary_dim a multiple of 16, score_s 0..62. Errors of

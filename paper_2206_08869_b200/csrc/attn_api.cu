@@ -229,7 +229,7 @@ int iodf_attn_forward(iodf_attn* h, int rows, const int8_t* q8, const uint8_t* q
   if (!q8 || !q_exp || !row_start || !held || !table || !y) return IODF_EINVAL;
   if (!aligned(q8, 16) || !aligned(row_start, 4) || !aligned(held, 4) || !aligned(table, 4) || !aligned(y, (size_t)a.y_bytes)) return IODF_EINVAL;
   if (width < 1 || ldt < width || ldt >= kMaxStride || ldy < N || ldy >= kMaxStride) return IODF_EINVAL;
-  if (width > (uint32_t)kAttnMaxBlocks || rows > (1 << 30) / a.group || n_req > (1 << 24)) return IODF_EUNSUPPORTED;
+  if (width > (uint32_t)kAttnMaxBlocks || rows > (1 << 30) / a.heads || n_req > (1 << 20)) return IODF_EUNSUPPORTED;
   const size_t blocks = (size_t)cache->blocks * a.kv;
   const Span outs[] = {{y, extent(R, ldy, N, (size_t)a.y_bytes)}};
   const Span ins[] = {{q8, R * N}, {q_exp, R * a.heads}, {row_start, 4 * (n + 1)}, {held, 4 * n}, {table, 4 * extent(n, ldt, width, 1)},

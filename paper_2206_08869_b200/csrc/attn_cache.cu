@@ -102,7 +102,7 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs p) {
       p.row_start[0] = 0;
       p.state_out[0] = head + taken >= N ? head + taken - N : head + taken;
       p.state_out[1] = min(N, count - taken + back);
-      if (count - taken + back > N) atomicAdd(p.status + 1, 1u);
+      if (count + back > N) atomicAdd(p.status + 1, 1u);
     }
   }
   const int r0 = (int)((long long)p.rows * blockIdx.x / gridDim.x), r1 = (int)((long long)p.rows * (blockIdx.x + 1) / gridDim.x);

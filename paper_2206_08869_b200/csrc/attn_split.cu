@@ -188,7 +188,6 @@ __global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) spl
   __syncthreads();
   const uint32_t tmem = sh.tmem, o_mem = tmem + kScores * kN;
   auto wait = [&](uint64_t* bar, uint32_t phase) { return ptx::quick_wait(abort_flag, a.status, bar, phase, kSpinLimit); };
-  auto lazy = [&](uint64_t* bar, uint32_t phase) { return ptx::lazy_wait(abort_flag, a.status, bar, phase); };
   auto warp_wait = [&](uint64_t* bar, uint32_t phase) { return __all_sync(0xFFFFFFFFu, wait(bar, phase)) != 0; };
   auto take = [&](const RingS& r, UnitS* u) {
     if (!wait(&sh.ufull[r.slot], r.phase)) return false;
@@ -321,7 +320,11 @@ __global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) spl
         u.row0 = __shfl_sync(0xFFFFFFFFu, ask.start, from);
         u.len = __shfl_sync(0xFFFFFFFFu, ask.len, from);
         u.held = __shfl_sync(0xFFFFFFFFu, ask.held, from);
-        const int at = in - (__shfl_sync(0xFFFFFFFFu, upto, from) - __shfl_sync(0xFFFFFFFFu, mine, from));
+        const int theirs = __shfl_sync(0xFFFFFFFFu, mine, from), at = in - (__shfl_sync(0xFFFFFFFFu, upto, from) - theirs);
+        if ((unsigned)at >= (unsigned)theirs) {         // requests that share rows, more of them than can be counted
+          cls = 0;
+          break;
+        }
         u.head = at % a.kv;
         u.flat0 = at / a.kv * kCols;
         u.cols = min(kCols, u.len * a.group - u.flat0);
@@ -333,7 +336,7 @@ __global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) spl
         const int b0 = low.first / kAttnBlock, n = high.last <= low.first ? 0 : (high.last + kAttnBlock - 1) / kAttnBlock - b0;
         u.b0 = b0 + u.member * n / u.team;
         u.n = b0 + (u.member + 1) * n / u.team - u.b0;
-        ok = __all_sync(0xFFFFFFFFu, lazy(&sh.uempty[ur.slot], ur.phase ^ 1));
+        ok = __all_sync(0xFFFFFFFFu, wait(&sh.uempty[ur.slot], ur.phase ^ 1));
         if (!ok) break;
         for (int i = lane; i < u.n; i += 32) {
           const int id = f.table[(long long)u.request * f.ldt + u.b0 + i];
@@ -358,7 +361,7 @@ __global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) spl
       }
       item -= items;                                    // of the next class
     }
-    ok = ok && __all_sync(0xFFFFFFFFu, lazy(&sh.uempty[ur.slot], ur.phase ^ 1));
+    ok = ok && __all_sync(0xFFFFFFFFu, wait(&sh.uempty[ur.slot], ur.phase ^ 1));
     if (ok && lane == 0) {
       sh.units[ur.slot].request = -1;
       ptx::mbar_arrive(ptx::smem_u32(&sh.ufull[ur.slot]));
@@ -369,7 +372,7 @@ __global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) spl
     UnitS u;
     bool ok = true;
     for (; ok && __all_sync(0xFFFFFFFFu, take(ur, &u)); ur.next(kUnitsS), qr.next(2)) {
-      ok = __all_sync(0xFFFFFFFFu, lazy(&sh.qempty[qr.slot], qr.phase ^ 1));
+      ok = __all_sync(0xFFFFFFFFu, wait(&sh.qempty[qr.slot], qr.phase ^ 1));
       for (int i = lane; ok && i < u.cols * (D / 16); i += 32) {
         const int r = i / (D / 16), piece = i % (D / 16), flat = u.flat0 + r;
         const long long row = u.row0 + flat / a.group;

@@ -100,11 +100,12 @@ struct Finder {
       load(a, f, lane);
     }
     const int from = __ffs((int)__ballot_sync(0xFFFFFFFFu, unit < before + upto)) - 1;
-    const int in = unit - before - (__shfl_sync(0xFFFFFFFFu, upto, from) - __shfl_sync(0xFFFFFFFFu, tiles, from) * a.kv);
+    const int mine = __shfl_sync(0xFFFFFFFFu, tiles, from) * a.kv, in = unit - before - (__shfl_sync(0xFFFFFFFFu, upto, from) - mine);
+    if ((unsigned)in >= (unsigned)mine) return false;                        // requests that share rows, more of them than can be counted
     u->request = base + from;
     u->row0 = __shfl_sync(0xFFFFFFFFu, start, from);
     u->len = __shfl_sync(0xFFFFFFFFu, len, from);
-    u->tile = __shfl_sync(0xFFFFFFFFu, tiles, from) - 1 - in / a.kv;       // the last rows, which see the most keys, first
+    u->tile = mine / a.kv - 1 - in / a.kv;       // the last rows, which see the most keys, first
     u->head = in % a.kv;
     u->held = min(max(f.held[u->request], 0), f.width * kAttnBlock);
     const Tile t(a, *u);
@@ -168,8 +169,7 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
   __syncthreads();
   ptx::tc_fence_after();
   const uint32_t tmem = sh.tmem, o_hi = tmem + 256, o_lo = o_hi + D;
-  auto wait = [&](uint64_t* bar, uint32_t phase) { return ptx::spin_wait(abort_flag, a.status, bar, phase); };
-  auto lazy = [&](uint64_t* bar, uint32_t phase) { return ptx::lazy_wait(abort_flag, a.status, bar, phase); };
+  auto wait = [&](uint64_t* bar, uint32_t phase) { return ptx::quick_wait(abort_flag, a.status, bar, phase, kSpinLimit); };
   auto warp_wait = [&](uint64_t* bar, uint32_t phase) { return __all_sync(0xFFFFFFFFu, wait(bar, phase)) != 0; };   // all lanes go on, or none
   // S of a block in the first pass: 0 to 3, each read by half of a group; of the lead 4 and 5, which lie where 0 and 1 do but have barriers of
   // their own: their reader is another one than that of 0, and who waits for a phase must not be two phases late. In the second pass
@@ -177,7 +177,7 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
   auto place = [](int j) { return j < kLead ? 4 + (j & 1) : j & 3; };
   // the unit of a consumer's turn; false when there are no more
   auto take = [&](const Ring& r, Unit* u) {
-    if (!lazy(&sh.ufull[r.slot], r.phase)) return false;
+    if (!wait(&sh.ufull[r.slot], r.phase)) return false;
     *u = sh.units[r.slot];
     return u->request >= 0;
   };
@@ -299,7 +299,7 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
       Unit u;
       more = finder.find(a, f, unit, lane, &u);
       if (!more) u.request = -1;
-      ok = __all_sync(0xFFFFFFFFu, lazy(&sh.uempty[ur.slot], ur.phase ^ 1));
+      ok = __all_sync(0xFFFFFFFFu, wait(&sh.uempty[ur.slot], ur.phase ^ 1));
       if (!ok) break;
       const int n = more ? u.b1 - u.b0 : 0;
       const int32_t* row = f.table + (long long)u.request * f.ldt + u.b0;
@@ -325,7 +325,7 @@ __global__ void __launch_bounds__(kThreads2, 1) tile_kernel(const __grid_constan
     Unit u;
     bool ok = true;
     for (; ok && __all_sync(0xFFFFFFFFu, take(ur, &u)); ur.next(kUnits), qr.next(2)) {
-      ok = __all_sync(0xFFFFFFFFu, lazy(&sh.qempty[qr.slot], qr.phase ^ 1));
+      ok = __all_sync(0xFFFFFFFFu, wait(&sh.qempty[qr.slot], qr.phase ^ 1));
       const Tile tile(a, u);
 #pragma unroll 8
       for (int i = lane; ok && i < kRows * (D / 16); i += 32) {

@@ -5,49 +5,6 @@
 namespace iodf {
 namespace ptx {
 
-// Waits of warps whose next step depends on it: tries one after another, five instructions each. (A try with a time limit becomes a loop
-// around a sleep, and waits written in C++ some twelve instructions: waiting warps then took half of the issue slots.)
-__device__ __forceinline__ bool mbar_spin(uint32_t bar, uint32_t parity, uint32_t tries) {
-  uint32_t ok;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t.reg .u32 n;\n\t"
-      "mov.u32 n, 0;\n\t"
-      "AGAIN:\n\t"
-      "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-      "@p bra DONE;\n\t"
-      "add.u32 n, n, 1;\n\t"
-      "setp.lt.u32 q, n, %3;\n\t"
-      "@q bra AGAIN;\n\t"
-      "DONE:\n\t"
-      "selp.u32 %0, 1, 0, p;\n\t}"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity), "r"(tries)
-      : "memory");
-  return ok != 0;
-}
-// Bounded by the clock: two seconds and more, then it gives up as settled_wait does (which lets what the thread has asked for end).
-constexpr long long kWaitClocks = 4000000000ll;
-constexpr uint32_t kWaitTries = 20000;
-template <bool kLazy>
-static __device__ __noinline__ bool clocked_wait(volatile uint32_t* abort_flag, uint32_t* status, uint64_t* bar, uint32_t parity) {
-  const uint32_t b = smem_u32(bar);
-  const long long start = clock64();
-  while (!*abort_flag && clock64() - start < kWaitClocks) {
-    if (mbar_spin(b, parity, kLazy ? 1 : kWaitTries)) return true;
-    if (kLazy) __nanosleep(400);
-  }
-  return settled_wait(abort_flag, status, bar, parity, 0);
-}
-__device__ __forceinline__ bool spin_wait(volatile uint32_t* abort_flag, uint32_t* status, uint64_t* bar, uint32_t parity) {
-  if (mbar_spin(smem_u32(bar), parity, kWaitTries)) return true;
-  return clocked_wait<false>(abort_flag, status, bar, parity);
-}
-// The same for warps that work ahead of the others: they sleep between their tries.
-__device__ __forceinline__ bool lazy_wait(volatile uint32_t* abort_flag, uint32_t* status, uint64_t* bar, uint32_t parity) {
-  if (mbar_spin(smem_u32(bar), parity, 1)) return true;
-  return clocked_wait<true>(abort_flag, status, bar, parity);
-}
-
 // 32 lanes x 32 bit, 32 consecutive columns: thread i of the warp reads lane (base + i). The wait is for all of the warp's loads; r, of one of
 // them, is valid from there on.
 __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {

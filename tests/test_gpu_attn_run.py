@@ -300,3 +300,18 @@ def test_bad_slots_positions_and_rows_are_counted():
     assert bool((y[0] == 0).all())
     with pytest.raises(G.IodfError):
         G.iodf_attn_check(attn)
+
+
+def test_more_free_blocks_than_the_ring_has_places_are_counted():
+    torch, G = _modules()
+    attn = G.iodf_attn_create(C.description(torch, 2, 1, 32, "int32"))
+    ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")            # noqa: E731
+    for count, add, bad in ((2, [-1, 1], 0), (3, [-1, 1], 1), (3, [-1, 200], 1)):
+        out = G.iodf_attn_plan(attn, ints([300, 0]), ints(add), ints([[0, 1, 2], [7, 7, 7]]), ints([3, 4, 5, 6, 7]), ints([0, count]), 200)
+        assert out[4].tolist()[1] <= 5
+        if bad:
+            with pytest.raises(G.IodfError) as e:
+                G.iodf_attn_check(attn)
+            assert e.value.status == -9
+        else:
+            G.iodf_attn_check(attn)
