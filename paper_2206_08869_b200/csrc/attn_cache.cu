@@ -133,9 +133,12 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs p) {
 
 // ---- append ----------------------------------------------------------------------------------------------------
 // A warp takes 128 neighbouring elements of a row of q, k or v at a time (one head of 128, two of 64, four of 32), a lane four of them; the
-// rotation's partner is in another lane (half layout) or the lane's own. Bound by the bytes of q, k and v: each is read once, but for the
-// first token of a block, whose size decides the block's exponent: a warp whose rows have it outside of them reads it again (from L2).
-// What comes next is instructions, about 45 for 128 elements. Values of a tile of rows go through shared memory to be turned around.
+// rotation's partner is in another lane (half layout) or the lane's own. The bytes: q, k and v are read once, but for the first token of a
+// block, whose size decides the block's exponent: a warp whose rows have it outside of them reads it again (from L2). Those of 32-bit inputs
+// take more than half of the time (16384 rows of 32 query and 8 cache heads of 128: 137 us, 3.7 TB/s); of 8-bit inputs the instructions
+// do, some hundred for 128 elements (20011 rows of 16 and 4 of 64, half of each rotated: 41 us, 76 % of the issue slots before exponents were
+// reduced as bits). The next chunk of q is on its way while one is rotated (51 us without, at eight CTAs to an SM instead of six). Values of
+// a tile of rows go through shared memory to be turned around.
 constexpr int kAppendWarps = 8;
 constexpr int kChunk = 128, kPitch = kChunk + 4;
 
@@ -147,40 +150,53 @@ __device__ __forceinline__ uint32_t pack16(int hi, int lo) {       // both satur
 __device__ __forceinline__ int low16(uint32_t v) { return (int)(short)(v & 0xFFFFu); }
 __device__ __forceinline__ int high16(uint32_t v) { return (int)v >> 16; }
 
-// A lane's four elements, in 16 bits: two words of two.
+// A lane's four elements: in 16 bits, two words of two, or in 8 bits as they come.
 struct Four {
   uint32_t a, b;
 };
+struct Bytes {
+  uint32_t w;
+};
 
-template <class X, bool kVector>
-__device__ __forceinline__ Four load(const X* p, bool live) {
+template <bool kVector>
+__device__ __forceinline__ Four load(const int* p, bool live) {
   if (!live) return {0, 0};
   int x[4];
-  if (kVector && sizeof(X) == 4) {
+  if (kVector) {
     const int4 v = *reinterpret_cast<const int4*>(p);
-    x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-  } else if (kVector) {
-    const char4 v = *reinterpret_cast<const char4*>(p);
     x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[i] = (int)p[i];
+    for (int i = 0; i < 4; ++i) x[i] = p[i];
   }
   return {pack16(x[1], x[0]), pack16(x[3], x[2])};
 }
+template <bool kVector>
+__device__ __forceinline__ Bytes load(const int8_t* p, bool live) {
+  if (!live) return {0};
+  if (kVector) return {*reinterpret_cast<const uint32_t*>(p)};
+  return {(uint32_t)(uint8_t)p[0] | (uint32_t)(uint8_t)p[1] << 8 | (uint32_t)(uint8_t)p[2] << 16 | (uint32_t)(uint8_t)p[3] << 24};
+}
+__device__ __forceinline__ void unpack(const Four& v, int (&x)[4]) { x[0] = low16(v.a); x[1] = high16(v.a); x[2] = low16(v.b); x[3] = high16(v.b); }
+__device__ __forceinline__ void unpack(const Bytes& v, int (&x)[4]) {
+  const char4 c = *reinterpret_cast<const char4*>(&v.w);
+  x[0] = c.x; x[1] = c.y; x[2] = c.z; x[3] = c.w;
+}
 
-// Factors of a lane's elements and of their partners, in 2^-14 (1 and 0 where nothing is rotated), and where the partners are.
+// Factors of a lane's elements and of their partners, in 2^-14 (1 and 0 where nothing is rotated), and where the partners are. For 8-bit elements
+// in one word, the partner's in its high half.
+template <class X>
 struct Rotation {
   int c[4], s[4], from;
 };
 
-template <int D, int kLayout>
-__device__ __forceinline__ Rotation rotation(const AttnArgs& a, int position, int lane) {
-  Rotation r;
+template <class X, int D, int kLayout>
+__device__ __forceinline__ Rotation<X> rotation(const AttnArgs& a, int position, int lane) {
+  Rotation<X> r;
   const int half = a.rot / 2, d0 = lane * 4 % D;
   const bool turned = d0 < a.rot, low = d0 < half;
   r.from = kLayout == kRotaryHalf && turned ? (low ? lane + half / 4 : lane - half / 4) : lane;
-  int4 cs = make_int4(16384, 16384, 16384, 16384);                  // cos in the low half of each, sin in the high one
+  int4 cs = make_int4(16384, 16384, 16384, 16384);
   if (turned) {
     const short2* t = a.rotary + (long long)position * half;
     if (kLayout == kRotaryHalf) {
@@ -190,48 +206,77 @@ __device__ __forceinline__ Rotation rotation(const AttnArgs& a, int position, in
       cs = make_int4(v.x, v.x, v.y, v.y);
     }
   }
-  const int v[4] = {cs.x, cs.y, cs.z, cs.w};
+  const uint32_t v[4] = {(uint32_t)cs.x, (uint32_t)cs.y, (uint32_t)cs.z, (uint32_t)cs.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    r.c[i] = low16((uint32_t)v[i]);
-    r.s[i] = (kLayout == kRotaryHalf ? low : i % 2 == 0) ? -high16((uint32_t)v[i]) : high16((uint32_t)v[i]);
+    const bool minus = kLayout == kRotaryHalf ? low : i % 2 == 0;
+    if (sizeof(X) == 1) {
+      r.c[i] = (int)(minus ? (v[i] & 0xFFFFu) | (0u - (v[i] & 0xFFFF0000u)) : v[i]);
+      r.s[i] = 0;
+    } else {
+      r.c[i] = low16(v[i]);
+      r.s[i] = minus ? -high16(v[i]) : high16(v[i]);
+    }
   }
   return r;
 }
 
 template <int kLayout>
-__device__ __forceinline__ void rotate(const Four& v, const Rotation& r, bool any, int (&x)[4]) {
-  x[0] = low16(v.a); x[1] = high16(v.a); x[2] = low16(v.b); x[3] = high16(v.b);
+__device__ __forceinline__ void rotate(const Four& v, const Rotation<int>& r, bool any, int (&x)[4]) {
+  unpack(v, x);
   if (!any) return;
   int o[4];
   if (kLayout == kRotaryHalf) {
-    const uint32_t a = __shfl_sync(0xFFFFFFFFu, v.a, r.from), b = __shfl_sync(0xFFFFFFFFu, v.b, r.from);
-    o[0] = low16(a); o[1] = high16(a); o[2] = low16(b); o[3] = high16(b);
+    unpack(Four{__shfl_sync(0xFFFFFFFFu, v.a, r.from), __shfl_sync(0xFFFFFFFFu, v.b, r.from)}, o);
   } else {
     o[0] = x[1]; o[1] = x[0]; o[2] = x[3]; o[3] = x[2];
   }
 #pragma unroll
   for (int i = 0; i < 4; ++i) x[i] = (x[i] * r.c[i] + o[i] * r.s[i] + 8192) >> 14;
 }
-
-template <int D>
-__device__ __forceinline__ int largest(const int (&x)[4], int lane) {        // |x| over the lanes of a head
-  const int m = max(max(abs(x[0]), abs(x[1])), max(abs(x[2]), abs(x[3])));
-  return __reduce_max_sync(D == 128 ? 0xFFFFFFFFu : D == 64 ? 0xFFFFu << (lane & 16) : 0xFFu << (lane & 24), m);
+// Of 8-bit elements: both products in one instruction, of two 16-bit factors and two bytes.
+template <int kLayout>
+__device__ __forceinline__ void rotate(const Bytes& v, const Rotation<int8_t>& r, bool any, int (&x)[4]) {
+  if (!any) return unpack(v, x);
+  const uint32_t o = kLayout == kRotaryHalf ? __shfl_sync(0xFFFFFFFFu, v.w, r.from) : __byte_perm(v.w, 0, 0x2301);
+  const int a = (int)__byte_perm(v.w, o, 0x5140), b = (int)__byte_perm(v.w, o, 0x7362);
+  x[0] = __dp2a_lo(r.c[0], a, 8192) >> 14;
+  x[1] = __dp2a_hi(r.c[1], a, 8192) >> 14;
+  x[2] = __dp2a_lo(r.c[2], b, 8192) >> 14;
+  x[3] = __dp2a_hi(r.c[3], b, 8192) >> 14;
 }
 
-// The smallest e with amax (8 + headroom) <= 1016 2^e.
+// The smallest e with amax (8 + headroom) <= 1016 2^e; 10 at most, since |x| <= 2^15.5 and headroom <= 8.
 __device__ __forceinline__ int exponent(int amax, int headroom) {
   const int z = amax * (8 + headroom), e = max(22 - __clz(z), 0);      // z < 2^(e + 10)
   return e + (z > 1016 << e);
 }
 
-// The elements in 8 bits, -127 .. 127.
+// The exponent of a lane's head. Of heads of less than a warp the largest of the lanes' exponents, each a bit in its head's 16 of a word: lanes
+// with masks of their own would be reduced one head after another (the 41 us above were 45).
+template <int D>
+__device__ __forceinline__ int exponent(const int (&x)[4], int headroom, int lane) {
+  const int m = max(max(abs(x[0]), abs(x[1])), max(abs(x[2]), abs(x[3])));
+  if (D == 128) return exponent(__reduce_max_sync(0xFFFFFFFFu, m), headroom);
+  const int field = D == 64 ? lane & 16 : 2 * (lane & 8);
+  const unsigned mine = 1u << (exponent(m, headroom) + field);
+  unsigned all;
+  if (D == 64) {
+    all = __reduce_or_sync(0xFFFFFFFFu, mine);
+  } else {
+    const unsigned low = __reduce_or_sync(0xFFFFFFFFu, lane < 16 ? mine : 0), high = __reduce_or_sync(0xFFFFFFFFu, lane < 16 ? 0 : mine);
+    all = lane < 16 ? low : high;
+  }
+  return 31 - __clz((int)(all >> field & 0xFFFFu));
+}
+
+// The elements in 8 bits, -127 .. 127 (kFits: none is beyond 127 2^e).
+template <bool kFits>
 __device__ __forceinline__ uint32_t pack8(const int (&x)[4], int e) {
   const int half = (1 << e) >> 1;
   int y[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) y[i] = max((x[i] + half) >> e, -127);
+  for (int i = 0; i < 4; ++i) y[i] = kFits ? (x[i] + half) >> e : max((x[i] + half) >> e, -127);
   uint32_t r;
   asm("{\n\t.reg .b32 t;\n\t"
       "cvt.pack.sat.s8.s32.b32 t, %4, %3, 0;\n\t"
@@ -242,7 +287,7 @@ __device__ __forceinline__ uint32_t pack8(const int (&x)[4], int e) {
 }
 
 template <class X, int D, int kLayout, bool kVector>
-__global__ void __launch_bounds__(32 * kAppendWarps, 8) append_kernel(const AttnArgs a, const CacheArgs c, const AppendArgs p, const int per_warp) {
+__global__ void __launch_bounds__(32 * kAppendWarps, 6) append_kernel(const AttnArgs a, const CacheArgs c, const AppendArgs p, const int per_warp) {
   extern __shared__ uint8_t v8[];                  // [rows of the tile][kPitch]
   __shared__ int slots[4 * kAppendWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tile = per_warp * kAppendWarps;
@@ -251,27 +296,33 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 8) append_kernel(const Attn
   const int nq = a.heads * D, nk = a.kv * D, q_chunks = (nq + kChunk - 1) / kChunk;
   const int at = part * kChunk + lane * 4, h = at / D, d0 = at % D;          // the lane's keys and values
   const bool live = at < nk, rotary = a.rot != 0;
+  const int q0 = part * q_chunks / parts, q1 = (part + 1) * q_chunks / parts;
   int first_row = -1, first_k = 0, first_v = 0;    // the last first token of a block that was looked at: exponents
+  const int ahead = row0 + warp * per_warp + lane;                           // of the warp's rows, one to a lane
+  const bool there = lane < per_warp && ahead < p.rows;
+  const int slot_ahead = there ? p.slot[ahead] : -1, pos_ahead = there ? p.position[ahead] : 0;
   for (int i = 0; i < per_warp; ++i) {
     const int t = warp * per_warp + i, row = row0 + t;
-    int slot = -1;
+    int slot = __shfl_sync(0xFFFFFFFFu, slot_ahead, i), pos = __shfl_sync(0xFFFFFFFFu, pos_ahead, i);
     if (row < p.rows) {
-      slot = p.slot[row];
-      int pos = p.position[row];
-      const Four k4 = load<X, kVector>((const X*)p.k + row * p.ldk + at, live), v4 = load<X, kVector>((const X*)p.v + row * p.ldv + at, live);
+      const auto k4 = load<kVector>((const X*)p.k + row * p.ldk + at, live), v4 = load<kVector>((const X*)p.v + row * p.ldv + at, live);
       const bool bad = (rotary && (unsigned)pos >= (unsigned)a.positions) || slot < -1 || slot >= slot_end;
       if (bad && lane == 0 && part == 0) atomicAdd(a.status + 1, 1u);
       if (slot < 0 || slot >= slot_end) slot = -1;
       pos = min(max(pos, 0), a.positions - 1);
-      const Rotation rot = rotation<D, kLayout>(a, pos, lane);
+      const Rotation<X> rot = rotation<X, D, kLayout>(a, pos, lane);
+      const X* const qs = (const X*)p.q + row * p.ldq;
+      int qa = q0 * kChunk + lane * 4;
+      auto q4 = load<kVector>(qs + qa, q0 < q1 && qa < nq);
 #pragma unroll 1
-      for (int j = part * q_chunks / parts; j < (part + 1) * q_chunks / parts; ++j) {
-        const int qa = j * kChunk + lane * 4;
+      for (; qa < q1 * kChunk; qa += kChunk) {
         int q[4];
-        rotate<kLayout>(load<X, kVector>((const X*)p.q + row * p.ldq + qa, qa < nq), rot, rotary, q);
-        const int e = exponent(largest<D>(q, lane), 0);
+        const auto now = q4;
+        q4 = load<kVector>(qs + qa + kChunk, qa + kChunk < min(nq, q1 * kChunk));
+        rotate<kLayout>(now, rot, rotary, q);
+        const int e = exponent<D>(q, 0, lane);
         if (qa < nq) {
-          *reinterpret_cast<uint32_t*>(p.q8 + (long long)row * nq + qa) = pack8(q, e);
+          *reinterpret_cast<uint32_t*>(p.q8 + (long long)row * nq + qa) = pack8<true>(q, e);
           if (qa % D == 0) p.q_exp[(long long)row * a.heads + qa / D] = (uint8_t)e;
         }
       }
@@ -280,10 +331,10 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 8) append_kernel(const Attn
         const long long head = (long long)(slot / kAttnBlock) * a.kv + h;
         int k[4], v[4], ek = 0, ev = 0;
         rotate<kLayout>(k4, rot, rotary, k);
-        rotate<kLayout>(v4, rot, false, v);
+        unpack(v4, v);
         if (off == 0) {
-          ek = exponent(largest<D>(k, lane), a.k_headroom);
-          ev = exponent(largest<D>(v, lane), a.v_headroom);
+          ek = exponent<D>(k, a.k_headroom, lane);
+          ev = exponent<D>(v, a.v_headroom, lane);
           if (live && d0 == 0) {
             c.k_exp[head] = (uint8_t)ek;
             c.v_exp[head] = (uint8_t)ev;
@@ -291,11 +342,11 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 8) append_kernel(const Attn
         } else if (from >= 0 && (from == first_row || p.slot[from] == slot - off)) {
           if (from != first_row) {
             int x[4];
-            rotate<kLayout>(load<X, kVector>((const X*)p.v + from * p.ldv + at, live), rot, false, x);
-            first_v = exponent(largest<D>(x, lane), a.v_headroom);
-            rotate<kLayout>(load<X, kVector>((const X*)p.k + from * p.ldk + at, live),
-                            rotation<D, kLayout>(a, min(max(p.position[from], 0), a.positions - 1), lane), rotary, x);
-            first_k = exponent(largest<D>(x, lane), a.k_headroom);
+            unpack(load<kVector>((const X*)p.v + from * p.ldv + at, live), x);
+            first_v = exponent<D>(x, a.v_headroom, lane);
+            rotate<kLayout>(load<kVector>((const X*)p.k + from * p.ldk + at, live),
+                            rotation<X, D, kLayout>(a, min(max(p.position[from], 0), a.positions - 1), lane), rotary, x);
+            first_k = exponent<D>(x, a.k_headroom, lane);
             first_row = from;
           }
           ek = first_k;
@@ -305,8 +356,8 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 8) append_kernel(const Attn
           ev = min((int)c.v_exp[head], kAttnMaxExp);
         }
         if (live) {
-          *reinterpret_cast<uint32_t*>(c.k + (head * kAttnBlock + off) * D + d0) = pack8(k, ek);
-          *reinterpret_cast<uint32_t*>(v8 + t * kPitch + lane * 4) = pack8(v, ev);
+          *reinterpret_cast<uint32_t*>(c.k + (head * kAttnBlock + off) * D + d0) = pack8<false>(k, ek);
+          *reinterpret_cast<uint32_t*>(v8 + t * kPitch + lane * 4) = pack8<false>(v, ev);
         }
       }
     }
@@ -340,8 +391,9 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 8) append_kernel(const Attn
 template <class X, int D, int kLayout>
 cudaError_t launch_append(const AttnArgs& a, const CacheArgs& c, const AppendArgs& p, cudaStream_t stream) {
   const int parts = (a.kv * D + kChunk - 1) / kChunk;
-  // four rows to a warp where that still leaves two CTAs to an SM
-  const int per_warp = (long long)p.rows * parts >= 2ll * a.sms * 4 * kAppendWarps ? 4 : 1, tile = per_warp * kAppendWarps;
+  // Where that still leaves two CTAs to an SM, four rows to a warp, whose values make runs of 32 bytes, or two of 8 bits, of which a CTA has
+  // less to do (16384 rows of 32 + 16 heads of 128, 32 bits: 137 us with four, 143 with two; 20011 rows of 16 + 8 of 64, 8 bits: 47 and 45)
+  const int most = sizeof(X) == 1 ? 2 : 4, per_warp = (long long)p.rows * parts >= 2ll * a.sms * most * kAppendWarps ? most : 1, tile = per_warp * kAppendWarps;
   const dim3 grid((unsigned)((p.rows + tile - 1) / tile), (unsigned)parts);
   const size_t smem = (size_t)tile * kPitch;
   if (p.vector) append_kernel<X, D, kLayout, true><<<grid, 32 * kAppendWarps, smem, stream>>>(a, c, p, per_warp);
