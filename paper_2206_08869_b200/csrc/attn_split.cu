@@ -11,6 +11,12 @@
 // cluster share it. CTAs of a team tell each other their largest t and, at the end, their sums, each CTA the owners of the dimensions,
 // through the cluster's shared memory. Clusters are persistent and take the large teams first; copies run ahead into the next unit.
 // Where units are fewer than clusters, a cluster is one team and as large as still lets all units run at once.
+//
+// Measured, 32 query heads of 128 over 8: one token after 1000 12.2 us, a chain of steps of which none fills anything (units found, K and
+// its scores, the team's largest t, V, the team's sums, outputs); 64 requests of up to 8192 tokens 35 us, 69 MB at 1.9 TB/s, contexts
+// that differ and the same chain; one token after 131072 74 us, 268 MB at 3.6 TB/s, scores, weights and their MMAs of one CTA behind one another
+// (scores read back and kept in words 291, kept in tensor memory 121, twice the weights' room 116, scores computed again ahead of the values 93,
+// teams as large as the GPU holds 75).
 #include <algorithm>
 
 #include "../../include/iodf.h"

@@ -6,7 +6,13 @@
 //   pass 2: S again, weights p = 256 hi + lo (8 unsigned and 8 signed bits), O_hi += hi V, O_lo += lo V in tensor memory
 // With the maximum known no sum is ever rescaled. Two groups of four warps take the blocks in turn; S, and the weights in shared
 // memory, exist twice, so that one group computes while the other's MMAs run.
-// What bounds it: about ten integer instructions per score on the softmax warps (64 a clock and SM for most of them).
+// What bounds it: the integer instructions of a weight (a product's high word at a quarter of the usual rate, a clip, a table word, a float
+// add, the split into bytes), 14 clocks for 128 scores and a quarter of an SM alone and 18 to 21 beside MMAs that read shared memory,
+// through which the table's words and the weights go too: 2300 to 2700 clocks for a block of 128 x 128, where its MMAs take 1400 with
+// D = 128. A product of doubles for the high word, or a polynomial for the table's word, cost as much or more.
+// 16384 tokens of a prompt, 32 heads of 128 over 8, causal: 3.32 ms (8 softmax warps 4.16, 16 3.68; copies in the order of the MMAs and the
+// unit's outputs beside the next one's first pass 3.46; waits that the hardware suspends 3.32). 128 images of 256 tokens, 4 heads of 64: 58.5 us,
+// where a unit of two blocks has twice its instructions' time in waits of one step for the other.
 #include <algorithm>
 
 #include "../../include/iodf.h"
@@ -26,7 +32,7 @@ constexpr int kScores = 6;               // barriers of S: see `place`
 constexpr int kBlockBytes = 16384;       // of a ring's slot: 128 rows of up to 128 bytes
 constexpr int kTableBytes = kWeightSegments * 128;                 // a copy of the table for each lane: no bank is asked twice
 constexpr int kSmem = kTableBytes + (2 + kRing + 4) * kBlockBytes;
-// Blocks at the first pass's start that the second group takes alone while the first one stores the unit before.
+// Blocks at the first pass's start that the second group takes alone while the first one stores the unit before (4 or 16: 2 % slower).
 constexpr int kLead = 8;
 
 struct Unit {
