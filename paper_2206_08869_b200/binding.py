@@ -1030,18 +1030,21 @@ def _table_of(t, attn, n):
     """Address, row stride and width of a block table [n, width] whose entries lie side by side."""
     if t.get_device() != attn.device or t.dtype is not attn.int32:
         _on(t, attn, attn.int32, "table")
-    if t.dim() != 2 or t.shape[0] != n or (t.shape[1] > 1 and t.stride(1) != 1):
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 2 or shape[0] != n or (strides[1] != 1 and shape[1] > 1):
         raise ValueError("table must be [%d, blocks] with a request's entries side by side" % n)
-    return t.data_ptr(), t.stride(0) if n > 1 else max(t.shape[1], t.stride(0)), t.shape[1]
+    return t.data_ptr(), strides[0] if n > 1 else max(shape[1], strides[0]), shape[1]
 
 
 def _cache_of(cache, attn):
     k, kv, dim = cache["k"], attn.kv_heads, attn.head_dim
     blocks = k.shape[0]
+    if blocks > _MOST:
+        raise ValueError("%d blocks are out of range" % blocks)
     return AttnCacheDesc(_flat(k, attn, attn.int8, (blocks, kv, IODF_ATTN_BLOCK, dim), "cache k"),
                          _flat(cache["v"], attn, attn.int8, (blocks, kv, dim, IODF_ATTN_BLOCK), "cache v"),
                          _flat(cache["k_exp"], attn, attn.uint8, (blocks, kv), "cache k_exp"),
-                         _flat(cache["v_exp"], attn, attn.uint8, (blocks, kv), "cache v_exp"), _fits(blocks, C.c_uint32, "blocks"))
+                         _flat(cache["v_exp"], attn, attn.uint8, (blocks, kv), "cache v_exp"), blocks)
 
 
 def iodf_attn_plan(attn, held, add, table, ring, state, rows, held_out=None, row_start=None, slot=None, position=None, state_out=None, stream=None):
