@@ -135,11 +135,11 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const PlanArgs p) {
 // A warp takes 128 neighbouring elements of a row of q, k or v at a time (one head of 128, two of 64, four of 32), a lane four of them; the
 // rotation's partner is in another lane (half layout) or the lane's own. The bytes: q, k and v are read once, but for the first token of a
 // block, whose size decides the block's exponent: a warp whose rows have it outside of them reads it again (from L2). Those of 32-bit inputs
-// take more than half of the time (16384 rows of 32 query and 8 cache heads of 128: 137 us, 3.7 TB/s); of 8-bit inputs the instructions
-// do, some hundred for 128 elements (20011 rows of 16 and 4 of 64, half of each rotated: 41 us, 76 % of the issue slots before exponents were
-// reduced as bits). The next chunk of q is on its way while one is rotated (51 us without, at eight CTAs to an SM instead of six). Values of
-// a tile of rows go through shared memory to be turned around.
-constexpr int kAppendWarps = 8;
+// take more than half of the time (16384 rows of 32 query and 8 cache heads of 128: 136 us, 3.7 TB/s); of 8-bit inputs the instructions
+// do, some hundred for 128 elements (20011 rows of 16 and 4 of 64, half of each rotated: 37.5 us, four fifths of the issue slots). The next
+// chunk of q is on its way while one is rotated (51 us had become 46 by it, with six CTAs to an SM instead of eight). Values of a tile of rows
+// go through shared memory to be turned around.
+constexpr int kAppendWarps = 8;          // rows of a tile: as many, or four times that
 constexpr int kChunk = 128, kPitch = kChunk + 4;
 
 __device__ __forceinline__ uint32_t pack16(int hi, int lo) {       // both saturated to 16 bits
@@ -253,7 +253,7 @@ __device__ __forceinline__ int exponent(int amax, int headroom) {
 }
 
 // The exponent of a lane's head. Of heads of less than a warp the largest of the lanes' exponents, each a bit in its head's 16 of a word: lanes
-// with masks of their own would be reduced one head after another (the 41 us above were 45).
+// with masks of their own would be reduced one head after another (the chunks above took 45 us, 41 with bits).
 template <int D>
 __device__ __forceinline__ int exponent(const int (&x)[4], int headroom, int lane) {
   const int m = max(max(abs(x[0]), abs(x[1])), max(abs(x[2]), abs(x[3])));
@@ -287,10 +287,10 @@ __device__ __forceinline__ uint32_t pack8(const int (&x)[4], int e) {
 }
 
 template <class X, int D, int kLayout, bool kVector>
-__global__ void __launch_bounds__(32 * kAppendWarps, 6) append_kernel(const AttnArgs a, const CacheArgs c, const AppendArgs p, const int per_warp) {
+__global__ void __launch_bounds__(32 * kAppendWarps, 6) append_kernel(const AttnArgs a, const CacheArgs c, const AppendArgs p, const int rows_log) {
   extern __shared__ uint8_t v8[];                  // [rows of the tile][kPitch]
   __shared__ int slots[4 * kAppendWarps];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, tile = per_warp * kAppendWarps;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, per_warp = 1 << rows_log, tile_log = rows_log + 3, tile = 1 << tile_log;
   const int row0 = blockIdx.x * tile, parts = gridDim.y, part = blockIdx.y;
   const int slot_end = c.blocks * kAttnBlock;      // below 2^31
   const int nq = a.heads * D, nk = a.kv * D, q_chunks = (nq + kChunk - 1) / kChunk;
@@ -311,19 +311,22 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 6) append_kernel(const Attn
       if (slot < 0 || slot >= slot_end) slot = -1;
       pos = min(max(pos, 0), a.positions - 1);
       const Rotation<X> rot = rotation<X, D, kLayout>(a, pos, lane);
-      const X* const qs = (const X*)p.q + row * p.ldq;
-      int qa = q0 * kChunk + lane * 4;
-      auto q4 = load<kVector>(qs + qa, q0 < q1 && qa < nq);
+      const X* from_q = (const X*)p.q + row * p.ldq + q0 * kChunk + lane * 4;
+      int8_t* to_q = p.q8 + (long long)row * nq + q0 * kChunk + lane * 4;
+      uint8_t* to_e = p.q_exp + (long long)row * a.heads + (q0 * kChunk + lane * 4) / D;
+      int left = min(nq, q1 * kChunk) - q0 * kChunk - lane * 4;                // above 0: the lane has queries in this chunk
+      auto q4 = load<kVector>(from_q, left > 0);
 #pragma unroll 1
-      for (; qa < q1 * kChunk; qa += kChunk) {
+      for (int j = q0; j < q1; ++j, left -= kChunk, to_q += kChunk, to_e += kChunk / D) {
         int q[4];
         const auto now = q4;
-        q4 = load<kVector>(qs + qa + kChunk, qa + kChunk < min(nq, q1 * kChunk));
+        from_q += kChunk;
+        q4 = load<kVector>(from_q, left > kChunk);
         rotate<kLayout>(now, rot, rotary, q);
         const int e = exponent<D>(q, 0, lane);
-        if (qa < nq) {
-          *reinterpret_cast<uint32_t*>(p.q8 + (long long)row * nq + qa) = pack8<true>(q, e);
-          if (qa % D == 0) p.q_exp[(long long)row * a.heads + qa / D] = (uint8_t)e;
+        if (left > 0) {
+          *reinterpret_cast<uint32_t*>(to_q) = pack8<true>(q, e);
+          if (lane * 4 % D == 0) *to_e = (uint8_t)e;
         }
       }
       if (slot >= 0) {
@@ -369,21 +372,23 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 6) append_kernel(const Attn
   const bool run = __syncthreads_and(s0 >= 0 && s0 % kAttnBlock + tile <= kAttnBlock && ((int)threadIdx.x >= tile || slots[threadIdx.x] == s0 + (int)threadIdx.x));
   if (run) {                                       // all rows of the tile one after another in one block
     int8_t* const base = c.v + ((long long)(s0 / kAttnBlock) * a.kv * D + part * kChunk) * kAttnBlock + s0 % kAttnBlock;
-    const int shift = s0 & 3, words = (shift + tile + 3) / 4;        // words of a dimension: the first and the last may be partly of others
-    for (int i = threadIdx.x; i < words * elements; i += 32 * kAppendWarps) {
-      const int el = i / words, t = (i - el * words) * 4 - shift;
+    const int shift = s0 & 3, words = tile / 4;      // of a dimension; the first and one more, behind them, may be partly of others
+    auto store = [&](int el, int t) {
       const uint8_t* x = v8 + t * kPitch + el;
-      int8_t* const to = base + (long long)el * kAttnBlock + t;
+      int8_t* const to = base + el * kAttnBlock + t;
       if (t >= 0 && t + 4 <= tile) {
         *reinterpret_cast<uint32_t*>(to) = x[0] | x[kPitch] << 8 | x[2 * kPitch] << 16 | (uint32_t)x[3 * kPitch] << 24;
       } else {
         for (int j = max(0, -t); j < min(4, tile - t); ++j) to[j] = (int8_t)x[j * kPitch];
       }
-    }
+    };
+    for (int i = threadIdx.x; i < elements * words; i += 32 * kAppendWarps) store(i >> (tile_log - 2), (i & (words - 1)) * 4 - shift);
+    if (shift)
+      for (int el = threadIdx.x; el < elements; el += 32 * kAppendWarps) store(el, tile - shift);
     return;
   }
   for (int i = threadIdx.x; i < tile * elements; i += 32 * kAppendWarps) {
-    const int t = i % tile, el = i / tile, s = slots[t];
+    const int t = i & (tile - 1), el = i >> tile_log, s = slots[t];
     if (s >= 0) c.v[((long long)(s / kAttnBlock) * a.kv * D + part * kChunk + el) * kAttnBlock + s % kAttnBlock] = (int8_t)v8[t * kPitch + el];
   }
 }
@@ -391,13 +396,12 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 6) append_kernel(const Attn
 template <class X, int D, int kLayout>
 cudaError_t launch_append(const AttnArgs& a, const CacheArgs& c, const AppendArgs& p, cudaStream_t stream) {
   const int parts = (a.kv * D + kChunk - 1) / kChunk;
-  // Where that still leaves two CTAs to an SM, four rows to a warp, whose values make runs of 32 bytes, or two of 8 bits, of which a CTA has
-  // less to do (16384 rows of 32 + 16 heads of 128, 32 bits: 137 us with four, 143 with two; 20011 rows of 16 + 8 of 64, 8 bits: 47 and 45)
-  const int most = sizeof(X) == 1 ? 2 : 4, per_warp = (long long)p.rows * parts >= 2ll * a.sms * most * kAppendWarps ? most : 1, tile = per_warp * kAppendWarps;
+  // four rows to a warp where that still leaves two CTAs to an SM: their values make runs of 32 bytes (16384 rows of 32 bits: 136 us, 143 with two)
+  const int rows_log = (long long)p.rows * parts >= 2ll * a.sms * (kAppendWarps << 2) ? 2 : 0, tile = kAppendWarps << rows_log;
   const dim3 grid((unsigned)((p.rows + tile - 1) / tile), (unsigned)parts);
   const size_t smem = (size_t)tile * kPitch;
-  if (p.vector) append_kernel<X, D, kLayout, true><<<grid, 32 * kAppendWarps, smem, stream>>>(a, c, p, per_warp);
-  else append_kernel<X, D, kLayout, false><<<grid, 32 * kAppendWarps, smem, stream>>>(a, c, p, per_warp);
+  if (p.vector) append_kernel<X, D, kLayout, true><<<grid, 32 * kAppendWarps, smem, stream>>>(a, c, p, rows_log);
+  else append_kernel<X, D, kLayout, false><<<grid, 32 * kAppendWarps, smem, stream>>>(a, c, p, rows_log);
   return cudaGetLastError();
 }
 
