@@ -109,3 +109,31 @@ def test_more_requests_than_the_kernel_for_few_rows_takes():
     rng = np.random.default_rng(0)
     held = rng.integers(0, 200, 9000)
     G.iodf_attn_check(T._forward_both(C.description(torch, 1, 1, 32), held.tolist(), np.minimum(held, rng.integers(0, 2, 9000)).tolist(), 1))
+
+
+@pytest.mark.parametrize("held,add,dim,window", [([131072], [5], 32, 0), ([131071, 1000], [2, 700], 64, 0), ([40000], [130], 128, 0), ([131072], [3], 128, 90000)])
+def test_long_contexts(many, held, add, dim, window):
+    torch, G = T._modules()
+    G.iodf_attn_check(T._forward_both(C.description(torch, 2, 1, dim, window=window), held, add, 5))
+
+
+@pytest.mark.parametrize("padding", [0, 4000])
+def test_rows_before_the_first_request(padding):
+    """Rows that no request has, before, between (a request of none) and behind them, stay as they are."""
+    torch, G = T._modules()
+    d = C.description(torch, 4, 2, 64)
+    rng = np.random.default_rng(9)
+    held, add = np.array([200, 0, 77], np.int32), [5, 0, 70]
+    start, table, blocks = C.requests(held, add, rng)
+    start += 3
+    rows = int(start[-1]) + 2 + padding
+    cache = C.cache(d, blocks, rng)
+    q8, e = C.queries(d, rows, rng)
+    y = torch.full((rows, 256), 3, dtype=torch.int8, device="cuda")
+    attn, g = G.iodf_attn_create(d), lambda x: C.on_gpu(torch, x)
+    G.iodf_attn_forward(attn, g(q8), g(e), g(start), g(held), g(table), g(cache), y=y)
+    from oracle import attention as A
+    want = A.forward(d, q8, e, start, held, table, cache, np.full((rows, 256), 3, np.int64))
+    np.testing.assert_array_equal(y.cpu().numpy(), want)
+    assert (want[:3] == 3).all() and (want[start[-1]:] == 3).all()
+    G.iodf_attn_check(attn)
