@@ -36,6 +36,18 @@ constexpr int kLeastCluster = 8, kMaxTeam = kAttnMaxTeam, kClasses = 5;         
 constexpr int kMaxPart = kAttnMaxBlocks / kLeastCluster;          // blocks of one CTA
 constexpr int kMaxChunks = kAttnSplitRequests / 32;
 
+// Dimensions of a row's output that one CTA of a team finishes. The last CTAs may have fewer, or none.
+__host__ __device__ constexpr int owned(int dim, int team) { return (dim + team - 1) / team; }
+// Places of a CTA's sums: each member of the team has `owned` of them, also where dimensions do not divide evenly (10 CTAs, 128 dimensions: 130).
+constexpr int most_places(int dim, int least, int most) {
+  int places = 0;
+  for (int team = least; team <= most; ++team) places = team * owned(dim, team) > places ? team * owned(dim, team) : places;
+  return places;
+}
+constexpr int kPlaces = 128, kPlacesBig = 140;           // teams of 1, 2, 4, 8; of up to 16
+static_assert(most_places(128, 1, 1) <= kPlaces && most_places(128, 2, 2) <= kPlaces && most_places(128, 4, 4) <= kPlaces && most_places(128, 8, 8) <= kPlaces, "teams within a cluster");
+static_assert(most_places(32, 1, kMaxTeam) <= kPlacesBig && most_places(64, 1, kMaxTeam) <= kPlacesBig && most_places(128, 1, kMaxTeam) <= kPlacesBig, "teams as large as a cluster");
+
 // Two shapes: one CTA to an SM, with room for the scores of many blocks, or two, so that one unit's waits are another's work.
 //   weights: hi = (p + 128) >> 8 and the low byte of p + 128, which is 128 more than lo; both are unsigned, so one MMA has rows of hi, rows of
 //   lo and a row of ones, whose product (the sum of v) takes the 128 off again. 16 rows need two MMAs: hi, and lo signed.
@@ -46,11 +58,12 @@ struct Shape {
   static constexpr int kRing = kBig ? 5 : 3, kColumns = kBig ? 512 : 256;                               // stages; of tensor memory
   static constexpr int kO = kCols == 4 ? 16 : 32;                                                      // of O: N of its MMAs, or twice 16
   static constexpr int kScores = (kColumns - 32) / kN, kHeld = kScores - 4;      // S: of the first blocks they stay, the last four take turns
-  static constexpr int kDynamic = (kBig ? 200 : 86) * 1024;
+  static constexpr int kSumPlaces = kBig ? kPlacesBig : kPlaces;
+  static constexpr int kDynamic = (kBig ? 200 : 86) * 1024 + (kSumPlaces - 128) * 16 * 8;               // the same for all kCols
   static constexpr int kOperand = kCols > 4 ? 4096 : 2048;                                             // of weights: rows of 128 bytes
   static constexpr int kQBytes = kCols > 8 ? 2048 : 1024;                                              // of queries; MMAs read 16 rows, the others may be anything
   static constexpr int kP = kRing * kTileBytes, kQ = kP + 2 * kGroups * kOperand, kSums = kQ + 2 * kQBytes + 1024;
-  static constexpr int kKept = kSums + 128 * kCols * 8;
+  static constexpr int kKept = kSums + kSumPlaces * kCols * 8;
   static constexpr int kKeptBlocks = (kDynamic - 1024 - kKept) / (kCols * 512) > 0 ? (kDynamic - 1024 - kKept) / (kCols * 512) : 0;      // t of 128 keys, 32 bits
   static constexpr int kKeep = kHeld + kKeptBlocks;
   static_assert(kKept + 1024 <= kDynamic, "shared memory");
@@ -601,7 +614,7 @@ __global__ void __launch_bounds__(128 + 128 * kGroups, kGroups == 4 ? 1 : 2) spl
           }
         }
       } else {
-        const int own = (D + u.team - 1) / u.team;      // dimensions that a CTA finishes
+        const int own = owned(D, u.team);
         if (key < D) {
           const uint32_t to = ptx::cluster_addr(osum + (uint32_t)((u.member * own + key % own) * kCols * 8), (uint32_t)(rank - u.member + key / own));
 #pragma unroll
@@ -703,7 +716,7 @@ cudaError_t launch(const AttnArgs& a, const CacheArgs& c, const ForwardArgs& f, 
   s.chunks = (f.n + 31) / 32;
   s.cluster = kLeastCluster;
   s.one_team = 0;
-  const bool pairs = units > a.sms;
+  const bool pairs = units > a.sms;                     // their sums have no room for a team of more than eight
   for (int n = std::min(kMaxTeam, f.width); n > kLeastCluster && !s.one_team && !pairs; --n) {
     if (a.clusters[n] < units) continue;
     s.cluster = n;
