@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 6) append_kernel(const Attn
   const int at = part * kChunk + lane * 4, h = at / D, d0 = at % D;          // the lane's keys and values
   const bool live = at < nk, rotary = a.rot != 0;
   const int q0 = part * q_chunks / parts, q1 = (part + 1) * q_chunks / parts;
-  int first_row = -1, first_k = 0, first_v = 0;    // the last first token of a block that was looked at: exponents
+  int first_row = -1, first_slot = -1, first_exps = 0;                       // the last first token of a block that was looked at: exponents of k, above four bits of v
   const int ahead = row0 + warp * per_warp + lane;                           // of the warp's rows, one to a lane
   const bool there = lane < per_warp && ahead < p.rows;
   const int slot_ahead = there ? p.slot[ahead] : -1, pos_ahead = there ? p.position[ahead] : 0;
@@ -330,7 +330,8 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 6) append_kernel(const Attn
         }
       }
       if (slot >= 0) {
-        const int off = slot % kAttnBlock, from = row - off;
+        const int off = slot % kAttnBlock, from = row - off, start = slot - off;
+        const bool known = from == first_row && start == first_slot;           // another block's rows may lie as far behind the same row
         const long long head = (long long)(slot / kAttnBlock) * a.kv + h;
         int k[4], v[4], ek = 0, ev = 0;
         rotate<kLayout>(k4, rot, rotary, k);
@@ -342,18 +343,19 @@ __global__ void __launch_bounds__(32 * kAppendWarps, 6) append_kernel(const Attn
             c.k_exp[head] = (uint8_t)ek;
             c.v_exp[head] = (uint8_t)ev;
           }
-        } else if (from >= 0 && (from == first_row || p.slot[from] == slot - off)) {
-          if (from != first_row) {
+        } else if (known || (from >= 0 && p.slot[from] == start)) {
+          if (!known) {
             int x[4];
             unpack(load<kVector>((const X*)p.v + from * p.ldv + at, live), x);
-            first_v = exponent<D>(x, a.v_headroom, lane);
+            first_exps = exponent<D>(x, a.v_headroom, lane) << 4;
             rotate<kLayout>(load<kVector>((const X*)p.k + from * p.ldk + at, live),
                             rotation<X, D, kLayout>(a, min(max(p.position[from], 0), a.positions - 1), lane), rotary, x);
-            first_k = exponent<D>(x, a.k_headroom, lane);
+            first_exps |= exponent<D>(x, a.k_headroom, lane);
             first_row = from;
+            first_slot = start;
           }
-          ek = first_k;
-          ev = first_v;
+          ek = first_exps & 15;
+          ev = first_exps >> 4;
         } else if (live) {
           ek = min((int)c.k_exp[head], kAttnMaxExp);
           ev = min((int)c.v_exp[head], kAttnMaxExp);
