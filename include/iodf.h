@@ -570,7 +570,8 @@ int iodf_norm_forward(iodf_norm* nm, int rows, const void* r, const iodf_view* r
  * The cache is the caller's: `blocks` blocks of 128 tokens, each with its keys and values of every cache head and an exponent for both,
  *   k DEV int8 [blocks][kv_heads][128][head_dim], v DEV int8 [blocks][kv_heads][head_dim][128] (both 16-byte aligned),
  *   k_exp, v_exp DEV uint8 [blocks][kv_heads]: an element stands for k 2^k_exp; exponents above 12 count as 12.
- * Token t of request q lies in block table[q][t / 128] at t % 128; its slot is that block * 128 + t % 128.
+ * Token t of request q lies in block table[q][t / 128] at t % 128; its slot is that block * 128 + t % 128. blocks * kv_heads, and the places of
+ * a ring, are at most 2^24 - 1 (EUNSUPPORTED).
  *
  * iodf_attn_plan: blocks for the new tokens of a call's requests. held[q] tokens are in the cache, add[q] >= 0 come with this call, -1: the
  * request ends. ring (ring_size = blocks of the cache) holds the free blocks from place state[0] on, state[1] of them, modulo its size.

@@ -120,11 +120,13 @@ bool overlap(const Span (&out)[N], const Span (&in)[M]) {
   return false;
 }
 
-// The cache's pointers and sizes: 8-bit rows are read in tiles of 16-byte pieces, and a slot is a 32-bit number.
-bool good_cache(const iodf_attn& h, const iodf_attn_cache* c) {
-  if (!c || !c->k || !c->v || !c->k_exp || !c->v_exp || c->blocks < 1 || c->blocks > (1u << 24) - 1) return false;
-  if ((uint64_t)c->blocks * h.args.kv * kAttnBlock > INT32_MAX) return false;             // rows of its tensor maps
-  return aligned(c->k, 16) && aligned(c->v, 16);
+// Blocks of a cache or a ring, times the heads of a block: a slot, and a row of the cache's tensor maps, is a 32-bit number.
+constexpr uint64_t kMostBlocks = (uint64_t)INT32_MAX / kAttnBlock;
+
+// The cache's pointers and sizes: 8-bit rows are read in tiles of 16-byte pieces.
+int check_cache(const iodf_attn& h, const iodf_attn_cache* c) {
+  if (!c || !c->k || !c->v || !c->k_exp || !c->v_exp || c->blocks < 1 || !aligned(c->k, 16) || !aligned(c->v, 16)) return IODF_EINVAL;
+  return (uint64_t)c->blocks * h.args.kv > kMostBlocks ? IODF_EUNSUPPORTED : IODF_OK;
 }
 
 CacheArgs cache_args(const iodf_attn_cache& c) { return {c.k, c.v, c.k_exp, c.v_exp, (int)c.blocks}; }
@@ -178,8 +180,8 @@ int iodf_attn_plan(iodf_attn* h, int n_req, const int32_t* held, const int32_t* 
                    int32_t* state_out, void* cuda_stream) {
   if (!h || n_req < 0 || rows < 0) return IODF_EINVAL;
   if (!state || !state_out || !row_start || (n_req && (!held || !add || !table || !held_out)) || (rows && (!slot || !position))) return IODF_EINVAL;
-  if (!ring || ring_size < 1 || ring_size > (1u << 24) - 1 || width < 1 || ldt < width || ldt >= kMaxStride) return IODF_EINVAL;
-  if (n_req > kAttnMaxRequests || width > (uint32_t)kAttnMaxBlocks || rows > (1 << 30)) return IODF_EUNSUPPORTED;
+  if (!ring || ring_size < 1 || width < 1 || ldt < width || ldt >= kMaxStride) return IODF_EINVAL;
+  if (n_req > kAttnMaxRequests || width > (uint32_t)kAttnMaxBlocks || ring_size > kMostBlocks || rows > (1 << 30)) return IODF_EUNSUPPORTED;
   for (const void* p : {(const void*)held, (const void*)add, (const void*)table, (const void*)ring, (const void*)state, (const void*)held_out,
                         (const void*)row_start, (const void*)slot, (const void*)position, (const void*)state_out})
     if (!aligned(p, 4)) return IODF_EINVAL;
@@ -198,7 +200,7 @@ int iodf_attn_plan(iodf_attn* h, int n_req, const int32_t* held, const int32_t* 
 int iodf_attn_append(iodf_attn* h, int rows, const void* q, size_t ldq, const void* k, size_t ldk, const void* v, size_t ldv, const int32_t* slot,
                      const int32_t* position, const iodf_attn_cache* cache, int8_t* q8, uint8_t* q_exp, void* cuda_stream) {
   if (!h || rows < 0) return IODF_EINVAL;
-  if (!good_cache(*h, cache)) return IODF_EINVAL;
+  if (const int rc = check_cache(*h, cache)) return rc;
   if (rows == 0) return IODF_OK;
   const AttnArgs& a = h->args;
   const size_t R = (size_t)rows, x = a.x_i8 ? 1 : 4, nq = (size_t)a.heads * a.dim, nk = (size_t)a.kv * a.dim;
@@ -222,7 +224,7 @@ int iodf_attn_append(iodf_attn* h, int rows, const void* q, size_t ldq, const vo
 int iodf_attn_forward(iodf_attn* h, int rows, const int8_t* q8, const uint8_t* q_exp, const int32_t* row_start, const int32_t* held, int n_req,
                       const int32_t* table, size_t ldt, uint32_t width, const iodf_attn_cache* cache, void* y, size_t ldy, void* cuda_stream) {
   if (!h || rows < 0 || n_req < 0) return IODF_EINVAL;
-  if (!good_cache(*h, cache)) return IODF_EINVAL;
+  if (const int rc = check_cache(*h, cache)) return rc;
   if (rows == 0 || n_req == 0) return IODF_OK;
   const AttnArgs& a = h->args;
   const size_t R = (size_t)rows, n = (size_t)n_req, N = (size_t)a.heads * a.dim;
