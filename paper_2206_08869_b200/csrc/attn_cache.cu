@@ -246,7 +246,7 @@ __device__ __forceinline__ void rotate(const Bytes& v, const Rotation<int8_t>& r
   x[3] = __dp2a_hi(r.c[3], b, 8192) >> 14;
 }
 
-// The smallest e with amax (8 + headroom) <= 1016 2^e; 10 at most, since |x| <= 2^15.5 and headroom <= 8.
+// The smallest e with amax (8 + headroom) <= 1016 2^e; 11 at most, since headroom <= 8 and |x| <= 2^16: both of a pair's factors may be 1.
 __device__ __forceinline__ int exponent(int amax, int headroom) {
   const int z = amax * (8 + headroom), e = max(22 - __clz(z), 0);      // z < 2^(e + 10)
   return e + (z > 1016 << e);

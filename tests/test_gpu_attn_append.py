@@ -2,6 +2,7 @@
 import numpy as np
 import pytest
 
+from oracle import attention as A
 from tests import attn_cases as C
 from tests import test_gpu_attn as T
 
@@ -58,3 +59,32 @@ def test_requests_of_any_lengths(dim, layout, seed, views, x):
     held, add = _filled(held, add, max(rows, sum(add) + 1))
     slot, position, blocks = T._slots(held, add, rng, padding=5)
     T._append_both(_description(torch, dim, x, 32, layout), len(slot), slot, position, blocks, seed, views)
+
+
+@pytest.mark.parametrize("dim,rot,layout", [(32, 32, "half"), (64, 64, "interleaved"), (64, 16, "half"), (128, 128, "half"), (128, 48, "interleaved")])
+@pytest.mark.parametrize("x", ["int8", "int32"])
+def test_factors_that_are_no_rotation(x, dim, rot, layout):
+    """Cosines and sines of 1 at once double the largest element: 2^16, whose exponent is 11 with all the headroom there is."""
+    torch, G = T._modules()
+    d = C.description(torch, 2, 2, dim, x, rot, layout, headroom=(8, 8))
+    d["rotary"]["table"] = np.stack([np.full((4, rot // 2, 2), 16384), np.full((4, rot // 2, 2), -16384)]).reshape(8, rot // 2, 2).astype(np.int16)
+    low, high = (-128, 127) if x == "int8" else (-2 ** 31, 2 ** 31 - 1)
+    rng = np.random.default_rng(dim)
+    rows = 96
+    slot, position, blocks = T._slots([0] * rows, [1] * rows, rng)
+    position = rng.integers(0, 8, rows)
+    values = np.where(rng.integers(0, 2, (rows, 1, 1)) == 0, np.int64(low), rng.choice([low, high, 0, 1], (rows, 6, dim))).reshape(rows, 6 * dim)
+    values = values.astype(np.int8 if x == "int8" else np.int32)
+    cache = C.cache(d, blocks, rng)
+    gx, gc = C.on_gpu(torch, values), C.on_gpu(torch, cache)
+    attn = G.iodf_attn_create(d)
+    cut = [0, 2 * dim, 4 * dim, 6 * dim]
+    q8, e = G.iodf_attn_append(attn, *(gx[:, a:b] for a, b in zip(cut, cut[1:])), C.on_gpu(torch, slot.astype(np.int32)),
+                               C.on_gpu(torch, position.astype(np.int32)), gc)
+    G.iodf_attn_check(attn)
+    w8, we = A.append(d, *(values[:, a:b] for a, b in zip(cut, cut[1:])), slot, position, cache)
+    assert cache["k_exp"][slot // 128].max() == (11 if x == "int32" else 3) and we.max() == (10 if x == "int32" else 2)
+    np.testing.assert_array_equal(q8.cpu().numpy(), w8)
+    np.testing.assert_array_equal(e.cpu().numpy(), we)
+    for name in cache:
+        np.testing.assert_array_equal(gc[name].cpu().numpy(), cache[name], err_msg=name)
