@@ -604,7 +604,12 @@ int iodf_norm_forward(iodf_norm* nm, int rows, const void* r, const iodf_view* r
  *   A = sum p_j v_j,  L = sum p_j 2^(V - v_exp),  y = clip(rq(o; out_m0, out_s)), o = A 2^(V + 8) / L
  * The power: with g = n mod 2^13 and c = floor(g / 128), 2^(n / 2^13) is m 2^floor(n / 2^13) / 2^23 with m = max(2^23, [2^(23 + (2 c + 1) / 128)] - 2^16)
  * + 2^10 (g mod 128). The quotient: L' = floor(L 2^a) with 2^31 <= L' < 2^32, rho = floor((2^63 - 1) / L'), o = floor((floor(A 2^(a - 8)) rho +
- * 2^(46 - V)) / 2^(47 - V)). Sums of integers: neither order nor split changes them. A row that sees nothing has o = 0. y: DEV rows of heads *
+ * 2^(46 - V)) / 2^(47 - V)). Sums of integers: neither order nor split changes them. A row that sees nothing has o = 0.
+ * Against softmax attention of the same 8-bit integers a weight is off by at most 0.47 % of itself and by 2^(V - v_exp - 16) of the row's largest
+ * weight. A block that a row sees, however little of its weight that block has, with a v_exp d above the others' so takes d bits from all
+ * weights: give a request's values like sizes. (1024 tokens, one of eight blocks like that and without weight, 40 rows: outputs off by 0.06 % of
+ * the row's largest in the median and 0.3 % at worst with d = 0, 0.2 and 1.1 with 3, 0.5 and 16 with 6, 4 and 49 with 9, 17 and 230 % with 12.)
+ * y: DEV rows of heads *
  * head_dim elements of y_type with row stride ldy in elements; y must not overlap an input. Rows in no request are not written, and no row is
  * in two. Bounds outside 0..rows are taken as the nearest, a request whose row_start falls has no rows; held outside 0..128 width (taken as the
  * nearest) of a request with rows and blocks outside the cache, which nobody sees, are counted. width <= 1024 (131072 tokens); it also tells the
