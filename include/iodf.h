@@ -564,12 +564,13 @@ int iodf_norm_forward(iodf_norm* nm, int rows, const void* r, const iodf_view* r
 
 /*
  * Attention of the rows of a request to the tokens before them, over a cache of blocks in 8 bits: what lets a network between the
- * flow and the coder look at pixels, patches or tokens that are coded already. Any cut of a request's tokens into calls gives the same
- * cache and the same outputs bit for bit: an encoder can pass over all tokens at once where its decoder takes one at a time.
+ * flow and the coder look at pixels, patches or tokens that are coded already. Any cut of a request's tokens into calls gives the same cache and,
+ * if causal, the same outputs bit for bit: an encoder can pass over all tokens at once where its decoder takes one at a time. (A row that is not
+ * causal sees the tokens that are held at its call, so its outputs are those of the cut.)
  *
  * The cache is the caller's: `blocks` blocks of 128 tokens, each with its keys and values of every cache head and an exponent for both,
  *   k DEV int8 [blocks][kv_heads][128][head_dim], v DEV int8 [blocks][kv_heads][head_dim][128] (both 16-byte aligned),
- *   k_exp, v_exp DEV uint8 [blocks][kv_heads]: an element stands for k 2^k_exp; exponents above 12 count as 12.
+ *   k_exp, v_exp DEV uint8 [blocks][kv_heads]: an element, -127 .. 127, stands for k 2^k_exp; exponents above 12 count as 12.
  * Token t of request q lies in block table[q][t / 128] at t % 128; its slot is that block * 128 + t % 128. blocks * kv_heads, and the places of
  * a ring, are at most 2^24 - 1 (EUNSUPPORTED).
  *
@@ -578,11 +579,12 @@ int iodf_norm_forward(iodf_norm* nm, int rows, const void* r, const iodf_view* r
  * Requests in order take ceil((held + add) / 128) - ceil(held / 128) blocks from its front into their row of `table` (row stride ldt, `width`
  * entries), the blocks of those that end go behind its end, for the next call to take; held_out[q] = held + add (0 at an end), row_start[q]
  * = sum of add before q; row r of request q gets position[r] = held[q] + r - row_start[q] and its slot[r]; rows behind the last request
- * get slot -1, position 0; state_out is the next call's state. A request that needs blocks when fewer than all taken so far and its own are
- * free, that would not fit into `width` entries or whose rows would not into `rows`, or with held outside 0..128 width or add below -1,
- * keeps what it holds, its rows get slot -1, and it is counted (iodf_attn_check: IODF_EDATA), as are more free blocks than the ring has places
- * and a row's block outside the cache (slot -1). The inputs but for table and ring stay as they are, no two operands may overlap (EINVAL),
- * and the call repeated on the same inputs gives the same. width <= 1024, n_req <= 16384.
+ * get slot -1, position 0; state_out is the next call's state. A request that would not fit into `width` entries or whose rows would not into
+ * `rows`, or with held outside 0..128 width or add below -1, keeps what it holds, its rows get slot -1, and it is counted (iodf_attn_check:
+ * IODF_EDATA). So it is with one that needs blocks when fewer are free than it and all requests before it ask for, those among them that were
+ * refused for want of blocks: behind the first of these no request of the call gets a block, and the ones that need none are served. Counted
+ * as well are more free blocks than the ring has places, and rows whose block is outside the cache (slot -1). The inputs but for table and ring
+ * stay as they are, no two operands may overlap (EINVAL), and the call repeated on the same inputs gives the same. width <= 1024, n_req <= 16384.
  *
  * iodf_attn_append: the call's tokens into the cache, its queries in 8 bits. q, k, v: DEV rows of x_type with strides in elements (columns of
  * one projection's output, say), heads * head_dim and kv_heads * head_dim of them; values are taken in 16 bits, clip(x, -2^15, 2^15 - 1).
@@ -660,8 +662,9 @@ int iodf_attn_append(iodf_attn* a, int rows, const void* q, size_t ldq, const vo
                      const int32_t* position, const iodf_attn_cache* cache, int8_t* q8, uint8_t* q_exp, void* cuda_stream);
 int iodf_attn_forward(iodf_attn* a, int rows, const int8_t* q8, const uint8_t* q_exp, const int32_t* row_start, const int32_t* held, int n_req,
                       const int32_t* table, size_t ldt, uint32_t width, const iodf_attn_cache* cache, void* y, size_t ldy, void* cuda_stream);
-/* Synchronise the stream; IODF_EDATA if a call since the last check met requests, rows or blocks that it could not serve (their number in
- * *bad, HOST, may be NULL), IODF_ETIMEOUT if a bounded wait gave up. Clears both. */
+/* Synchronise the stream; IODF_EDATA if a call since the last check met requests, rows or blocks that it could not serve, IODF_ETIMEOUT if a
+ * bounded wait gave up. *bad (HOST, may be NULL): how often. A request, a row, a ring and a context counts once a call; a block outside the
+ * cache that the attention meets counts for each unit of work that meets it, of which a request has one or more for each cache head. Clears both. */
 int iodf_attn_check(iodf_attn* a, void* cuda_stream, uint32_t* bad);
 
 /*

@@ -1120,4 +1120,4 @@ def iodf_attn_check(attn, stream=None):
     n = C.c_uint32(0)
     rc = load_library().iodf_attn_check(attn.handle, _layer_stream(stream, attn.device), C.byref(n))
     if rc != 0:
-        raise IodfError(rc, "iodf_attn_check (%d requests, rows or blocks)" % n.value)
+        raise IodfError(rc, "iodf_attn_check (%d reports of requests, rows or blocks)" % n.value)
